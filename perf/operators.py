@@ -60,7 +60,7 @@ def listed():
         # one sequence, guesses taken as the best tokens of each depth
         case("verify_top", "verify", T=64, V=32000),
         # a large batch whose guesses were drawn from their depth's distribution, an odd vocabulary
-        case("verify_batch_drawn", "verify", B=80, T=32, V=50257, draft=True),
+        case("verify_batch_drawn", "verify", B=80, T=32, V=50257, S=4096, draft=True),
     ]
 
 
