@@ -304,6 +304,148 @@ ppd_status ppd_node_argmax_noalloc(const float *logits, int B, int T, int V, int
                                    void *stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Sampled decoding over a long context: a cache held in 4 bits, the tree's
+ * attention over it, eviction by accumulated attention weight, and acceptance
+ * of drafted tokens with given random numbers (no paper counterpart; the paper's
+ * step verifies greedily or by the typical rule over a 16-bit cache).
+ *
+ * K/V heads may be shared: H counts K/V heads, each read by G query heads. Query
+ * tensors are [L,B,H*G,T,D] (query head h*G + g reads K/V head h), tree K/V and
+ * caches have H heads.  G = 1 is the layout of the entry points above.
+ *
+ * The 4-bit cache.  K and V each are codes uint8 [L,B,H,S_max,D/2] and scales
+ * uint8 [L,B,H,S_max,D/32], a scale for 32 channels.  A little-endian 32-bit word
+ * of codes holds eight channels: its nibble p (bits 4p..4p+3) is channel
+ * 2 (p % 4) + p / 4 of the eight.  A scale byte b stands for
+ * s = (1 + (b % 8) / 8) * 2^(b / 8 - 20), a code c for s * (c - 8): 4.25 bits a
+ * channel; every value is a bf16 number and any bytes are finite values.  All
+ * tensors are 16-byte aligned.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Rows into a 4-bit cache.  For every l, b, h and j < n_new[b]:
+ *     cache row start[b] + j  <-  quantise(new row rows[b][j], or j without rows)
+ * of K and V: the accepted path of a verification step (rows = path, n_new =
+ * accept_len, start = prefix_len) or a prompt's rows (rows NULL, T as long as
+ * the prompt; T may exceed the 512 of a tree here).
+ *   k_new, v_new [L,B,H,T,D] PPD_BF16 or PPD_F32; rows int32 [B,T] or NULL;
+ *   start, n_new int32 [B]; dev_status int32 [B]
+ * Quantisation of 32 channels x: a = max |x| (NaN left out), s the smallest scale
+ * >= a / 7 (the quotient in fp32; the largest scale where there is none),
+ * c = 8 + min(max(round(x / s), -7), 7), half to even; a NaN becomes 0.
+ * start or n_new outside the cache or n_new > T: PPD_ERR_CAPACITY, nothing
+ * written for that sequence.  A row index outside [0, T) writes nothing.
+ */
+ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache, uint8_t *k_scale,
+                          uint8_t *v_cache, uint8_t *v_scale, const int32_t *rows,
+                          const int32_t *start, const int32_t *n_new, int L, int B, int H, int T,
+                          int D, int S_max, ppd_dtype dt, int32_t *dev_status, void *stream);
+
+/*
+ * Rows out of a 4-bit cache (K or V): out [L,B,H,N,D] (PPD_BF16 or PPD_F32, exact
+ * in both) row j is the value of cache row start[b] + j for j < n[b], zero for
+ * the other j < N and for rows outside the cache.
+ */
+ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_t *start,
+                        const int32_t *n, int L, int B, int H, int N, int D, int S_max, void *out,
+                        ppd_dtype dt, void *stream);
+
+/*
+ * Tree-masked attention over a 4-bit cache: as ppd_tree_attention, the prefix
+ * rows being the values that the cache holds, the tree's keys and values 16-bit
+ * rows (dt PPD_BF16, or PPD_F32 rounded to bf16 on load).  T = 1 is plain
+ * decoding.  out is bf16 [L,B,H*G,T,D]: products and sums are fp32, and the
+ * probabilities meet V as two bf16 terms (2^-18), so that the output's rounding is
+ * all that shows; lse fp32 [L,B,H*G,T] or NULL.  parent, prefix_len, dev_status as in ppd_tree_attention.  A NaN or
+ * an infinity in a tree row may reach every query of the tree.
+ * Workspace: ppd_kv4_attention_workspace_bytes(...) bytes (0 where none is
+ * used); without one the keys of a slice are not shared out to several SMs.
+ */
+size_t ppd_kv4_attention_workspace_bytes(int L, int B, int H, int G, int T, int D, int S_max);
+ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const uint8_t *k_scale,
+                                  const uint8_t *v_cache, const uint8_t *v_scale, const void *k_tree,
+                                  const void *v_tree, const int32_t *prefix_len, const int32_t *parent,
+                                  int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt,
+                                  float scale, void *out, float *lse, int32_t *dev_status,
+                                  void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Attention weight per cached row, added up.  For the accepted nodes a_0 .. a_{n-1}
+ * of sequence b (n = accept_len[b], a_i = path[b][i]) and every l, h, with
+ * w(i, k) = sum over the G query heads of exp(scale * <q_{a_i}, k> - lse_{a_i}):
+ *     weight[j]     += sum_i w(i, k_cache[j])           j < P = prefix_len[b]
+ *     weight[P + i]  = sum_{i' >= i} w(i', k_tree[a_i])  i < n, P + i < S_max
+ * i.e. the probabilities that the step's attention gave (lse from
+ * ppd_tree_attention or ppd_tree_attention_kv4), the new rows' counted from the
+ * step that accepts them.  weight fp32 [L,B,H,S_max]; other entries stay.
+ *   q [L,B,H*G,T,D] and k_tree [L,B,H,T,D] of dtype dt; lse fp32 [L,B,H*G,T];
+ *   k_cache: with k_scale the codes of a 4-bit cache, without (NULL) bf16
+ *   [L,B,H,S_max,D].  Run it before or after the rows enter the cache.
+ * accept_len < 1 (a failed sequence) or a prefix outside the cache: nothing.
+ */
+ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cache,
+                             const uint8_t *k_scale, const void *k_tree, const int32_t *path,
+                             const int32_t *accept_len, const int32_t *prefix_len, int L, int B, int H,
+                             int G, int T, int D, int S_max, ppd_dtype dt, float scale, float *weight,
+                             void *stream);
+
+/*
+ * Eviction: a cache cut down to `budget` rows per (layer, sequence, head).  Of
+ * rows [0, length[b]) are kept the first n_sink, the last n_recent, and of those
+ * between the ones of the largest weight until there are budget (a NaN ranks
+ * above numbers, -0 equals +0, ties go to the lowest index); all of them where
+ * length[b] <= budget.  Kept rows keep their order and move to rows 0, 1, ...
+ *   planes[i]      [L,B,H,S_max,row_bytes[i]]  any rows of 1..1024 bytes: K and V of
+ *                  a bf16 cache, codes and scales of a 4-bit one; n_planes <= 8
+ *   out_planes[i]  [L,B,H,S_out,row_bytes[i]]: planes[i] itself (in place;
+ *                  S_out = S_max) or memory that no other plane uses
+ *   weight, out_weight fp32 [L,B,H,S_max] / [L,B,H,S_out], moved like the planes
+ *   kept int32 [L,B,H,budget]: the kept rows' indices, ascending, then -1
+ *   new_len int32 [B] = min(length, budget); rows beyond it are not written
+ *   dev_status int32 [B]: PPD_ERR_CAPACITY for a length outside [0, S_max]
+ *   (nothing moves, kept -1, new_len = length)
+ * planes, out_planes and row_bytes are host arrays, read before the call returns.
+ * budget <= S_max and S_out, n_sink + n_recent <= budget.
+ */
+ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *const *planes,
+                        void *const *out_planes, const int *row_bytes, int n_planes,
+                        const int32_t *length, int L, int B, int H, int S_max, int S_out, int budget,
+                        int n_sink, int n_recent, int32_t *kept, int32_t *new_len, int32_t *dev_status,
+                        void *stream);
+
+/*
+ * Acceptance by sampling: the emitted tokens have the target model's distribution
+ * softmax(logits / temperature), whatever the drafts.  The walk starts at node 0
+ * with R = softmax(logits[b][0] / temperature).  The children of the current node
+ * with cand_tokens t >= 0 are tested in index order:
+ *     a = min(1, R_t / (q_t sum R)),  accepted when u[b][c] < a
+ * with q = draft_probs[b][draft_row[b][c]] for a child drawn from that
+ * distribution, and q_t = 1 for one that was chosen (draft_row -1, or no drafts:
+ * the top guesses of ppd_next_tree).  A rejected child leaves
+ * R <- max(R / sum R - q, 0) (drawn) or R_t <- 0 (chosen); an accepted one
+ * becomes the current node.  After the last node, next_token = the first v of
+ * the largest R_v / noise[b][v]: with exponentially distributed noise a draw from R.
+ * Where the rejections left nothing, R is the node's whole distribution.  A row that
+ * holds a NaN or +inf, or only -inf, has no distribution: its children are rejected
+ * and next_token is its first NaN, or the first of its largest entries.
+ *   logits fp32 [B,T,V]; u fp32 [B,T] in [0, 1); noise fp32 [B,V] > 0;
+ *   draft_probs fp32 [B,n_draft,V] and draft_row int32 [B,T], or both NULL;
+ *   accept_prob fp32 [B,T] or NULL: a of the tested nodes, -1 elsewhere
+ * Other arguments, outputs and errors as in ppd_accept_path (a draft_row outside
+ * [-1, n_draft) of a candidate: PPD_ERR_TREE).  temperature > 0; V <= 393,216.
+ * A test whose sides agree to within float rounding, and a draw between tokens that
+ * do, may go either way against a higher-precision evaluation.
+ */
+ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, const int32_t *parent,
+                             const int32_t *prefix_len, const float *draft_probs,
+                             const int32_t *draft_row, const float *u, const float *noise, int B, int T,
+                             int V, int n_draft, int S_max, float temperature, int32_t *accept_len,
+                             int32_t *path, int32_t *next_token, int32_t *new_prefix_len,
+                             float *accept_prob, int32_t *dev_status, void *stream);
+
+/*
  * Kernel launches one ppd_verify_step call (typical == 0) or
  * ppd_verify_step_typical call (typical != 0) enqueues for these sizes, with
  * a workspace of ppd_workspace_bytes(...) bytes and the whole GPU available.

@@ -895,4 +895,234 @@ ppd_status ppd_selftest_umma(const void *a, const void *b, float *d, int mode, i
     return cuda_status(ppd::launch_selftest_umma(ma, mb, a, b, d, mode, N, static_cast<cudaStream_t>(stream)));
 }
 
+// ------------------------------------------------------------------ 4-bit cache, eviction, sampling
+
+// Shapes of a 4-bit cache's slices; G query heads share a K/V head.
+static bool kv4_dims_ok(int L, int B, int H, int G, int T, int D, int S_max)
+{
+    if (L < 1 || B < 1 || H < 1 || G < 1 || T < 1 || S_max < 1 || (D != 64 && D != 128)) return false;
+    const double slices = (double)L * B * H;
+    return slices * 64 <= 2147483647.0 && slices * G * T <= 2147483647.0 && slices * S_max * D <= 9.0e15;
+}
+
+ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache, uint8_t *k_scale,
+                          uint8_t *v_cache, uint8_t *v_scale, const int32_t *rows,
+                          const int32_t *start, const int32_t *n_new, int L, int B, int H, int T,
+                          int D, int S_max, ppd_dtype dt, int32_t *dev_status, void *stream)
+{
+    if (!k_new || !v_new || !k_cache || !k_scale || !v_cache || !v_scale || !start || !n_new || !dev_status)
+        return PPD_ERR_INVALID_ARG;
+    if (!kv4_dims_ok(L, B, H, 1, T, D, S_max) || (dt != PPD_BF16 && dt != PPD_F32)) return PPD_ERR_INVALID_ARG;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+        !aligned(k_scale, 16) || !aligned(v_scale, 16))
+        return PPD_ERR_INVALID_ARG;
+    ppd::Kv4AppendParams p{k_new, v_new, k_cache, v_cache, k_scale, v_scale, rows, start, n_new, dev_status,
+                           (long long)L * B * H, B, H, T, D, S_max, dt == PPD_F32};
+    return cuda_status(ppd::launch_kv4_append(p, static_cast<cudaStream_t>(stream)));
+}
+
+ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_t *start,
+                        const int32_t *n, int L, int B, int H, int N, int D, int S_max, void *out,
+                        ppd_dtype dt, void *stream)
+{
+    if (!cache || !scale || !start || !n || !out) return PPD_ERR_INVALID_ARG;
+    if (!kv4_dims_ok(L, B, H, 1, N, D, S_max) || (dt != PPD_BF16 && dt != PPD_F32)) return PPD_ERR_INVALID_ARG;
+    if (!aligned(cache, 16) || !aligned(scale, 16) || !aligned(out, 16)) return PPD_ERR_INVALID_ARG;
+    ppd::Kv4ReadParams p{cache, scale, start, n, out, (long long)L * B * H, B, H, N, D, S_max, dt == PPD_F32};
+    return cuda_status(ppd::launch_kv4_read(p, static_cast<cudaStream_t>(stream)));
+}
+
+// Parts that the keys of a slice are shared out to: three blocks fit an SM.  Fewer units
+// than that in all get one wave of parts; more are cut where whole units would leave over a
+// tenth of the last wave idle.  A part has at least eight chunks of 32 keys, two a warp.
+static int kv4_splits(long long slices, int row_blocks, int T, int S_max)
+{
+    const long long units = slices * row_blocks, slots = 3ll * num_sms();
+    const long long chunks = (S_max + 31) / 32 + (T + 31) / 32;
+    long long n = 1;
+    if (units < slots)
+        n = slots / units;
+    else
+        while (n < 4 && 10 * ((units * n + slots - 1) / slots) * slots > 11 * units * n) ++n;
+    const long long most = chunks / 8 < 1 ? 1 : chunks / 8;
+    return (int)(n < most ? n : most);
+}
+
+struct Kv4Ws {
+    size_t o, ml, total;
+    int row_blocks, splits;
+};
+static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
+{
+    Kv4Ws w{};
+    const long long slices = (long long)L * B * H, rows = (long long)G * T;
+    w.row_blocks = (int)((rows + 15) / 16);
+    w.splits = kv4_splits(slices, w.row_blocks, T, S_max);
+    if (w.splits > 1) {
+        const size_t n = (size_t)slices * w.splits * rows;
+        w.ml = align_up(n * D * 4);
+        w.total = align_up(w.ml + n * 8);
+    }
+    return w;
+}
+
+size_t ppd_kv4_attention_workspace_bytes(int L, int B, int H, int G, int T, int D, int S_max)
+{
+    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT) return 0;
+    return kv4_workspace(L, B, H, G, T, D, S_max).total;
+}
+
+ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const uint8_t *k_scale,
+                                  const uint8_t *v_cache, const uint8_t *v_scale, const void *k_tree,
+                                  const void *v_tree, const int32_t *prefix_len, const int32_t *parent,
+                                  int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt,
+                                  float scale, void *out, float *lse, int32_t *dev_status,
+                                  void *workspace, size_t ws_bytes, void *stream)
+{
+    if (!q || !k_cache || !k_scale || !v_cache || !v_scale || !k_tree || !v_tree || !prefix_len || !parent ||
+        !out || !dev_status)
+        return PPD_ERR_INVALID_ARG;
+    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT || (dt != PPD_BF16 && dt != PPD_F32) || !std::isfinite(scale))
+        return PPD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(k_scale, 16) || !aligned(v_cache, 16) ||
+        !aligned(v_scale, 16) || !aligned(k_tree, 16) || !aligned(v_tree, 16) || !aligned(out, 16) || !aligned(lse, 4))
+        return PPD_ERR_INVALID_ARG;
+    const long long slices = (long long)L * B * H;
+    const Kv4Ws w = kv4_workspace(L, B, H, G, T, D, S_max);
+    const bool ws_ok = workspace && ws_bytes >= w.total && aligned(workspace, kAlign);
+    ppd::Kv4AttnParams p{};
+    p.q = q;
+    p.k_cache = k_cache, p.k_scale = k_scale, p.v_cache = v_cache, p.v_scale = v_scale;
+    p.k_tree = k_tree, p.v_tree = v_tree;
+    p.prefix_len = prefix_len, p.parent = parent;
+    p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
+    p.dev_status = dev_status;
+    p.scale_bytes = (size_t)slices * S_max * (D / 32);
+    p.slices = slices;
+    p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
+    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
+    p.row_blocks = w.row_blocks;
+    p.splits = ws_ok ? w.splits : 1;
+    if (p.splits > 1) {
+        p.part_o = static_cast<float *>(workspace);
+        p.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + w.ml);
+    }
+    if (slices * p.splits * p.row_blocks > 2147483647ll) return PPD_ERR_UNSUPPORTED;
+    return cuda_status(ppd::launch_kv4_attention(p, D, static_cast<cudaStream_t>(stream)));
+}
+
+ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cache, const uint8_t *k_scale,
+                             const void *k_tree, const int32_t *path, const int32_t *accept_len,
+                             const int32_t *prefix_len, int L, int B, int H, int G, int T, int D, int S_max,
+                             ppd_dtype dt, float scale, float *weight, void *stream)
+{
+    if (!q || !lse || !k_cache || !k_tree || !path || !accept_len || !prefix_len || !weight) return PPD_ERR_INVALID_ARG;
+    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT || (dt != PPD_BF16 && dt != PPD_F32) || !std::isfinite(scale))
+        return PPD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(k_scale, 16) || !aligned(k_tree, 16) || !aligned(lse, 4) ||
+        !aligned(weight, 4))
+        return PPD_ERR_INVALID_ARG;
+    ppd::KvWeightParams p{};
+    p.q = q;
+    p.lse = lse;
+    p.k_cache = static_cast<const uint8_t *>(k_cache);
+    p.k_scale = k_scale;
+    p.k_tree = k_tree;
+    p.path = path, p.accept_len = accept_len, p.prefix_len = prefix_len;
+    p.weight = weight;
+    p.slices = (long long)L * B * H;
+    p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
+    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
+    p.splits = kv4_splits(p.slices, 1, T, S_max);
+    return cuda_status(ppd::launch_kv_weight(p, D, static_cast<cudaStream_t>(stream)));
+}
+
+ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *const *planes, void *const *out_planes,
+                        const int *row_bytes, int n_planes, const int32_t *length, int L, int B, int H, int S_max,
+                        int S_out, int budget, int n_sink, int n_recent, int32_t *kept, int32_t *new_len,
+                        int32_t *dev_status, void *stream)
+{
+    if (!weight || !out_weight || !length || !kept || !new_len || !dev_status || n_planes < 0 ||
+        n_planes >= ppd::kMaxPlanes || (n_planes > 0 && (!planes || !out_planes || !row_bytes)))
+        return PPD_ERR_INVALID_ARG;
+    const double slices = (double)L * B * H;
+    if (L < 1 || B < 1 || H < 1 || S_max < 1 || S_out < 1 || slices * 64 > 2147483647.0) return PPD_ERR_INVALID_ARG;
+    if (budget < 1 || budget > S_max || budget > S_out || n_sink < 0 || n_recent < 0 || n_sink > budget ||
+        n_recent > budget - n_sink)
+        return PPD_ERR_INVALID_ARG;
+    if (!aligned(weight, 4) || !aligned(out_weight, 4) || slices * S_max * 1024 > 9.0e15 || slices * S_out * 1024 > 9.0e15)
+        return PPD_ERR_INVALID_ARG;
+    ppd::KvEvictParams p{};
+    p.weight = weight;
+    p.length = length;
+    p.kept = kept;
+    p.new_len = new_len;
+    p.dev_status = dev_status;
+    p.slices = (long long)L * B * H;
+    p.B = B, p.H = H, p.S_max = S_max, p.S_out = S_out, p.budget = budget, p.sink = n_sink, p.recent = n_recent;
+    p.planes = n_planes + 1;
+    for (int i = 0; i <= n_planes; ++i) {
+        ppd::KvPlane &pl = p.plane[i];
+        pl.src = i < n_planes ? planes[i] : weight;
+        pl.dst = i < n_planes ? out_planes[i] : out_weight;
+        pl.row_bytes = i < n_planes ? row_bytes[i] : 4;
+        if (!pl.src || !pl.dst || pl.row_bytes < 1 || pl.row_bytes > 1024) return PPD_ERR_INVALID_ARG;
+        if (pl.src == pl.dst && S_out != S_max) return PPD_ERR_INVALID_ARG;
+        pl.unit = 16;
+        while (pl.row_bytes % pl.unit || !aligned(pl.src, pl.unit) || !aligned(pl.dst, pl.unit)) pl.unit /= 2;
+    }
+    // a destination may be its own source, and shares no byte with another plane
+    for (int i = 0; i < p.planes; ++i)
+        for (int j = 0; j < p.planes; ++j) {
+            const size_t ni = (size_t)p.slices * S_out * p.plane[i].row_bytes;
+            const size_t ns = (size_t)p.slices * S_max * p.plane[j].row_bytes;
+            const size_t nd = (size_t)p.slices * S_out * p.plane[j].row_bytes;
+            if (i != j && overlaps(p.plane[i].dst, ni, p.plane[j].dst, nd)) return PPD_ERR_INVALID_ARG;
+            if (!(i == j && p.plane[i].src == p.plane[i].dst) && overlaps(p.plane[i].dst, ni, p.plane[j].src, ns))
+                return PPD_ERR_INVALID_ARG;
+        }
+    for (int i = 0; i < p.planes; ++i) {
+        ppd::KvPlane &pl = p.plane[i];
+        const int per_row = pl.row_bytes / pl.unit;
+        if (pl.src == pl.dst) {
+            // in place: columns of 32 bytes or more, until the blocks fill the GPU twice
+            const int most = pl.row_bytes / 32;
+            pl.parts = 1;
+            while (pl.parts * 2 <= most && per_row % (pl.parts * 2) == 0 && p.slices * pl.parts < 4ll * num_sms()) pl.parts *= 2;
+        } else {
+            const long long steps = ((long long)budget * per_row + 1023) / 1024;
+            pl.parts = (int)((steps + 3) / 4);
+        }
+        p.move_blocks += pl.parts;
+    }
+    if ((double)p.slices * p.move_blocks > 2147483647.0) return PPD_ERR_UNSUPPORTED;
+    return cuda_status(ppd::launch_kv_evict(p, static_cast<cudaStream_t>(stream)));
+}
+
+ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, const int32_t *parent,
+                             const int32_t *prefix_len, const float *draft_probs, const int32_t *draft_row,
+                             const float *u, const float *noise, int B, int T, int V, int n_draft, int S_max,
+                             float temperature, int32_t *accept_len, int32_t *path, int32_t *next_token,
+                             int32_t *new_prefix_len, float *accept_prob, int32_t *dev_status, void *stream)
+{
+    if (!logits || !cand_tokens || !parent || !prefix_len || !u || !noise || !accept_len || !path || !next_token ||
+        !new_prefix_len || !dev_status || !draft_probs != !draft_row)
+        return PPD_ERR_INVALID_ARG;
+    if (B < 1 || T < 1 || T > kMaxT || V < 1 || S_max < 1 || (draft_probs && n_draft < 1) || (double)B * T * V > 9.0e15 ||
+        (double)B * 8 > 2147483647.0 || (draft_probs && (double)B * n_draft * V > 9.0e15))
+        return PPD_ERR_INVALID_ARG;
+    if (!std::isfinite(temperature) || temperature <= 0.f || !std::isfinite(1.4426950408889634f / temperature))
+        return PPD_ERR_INVALID_ARG;
+    if (!aligned(logits, 4) || !aligned(draft_probs, 4) || !aligned(u, 4) || !aligned(noise, 4) || !aligned(accept_prob, 4))
+        return PPD_ERR_INVALID_ARG;
+    const int cluster = ppd::kMaxCluster;
+    const int chunk = ((V + cluster - 1) / cluster + 3) & ~3;
+    if (chunk > ppd::kSampleMaxChunk) return PPD_ERR_UNSUPPORTED;
+    ppd::SampleParams p{logits, cand_tokens, parent, prefix_len, draft_probs, draft_row, u, noise, accept_len, path,
+                        next_token, new_prefix_len, dev_status, accept_prob, B, T, V, S_max, draft_probs ? n_draft : 0,
+                        1.4426950408889634f / temperature, chunk};
+    return cuda_status(ppd::launch_sample_accept(p, cluster, static_cast<cudaStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -271,6 +271,17 @@ PPD_DEV float4 ld_cluster_v4(uint32_t a)
     return v;
 }
 
+// Stores into a peer's shared memory; cluster_sync() makes them seen.
+PPD_DEV void st_cluster_v2(uint32_t a, float x, float y)
+{
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(x), "f"(y) : "memory");
+}
+
+PPD_DEV void st_cluster_u64(uint32_t a, unsigned long long v)
+{
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
+
 // ---------------------------------------------------------------- TMA
 
 PPD_DEV void tma_prefetch_map(const CUtensorMap *map)

@@ -1,0 +1,374 @@
+// ppd_evict.cu -- a cache cut down by attention weight: the weight that accepted tokens
+// gave each cached row, added up (ppd_kv_weight_add), and the rows kept (ppd_kv_evict).
+#include "ppd_kv4.cuh"
+
+namespace ppd {
+
+// ------------------------------------------------------------------ weight per cached row
+
+// A warp takes chunks of 32 keys of a slice: S = Q K^T by mma.sync for blocks of 16 of the
+// slice's G n accepted query rows, p = exp(scale S - lse), and each key's sum over the rows
+// by a halving exchange over the eight lanes that hold its column, which leaves one key
+// to each lane.  Keys are columns as in the attention of few rows: column c of a block of
+// eight is its row c / 2 + 4 (c % 2).  Tree keys come last: the path's own rows, each seen by
+// itself and the nodes after it.
+template <int D, bool KV4>
+__global__ void __launch_bounds__(128, 3) kv_weight_kernel(const KvWeightParams p)
+{
+    __shared__ int path_s[kMaxTree];
+    pdl_release();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int split = (int)(blockIdx.x % p.splits);
+    const long long u = blockIdx.x / p.splits;
+    const int b = (int)(u / p.H % p.B);
+    const int T = p.T;
+    const int P = ld_input(p.prefix_len + b);
+    const int n = min(ld_input(p.accept_len + b), T);
+    if (n < 1 || P < 0 || P > p.S_max) return;   // uniform over the block
+    for (int i = threadIdx.x; i < n; i += 128) path_s[i] = ld_input(p.path + (size_t)b * T + i);
+    __syncthreads();
+    const int n_pref = (P + 31) / 32, n_all = n_pref + (n + 31) / 32;
+    const int c0 = (int)((long long)n_all * split / p.splits), c1 = (int)((long long)n_all * (split + 1) / p.splits);
+    const int rows = p.G * n, blocks = (rows + 15) / 16;
+    const size_t row0 = (size_t)u * p.S_max;
+    const int perm = (g >> 1) + 4 * (g & 1);
+    // first channel of step s of a quad's thread: as the thread's loads of K bring them
+    auto channel = [&](int s) { return KV4 ? (D / 4) * t + 4 * s : 32 * (s >> 1) + 8 * t + 4 * (s & 1); };
+
+    uint32_t q[D / 16][4];
+    float neg_lse[2];
+    int at_a[2];   // the rows' places on the path
+    auto load_rows = [&](int block) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = block * 16 + g + 8 * h;
+            const int a = r % n, node = r < rows ? path_s[a] : -1;
+            const bool real = node >= 0 && node < T;
+            const size_t row = ((size_t)u * p.G + (real ? r / n : 0)) * T + (real ? node : 0);
+            at_a[h] = a;
+            neg_lse[h] = real ? -1.4426950408889634f * ld_input(p.lse + row) : -INFINITY;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                q[s][h] = real ? ld_pair(p.q, row * D + channel(s), p.f32) : 0u;
+                q[s][2 + h] = real ? ld_pair(p.q, row * D + channel(s) + 2, p.f32) : 0u;
+            }
+        }
+    };
+    load_rows(0);
+
+    // K of a chunk in registers: the codes of four keys (and each lane's key's scales), or
+    // their bf16 channels
+    constexpr int KW = KV4 ? D / 32 : D / 8;   // words of a key in a thread
+    struct Keys {
+        uint32_t w[4][KW];
+        uint32_t scale;
+    };
+    auto load_keys = [&](int c, Keys &k) {
+        const int k0 = c * 32;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = k0 + 8 * i + perm;
+            const size_t row = row0 + (j < P ? j : 0);
+            if constexpr (KV4 && D == 128) {
+                const uint4 v = j < P ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * 64) + t) : make_uint4(0, 0, 0, 0);
+                k.w[i][0] = v.x, k.w[i][1] = v.y, k.w[i][2] = v.z, k.w[i][3] = v.w;
+            } else if constexpr (KV4) {
+                uint2 v = make_uint2(0, 0);
+                if (j < P)
+                    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p.k_cache + row * 32 + t * 8) : "memory");
+                k.w[i][0] = v.x, k.w[i][1] = v.y;
+            } else {
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {
+                    const uint4 v = j < P ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * D * 2) + 4 * x + t) : make_uint4(0, 0, 0, 0);
+                    k.w[i][4 * x] = v.x, k.w[i][4 * x + 1] = v.y, k.w[i][4 * x + 2] = v.z, k.w[i][4 * x + 3] = v.w;
+                }
+            }
+        }
+        k.scale = 0;
+        if (KV4 && k0 + lane < P) {
+            const uint8_t *s = p.k_scale + (row0 + k0 + lane) * (D / kKv4Group);
+            if constexpr (D == 128) k.scale = (uint32_t)ld_input(reinterpret_cast<const int *>(s));
+            else asm volatile("ld.global.u16 %0, [%1];" : "=r"(k.scale) : "l"(s) : "memory");
+        }
+    };
+    // 4-bit keys a chunk ahead; bf16 ones fill the registers as they are
+    Keys cur, nxt;
+    int c = c0 + warp;
+    if (KV4 && c < min(c1, n_pref)) load_keys(c, nxt);
+    for (; c < c1; c += 4) {
+        const bool tree = c >= n_pref;
+        const int k0 = (tree ? c - n_pref : c) * 32;
+        if constexpr (KV4) {
+            cur = nxt;
+            if (c + 4 < min(c1, n_pref)) load_keys(c + 4, nxt);
+        } else if (!tree) {
+            load_keys(c, cur);
+        }
+        const int mine = k0 + 8 * (g >> 1) + t + 4 * (g & 1);   // this lane's key in the end
+        const bool stays = tree ? mine < n && P + mine < p.S_max : mine < P;
+        float *out = p.weight + row0 + (tree ? P : 0) + (stays ? mine : 0);
+        float old = 0.f;
+        if (stays && !tree) old = ld_input(out);
+        float sum[8] = {};
+        for (int block = 0; block < blocks; ++block) {
+            if (blocks > 1) load_rows(block);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                if (tree) {
+                    const int a = k0 + 8 * i + perm, node = a < n ? path_s[a] : -1;
+                    const bool real = node >= 0 && node < T;
+                    const size_t row = ((size_t)u * T + (real ? node : 0)) * D;
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_bf16(s, q[x], real ? ld_pair(p.k_tree, row + channel(x), p.f32) : 0u,
+                                 real ? ld_pair(p.k_tree, row + channel(x) + 2, p.f32) : 0u);
+                } else if constexpr (KV4) {
+                    const uint32_t sw = __shfl_sync(0xffffffffu, cur.scale, 8 * i + perm);
+                    const uint32_t s2 = kv4_scale2(((sw >> (D == 128 ? 8 * t : 8 * (t >> 1))) & 0xFFu) * 0x10001u);
+                    const uint32_t o2 = kv4_offset2(s2);
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x)
+                        mma_bf16(s, q[x], kv4_pair(cur.w[i][x >> 1] >> (8 * (x & 1)), s2, o2),
+                                 kv4_pair(cur.w[i][x >> 1] >> (8 * (x & 1) + 4), s2, o2));
+                } else {
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) mma_bf16(s, q[x], cur.w[i][2 * x], cur.w[i][2 * x + 1]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float w = ex2(fmaf(s[e], p.scale_log2, neg_lse[e >> 1]));
+                    if (tree && at_a[e >> 1] < k0 + 8 * i + t + 4 * (e & 1)) w = 0.f;   // a later node's row
+                    sum[2 * i + (e & 1)] += w;
+                }
+            }
+        }
+        // eight values over the eight lanes of equal t: lane (g, t) ends with value g
+#pragma unroll
+        for (int half = 4; half >= 1; half >>= 1) {
+            const bool up = (g & half) != 0;
+#pragma unroll
+            for (int i = 0; i < half; ++i) {
+                const float send = up ? sum[i] : sum[i + half], keep = up ? sum[i + half] : sum[i];
+                sum[i] = keep + __shfl_xor_sync(0xffffffffu, send, 4 * half);
+            }
+        }
+        if (stays) *out = old + sum[0];
+    }
+}
+
+template <int D>
+static cudaError_t launch_weight_t(const KvWeightParams &p, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)(p.slices * p.splits));
+    return p.k_scale ? launch_chained(kv_weight_kernel<D, true>, grid, dim3(128), dim3(1), stream, p)
+                     : launch_chained(kv_weight_kernel<D, false>, grid, dim3(128), dim3(1), stream, p);
+}
+
+cudaError_t launch_kv_weight(const KvWeightParams &p, int D, cudaStream_t stream)
+{
+    return D == 128 ? launch_weight_t<128>(p, stream) : launch_weight_t<64>(p, stream);
+}
+
+// ------------------------------------------------------------------ the rows to keep
+
+constexpr int kSelThreads = 512, kSelBins = 2048;
+
+// Weights in order as unsigned numbers (-0 as +0); a NaN above every number.
+PPD_DEV uint32_t weight_rank(float w)
+{
+    if (w != w) return 0xFFFFFFFEu;
+    const uint32_t x = __float_as_uint(w + 0.f);
+    return x & 0x80000000u ? ~x : x | 0x80000000u;
+}
+
+// One block per slice: the rank of the last row kept by three rounds of counting (11, 11
+// and 10 bits), then one ordered pass that writes the kept rows' indices: all above that
+// rank, and of those equal to it the first ones.  The first and last rows rank above all.
+__global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvEvictParams p)
+{
+    __shared__ uint32_t hist[kSelBins];
+    __shared__ uint32_t warp_sum[2][kSelThreads / 32];
+    __shared__ uint32_t found[2];   // the bin, and how many rows rank above it
+    pdl_release();
+    pdl_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long u = blockIdx.x;
+    const int b = (int)(u / p.H % p.B);
+    const int len = ld_input(p.length + b);
+    const bool bad = len < 0 || len > p.S_max;
+    if (u / p.H < p.B && u % p.H == 0 && tid == 0) {
+        p.dev_status[b] = bad ? kErrCapacity : kOk;
+        p.new_len[b] = bad ? len : min(len, p.budget);
+    }
+    int32_t *kept = p.kept + (size_t)u * p.budget;
+    if (bad || len <= p.budget) {
+        for (int i = tid; i < p.budget; i += kSelThreads) kept[i] = !bad && i < len ? i : -1;
+        return;
+    }
+    const float *w = p.weight + (size_t)u * p.S_max;
+    auto rank = [&](int j) {
+        return j < p.sink || j >= len - p.recent ? 0xFFFFFFFFu : weight_rank(ld_input(w + j));
+    };
+    uint32_t prefix = 0, need = (uint32_t)p.budget;   // of the rows with the digits found so far, `need` are kept
+    int shift = 32;
+    for (int round = 0; round < 3; ++round) {
+        const int bits = round < 2 ? 11 : 10, bins = 1 << bits;
+        const uint32_t above = shift == 32 ? 0u : 0xFFFFFFFFu << shift;
+        shift -= bits;
+        for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < len; j += kSelThreads) {
+            const uint32_t r = rank(j);
+            if ((r & above) == prefix) atomicAdd(hist + ((r >> shift) & (bins - 1)), 1u);
+        }
+        __syncthreads();
+        // rows ranking in a higher bin, from the top: thread i has bins 4 i .. of the order
+        constexpr int per = kSelBins / kSelThreads;
+        uint32_t c[per], s = 0;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const int bin = bins - 1 - (tid * per + i);
+            c[i] = bin >= 0 ? hist[bin] : 0u;
+            s += c[i];
+        }
+        uint32_t inc = s;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += x;
+        }
+        if (lane == 31) warp_sum[0][warp] = inc;
+        __syncthreads();
+        uint32_t before = inc - s;
+        for (int i = 0; i < warp; ++i) before += warp_sum[0][i];
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            if (before < need && need <= before + c[i]) {
+                found[0] = (uint32_t)(bins - 1 - (tid * per + i));
+                found[1] = before;
+            }
+            before += c[i];
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        need -= found[1];
+        __syncthreads();
+    }
+    // rows ranking above `prefix`, and the first `need` that equal it, in order
+    uint32_t n_out = 0, n_eq = 0;
+    for (int j0 = 0; j0 < len; j0 += kSelThreads) {
+        const int j = j0 + tid;
+        const uint32_t r = j < len ? rank(j) : 0u;
+        const uint32_t gt = __ballot_sync(0xffffffffu, j < len && r > prefix);
+        const uint32_t eq = __ballot_sync(0xffffffffu, j < len && r == prefix);
+        if (lane == 0) warp_sum[0][warp] = __popc(gt) | (uint32_t)__popc(eq) << 16;
+        __syncthreads();
+        uint32_t g_before = 0, e_before = 0, g_all = 0, e_all = 0;
+#pragma unroll
+        for (int i = 0; i < kSelThreads / 32; ++i) {
+            const uint32_t x = warp_sum[0][i];
+            if (i < warp) g_before += x & 0xFFFFu, e_before += x >> 16;
+            g_all += x & 0xFFFFu, e_all += x >> 16;
+        }
+        const uint32_t low = (1u << lane) - 1u;
+        const uint32_t my_g = g_before + __popc(gt & low), my_e = n_eq + e_before + __popc(eq & low);
+        const bool is_g = (gt >> lane) & 1u, is_e = ((eq >> lane) & 1u) && my_e < need;
+        // kept rows before this one: those above, and the equal ones taken so far
+        if (is_g || is_e) kept[n_out + my_g + (min(my_e, need) - min(n_eq, need))] = j;
+        n_out += g_all + (min(n_eq + e_all, need) - min(n_eq, need));
+        n_eq += e_all;
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ moving them
+
+template <int BYTES>
+struct MoveUnit;
+template <> struct MoveUnit<16> { using T = uint4; };
+template <> struct MoveUnit<8> { using T = uint2; };
+template <> struct MoveUnit<4> { using T = uint32_t; };
+template <> struct MoveUnit<2> { using T = uint16_t; };
+template <> struct MoveUnit<1> { using T = uint8_t; };
+
+constexpr int kMoveThreads = 256, kMoveDeep = 4;
+
+// Kept row i goes to row i of the destination: each step of a block reads 1024 units (16
+// bytes where rows and addresses allow), then writes them.  In place a block takes its
+// columns of the whole slice alone, in order: the rows of a step lie at or above their places,
+// and so do those of every later step, so what a step overwrites has been read.
+template <int BYTES>
+PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, long long u, int c0, int c1, int i0, int i1)
+{
+    using T = typename MoveUnit<BYTES>::T;
+    const T *src = reinterpret_cast<const T *>(static_cast<const uint8_t *>(pl.src) + (size_t)u * p.S_max * pl.row_bytes);
+    T *dst = reinterpret_cast<T *>(static_cast<uint8_t *>(pl.dst) + (size_t)u * p.S_out * pl.row_bytes);
+    const int per_row = pl.row_bytes / BYTES, w = c1 - c0;   // this block's units of a row
+    const bool in_place = pl.src == pl.dst;
+    const int rows = kMoveThreads * kMoveDeep / w;           // of a step (w divides the threads or is below)
+    for (int r0 = i0; r0 < i1; r0 += rows) {
+        T v[kMoveDeep];
+        bool go[kMoveDeep];
+#pragma unroll
+        for (int x = 0; x < kMoveDeep; ++x) {
+            const int unit = x * kMoveThreads + (int)threadIdx.x, row = unit / w;
+            const int i = r0 + row;
+            go[x] = row < rows && i < i1;
+            const int from = go[x] ? ld_input(kept + i) : -1;
+            go[x] = go[x] && from >= 0 && !(in_place && from == i);
+            if (go[x]) v[x] = src[(size_t)from * per_row + c0 + unit % w];
+        }
+        if (in_place) __syncthreads();
+#pragma unroll
+        for (int x = 0; x < kMoveDeep; ++x) {
+            const int unit = x * kMoveThreads + (int)threadIdx.x;
+            if (go[x]) dst[(size_t)(r0 + unit / w) * per_row + c0 + unit % w] = v[x];
+        }
+    }
+}
+
+// A slice's blocks: those of each plane in turn, each a range of rows (to another cache) or
+// of columns (in place).
+__global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const KvEvictParams p)
+{
+    pdl_release();
+    pdl_wait();
+    const long long u = blockIdx.x / p.move_blocks;
+    int part = (int)(blockIdx.x % p.move_blocks), x = 0;
+    while (part >= p.plane[x].parts) part -= p.plane[x++].parts;
+    const KvPlane &pl = p.plane[x];
+    const int b = (int)(u / p.H % p.B);
+    const int len = ld_input(p.length + b);
+    if (len < 0 || len > p.S_max) return;
+    const int n = min(len, p.budget);
+    if (pl.src == pl.dst && len <= p.budget) return;   // every row is in its place
+    const int32_t *kept = p.kept + (size_t)u * p.budget;
+    const int per_row = pl.row_bytes / pl.unit;
+    int c0 = 0, c1 = per_row, i0 = 0, i1 = n;
+    if (pl.src == pl.dst) {
+        c0 = per_row * part / pl.parts;
+        c1 = per_row * (part + 1) / pl.parts;
+    } else {
+        i0 = (int)((long long)p.budget * part / pl.parts);
+        i1 = min(n, (int)((long long)p.budget * (part + 1) / pl.parts));
+    }
+    switch (pl.unit) {
+    case 16: move_rows<16>(p, pl, kept, u, c0, c1, i0, i1); break;
+    case 8: move_rows<8>(p, pl, kept, u, c0, c1, i0, i1); break;
+    case 4: move_rows<4>(p, pl, kept, u, c0, c1, i0, i1); break;
+    case 2: move_rows<2>(p, pl, kept, u, c0, c1, i0, i1); break;
+    default: move_rows<1>(p, pl, kept, u, c0, c1, i0, i1); break;
+    }
+}
+
+cudaError_t launch_kv_evict(const KvEvictParams &p, cudaStream_t stream)
+{
+    const cudaError_t e = launch_chained(kv_select_kernel, dim3((unsigned)p.slices), dim3(kSelThreads), dim3(1), stream, p);
+    if (e != cudaSuccess) return e;
+    return launch_chained(kv_move_kernel, dim3((unsigned)(p.slices * p.move_blocks)), dim3(kMoveThreads), dim3(1), stream, p);
+}
+
+}  // namespace ppd

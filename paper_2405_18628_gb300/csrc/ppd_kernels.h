@@ -255,6 +255,44 @@ inline cudaError_t launch_chained(void (*kern)(KArgs...), dim3 grid, dim3 block,
     return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// The same with dynamic shared memory (allowed first, once per kernel and device).
+template <typename Kern>
+inline cudaError_t allow_smem(Kern kern, uint32_t bytes, std::atomic<uint64_t> &configured)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? (1ull << dev) : 0ull;
+    if (bit && (configured.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) configured.fetch_or(bit, std::memory_order_acq_rel);
+    return e;
+}
+
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_chained_smem(void (*kern)(KArgs...), dim3 grid, dim3 block, dim3 cluster,
+                                       uint32_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (cluster.x * cluster.y * cluster.z > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster.x;
+        attr[1].val.clusterDim.y = cluster.y;
+        attr[1].val.clusterDim.z = cluster.z;
+        cfg.numAttrs = 2;
+    }
+    cfg.attrs = attr;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
 // Splits per node row of the argmax: about 512 blocks over all rows, chunks of
 // at least 2048 logits, at most 64 splits.
 inline int argmax_split_count(int64_t rows, int V)
@@ -355,6 +393,103 @@ cudaError_t launch_round_bf16(const RoundArgs &r, int64_t lbh, bool chained, cud
 // Zero `n` status words once the preceding grid has completed, as a
 // programmatic dependent launch that lets the next grid launch at once.
 cudaError_t launch_zero_status(int32_t *status, int n, cudaStream_t stream);
+
+// ---- 4-bit cache (ppd_kv4.cuh has the format): slices = L * B * H
+struct Kv4AppendParams {
+    const void *k_new, *v_new;       // [slices][T][D] bf16 or (f32) fp32
+    uint8_t *k_cache, *v_cache;      // [slices][S_max][D / 2]
+    uint8_t *k_scale, *v_scale;      // [slices][S_max][D / 32]
+    const int32_t *rows;             // [B,T] or null
+    const int32_t *start, *n_new;    // [B]
+    int32_t *dev_status;             // [B]
+    long long slices;
+    int B, H, T, D, S_max, f32;
+};
+cudaError_t launch_kv4_append(const Kv4AppendParams &p, cudaStream_t stream);
+
+struct Kv4ReadParams {
+    const uint8_t *cache, *scale;    // K's or V's
+    const int32_t *start, *n;        // [B]
+    void *out;                       // [slices][N][D] bf16 or fp32
+    long long slices;
+    int B, H, N, D, S_max, f32;
+};
+cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream);
+
+// Attention over a 4-bit cache: query rows of a slice are its G heads' T tokens.
+struct Kv4AttnParams {
+    const void *q;                   // [slices][G * T][D] bf16 or fp32
+    const uint8_t *k_cache, *k_scale, *v_cache, *v_scale;
+    const void *k_tree, *v_tree;     // [slices][T][D]
+    const int32_t *prefix_len, *parent;
+    uint16_t *out;                   // bf16 [slices][G * T][D]
+    float *lse;                      // [slices][G * T] or null
+    int32_t *dev_status;
+    size_t scale_bytes;              // of k_scale, and of v_scale
+    long long slices;
+    int B, H, G, T, S_max, f32;
+    float scale_log2;                // softmax scale * log2(e)
+    int row_blocks;                  // blocks of query rows of a slice
+    int splits;                      // parts that a slice's keys are shared out to
+    float *part_o;                   // splits > 1: [slices][splits][G * T][D] unnormalised outputs
+    float2 *part_ml;                 // [slices][splits][G * T] maxima (log2) and sums
+};
+cudaError_t launch_kv4_attention(const Kv4AttnParams &p, int D, cudaStream_t stream);
+
+// Attention weight of the accepted nodes, added up per cached row.
+struct KvWeightParams {
+    const void *q;                   // [slices][G][T][D] bf16 or fp32
+    const float *lse;                // [slices][G][T]
+    const uint8_t *k_cache;          // bf16 rows, or codes with
+    const uint8_t *k_scale;          // their scales (null: bf16)
+    const void *k_tree;              // [slices][T][D]
+    const int32_t *path, *accept_len, *prefix_len;
+    float *weight;                   // [slices][S_max]
+    long long slices;
+    int B, H, G, T, S_max, f32;
+    float scale_log2;
+    int splits;                      // blocks of a slice
+};
+cudaError_t launch_kv_weight(const KvWeightParams &p, int D, cudaStream_t stream);
+
+// The rows kept of each slice, and the planes they are rows of.
+struct KvPlane {
+    const void *src;                 // [slices][S_max][row_bytes]
+    void *dst;                       // [slices][S_out][row_bytes]; src: in place
+    int row_bytes, unit;             // bytes moved at once: a power of two up to 16
+    int parts;                       // blocks of a slice
+};
+constexpr int kMaxPlanes = 9;        // eight of the caller's, and the weights
+struct KvEvictParams {
+    const float *weight;             // [slices][S_max]
+    const int32_t *length;           // [B]
+    int32_t *kept;                   // [slices][budget]
+    int32_t *new_len, *dev_status;   // [B]
+    long long slices;
+    int B, H, S_max, S_out, budget, sink, recent;
+    KvPlane plane[kMaxPlanes];
+    int planes, move_blocks;         // the planes' parts together
+};
+cudaError_t launch_kv_evict(const KvEvictParams &p, cudaStream_t stream);
+
+// Drafted tokens verified with given random numbers.
+struct SampleParams {
+    const float *logits;             // [B,T,V]
+    const int32_t *cand, *parent;    // [B,T]
+    const int32_t *prefix_len;       // [B]
+    const float *draft_probs;        // [B,n_draft,V] or null
+    const int32_t *draft_row;        // [B,T] or null
+    const float *u;                  // [B,T]
+    const float *noise;              // [B,V]
+    int32_t *accept_len, *path, *next_token, *new_prefix_len, *dev_status;
+    float *accept_prob;              // [B,T] or null
+    int B, T, V, S_max, n_draft;
+    float k;                         // log2(e) / temperature
+    int chunk;                       // logits of a CTA of the cluster (a multiple of 4)
+};
+// Logits of a CTA at most (its shared memory).
+constexpr int kSampleMaxChunk = 48 * 1024;
+cudaError_t launch_sample_accept(const SampleParams &p, int cluster, cudaStream_t stream);
 
 cudaError_t launch_selftest_umma(const CUtensorMap &ma, const CUtensorMap &mb, const void *a_raw,
                                  const void *b_raw, float *d, int mode, int N, cudaStream_t stream);

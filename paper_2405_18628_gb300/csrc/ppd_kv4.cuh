@@ -1,0 +1,113 @@
+// ppd_kv4.cuh -- the 4-bit cache format, and what the kernels that read it share.
+//
+// A row of D channels is D / 2 bytes of codes and one scale byte for each 32 channels.
+// A 32-bit word holds eight channels: nibble p is channel 2 (p % 4) + p / 4, so that one
+// mask takes a pair of neighbouring channels out of a word into the halves of a register.
+// A code c stands for s (c - 8), a scale byte b for s = (1 + (b % 8) / 8) 2^(b / 8 - 20).
+// s has four significant bits and c - 8 at most three, so that every value is a bf16
+// number: the tensor cores multiply exactly what the cache holds.
+#pragma once
+
+#include "ppd_device.cuh"
+
+#include <cuda_bf16.h>
+#include <cstdint>
+
+namespace ppd {
+
+constexpr int kKv4Group = 32;   // channels of a scale
+
+// A scale byte as bf16 bits in both halves of a register: `two` holds the byte in bits
+// 0..7 and in bits 16..23.  The byte's exponent field counts from 2^-20, bf16's from 2^-127.
+PPD_DEV uint32_t kv4_scale2(uint32_t two) { return (two + 0x03580358u) << 4; }
+
+PPD_DEV float kv4_scale(uint32_t b) { return __uint_as_float((b + 856u) << 20); }
+
+PPD_DEV uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+
+// -136 s for a pair of scales (17 times four significant bits: exact).
+PPD_DEV uint32_t kv4_offset2(uint32_t s2) { return bf16x2_fma(s2, 0xC308C308u, 0x80008000u); }
+
+// The values of two codes, in bits 0..3 and 16..19 of `pair` (other bits ignored): the
+// codes become the low bits of 128 + c, and one fused multiply-add gives s (128 + c) - 136 s.
+PPD_DEV uint32_t kv4_pair(uint32_t pair, uint32_t s2, uint32_t o2)
+{
+    return bf16x2_fma((pair & 0x000F000Fu) | 0x43004300u, s2, o2);
+}
+
+// Two fp32 values as a bf16 pair, the first in the low half.
+PPD_DEV uint32_t bf16x2(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// D += A B: A 16 x 16 rows of bf16, B 16 x 8, fp32 accumulators.
+PPD_DEV void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Asynchronous copies into shared memory; bytes beyond `n` of the 16 (or 4) read as zero.
+PPD_DEV void cp_async16(uint32_t dst, const void *src, uint32_t n)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+PPD_DEV void cp_async4(uint32_t dst, const void *src, uint32_t n)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+PPD_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+PPD_DEV void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+PPD_DEV uint32_t ld_shared_u32(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+PPD_DEV uint2 ld_shared_u64(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+PPD_DEV uint4 ld_shared_u128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+// Element i, i + 1 of a bf16 or fp32 tensor as a bf16 pair (fp32 rounded to nearest);
+// i even.
+PPD_DEV uint32_t ld_pair(const void *p, size_t i, bool f32)
+{
+    if (!f32) return (uint32_t)ld_input(reinterpret_cast<const int *>(p) + (i >> 1));
+    const float *f = reinterpret_cast<const float *>(p) + i;
+    return bf16x2(ld_input(f), ld_input(f + 1));
+}
+
+// What dev_status says of a sequence: a malformed tree, or a prefix outside the cache.
+// Every lane of one warp gets the answer.
+PPD_DEV int tree_status(const int32_t *parent, int T, int prefix, int S_max, int lane)
+{
+    bool bad = false;
+    for (int i = lane; i < T; i += 32) {
+        const int p = ld_input(parent + i);
+        bad |= i == 0 ? p != -1 : (p < 0 || p >= i);
+    }
+    if (__any_sync(0xffffffffu, bad)) return kErrTree;
+    return prefix < 0 || prefix > S_max ? kErrCapacity : kOk;
+}
+
+}  // namespace ppd

@@ -66,6 +66,13 @@ def load() -> ctypes.CDLL:
                                   [vp, sz, vp], i32),
             "ppd_next_tree": ([vp] * 6 + [i32] * 5 + [vp, vp, i32, i32] + [vp] * 4 + [vp, sz, vp],
                               i32),
+            "ppd_kv4_append": ([vp] * 9 + [i32] * 7 + [vp, vp], i32),
+            "ppd_kv4_read": ([vp] * 4 + [i32] * 6 + [vp, i32, vp], i32),
+            "ppd_kv4_attention_workspace_bytes": ([i32] * 7, sz),
+            "ppd_tree_attention_kv4": ([vp] * 9 + [i32] * 8 + [f32, vp, vp, vp, vp, sz, vp], i32),
+            "ppd_kv_weight_add": ([vp] * 8 + [i32] * 8 + [f32, vp, vp], i32),
+            "ppd_kv_evict": ([vp] * 5 + [i32, vp] + [i32] * 8 + [vp] * 4, i32),
+            "ppd_sample_accept": ([vp] * 8 + [i32] * 5 + [f32] + [vp] * 7, i32),
             "ppd_verify_step_typical": ([vp] * 9 + [i32] * 8 + [f32] * 4 + [vp] * 8 +
                                         [vp, sz, vp], i32),
         }
@@ -277,6 +284,166 @@ def ppd_next_tree(logits, parent, cand_tokens, path, accept_len, next_token, tmp
     st = load().ppd_next_tree_ept(*a[:6], B, T, V, n_states, T_next, *a[6:8], int(K), int(n_ept),
                                   int(ept_mean == "probs"), *a[8:], workspace.numel(), _stream(stream))
     _check(st, "ppd_next_tree")
+
+
+def _kv4(codes, scales):
+    """Checks a 4-bit cache's pair of tensors; returns its head dim."""
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise TypeError("a 4-bit cache is uint8 codes and uint8 scales")
+    D = 2 * codes.shape[-1]
+    if scales.shape != (*codes.shape[:-1], D // 32):
+        raise ValueError(f"scales of codes {tuple(codes.shape)} are {(*codes.shape[:-1], D // 32)}, not {tuple(scales.shape)}")
+    return D
+
+
+def _shape(t, name, *want):
+    if t is not None and tuple(t.shape) != want:
+        raise ValueError(f"{name} is {want}, not {tuple(t.shape)}")
+
+
+def _is(dtype, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def kv4_cache(L, B, H, S_max, D, device="cuda"):
+    """An empty 4-bit cache of K, or of V: codes [L,B,H,S_max,D/2] and scales [L,B,H,S_max,D/32]."""
+    return (torch.zeros((L, B, H, S_max, D // 2), dtype=torch.uint8, device=device),
+            torch.zeros((L, B, H, S_max, D // 32), dtype=torch.uint8, device=device))
+
+
+def ppd_kv4_append(k_new, v_new, k_cache, k_scale, v_cache, v_scale, start, n_new, dev_status,
+                   rows=None, stream=None):
+    """Rows k_new, v_new [L,B,H,T,D] (those of rows [B,T], or all in order), n_new [B] of them,
+    quantised into a 4-bit cache from row start [B] on."""
+    L, B, H, T, D = k_new.shape
+    S_max = k_cache.shape[3]
+    for c, s in ((k_cache, k_scale), (v_cache, v_scale)):
+        _kv4(c, s)
+        _shape(c, "the cache", L, B, H, S_max, D // 2)
+    _shape(v_new, "v_new", L, B, H, T, D)
+    _is(k_new.dtype, v_new=v_new)
+    _is(torch.int32, start=start, n_new=n_new, dev_status=dev_status, rows=rows)
+    _shape(start, "start", B), _shape(n_new, "n_new", B), _shape(dev_status, "dev_status", B), _shape(rows, "rows", B, T)
+    a = _ptrs(k_new, v_new, k_cache, k_scale, v_cache, v_scale, rows, start, n_new, dev_status)
+    st = load().ppd_kv4_append(*a[:9], L, B, H, T, D, S_max, _dtype(k_new), a[9], _stream(stream))
+    _check(st, "ppd_kv4_append")
+
+
+def ppd_kv4_read(cache, scale, start, n, out, stream=None):
+    """Rows start .. start + n - 1 [B] of a 4-bit cache as bf16 or fp32 values: out [L,B,H,N,D], zero from row n on."""
+    L, B, H, N, D = out.shape
+    S_max = cache.shape[3]
+    _kv4(cache, scale)
+    _shape(cache, "the cache", L, B, H, S_max, D // 2)
+    _is(torch.int32, start=start, n=n)
+    _shape(start, "start", B), _shape(n, "n", B)
+    a = _ptrs(cache, scale, start, n, out)
+    st = load().ppd_kv4_read(*a[:4], L, B, H, N, D, S_max, a[4], _dtype(out), _stream(stream))
+    _check(st, "ppd_kv4_read")
+
+
+def ppd_kv4_attention_workspace_bytes(L, B, H, G, T, D, S_max) -> int:
+    return int(load().ppd_kv4_attention_workspace_bytes(L, B, H, G, T, D, S_max))
+
+
+def ppd_tree_attention_kv4(q, k_cache, k_scale, v_cache, v_scale, k_tree, v_tree, prefix_len, parent, out,
+                           dev_status, lse=None, scale: float = 0.0, workspace=None, stream=None):
+    """Tree attention over a 4-bit cache: q [L,B,H*G,T,D] (bf16 or fp32), k_tree/v_tree [L,B,H,T,D], out bf16
+    [L,B,H*G,T,D].  Without a workspace the keys of a slice are not shared out to several SMs."""
+    L, B, Hq, T, D = q.shape
+    H, S_max = k_cache.shape[2:4]
+    for c, s in ((k_cache, k_scale), (v_cache, v_scale)):
+        _kv4(c, s)
+        _shape(c, "the cache", L, B, H, S_max, D // 2)
+    if H < 1 or Hq % H:
+        raise ValueError(f"{Hq} query heads over {H} K/V heads")
+    _shape(k_tree, "k_tree", L, B, H, T, D), _shape(v_tree, "v_tree", L, B, H, T, D)
+    _shape(out, "out", L, B, Hq, T, D), _shape(lse, "lse", L, B, Hq, T)
+    _shape(parent, "parent", B, T), _shape(prefix_len, "prefix_len", B), _shape(dev_status, "dev_status", B)
+    _is(q.dtype, k_tree=k_tree, v_tree=v_tree)
+    _is(torch.bfloat16, out=out), _is(torch.float32, lse=lse)
+    _is(torch.int32, prefix_len=prefix_len, parent=parent, dev_status=dev_status)
+    ws_n = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    a = _ptrs(q, k_cache, k_scale, v_cache, v_scale, k_tree, v_tree, prefix_len, parent, out, lse, dev_status, workspace)
+    st = load().ppd_tree_attention_kv4(*a[:9], L, B, H, Hq // H, T, D, S_max, _dtype(q), float(scale), *a[9:],
+                                       ws_n, _stream(stream))
+    _check(st, "ppd_tree_attention_kv4")
+
+
+def ppd_kv_weight_add(q, lse, k_cache, k_tree, path, accept_len, prefix_len, weight, k_scale=None,
+                      scale: float = 0.0, stream=None):
+    """Adds to weight fp32 [L,B,H,S_max] the attention that the accepted nodes gave each cached row of a bf16
+    cache [L,B,H,S_max,D], or with k_scale of a 4-bit one; the new rows' weights are set."""
+    L, B, Hq, T, D = q.shape
+    H, S_max = k_cache.shape[2:4]
+    if k_scale is not None:
+        _kv4(k_cache, k_scale)
+    else:
+        _is(torch.bfloat16, k_cache=k_cache)
+    _shape(k_cache, "the cache", L, B, H, S_max, D if k_scale is None else D // 2)
+    if H < 1 or Hq % H:
+        raise ValueError(f"{Hq} query heads over {H} K/V heads")
+    _shape(lse, "lse", L, B, Hq, T), _shape(k_tree, "k_tree", L, B, H, T, D), _shape(weight, "weight", L, B, H, S_max)
+    _shape(path, "path", B, T), _shape(accept_len, "accept_len", B), _shape(prefix_len, "prefix_len", B)
+    _is(q.dtype, k_tree=k_tree), _is(torch.float32, lse=lse, weight=weight)
+    _is(torch.int32, path=path, accept_len=accept_len, prefix_len=prefix_len)
+    a = _ptrs(q, lse, k_cache, k_scale, k_tree, path, accept_len, prefix_len, weight)
+    st = load().ppd_kv_weight_add(*a[:8], L, B, H, Hq // H, T, D, S_max, _dtype(q), float(scale), a[8], _stream(stream))
+    _check(st, "ppd_kv_weight_add")
+
+
+def ppd_kv_evict(weight, planes, length, budget: int, n_sink: int, n_recent: int, kept, new_len, dev_status,
+                 out_weight=None, out_planes=None, stream=None):
+    """Cuts a cache down to `budget` rows per head by weight fp32 [L,B,H,S_max].  planes: its tensors
+    [L,B,H,S_max,...], moved in place or into out_planes [L,B,H,S_out,...] (with out_weight)."""
+    L, B, H, S_max = weight.shape
+    if (out_planes is None) != (out_weight is None):
+        raise ValueError("out_planes and out_weight are given together")
+    out_planes, out_weight = (planes, weight) if out_planes is None else (out_planes, out_weight)
+    S_out = out_weight.shape[3]
+    _shape(out_weight, "out_weight", L, B, H, S_out)
+    _is(torch.float32, weight=weight, out_weight=out_weight)
+    _is(torch.int32, length=length, kept=kept, new_len=new_len, dev_status=dev_status)
+    _shape(kept, "kept", L, B, H, int(budget))
+    _shape(length, "length", B), _shape(new_len, "new_len", B), _shape(dev_status, "dev_status", B)
+    if len(planes) != len(out_planes):
+        raise ValueError("as many out_planes as planes")
+    n = len(planes)
+    row = []
+    for x, y in zip(planes, out_planes):
+        _shape(x, "a plane", L, B, H, S_max, *x.shape[4:])
+        _shape(y, "an out plane", L, B, H, S_out, *x.shape[4:])
+        _is(x.dtype, out_plane=y)
+        row.append(x.element_size() * (x[0, 0, 0, 0].numel() if x.dim() > 4 else 1))
+    src, dst = (ctypes.c_void_p * max(n, 1))(*_ptrs(*planes)), (ctypes.c_void_p * max(n, 1))(*_ptrs(*out_planes))
+    a = _ptrs(weight, out_weight, length, kept, new_len, dev_status)
+    st = load().ppd_kv_evict(a[0], a[1], src, dst, (ctypes.c_int * max(n, 1))(*row), n, a[2], L, B, H, S_max, S_out,
+                             int(budget), int(n_sink), int(n_recent), *a[3:], _stream(stream))
+    _check(st, "ppd_kv_evict")
+
+
+def ppd_sample_accept(logits, cand_tokens, parent, prefix_len, S_max, temperature: float, u, noise, accept_len,
+                      path, next_token, new_prefix_len, dev_status, draft_probs=None, draft_row=None,
+                      accept_prob=None, stream=None):
+    """Acceptance by sampling with given random numbers: u fp32 [B,T] uniform in [0, 1), noise fp32 [B,V]
+    exponential; draft_probs fp32 [B,n_draft,V] and draft_row [B,T] for candidates drawn from distributions."""
+    B, T, V = logits.shape
+    n_draft = draft_probs.shape[1] if draft_probs is not None else 0
+    _is(torch.float32, logits=logits, u=u, noise=noise, draft_probs=draft_probs, accept_prob=accept_prob)
+    _is(torch.int32, cand_tokens=cand_tokens, parent=parent, prefix_len=prefix_len, draft_row=draft_row,
+        accept_len=accept_len, path=path, next_token=next_token, new_prefix_len=new_prefix_len, dev_status=dev_status)
+    _shape(u, "u", B, T), _shape(noise, "noise", B, V), _shape(draft_probs, "draft_probs", B, n_draft, V)
+    _shape(draft_row, "draft_row", B, T), _shape(accept_prob, "accept_prob", B, T)
+    _shape(cand_tokens, "cand_tokens", B, T), _shape(parent, "parent", B, T), _shape(path, "path", B, T)
+    for name, t in (("prefix_len", prefix_len), ("accept_len", accept_len), ("next_token", next_token),
+                    ("new_prefix_len", new_prefix_len), ("dev_status", dev_status)):
+        _shape(t, name, B)
+    a = _ptrs(logits, cand_tokens, parent, prefix_len, draft_probs, draft_row, u, noise, accept_len, path, next_token,
+              new_prefix_len, accept_prob, dev_status)
+    st = load().ppd_sample_accept(*a[:8], B, T, V, n_draft, int(S_max), float(temperature), *a[8:], _stream(stream))
+    _check(st, "ppd_sample_accept")
 
 
 def ppd_selftest_umma(a, b, d, mode: int, N: int, stream=None):
