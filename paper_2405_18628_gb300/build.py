@@ -18,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libppd.so")
 SOURCES = ["ppd_api.cu", "ppd_attention.cu", "ppd_attention_rows.cu", "ppd_verify.cu", "ppd_next.cu",
-           "ppd_kv4.cu", "ppd_evict.cu", "ppd_sample.cu"]
+           "ppd_kv4.cu", "ppd_kv4_wide.cu", "ppd_evict.cu", "ppd_sample.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

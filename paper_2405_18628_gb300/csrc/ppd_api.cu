@@ -948,14 +948,28 @@ static int kv4_splits(long long slices, int row_blocks, int T, int S_max)
     return (int)(n < most ? n : most);
 }
 
+// How an attention call runs: up to 16 query rows of a slice in registers, its keys in
+// `splits` parts; more on the tensor cores in blocks of tp rows, all key tiles shared out
+// (`share`; a batch that the sharing's plan holds).
 struct Kv4Ws {
-    size_t o, ml, total;
-    int row_blocks, splits;
+    size_t o, ml, rec, total;
+    int row_blocks, splits, tp, share;
 };
 static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
 {
     Kv4Ws w{};
     const long long slices = (long long)L * B * H, rows = (long long)G * T;
+    w.splits = 1;
+    if (rows > 16) {
+        w.tp = rows <= 32 ? 32 : 64;
+        w.row_blocks = (int)((rows + w.tp - 1) / w.tp);
+        w.share = B <= ppd::kSplitMaxB;
+        if (w.share) {
+            w.rec = align_up((size_t)2 * split_grid() * ppd::kv4_slot_floats(D, w.tp) * 4);
+            w.total = align_up(w.rec + (size_t)split_grid() * sizeof(ppd::SplitRecord));
+        }
+        return w;
+    }
     w.row_blocks = (int)((rows + 15) / 16);
     w.splits = kv4_splits(slices, w.row_blocks, T, S_max);
     if (w.splits > 1) {
@@ -1003,6 +1017,27 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
     p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
     p.row_blocks = w.row_blocks;
+    if (w.tp) {
+        ppd::AttnParams a{};
+        a.prefix_len = prefix_len, a.parent = parent;
+        a.dev_status = dev_status;
+        a.L = L, a.B = B, a.H = H, a.T = T, a.S_max = S_max;
+        if (slices * w.row_blocks > 2147483647ll) return PPD_ERR_UNSUPPORTED;
+        a.n_qb = w.row_blocks;
+        a.n_units = (int)(slices * w.row_blocks);
+        a.n_tt = (T + 127) / 128;
+        a.cluster = 1;
+        a.scale_log2 = p.scale_log2;
+        const long long tiles = (long long)a.n_units * ((S_max + 127) / 128 + a.n_tt);
+        a.split = w.share && ws_ok;
+        if (a.split) {
+            a.split_part = static_cast<float *>(workspace);
+            a.split_rec = reinterpret_cast<ppd::SplitRecord *>(static_cast<uint8_t *>(workspace) + w.rec);
+        }
+        const long long most = a.split ? tiles : a.n_units;
+        const int grid = (int)(most < split_grid() ? most : split_grid());
+        return cuda_status(ppd::launch_kv4_attention_wide(a, p, D, w.tp, grid, static_cast<cudaStream_t>(stream)));
+    }
     p.splits = ws_ok ? w.splits : 1;
     if (p.splits > 1) {
         p.part_o = static_cast<float *>(workspace);

@@ -436,6 +436,11 @@ struct Kv4AttnParams {
 };
 cudaError_t launch_kv4_attention(const Kv4AttnParams &p, int D, cudaStream_t stream);
 
+// More query rows: units are blocks of TP rows of a slice (p.n_qb of them, n_tt tiles of tree
+// keys each), shared out by their key tiles when p.split, on `grid` CTAs.
+inline __host__ __device__ size_t kv4_slot_floats(int D, int TP) { return (size_t)TP * (D + 2); }
+cudaError_t launch_kv4_attention_wide(const AttnParams &p, const Kv4AttnParams &x, int D, int TP, int grid, cudaStream_t stream);
+
 // Attention weight of the accepted nodes, added up per cached row.
 struct KvWeightParams {
     const void *q;                   // [slices][G][T][D] bf16 or fp32

@@ -88,6 +88,13 @@ PPD_DEV uint4 ld_shared_u128(uint32_t a)
     return v;
 }
 
+// A warpgroup gives registers back, or takes up what others gave (a multiple of 8 a thread;
+// all its warps execute it).
+template <int N>
+PPD_DEV void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+PPD_DEV void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // Element i, i + 1 of a bf16 or fp32 tensor as a bf16 pair (fp32 rounded to nearest);
 // i even.
 PPD_DEV uint32_t ld_pair(const void *p, size_t i, bool f32)
