@@ -37,7 +37,9 @@ PPD_DEV uint32_t kv4_offset2(uint32_t s2) { return bf16x2_fma(s2, 0xC308C308u, 0
 // codes become the low bits of 128 + c, and one fused multiply-add gives s (128 + c) - 136 s.
 PPD_DEV uint32_t kv4_pair(uint32_t pair, uint32_t s2, uint32_t o2)
 {
-    return bf16x2_fma((pair & 0x000F000Fu) | 0x43004300u, s2, o2);
+    uint32_t x;   // (pair & mask) | 128: one instruction, said so
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(pair), "r"(0x000F000Fu), "r"(0x43004300u));
+    return bf16x2_fma(x, s2, o2);
 }
 
 // Two fp32 values as a bf16 pair, the first in the low half.
@@ -45,6 +47,19 @@ PPD_DEV uint32_t bf16x2(float lo, float hi)
 {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// The pair pp as bf16 hi + lo like split_bf16x2, the rounding done by packed fp32 operations:
+// s = p + 2^16 p has 24 bits, so s - 2^16 p is p to eight.  (p below 2^111.)
+PPD_DEV void split_bf16x2_fma(uint64_t pp, uint32_t &hi, uint32_t &lo)
+{
+    const uint64_t big = pack2(65536.f, 65536.f), neg = pack2(-65536.f, -65536.f), m1 = pack2(-1.f, -1.f);
+    const uint64_t h = fma2(pp, neg, fma2(pp, big, pp));
+    float h0, h1, l0, l1;
+    unpack2(h, h0, h1);
+    unpack2(fma2(h, m1, pp), l0, l1);
+    hi = __byte_perm(__float_as_uint(h0), __float_as_uint(h1), 0x7632);
+    lo = bf16x2(l0, l1);
 }
 
 // D += A B: A 16 x 16 rows of bf16, B 16 x 8, fp32 accumulators.

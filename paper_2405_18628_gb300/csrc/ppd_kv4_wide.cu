@@ -93,7 +93,8 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
     using Lay = Kv4Wide<D, TP>;
     using VPos = RingPos<Lay::VS>;
     constexpr int NC = Lay::NC;
-    using Cols = uint32_t[NC];
+    using Cols = uint32_t[Lay::NC];
+    using Probs = uint64_t[Lay::NC / 2];
     extern __shared__ __align__(1024) uint8_t smem[];
     if (smem_addr(smem) & 1023u) {   // the swizzled tiles' alignment: uniform over the CTA
         if (threadIdx.x == 0)
@@ -150,24 +151,43 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         constexpr int UPR = Lay::RB / 16;        // 16-byte pieces of a row's codes, 32 channels each
         TileWalk<SPLIT> ahead(wr), at(wr);
         bool more = true;
+        // piece i of this lane: row i * 32 / UPR + lane / UPR of the warp's 32, 512 bytes on from
+        // piece i - 1 on both sides.  A thread reads one row: eight rows' equal pieces lie in
+        // different banks.
+        const int f_row = lane / UPR;
+        const uint32_t f_to = (uint32_t)(f_row * UPR + ((lane % UPR) ^ (UPR == 4 ? (f_row >> 1) & 3 : (f_row >> 2) & 1))) * 16;
         auto fetch = [&](int stage) {
             if (more) more = ahead.next(p);
-            if (more && ahead.j < ahead.sg.ui.n_pref) {
-                const int k0 = ahead.j * Lay::KT + wq * 32, n = ahead.sg.ui.P - k0;   // rows from k0 on
-                const size_t row0 = (size_t)ahead.sg.ui.lbh * p.S_max + (n > 0 ? k0 : 0);
+            if (more) {
+                const UnitInfo &ui = ahead.sg.ui;
                 const uint32_t dst = ring + stage * Lay::STAGE;
+                if (ahead.j < ui.n_pref) {
+                    const int k0 = ahead.j * Lay::KT + wq * 32, n = ui.P - k0;   // rows from k0 on
+                    const size_t row0 = (size_t)ui.lbh * p.S_max + (n > 0 ? k0 : 0);
+                    const uint8_t *src = codes + row0 * Lay::RB + lane * 16, *sc = scales + row0 * Lay::SB;
+                    if (D == 128 && n >= 32) {
 #pragma unroll
-                for (int i = 0; i < UPR; ++i) {
-                    const int row = (i * 32 + lane) / UPR, c = lane % UPR;
-                    const bool in = row < n;
-                    // a thread reads one row: eight rows' equal pieces lie in different banks
-                    const uint32_t to = (uint32_t)(row * UPR + (UPR == 4 ? c ^ ((row >> 1) & 3) : c ^ ((row >> 2) & 1))) * 16;
-                    cp_async16(dst + to, codes + (row0 + (in ? row : 0)) * Lay::RB + c * 16, in ? 16u : 0u);
+                        for (int i = 0; i < UPR; ++i) cp_async16(dst + f_to + i * 512, src + i * 512, 16u);
+                        cp_async4(dst + Lay::CODES + lane * 4, sc + lane * 4, 4u);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < UPR; ++i) {
+                            const bool in = i * 32 / UPR + f_row < n;
+                            cp_async16(dst + f_to + i * 512, in ? src + i * 512 : codes, in ? 16u : 0u);
+                        }
+                        const bool in = lane < n;
+                        const size_t a = (row0 * Lay::SB + (in ? lane * Lay::SB : 0)) & ~(size_t)3;
+                        const size_t left = x.scale_bytes - a;
+                        cp_async4(dst + Lay::CODES + lane * 4, scales + a, in ? (left < 4 ? (uint32_t)left : 4u) : 0u);
+                    }
+                } else {
+                    // a tree tile is read from L2 when its turn comes
+                    const int jt = (ahead.j - ui.n_pref) * Lay::KT + t;
+                    const int bytes = x.f32 ? 4 * D : 2 * D;
+                    const uint8_t *row = reinterpret_cast<const uint8_t *>(tree_rows) + ((size_t)ui.lbh * T + (jt < T ? jt : 0)) * bytes;
+                    if (jt < T)
+                        for (int i = 0; i < bytes; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
                 }
-                const bool in = lane < n;
-                const size_t a = ((row0 + (in ? lane : 0)) * Lay::SB) & ~(size_t)3;
-                const size_t left = x.scale_bytes - a;
-                cp_async4(dst + Lay::CODES + lane * 4, scales + a, in ? (left < 4 ? (uint32_t)left : 4u) : 0u);
             }
             cp_async_commit();
         };
@@ -218,21 +238,28 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 const size_t row = ((size_t)at.sg.ui.lbh * T + (in ? jt : 0)) * D;
                 if (g >= 2) mbar_wait(free_bar, ((g >> 1) - 1) & 1, abort_flag);
                 tc_fence_after();
+                if (!x.f32) {
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t r[16];
-                    if (!x.f32) {
+                    for (int c = 0; c < D / 32; c += 2) {   // 64 channels' loads in flight
+                        uint32_t r[2][16];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < 8; ++i) {
                             const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(tree_rows) + row + 32 * c) + i)
                                                : make_uint4(0, 0, 0, 0);
-                            r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
+                            uint32_t *to = &r[i >> 2][4 * (i & 3)];
+                            to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
                         }
-                    } else {
+                        store(c, r[0]);
+                        store(c + 1, r[1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t r[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) r[i] = in ? ld_pair(tree_rows, row + 32 * c + 2 * i, true) : 0u;
+                        store(c, r);
                     }
-                    store(c, r);
                 }
             }
             if (!kv) {
@@ -381,15 +408,14 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         int pend_f = 0, pend_u = 0, pend_g = 0;
 
         // Probabilities of this thread's key row for its NC query columns from its raw
-        // scores r, against the current running maxima, exponents clamped at 64 so
-        // nothing overflows before a rescale.  STORE: split into bf16 hi + lo, store
-        // into the probability tile at byte offset `pbuf` and add to lacc.  UNDO: subtract the
-        // same values from lacc again (bit-identical to an earlier STORE with the same
-        // maxima).  Returns the largest unclamped exponent.
-        auto emit = [&](auto bits_c, auto undo_c, const Cols &r, uint32_t bits, uint32_t pbuf) {
+        // scores r, against the current running maxima: split into bf16 hi + lo, stored
+        // into the probability tile at byte offset `pbuf`, and kept in pr for the row sums.
+        // Returns their sum: above 2^16 (or no number) where one of them is too large, and
+        // the exact path then writes the tile again.  (Adding is the FMA pipe's work, a maximum
+        // and a split by shifts and masks the integer pipe's, which bounds this loop.)
+        auto emit = [&](auto bits_c, const Cols &r, uint32_t bits, uint32_t pbuf, Probs &pr) {
             constexpr bool BITS = decltype(bits_c)::value != 0;
-            constexpr bool UNDO = decltype(undo_c)::value != 0;
-            float maxd = -INFINITY;
+            uint64_t total[2] = {0ull, 0ull};
 #pragma unroll
             for (int h = 0; h < NC; h += 8) {
                 const ulonglong2 na = *reinterpret_cast<const ulonglong2 *>(nm + h);
@@ -405,44 +431,35 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                         d0 = ((bits >> (h + e)) & 1u) ? d0 : -INFINITY;
                         d1 = ((bits >> (h + e + 1)) & 1u) ? d1 : -INFINITY;
                     }
-                    maxd = max3(maxd, d0, d1);
-                    const float p0 = ex2(fminf(d0, 64.f)), p1 = ex2(fminf(d1, 64.f));
-                    if (UNDO) {
-                        lacc[(h + e) >> 1] = add2(lacc[(h + e) >> 1], pack2(-p0, -p1));
-                    } else {
-                        const uint64_t pp = pack2(p0, p1);
-                        lacc[(h + e) >> 1] = add2(lacc[(h + e) >> 1], pp);
-                        split_bf16x2(pp, p0, p1, hw[e >> 1], lw[e >> 1]);
-                    }
+                    const uint64_t pp = pack2(ex2(d0), ex2(d1));
+                    pr[(h + e) >> 1] = pp;
+                    total[(e >> 1) & 1] = add2(total[(e >> 1) & 1], pp);
+                    split_bf16x2_fma(pp, hw[e >> 1], lw[e >> 1]);
                 }
-                if (!UNDO) {
-                    const int ch = q0 + h, cl = TP + q0 + h;   // hi and lo columns
-                    const uint32_t ah = p_row + pbuf + (uint32_t)(ch >> 6) * Lay::GROUP_BYTES +
-                                        ((((uint32_t)(ch & 63) >> 3) ^ p_swz) << 4);
-                    const uint32_t al = p_row + pbuf + (uint32_t)(cl >> 6) * Lay::GROUP_BYTES +
-                                        ((((uint32_t)(cl & 63) >> 3) ^ p_swz) << 4);
-                    st_shared_v4(ah, hw[0], hw[1], hw[2], hw[3]);
-                    st_shared_v4(al, lw[0], lw[1], lw[2], lw[3]);
-                }
+                const int ch = q0 + h, cl = TP + q0 + h;   // hi and lo columns
+                const uint32_t ah = p_row + pbuf + (uint32_t)(ch >> 6) * Lay::GROUP_BYTES +
+                                    ((((uint32_t)(ch & 63) >> 3) ^ p_swz) << 4);
+                const uint32_t al = p_row + pbuf + (uint32_t)(cl >> 6) * Lay::GROUP_BYTES +
+                                    ((((uint32_t)(cl & 63) >> 3) ^ p_swz) << 4);
+                st_shared_v4(ah, hw[0], hw[1], hw[2], hw[3]);
+                st_shared_v4(al, lw[0], lw[1], lw[2], lw[3]);
             }
-            return maxd;
+            float s0, s1;
+            unpack2(add2(total[0], total[1]), s0, s1);
+            return s0 + s1;
         };
-        using store_t = kind_t<0>;
-        using undo_t = kind_t<1>;
 
         auto load_cols = [&](uint32_t taddr, Cols &r) {   // then tmem_wait_ld
             if constexpr (NC == 32) tmem_ld32(taddr, r);
             else tmem_ld16(taddr, r);
         };
 
-        // A score jumped past its column's maximum by more than 2^16: the optimistic
-        // contributions are taken back out of the row sums; every column's maximum
-        // over the 128 key rows is a warp max (redux) combined across the four warps;
-        // the row sums, and O unless this is the unit's first tile, are rescaled; the
-        // probabilities are recomputed.
-        auto exact_tile = [&](auto bits_c, const Cols &r, uint32_t bits, uint32_t pbuf, bool first) {
+        // A score jumped past its column's maximum by about 2^16: every column's maximum
+        // over the 128 key rows is a warp max (redux) combined across the four warps; the row
+        // sums, and O unless this is the unit's first tile, are rescaled; the probabilities are
+        // computed again.
+        auto exact_tile = [&](auto bits_c, const Cols &r, uint32_t bits, uint32_t pbuf, bool first, Probs &pr) {
             constexpr bool BITS = decltype(bits_c)::value != 0;
-            (void)emit(bits_c, undo_t{}, r, bits, pbuf);
 #pragma unroll
             for (int e = 0; e < NC; ++e) {
                 const bool vis = !BITS || ((bits >> e) & 1u) != 0;
@@ -487,7 +504,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 }
             }
             if (!first) tmem_wait_st();
-            (void)emit(bits_c, store_t{}, r, bits, pbuf);
+            (void)emit(bits_c, r, bits, pbuf, pr);
         };
 
         // O (hi + lo) of a finished unit's accumulator: one head-dim element per thread,
@@ -583,18 +600,20 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 // Done optimistically with the current running maxima; when a score
                 // exceeds its maximum by more than 2^16, again by the exact path.
                 const uint32_t bits = tree ? dbits : (t < n_valid ? 0xffffffffu : 0u);
+                Probs pr;
                 if (!masked) {
-                    const float maxd = emit(kind_t<0>{}, store_t{}, r, bits, pbuf);
-                    if (named_bar_or(1 + wg, 128, maxd > 16.f)) exact_tile(kind_t<0>{}, r, bits, pbuf, first);
+                    const float sum = emit(kind_t<0>{}, r, bits, pbuf, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= 65536.f))) exact_tile(kind_t<0>{}, r, bits, pbuf, first, pr);
                 } else {
-                    const float maxd = emit(kind_t<1>{}, store_t{}, r, bits, pbuf);
-                    if (named_bar_or(1 + wg, 128, maxd > 16.f)) exact_tile(kind_t<1>{}, r, bits, pbuf, first);
+                    const float sum = emit(kind_t<1>{}, r, bits, pbuf, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= 65536.f))) exact_tile(kind_t<1>{}, r, bits, pbuf, first, pr);
                 }
-
                 fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + Lay::B_PFULL + ps);
+#pragma unroll
+                for (int c = 0; c < NC / 2; ++c) lacc[c] = add2(lacc[c], pr[c]);
 
                 // the previous segment's output, once this segment's first tile is on its way
                 if (first && pend_f) {
