@@ -286,17 +286,28 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             const int r0 = sg.ui.qb * TP;
             const size_t row0 = (size_t)sg.ui.lbh * R + r0;
             constexpr int CPR = D / 8;   // 16-byte chunks of a row
-#pragma unroll 4
-            for (int i = lane; i < TP * CPR; i += 32) {
-                const int row = i / CPR, c = i % CPR;
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (r0 + row < R) {
-                    const size_t a = (row0 + row) * D + 8 * c;
-                    if (!x.f32) v = ld_input(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(x.q) + a));
-                    else v = make_uint4(ld_pair(x.q, a, true), ld_pair(x.q, a + 2, true), ld_pair(x.q, a + 4, true), ld_pair(x.q, a + 6, true));
+            auto chunk_at = [&](int row, int c) {
+                return dst + (uint32_t)(c >> 3) * Lay::Q_GROUP_BYTES + (uint32_t)(row >> 3) * 1024u + (uint32_t)(row & 7) * 128u +
+                       (uint32_t)(((c & 7) ^ (row & 7)) << 4);
+            };
+            if (!x.f32) {   // every chunk on its way at once
+                const uint8_t *src = reinterpret_cast<const uint8_t *>(x.q) + row0 * D * 2;
+#pragma unroll 8
+                for (int i = lane; i < TP * CPR; i += 32) {
+                    const bool in = r0 + i / CPR < R;
+                    cp_async16(chunk_at(i / CPR, i % CPR), in ? src + (size_t)i * 16 : reinterpret_cast<const uint8_t *>(x.q), in ? 16u : 0u);
                 }
-                st_shared_v4(dst + (uint32_t)(c >> 3) * Lay::Q_GROUP_BYTES + (uint32_t)(row >> 3) * 1024u + (uint32_t)(row & 7) * 128u +
-                                 (uint32_t)(((c & 7) ^ (row & 7)) << 4), v.x, v.y, v.z, v.w);
+                cp_async_commit();
+                cp_async_wait<0>();
+            } else {
+#pragma unroll 4
+                for (int i = lane; i < TP * CPR; i += 32) {
+                    const int row = i / CPR, c = i % CPR;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    const size_t a = (row0 + row) * D + 8 * c;
+                    if (r0 + row < R) v = make_uint4(ld_pair(x.q, a, true), ld_pair(x.q, a + 2, true), ld_pair(x.q, a + 4, true), ld_pair(x.q, a + 6, true));
+                    st_shared_v4(chunk_at(row, c), v.x, v.y, v.z, v.w);
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();
