@@ -916,6 +916,7 @@ ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
         !aligned(k_scale, 16) || !aligned(v_scale, 16))
         return PPD_ERR_INVALID_ARG;
+    if (T > 65535 * 64) return PPD_ERR_UNSUPPORTED;
     ppd::Kv4AppendParams p{k_new, v_new, k_cache, v_cache, k_scale, v_scale, rows, start, n_new, dev_status,
                            (long long)L * B * H, B, H, T, D, S_max, dt == PPD_F32};
     return cuda_status(ppd::launch_kv4_append(p, static_cast<cudaStream_t>(stream)));
@@ -963,7 +964,10 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
     if (rows > 16) {
         w.tp = rows <= 32 ? 32 : 64;
         w.row_blocks = (int)((rows + w.tp - 1) / w.tp);
-        w.share = B <= ppd::kSplitMaxB;
+        // whole units where sharing their tiles out would save less than it costs (about six tiles'
+        // time: the merge grid and the parts' way through memory)
+        const long long units = slices * w.row_blocks, t_u = (S_max + 127) / 128 + (T + 127) / 128, sms = split_grid();
+        w.share = B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + 6 < (units + sms - 1) / sms * t_u;
         if (w.share) {
             w.rec = align_up((size_t)2 * split_grid() * ppd::kv4_slot_floats(D, w.tp) * 4);
             w.total = align_up(w.rec + (size_t)split_grid() * sizeof(ppd::SplitRecord));

@@ -8,15 +8,19 @@ namespace ppd {
 
 // ------------------------------------------------------------------ rows in
 
-// Four channels of a source row as fp32.
-PPD_DEV float4 ld_quad(const void *p, size_t i, bool f32)
+// Eight channels of a source row as fp32.
+PPD_DEV void ld_eight(const void *p, size_t i, bool f32, float (&v)[8])
 {
-    if (f32) return ld_input(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(p) + i));
-    const uint16_t *s = reinterpret_cast<const uint16_t *>(p) + i;
-    uint2 v;
-    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(s) : "memory");
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
-                       __uint_as_float(v.y & 0xFFFF0000u));
+    if (f32) {
+        const float4 *f = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(p) + i);
+        const float4 a = ld_input(f), b = ld_input(f + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        return;
+    }
+    const uint4 a = ld_input(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(p) + i));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
 }
 
 // A sequence's rows are refused as a whole: a start or a count outside the cache.
@@ -25,55 +29,66 @@ PPD_DEV int append_status(int start, int n, int T, int S_max)
     return start < 0 || n < 0 || n > T || start > S_max || n > S_max - start ? kErrCapacity : kOk;
 }
 
-// Eight lanes hold a group of 32 channels, four neighbours each: the largest magnitude by
-// shuffles, then each lane has its four codes and pairs of lanes put a word of eight
-// together.  Two roundings alone, both IEEE: a / 7 (then up to the next scale) and x / s.
+// A block takes kAppendRows new rows of a slice, K and V.  A thread quantises the eight channels
+// of one word of codes, four threads share a scale: the largest magnitude by two shuffles, then
+// two roundings alone: a / 7 (then up to the next scale) and x / s.  The quotient is x times
+// the rounded reciprocal with one Newton step, which rounds it correctly (Markstein's theorem:
+// an fp32 reciprocal rounded to nearest, and a fused residual); halves are then exact, and
+// adding 1.5 * 2^23 + 8 rounds to the nearest integer, half to even, and leaves the code in the low
+// bits.  Divisions in their place were 43 of a prompt's 67 us.  Four rows' loads a thread in flight.
+constexpr int kAppendRows = 64, kAppendDeep = 4;
+template <int D>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4AppendParams p)
 {
     pdl_release();
     pdl_wait();
-    const int quads = p.D / 4, lanes = p.D / 4;   // lanes of a row: 16 or 32
-    const int row_in_block = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    const int rows = blockDim.x / lanes;
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int b = threadIdx.x; b < p.B; b += blockDim.x)
-            p.dev_status[b] = append_status(ld_input(p.start + b), ld_input(p.n_new + b), p.T, p.S_max);
-    (void)quads;
-    const int j = (int)blockIdx.x * rows + row_in_block;   // the sequence's j-th new row
-    for (long long u = blockIdx.y; u < p.slices; u += gridDim.y) {
-        const int b = (int)(u / p.H % p.B);
-        const int start = ld_input(p.start + b), n = ld_input(p.n_new + b);
-        int src = j < n && append_status(start, n, p.T, p.S_max) == kOk ? j : -1;
-        if (src >= 0 && p.rows) src = ld_input(p.rows + (size_t)b * p.T + j);
-        const bool real = src >= 0 && src < p.T;
+    constexpr int LANES = D / 8;
+    const int lane = threadIdx.x % LANES, first = threadIdx.x / LANES;
+    constexpr int STEP = 256 / LANES;   // (row, K or V) pairs of a pass
+    const long long u = blockIdx.x;
+    const int b = (int)(u / p.H % p.B);
+    const int start = ld_input(p.start + b), n = ld_input(p.n_new + b);
+    const int status = append_status(start, n, p.T, p.S_max);
+    if (u / p.H < p.B && u % p.H == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.dev_status[b] = status;
+    if (status != kOk) return;
+    const int j0 = (int)blockIdx.y * kAppendRows, pairs = 2 * (min(n, j0 + kAppendRows) - j0);
+    for (int i0 = 0; i0 < pairs; i0 += kAppendDeep * STEP) {   // the same for every thread: shuffles follow
+        float v[kAppendDeep][8];
+        bool real[kAppendDeep];
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            const void *x = kv ? p.v_new : p.k_new;
-            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (real) f = ld_quad(x, ((size_t)u * p.T + src) * p.D + 4 * lane, p.f32);
-            // fmaxf passes a NaN by
-            float a = fmaxf(fmaxf(fmaxf(fabsf(f.x), fabsf(f.y)), fmaxf(fabsf(f.z), fabsf(f.w))), 0.f);
+        for (int k = 0; k < kAppendDeep; ++k) {
+            const int i = i0 + k * STEP + first, j = j0 + (i >> 1);
+            int src = i < pairs ? j : -1;
+            if (src >= 0 && p.rows) src = ld_input(p.rows + (size_t)b * p.T + j);
+            real[k] = src >= 0 && src < p.T;
 #pragma unroll
-            for (int o = 1; o < 8; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+            for (int e = 0; e < 8; ++e) v[k][e] = 0.f;
+            if (real[k]) ld_eight(i & 1 ? p.v_new : p.k_new, ((size_t)u * p.T + src) * D + 8 * lane, p.f32, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAppendDeep; ++k) {
+            if (i0 + k * STEP >= pairs) break;
+            float a = 0.f;   // fmaxf passes a NaN by
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a = fmaxf(a, fabsf(v[k][e]));
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
             const int up = (int)((__float_as_uint(__fdiv_rn(a, 7.f)) + 0xFFFFFu) >> 20) - 107 * 8;
             const uint32_t sb = (uint32_t)min(max(up, 0), 255);
-            const float s = kv4_scale(sb);
-            const float v[4] = {f.x, f.y, f.z, f.w};
-            uint32_t c[4];
+            const float s = kv4_scale(sb), top = 7.f * s, inv = __frcp_rn(s);   // (7 s is exact)
+            uint32_t word = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float q = rintf(__fdiv_rn(v[e], s));
-                c[e] = q == q ? (uint32_t)((int)fminf(fmaxf(q, -7.f), 7.f) + 8) : 8u;
+            for (int e = 0; e < 8; ++e) {
+                const float x = v[k][e] == v[k][e] ? fminf(fmaxf(v[k][e], -top), top) : 0.f;
+                const float t = x * inv;
+                const uint32_t c = __float_as_uint(fmaf(fmaf(-t, s, x), inv, t) + 12582920.f) & 15u;
+                word |= c << (4 * (e >> 1) + 16 * (e & 1));   // even channels in the low half, odd ones in the high half
             }
-            // an even lane holds channels 0..3 of a word, its neighbour 4..7: even channels
-            // in the low half of the word, odd ones in the high half
-            const uint32_t mine = c[0] | c[2] << 4 | c[1] << 16 | c[3] << 20;
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
-            if (real) {
-                const size_t row = (size_t)u * p.S_max + start + j;
-                uint8_t *codes = kv ? p.v_cache : p.k_cache, *scales = kv ? p.v_scale : p.k_scale;
-                if (!(lane & 1)) *reinterpret_cast<uint32_t *>(codes + row * (p.D / 2) + 2 * lane) = mine | other << 8;
-                if (!(lane & 7)) scales[row * (p.D / kKv4Group) + lane / 8] = (uint8_t)sb;
+            const int i = i0 + k * STEP + first;
+            if (real[k]) {
+                const size_t row = (size_t)u * p.S_max + start + j0 + (i >> 1);
+                reinterpret_cast<uint32_t *>(i & 1 ? p.v_cache : p.k_cache)[row * LANES + lane] = word;
+                if (!(lane & 3)) (i & 1 ? p.v_scale : p.k_scale)[row * (D / kKv4Group) + lane / 4] = (uint8_t)sb;
             }
         }
     }
@@ -81,53 +96,68 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4AppendParams p
 
 cudaError_t launch_kv4_append(const Kv4AppendParams &p, cudaStream_t stream)
 {
-    const int rows = 256 / (p.D / 4);
-    const dim3 grid((unsigned)((p.T + rows - 1) / rows), (unsigned)(p.slices < 65535 ? p.slices : 65535));
-    return launch_chained(kv4_append_kernel, grid, dim3(256), dim3(1), stream, p);
+    const dim3 grid((unsigned)p.slices, (unsigned)((p.T + kAppendRows - 1) / kAppendRows));
+    return p.D == 128 ? launch_chained(kv4_append_kernel<128>, grid, dim3(256), dim3(1), stream, p)
+                      : launch_chained(kv4_append_kernel<64>, grid, dim3(256), dim3(1), stream, p);
 }
 
 // ------------------------------------------------------------------ rows out
 
+// A thread a word of codes, all slices' rows end to end; four words a thread in flight.
+constexpr int kReadDeep = 4;
+template <int D>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4ReadParams p)
 {
     pdl_release();
     pdl_wait();
-    const int words = p.D / 8;   // words of a row, one per thread
-    const int rows = blockDim.x / words;
-    const int j = (int)blockIdx.x * rows + (int)threadIdx.x / words, w = (int)threadIdx.x % words;
-    if (j >= p.N) return;
-    for (long long u = blockIdx.y; u < p.slices; u += gridDim.y) {
-        const int b = (int)(u / p.H % p.B);
+    constexpr int WORDS = D / 8;
+    const uint32_t rows = (uint32_t)(p.slices * p.N);   // below 2^31
+    const int w = threadIdx.x % WORDS;
+    const uint32_t row0 = blockIdx.x * (kReadDeep * 256 / WORDS) + threadIdx.x / WORDS;
+    uint32_t c[kReadDeep], sb[kReadDeep];
+#pragma unroll
+    for (int k = 0; k < kReadDeep; ++k) {
+        const uint32_t r = row0 + k * (256 / WORDS);
+        c[k] = 0x88888888u;   // zeros
+        sb[k] = 0;
+        if (r >= rows) continue;
+        const uint32_t u = r / (uint32_t)p.N;
+        const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B), j = (int)(r - u * p.N);
         const int start = ld_input(p.start + b), n = ld_input(p.n + b);
-        uint32_t r[4] = {0u, 0u, 0u, 0u};
         if (j < n && start >= 0 && start <= p.S_max && j < p.S_max - start) {
             const size_t row = (size_t)u * p.S_max + start + j;
-            const uint32_t c = (uint32_t)ld_input(reinterpret_cast<const int *>(p.cache + row * (p.D / 2)) + w);
-            uint32_t sb;
-            asm volatile("ld.global.u8 %0, [%1];" : "=r"(sb) : "l"(p.scale + row * (p.D / kKv4Group) + w / 4) : "memory");
-            const uint32_t s2 = kv4_scale2(sb * 0x10001u), o2 = kv4_offset2(s2);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) r[k] = kv4_pair(c >> (4 * k), s2, o2);
+            c[k] = (uint32_t)ld_input(reinterpret_cast<const int *>(p.cache) + row * WORDS + w);
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(sb[k]) : "l"(p.scale + row * (D / kKv4Group) + w / 4) : "memory");
         }
-        const size_t at = ((size_t)u * p.N + j) * p.D + 8 * w;
+    }
+#pragma unroll
+    for (int k = 0; k < kReadDeep; ++k) {
+        const uint32_t r = row0 + k * (256 / WORDS);
+        if (r >= rows) return;
+        const uint32_t s2 = kv4_scale2(sb[k] * 0x10001u), o2 = kv4_offset2(s2);
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = kv4_pair(c[k] >> (4 * e), s2, o2);
+        const size_t at = (size_t)r * D + 8 * w;
         if (!p.f32) {
-            *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(p.out) + at) = make_uint4(r[0], r[1], r[2], r[3]);
+            *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(p.out) + at) = make_uint4(v[0], v[1], v[2], v[3]);
         } else {
             float *o = reinterpret_cast<float *>(p.out) + at;
 #pragma unroll
-            for (int k = 0; k < 4; k += 2)
-                *reinterpret_cast<float4 *>(o + 2 * k) =
-                    make_float4(__uint_as_float(r[k] << 16), __uint_as_float(r[k] & 0xFFFF0000u),
-                                __uint_as_float(r[k + 1] << 16), __uint_as_float(r[k + 1] & 0xFFFF0000u));
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<float4 *>(o + 2 * e) =
+                    make_float4(__uint_as_float(v[e] << 16), __uint_as_float(v[e] & 0xFFFF0000u),
+                                __uint_as_float(v[e + 1] << 16), __uint_as_float(v[e + 1] & 0xFFFF0000u));
         }
     }
 }
 
 cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream)
 {
-    const int rows = 256 / (p.D / 8);
-    const dim3 grid((unsigned)((p.N + rows - 1) / rows), (unsigned)(p.slices < 65535 ? p.slices : 65535));
-    return launch_chained(kv4_read_kernel, grid, dim3(256), dim3(1), stream, p);
+    const long long per = kReadDeep * 256 / (p.D / 8), rows = p.slices * p.N;
+    const dim3 grid((unsigned)((rows + per - 1) / per));
+    return p.D == 128 ? launch_chained(kv4_read_kernel<128>, grid, dim3(256), dim3(1), stream, p)
+                      : launch_chained(kv4_read_kernel<64>, grid, dim3(256), dim3(1), stream, p);
 }
 
 // ------------------------------------------------------------------ attention, few rows

@@ -9,6 +9,7 @@ raises immediately.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 
@@ -286,25 +287,24 @@ def ppd_next_tree(logits, parent, cand_tokens, path, accept_len, next_token, tmp
     _check(st, "ppd_next_tree")
 
 
-def _kv4(codes, scales):
-    """Checks a 4-bit cache's pair of tensors; returns its head dim."""
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
-        raise TypeError("a 4-bit cache is uint8 codes and uint8 scales")
-    D = 2 * codes.shape[-1]
-    if scales.shape != (*codes.shape[:-1], D // 32):
-        raise ValueError(f"scales of codes {tuple(codes.shape)} are {(*codes.shape[:-1], D // 32)}, not {tuple(scales.shape)}")
-    return D
-
-
-def _shape(t, name, *want):
-    if t is not None and tuple(t.shape) != want:
-        raise ValueError(f"{name} is {want}, not {tuple(t.shape)}")
-
-
-def _is(dtype, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.dtype != dtype:
+def _take(*specs):
+    """Device addresses of (name, tensor, dtype, shape) as ctypes takes them (None for None):
+    each tensor of that type and shape, contiguous, on the GPU.  One loop, half a microsecond a
+    tensor; a call's kernels take little longer."""
+    out, fine = [], True
+    for name, t, dtype, shape in specs:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} is {tuple(shape)}, not {tuple(t.shape)}")
+        fine = fine and t.is_cuda and t.is_contiguous()
+        out.append(t.data_ptr())
+    if not fine:
+        raise ValueError("libppd takes contiguous CUDA tensors")
+    return out
 
 
 def kv4_cache(L, B, H, S_max, D, device="cuda"):
@@ -317,29 +317,24 @@ def ppd_kv4_append(k_new, v_new, k_cache, k_scale, v_cache, v_scale, start, n_ne
                    rows=None, stream=None):
     """Rows k_new, v_new [L,B,H,T,D] (those of rows [B,T], or all in order), n_new [B] of them,
     quantised into a 4-bit cache from row start [B] on."""
-    L, B, H, T, D = k_new.shape
+    L, B, H, T, D = new = k_new.shape
     S_max = k_cache.shape[3]
-    for c, s in ((k_cache, k_scale), (v_cache, v_scale)):
-        _kv4(c, s)
-        _shape(c, "the cache", L, B, H, S_max, D // 2)
-    _shape(v_new, "v_new", L, B, H, T, D)
-    _is(k_new.dtype, v_new=v_new)
-    _is(torch.int32, start=start, n_new=n_new, dev_status=dev_status, rows=rows)
-    _shape(start, "start", B), _shape(n_new, "n_new", B), _shape(dev_status, "dev_status", B), _shape(rows, "rows", B, T)
-    a = _ptrs(k_new, v_new, k_cache, k_scale, v_cache, v_scale, rows, start, n_new, dev_status)
+    u8, i32, dt = torch.uint8, torch.int32, k_new.dtype
+    codes, scales = (L, B, H, S_max, D // 2), (L, B, H, S_max, D // 32)
+    a = _take(("k_new", k_new, dt, new), ("v_new", v_new, dt, new), ("k_cache", k_cache, u8, codes), ("k_scale", k_scale, u8, scales),
+              ("v_cache", v_cache, u8, codes), ("v_scale", v_scale, u8, scales), ("rows", rows, i32, (B, T)), ("start", start, i32, (B,)),
+              ("n_new", n_new, i32, (B,)), ("dev_status", dev_status, i32, (B,)))
     st = load().ppd_kv4_append(*a[:9], L, B, H, T, D, S_max, _dtype(k_new), a[9], _stream(stream))
     _check(st, "ppd_kv4_append")
 
 
 def ppd_kv4_read(cache, scale, start, n, out, stream=None):
     """Rows start .. start + n - 1 [B] of a 4-bit cache as bf16 or fp32 values: out [L,B,H,N,D], zero from row n on."""
-    L, B, H, N, D = out.shape
+    L, B, H, N, D = rows = out.shape
     S_max = cache.shape[3]
-    _kv4(cache, scale)
-    _shape(cache, "the cache", L, B, H, S_max, D // 2)
-    _is(torch.int32, start=start, n=n)
-    _shape(start, "start", B), _shape(n, "n", B)
-    a = _ptrs(cache, scale, start, n, out)
+    u8, i32 = torch.uint8, torch.int32
+    a = _take(("cache", cache, u8, (L, B, H, S_max, D // 2)), ("scale", scale, u8, (L, B, H, S_max, D // 32)), ("start", start, i32, (B,)),
+              ("n", n, i32, (B,)), ("out", out, out.dtype, rows))
     st = load().ppd_kv4_read(*a[:4], L, B, H, N, D, S_max, a[4], _dtype(out), _stream(stream))
     _check(st, "ppd_kv4_read")
 
@@ -352,23 +347,21 @@ def ppd_tree_attention_kv4(q, k_cache, k_scale, v_cache, v_scale, k_tree, v_tree
                            dev_status, lse=None, scale: float = 0.0, workspace=None, stream=None):
     """Tree attention over a 4-bit cache: q [L,B,H*G,T,D] (bf16 or fp32), k_tree/v_tree [L,B,H,T,D], out bf16
     [L,B,H*G,T,D].  Without a workspace the keys of a slice are not shared out to several SMs."""
-    L, B, Hq, T, D = q.shape
+    L, B, Hq, T, D = rows = q.shape
     H, S_max = k_cache.shape[2:4]
-    for c, s in ((k_cache, k_scale), (v_cache, v_scale)):
-        _kv4(c, s)
-        _shape(c, "the cache", L, B, H, S_max, D // 2)
     if H < 1 or Hq % H:
         raise ValueError(f"{Hq} query heads over {H} K/V heads")
-    _shape(k_tree, "k_tree", L, B, H, T, D), _shape(v_tree, "v_tree", L, B, H, T, D)
-    _shape(out, "out", L, B, Hq, T, D), _shape(lse, "lse", L, B, Hq, T)
-    _shape(parent, "parent", B, T), _shape(prefix_len, "prefix_len", B), _shape(dev_status, "dev_status", B)
-    _is(q.dtype, k_tree=k_tree, v_tree=v_tree)
-    _is(torch.bfloat16, out=out), _is(torch.float32, lse=lse)
-    _is(torch.int32, prefix_len=prefix_len, parent=parent, dev_status=dev_status)
-    ws_n = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    a = _ptrs(q, k_cache, k_scale, v_cache, v_scale, k_tree, v_tree, prefix_len, parent, out, lse, dev_status, workspace)
-    st = load().ppd_tree_attention_kv4(*a[:9], L, B, H, Hq // H, T, D, S_max, _dtype(q), float(scale), *a[9:],
-                                       ws_n, _stream(stream))
+    u8, i32, dt = torch.uint8, torch.int32, q.dtype
+    codes, scales, tree = (L, B, H, S_max, D // 2), (L, B, H, S_max, D // 32), (L, B, H, T, D)
+    a = _take(("q", q, dt, rows), ("k_cache", k_cache, u8, codes), ("k_scale", k_scale, u8, scales), ("v_cache", v_cache, u8, codes),
+              ("v_scale", v_scale, u8, scales), ("k_tree", k_tree, dt, tree), ("v_tree", v_tree, dt, tree), ("prefix_len", prefix_len, i32, (B,)),
+              ("parent", parent, i32, (B, T)), ("out", out, torch.bfloat16, rows), ("lse", lse, torch.float32, (L, B, Hq, T)),
+              ("dev_status", dev_status, i32, (B,)))
+    ws, ws_n = None, 0
+    if workspace is not None:
+        (ws,), ws_n = _ptrs(workspace), workspace.nbytes
+    st = load().ppd_tree_attention_kv4(*a[:9], L, B, H, Hq // H, T, D, S_max, _dtype(q), float(scale), *a[9:], ws, ws_n,
+                                       _stream(stream))
     _check(st, "ppd_tree_attention_kv4")
 
 
@@ -376,20 +369,15 @@ def ppd_kv_weight_add(q, lse, k_cache, k_tree, path, accept_len, prefix_len, wei
                       scale: float = 0.0, stream=None):
     """Adds to weight fp32 [L,B,H,S_max] the attention that the accepted nodes gave each cached row of a bf16
     cache [L,B,H,S_max,D], or with k_scale of a 4-bit one; the new rows' weights are set."""
-    L, B, Hq, T, D = q.shape
+    L, B, Hq, T, D = rows = q.shape
     H, S_max = k_cache.shape[2:4]
-    if k_scale is not None:
-        _kv4(k_cache, k_scale)
-    else:
-        _is(torch.bfloat16, k_cache=k_cache)
-    _shape(k_cache, "the cache", L, B, H, S_max, D if k_scale is None else D // 2)
     if H < 1 or Hq % H:
         raise ValueError(f"{Hq} query heads over {H} K/V heads")
-    _shape(lse, "lse", L, B, Hq, T), _shape(k_tree, "k_tree", L, B, H, T, D), _shape(weight, "weight", L, B, H, S_max)
-    _shape(path, "path", B, T), _shape(accept_len, "accept_len", B), _shape(prefix_len, "prefix_len", B)
-    _is(q.dtype, k_tree=k_tree), _is(torch.float32, lse=lse, weight=weight)
-    _is(torch.int32, path=path, accept_len=accept_len, prefix_len=prefix_len)
-    a = _ptrs(q, lse, k_cache, k_scale, k_tree, path, accept_len, prefix_len, weight)
+    i32, f32, dt, kv4 = torch.int32, torch.float32, q.dtype, k_scale is not None
+    a = _take(("q", q, dt, rows), ("lse", lse, f32, (L, B, Hq, T)),
+              ("k_cache", k_cache, torch.uint8 if kv4 else torch.bfloat16, (L, B, H, S_max, D // 2 if kv4 else D)),
+              ("k_scale", k_scale, torch.uint8, (L, B, H, S_max, D // 32)), ("k_tree", k_tree, dt, (L, B, H, T, D)), ("path", path, i32, (B, T)),
+              ("accept_len", accept_len, i32, (B,)), ("prefix_len", prefix_len, i32, (B,)), ("weight", weight, f32, (L, B, H, S_max)))
     st = load().ppd_kv_weight_add(*a[:8], L, B, H, Hq // H, T, D, S_max, _dtype(q), float(scale), a[8], _stream(stream))
     _check(st, "ppd_kv_weight_add")
 
@@ -402,25 +390,20 @@ def ppd_kv_evict(weight, planes, length, budget: int, n_sink: int, n_recent: int
     if (out_planes is None) != (out_weight is None):
         raise ValueError("out_planes and out_weight are given together")
     out_planes, out_weight = (planes, weight) if out_planes is None else (out_planes, out_weight)
-    S_out = out_weight.shape[3]
-    _shape(out_weight, "out_weight", L, B, H, S_out)
-    _is(torch.float32, weight=weight, out_weight=out_weight)
-    _is(torch.int32, length=length, kept=kept, new_len=new_len, dev_status=dev_status)
-    _shape(kept, "kept", L, B, H, int(budget))
-    _shape(length, "length", B), _shape(new_len, "new_len", B), _shape(dev_status, "dev_status", B)
-    if len(planes) != len(out_planes):
+    S_out, budget, n = out_weight.shape[3], int(budget), len(planes)
+    if len(out_planes) != n:
         raise ValueError("as many out_planes as planes")
-    n = len(planes)
-    row = []
+    f32, i32 = torch.float32, torch.int32
+    a = _take(("weight", weight, f32, (L, B, H, S_max)), ("out_weight", out_weight, f32, (L, B, H, S_out)), ("length", length, i32, (B,)),
+              ("kept", kept, i32, (L, B, H, budget)), ("new_len", new_len, i32, (B,)), ("dev_status", dev_status, i32, (B,)))
+    src, dst, row = [], [], []
     for x, y in zip(planes, out_planes):
-        _shape(x, "a plane", L, B, H, S_max, *x.shape[4:])
-        _shape(y, "an out plane", L, B, H, S_out, *x.shape[4:])
-        _is(x.dtype, out_plane=y)
-        row.append(x.element_size() * (x[0, 0, 0, 0].numel() if x.dim() > 4 else 1))
-    src, dst = (ctypes.c_void_p * max(n, 1))(*_ptrs(*planes)), (ctypes.c_void_p * max(n, 1))(*_ptrs(*out_planes))
-    a = _ptrs(weight, out_weight, length, kept, new_len, dev_status)
-    st = load().ppd_kv_evict(a[0], a[1], src, dst, (ctypes.c_int * max(n, 1))(*row), n, a[2], L, B, H, S_max, S_out,
-                             int(budget), int(n_sink), int(n_recent), *a[3:], _stream(stream))
+        cols = x.shape[4:]
+        p, o = _take(("a plane", x, x.dtype, (L, B, H, S_max, *cols)), ("an out plane", y, x.dtype, (L, B, H, S_out, *cols)))
+        src.append(p), dst.append(o), row.append(x.element_size() * math.prod(cols))
+    vps = ctypes.c_void_p * n
+    st = load().ppd_kv_evict(a[0], a[1], vps(*src), vps(*dst), (ctypes.c_int * n)(*row), n, a[2], L, B, H, S_max, S_out, budget, int(n_sink),
+                             int(n_recent), *a[3:], _stream(stream))
     _check(st, "ppd_kv_evict")
 
 
@@ -429,19 +412,13 @@ def ppd_sample_accept(logits, cand_tokens, parent, prefix_len, S_max, temperatur
                       accept_prob=None, stream=None):
     """Acceptance by sampling with given random numbers: u fp32 [B,T] uniform in [0, 1), noise fp32 [B,V]
     exponential; draft_probs fp32 [B,n_draft,V] and draft_row [B,T] for candidates drawn from distributions."""
-    B, T, V = logits.shape
+    B, T, V = rows = logits.shape
     n_draft = draft_probs.shape[1] if draft_probs is not None else 0
-    _is(torch.float32, logits=logits, u=u, noise=noise, draft_probs=draft_probs, accept_prob=accept_prob)
-    _is(torch.int32, cand_tokens=cand_tokens, parent=parent, prefix_len=prefix_len, draft_row=draft_row,
-        accept_len=accept_len, path=path, next_token=next_token, new_prefix_len=new_prefix_len, dev_status=dev_status)
-    _shape(u, "u", B, T), _shape(noise, "noise", B, V), _shape(draft_probs, "draft_probs", B, n_draft, V)
-    _shape(draft_row, "draft_row", B, T), _shape(accept_prob, "accept_prob", B, T)
-    _shape(cand_tokens, "cand_tokens", B, T), _shape(parent, "parent", B, T), _shape(path, "path", B, T)
-    for name, t in (("prefix_len", prefix_len), ("accept_len", accept_len), ("next_token", next_token),
-                    ("new_prefix_len", new_prefix_len), ("dev_status", dev_status)):
-        _shape(t, name, B)
-    a = _ptrs(logits, cand_tokens, parent, prefix_len, draft_probs, draft_row, u, noise, accept_len, path, next_token,
-              new_prefix_len, accept_prob, dev_status)
+    f32, i32, one, tree = torch.float32, torch.int32, (B,), (B, T)
+    a = _take(("logits", logits, f32, rows), ("cand_tokens", cand_tokens, i32, tree), ("parent", parent, i32, tree), ("prefix_len", prefix_len, i32, one),
+              ("draft_probs", draft_probs, f32, (B, n_draft, V)), ("draft_row", draft_row, i32, tree), ("u", u, f32, tree), ("noise", noise, f32, (B, V)),
+              ("accept_len", accept_len, i32, one), ("path", path, i32, tree), ("next_token", next_token, i32, one),
+              ("new_prefix_len", new_prefix_len, i32, one), ("accept_prob", accept_prob, f32, tree), ("dev_status", dev_status, i32, one))
     st = load().ppd_sample_accept(*a[:8], B, T, V, n_draft, int(S_max), float(temperature), *a[8:], _stream(stream))
     _check(st, "ppd_sample_accept")
 
