@@ -933,18 +933,19 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
     return cuda_status(ppd::launch_kv4_read(p, static_cast<cudaStream_t>(stream)));
 }
 
-// Parts that the keys of a slice are shared out to: three blocks fit an SM.  Fewer units
-// than that in all get one wave of parts; more are cut where whole units would leave over a
-// tenth of the last wave idle.  A part has at least eight chunks of 32 keys, two a warp.
-static int kv4_splits(long long slices, int row_blocks, int T, int S_max)
+// Parts that the keys of a slice are shared out to, blocks of which `per_sm` fit an SM.  Fewer
+// slices than that in all get one wave of parts; more are cut where whole slices would
+// leave over a tenth of the last wave idle.  A part has at least eight chunks of 32 keys,
+// two a warp.
+static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 {
-    const long long units = slices * row_blocks, slots = 3ll * num_sms();
+    const long long slots = (long long)per_sm * num_sms();
     const long long chunks = (S_max + 31) / 32 + (T + 31) / 32;
     long long n = 1;
-    if (units < slots)
-        n = slots / units;
+    if (slices < slots)
+        n = slots / slices;
     else
-        while (n < 4 && 10 * ((units * n + slots - 1) / slots) * slots > 11 * units * n) ++n;
+        while (n < 4 && 10 * ((slices * n + slots - 1) / slots) * slots > 11 * slices * n) ++n;
     const long long most = chunks / 8 < 1 ? 1 : chunks / 8;
     return (int)(n < most ? n : most);
 }
@@ -974,8 +975,7 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
         }
         return w;
     }
-    w.row_blocks = (int)((rows + 15) / 16);
-    w.splits = kv4_splits(slices, w.row_blocks, T, S_max);
+    w.splits = kv4_splits(slices, T, S_max, rows <= 8 ? 4 : 3);
     if (w.splits > 1) {
         const size_t n = (size_t)slices * w.splits * rows;
         w.ml = align_up(n * D * 4);
@@ -1020,7 +1020,6 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
     p.slices = slices;
     p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
-    p.row_blocks = w.row_blocks;
     if (w.tp) {
         ppd::AttnParams a{};
         a.prefix_len = prefix_len, a.parent = parent;
@@ -1047,7 +1046,7 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
         p.part_o = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + w.ml);
     }
-    if (slices * p.splits * p.row_blocks > 2147483647ll) return PPD_ERR_UNSUPPORTED;
+    if (slices * p.splits > 2147483647ll) return PPD_ERR_UNSUPPORTED;
     return cuda_status(ppd::launch_kv4_attention(p, D, static_cast<cudaStream_t>(stream)));
 }
 
@@ -1073,7 +1072,7 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
     p.slices = (long long)L * B * H;
     p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
-    p.splits = kv4_splits(p.slices, 1, T, S_max);
+    p.splits = kv4_splits(p.slices, T, S_max, 3);
     return cuda_status(ppd::launch_kv_weight(p, D, static_cast<cudaStream_t>(stream)));
 }
 

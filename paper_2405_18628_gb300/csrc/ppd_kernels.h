@@ -429,7 +429,6 @@ struct Kv4AttnParams {
     long long slices;
     int B, H, G, T, S_max, f32;
     float scale_log2;                // softmax scale * log2(e)
-    int row_blocks;                  // blocks of query rows of a slice
     int splits;                      // parts that a slice's keys are shared out to
     float *part_o;                   // splits > 1: [slices][splits][G * T][D] unnormalised outputs
     float2 *part_ml;                 // [slices][splits][G * T] maxima (log2) and sums

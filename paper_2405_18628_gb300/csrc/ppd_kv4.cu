@@ -162,56 +162,54 @@ cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream)
 
 // ------------------------------------------------------------------ attention, few rows
 
-// Blocks of 16 query rows (the G query heads of a K/V head times the T tree tokens) against
-// a range of one slice's keys, in registers: four warps take chunks of 32 keys in turn,
+// Up to 16 query rows of a slice (the G query heads of a K/V head times the T tree tokens, in NB
+// blocks of eight) against a range of its keys, in registers: four warps take chunks of 32 keys
+// in turn.  Keys and channels fill the products' 16 rows, queries their eight columns:
 //
-//   S = Q K^T    mma.sync, K's fragments made from the codes a thread loads: thread t of a
-//                quad holds channels [t D / 4, (t + 1) D / 4) of its key, the order of the
-//                channels in the sum being free as long as Q follows it
-//   O += P V     P from S's accumulators, V's fragments from the codes of two keys at once:
-//                columns 2t and 2t + 1 of a block of eight keys are its rows t and t + 4, so
-//                that a warp's loads of V meet every bank once
+//   S^T = K Q^T      K's fragments made from the codes a thread loads: thread t of a quad holds
+//                    channels [t D / 4, (t + 1) D / 4) of two keys, the order of the channels in
+//                    the sum being free as long as Q follows it
+//   O^T += V^T P^T   P^T's fragments are S^T's accumulators, transposed in 8 x 8 tiles by
+//                    movmatrix; V^T's are made from the codes of two neighbouring keys at once,
+//                    thread g of a column holding channels [g D / 8, (g + 1) D / 8)
 //
 // with a running maximum that moves when a score passes it by 2^8, and P as bf16 hi + lo
-// (2^-18: V's values are exact, so the output's own rounding is all that shows).  Up to
-// eight query rows leave the lower half of a product's 16 rows free: lo goes there and costs
-// nothing; more rows take two products.  Each warp's state is merged in shared memory, those of
-// a split slice by kv4_merge_kernel.  A chunk's codes and
-// scales come by asynchronous copies into a ring of the warp's own: no barrier in the loop.
+// (2^-18: V's values are exact, so the output's own rounding is all that shows).  Each warp's
+// state is merged in shared memory, those of a split slice by kv4_merge_kernel.  A chunk's
+// codes and scales come by asynchronous copies into a ring of the warp's own: no barrier in the
+// loop.
 template <int D>
 struct Kv4Few {
-    static constexpr int WARPS = 4, THREADS = 128, STAGES = 4, KEYS = 32;
+    static constexpr int WARPS = 4, THREADS = 128, KEYS = 32;
+    static constexpr int STAGES = 3;
     static constexpr int RB = D / 2;                         // bytes of a row's codes
     static constexpr int SB = D / kKv4Group;                 // scale bytes of a row
     static constexpr uint32_t CODES = KEYS * RB;             // of K, or V, in a stage
+    static constexpr uint32_t OFF_SC = 2 * CODES;            // scales, a word a key: K's, then V's
     static constexpr uint32_t STAGE = 2 * CODES + 2 * KEYS * 4;
-    static constexpr uint32_t OFF_STATE = 0;                 // merge: [WARPS][16][D] over the ring
-    static constexpr uint32_t RING = WARPS * STAGES * STAGE;
+    static constexpr uint32_t RING = WARPS * STAGES * STAGE; // merge: [WARPS][rows][D] over the ring
     static constexpr uint32_t OFF_ML = RING;                 // [WARPS][16]: maximum, sum
     static constexpr uint32_t OFF_PARENT = OFF_ML + WARPS * 16 * 8;
     static constexpr uint32_t SMEM = OFF_PARENT + kMaxTree * 4;
     static_assert(WARPS * 16 * D * 4 <= RING, "the states fit over the ring");
 };
 
-template <int D, bool HALF>   // HALF: at most eight rows
-__global__ void __launch_bounds__(Kv4Few<D>::THREADS, 3) kv4_attention_few_kernel(const Kv4AttnParams p)
+template <int D, int NB>
+__global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_attention_few_kernel(const Kv4AttnParams p)
 {
     using C = Kv4Few<D>;
-    constexpr int NH = HALF ? 1 : 2;   // rows of a thread: g, and g + 8
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_release();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    // row block fastest, then the split, then the slice
-    const int rb = (int)(blockIdx.x % p.row_blocks);
-    const int us = (int)(blockIdx.x / p.row_blocks), split = us % p.splits;
-    const long long u = us / p.splits;
-    const int b = (int)(u / p.H % p.B);
-    const int T = p.T, R = p.G * T, r0 = rb * 16;
+    const int split = (int)(blockIdx.x % p.splits);
+    const uint32_t u = blockIdx.x / p.splits;
+    const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B);
+    const int T = p.T, R = p.G * T;
     const int32_t *parent = p.parent + (size_t)b * T;
     const int P_in = ld_input(p.prefix_len + b);
     const int P = min(max(P_in, 0), p.S_max);
-    if (u % p.H == 0 && u / p.H < p.B && split == 0 && rb == 0 && warp == 0) {
+    if (u % p.H == 0 && u / p.H < p.B && split == 0 && warp == 0) {
         const int st = tree_status(parent, T, P_in, p.S_max, lane);
         if (lane == 0) p.dev_status[b] = st;
     }
@@ -223,30 +221,35 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, 3) kv4_attention_few_kerne
 
     const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE;
     const size_t row0 = (size_t)u * p.S_max;
-    // a chunk's copies: rows past the prefix arrive as zeros (finite: scale 2^-20)
+    // Where the warp's loads of V take a row's 16-byte pieces: rows 2t of a column's threads
+    // (2t + 1 likewise) lie in different banks.
+    auto v_swizzle = [](int row) {
+        return D == 128 ? (((row >> 1) & 1) << 1) | (((row >> 2) & 1) << 2) : ((row >> 2) & 1) << 1;
+    };
+    constexpr int UPR = C::RB / 16;   // 16-byte pieces of a row; piece i of a lane is 512 bytes on from piece i - 1
+    const int f_row = lane / UPR;
     auto fetch = [&](int c, int stage) {
         if (c < min(c1, n_pref)) {
-            const int k0 = c * C::KEYS;
+            const int k0 = c * C::KEYS, n = P - k0;
             const uint32_t dst = ring + stage * C::STAGE;
-            constexpr int UPR = C::RB / 16;   // 16-byte units of a row
+            const size_t at = (row0 + k0) * C::RB + lane * 16;
+            const uint8_t *k = p.k_cache + at, *v = p.v_cache + at;
 #pragma unroll
-            for (int i = 0; i < C::KEYS * UPR / 32; ++i) {
-                const int unit = i * 32 + lane, row = unit / UPR;
-                const bool in = k0 + row < P;
-                const size_t src = (row0 + (in ? k0 : 0)) * C::RB + (in ? unit * 16 : 0);
-                const uint32_t uk = unit ^ (((row >> 2) & 1) << 2);
-                const uint32_t uv = D == 128 ? unit ^ (((row >> 1) & 1) << 1) : unit;
-                cp_async16(dst + uk * 16, p.k_cache + src, in ? 16u : 0u);
-                cp_async16(dst + C::CODES + uv * 16, p.v_cache + src, in ? 16u : 0u);
+            for (int i = 0; i < UPR; ++i) {
+                const int row = i * (32 / UPR) + f_row;
+                const uint32_t to = dst + i * 512 + lane * 16, to_v = dst + C::CODES + (uint32_t)((i * 32 + lane) ^ v_swizzle(row)) * 16;
+                const bool in = row < n;   // rows past the prefix arrive as zeros (finite: scale 2^-20)
+                cp_async16(to, in ? k + i * 512 : p.k_cache, in ? 16u : 0u);
+                cp_async16(to_v, in ? v + i * 512 : p.v_cache, in ? 16u : 0u);
             }
             // a word holds the row's scales (D = 64: those of an even and an odd row; the
             // tensors' last word may be half one)
-            const bool in = k0 + lane < P;
-            const size_t at = ((row0 + (in ? k0 + lane : 0)) * C::SB) & ~(size_t)3;
-            const size_t left = p.scale_bytes - at;
-            const uint32_t n = in ? (left < 4 ? (uint32_t)left : 4u) : 0u;
-            cp_async4(dst + 2 * C::CODES + lane * 4, p.k_scale + at, n);
-            cp_async4(dst + 2 * C::CODES + 128 + lane * 4, p.v_scale + at, n);
+            const bool in = lane < n;
+            const size_t a = ((row0 + (in ? k0 + lane : 0)) * C::SB) & ~(size_t)3;
+            const size_t left = p.scale_bytes - a;
+            const uint32_t m = in ? (left < 4 ? (uint32_t)left : 4u) : 0u;
+            cp_async4(dst + C::OFF_SC + lane * 4, p.k_scale + a, m);
+            cp_async4(dst + C::OFF_SC + 128 + lane * 4, p.v_scale + a, m);
         }
         cp_async_commit();
     };
@@ -254,255 +257,278 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, 3) kv4_attention_few_kerne
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s, next += C::WARPS) fetch(next, s);
 
-    // Q fragments: rows g and g + 8 of the block
+    // Q's fragments: rows g of the blocks
     const size_t q_row0 = (size_t)u * R;
-    uint32_t q[D / 16][4];
+    uint32_t q[NB][D / 16][2];
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = 8 * nb + g;
+        const size_t at = (q_row0 + (r < R ? r : 0)) * D + (D / 4) * t;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = h < NH ? r0 + g + 8 * h : R;
-            const size_t at = (q_row0 + (r < R ? r : 0)) * D + (D / 4) * t + 4 * s;
-            q[s][h] = r < R ? ld_pair(p.q, at, p.f32) : 0u;
-            q[s][2 + h] = r < R ? ld_pair(p.q, at + 2, p.f32) : 0u;
-        }
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) q[nb][s][e] = r < R ? ld_pair(p.q, at + 4 * s + 2 * e, p.f32) : 0u;
     }
-    float o[D / 8][4] = {};   // rows g, g + 8; HALF: row g's hi and lo parts
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float o[D / 16][NB][4] = {};   // channels g D / 8 + i and D / 16 on, queries 2t and 2t + 1
+    float m[NB][2], l[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) m[nb][0] = m[nb][1] = -INFINITY, l[nb][0] = l[nb][1] = 0.f;
     __syncthreads();   // the parents are in shared memory
 
-    const int perm = (g >> 1) + 4 * (g & 1);   // key of column g in a block of eight
     int stage = 0;
     for (int c = c0 + warp; c < c1; c += C::WARPS) {
-        fetch(next, (stage + C::STAGES - 1) % C::STAGES);
+        fetch(next, stage == 0 ? C::STAGES - 1 : stage - 1);
         next += C::WARPS;
         cp_async_wait<C::STAGES - 1>();
         __syncwarp();
         const bool tree = c >= n_pref;
         const int k0 = (tree ? c - n_pref : c) * C::KEYS;
         const uint32_t src = ring + stage * C::STAGE;
-        float s[4][4] = {};
-        if (!tree) {
-            const uint32_t ks = ld_shared_u32(src + 2 * C::CODES + lane * 4) >>
-                                (D == 64 ? (uint32_t)((row0 + k0 + lane) & 1) * 16u : 0u);
+        const uint32_t odd = D == 64 ? (uint32_t)(row0 + k0) & 1u : 0u;   // which half of a word is row 0's
+        float s[2][NB][4] = {};
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int row = 8 * n + perm;
-                const uint32_t sw = __shfl_sync(0xffffffffu, ks, row);
-                const uint32_t s2 = kv4_scale2(((sw >> (D == 128 ? 8 * t : 8 * (t >> 1))) & 0xFFu) * 0x10001u);
-                const uint32_t o2 = kv4_offset2(s2);
-                uint32_t w[D / 32];
-                const uint32_t x = ((row >> 2) & 1) * 64u;
-                if constexpr (D == 128) {
-                    const uint4 v = ld_shared_u128(src + (((uint32_t)row * 64u + t * 16u) ^ x));
-                    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-                } else {
-                    const uint2 v = ld_shared_u64(src + (((uint32_t)row * 32u + t * 8u) ^ x));
-                    w[0] = v.x, w[1] = v.y;
-                }
+        for (int mt = 0; mt < 2; ++mt) {
+            if (!tree) {
+                uint32_t w[2][D / 32], s2[2], o2[2];
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_bf16(s[n], q[k], kv4_pair(w[k >> 1] >> (8 * (k & 1)), s2, o2),
-                             kv4_pair(w[k >> 1] >> (8 * (k & 1) + 4), s2, o2));
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int j = k0 + 8 * n + perm;
-                const size_t at = ((size_t)u * T + (j < T ? j : 0)) * D + (D / 4) * t;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_bf16(s[n], q[k], j < T ? ld_pair(p.k_tree, at + 4 * k, p.f32) : 0u,
-                             j < T ? ld_pair(p.k_tree, at + 4 * k + 2, p.f32) : 0u);
-            }
-        }
-        // visible keys of the chunk for rows g and g + 8
-        uint32_t see[2];
-        if (!tree) {
-            see[0] = see[1] = P - k0 >= 32 ? 0xffffffffu : (1u << (P - k0)) - 1u;
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = h < NH ? r0 + g + 8 * h : R;
-                see[h] = 0u;
-                for (int a = r < R ? r % T : -1; a >= k0;) {   // up the tree, strictly
-                    if (a - k0 < 32) see[h] |= 1u << (a - k0);
-                    const int up = par[a];
-                    a = up < a ? up : -1;
-                }
-            }
-        }
-        if (__any_sync(0xffffffffu, (see[0] & see[1]) != 0xffffffffu)) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int e = 0; e < 2 * NH; ++e)
-                    if (!((see[e >> 1] >> (8 * n + t + 4 * (e & 1))) & 1u)) s[n][e] = -INFINITY;
-        }
-        float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int h = 0; h < NH; ++h) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) mx[h] = max3(mx[h], s[n][2 * h], s[n][2 * h + 1]);
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2)) * p.scale_log2;
-        }
-        if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.f || mx[1] > m[1] + 8.f)) {
-            float a[2];
-#pragma unroll
-            for (int h = 0; h < NH; ++h) {
-                const float nw = fmaxf(m[h], mx[h]);
-                a[h] = m[h] == nw ? 1.f : ex2(m[h] - nw);
-                m[h] = nw;
-                l[h] *= a[h];
-            }
-            if (HALF) a[1] = a[0];
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][e] *= a[e >> 1];
-        }
-        // a row that has seen no key yet: every score is -inf, every probability 0
-        const float nm[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
-        // P's fragments of 16 keys: hi and lo in the two halves of the rows, or one after the other
-        uint32_t pa[2][HALF ? 1 : 2][4];
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int h = 0; h < NH; ++h) {
-                const float p0 = ex2(fmaf(s[n][2 * h], p.scale_log2, nm[h])), p1 = ex2(fmaf(s[n][2 * h + 1], p.scale_log2, nm[h]));
-                l[h] += p0 + p1;
-                uint32_t hi, lo;
-                split_bf16x2(pack2(p0, p1), p0, p1, hi, lo);
-                pa[n >> 1][0][2 * (n & 1) + h] = hi;
-                if (HALF) pa[n >> 1][0][2 * (n & 1) + 1] = lo;
-                else pa[n >> 1][NH - 1][2 * (n & 1) + h] = lo;
-            }
-        auto add_pv = [&](int kk, float (&acc)[4], uint32_t b0, uint32_t b1) {
-            mma_bf16(acc, pa[kk][0], b0, b1);
-            if (!HALF) mma_bf16(acc, pa[kk][NH - 1], b0, b1);
-        };
-        // O += P V, 16 keys at a time: rows t, t + 4 | t + 8, t + 12 of the 16
-        if (!tree) {
-            const uint32_t vs = ld_shared_u32(src + 2 * C::CODES + 128 + lane * 4) >>
-                                (D == 64 ? (uint32_t)((row0 + k0 + lane) & 1) * 16u : 0u);
-            const uint32_t v0 = src + C::CODES;
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                uint32_t w[4][D / 64], s2[2], o2[2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t row = 16 * kk + t + 4 * i;
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t row = 16 * mt + 8 * h + g;
                     if constexpr (D == 128) {
-                        const uint2 v = ld_shared_u64(v0 + ((row * 64u + g * 8u) ^ (((row >> 1) & 1) * 32u)));
-                        w[i][0] = v.x, w[i][1] = v.y;
+                        const uint4 v = ld_shared_u128(src + row * 64u + t * 16u);
+                        w[h][0] = v.x, w[h][1] = v.y, w[h][2] = v.z, w[h][3] = v.w;
                     } else {
-                        w[i][0] = ld_shared_u32(v0 + row * 32u + g * 4u);
+                        const uint2 v = ld_shared_u64(src + row * 32u + t * 8u);
+                        w[h][0] = v.x, w[h][1] = v.y;
+                    }
+                    const uint32_t at = D == 128 ? t : (((row ^ odd) & 1u) << 1) + (t >> 1);
+                    s2[h] = kv4_scale2(ld_shared_u8(src + C::OFF_SC + row * 4u + at) * 0x10001u);
+                    o2[h] = kv4_offset2(s2[h]);
+                }
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t a[4] = {kv4_pair(w[0][k >> 1] >> (8 * (k & 1)), s2[0], o2[0]), kv4_pair(w[1][k >> 1] >> (8 * (k & 1)), s2[1], o2[1]),
+                                           kv4_pair(w[0][k >> 1] >> (8 * (k & 1) + 4), s2[0], o2[0]), kv4_pair(w[1][k >> 1] >> (8 * (k & 1) + 4), s2[1], o2[1])};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma_bf16(s[mt][nb], a, q[nb][k][0], q[nb][k][1]);
+                }
+            } else {
+                const int j0 = k0 + 16 * mt + g, j1 = j0 + 8;
+                const size_t at0 = ((size_t)u * T + (j0 < T ? j0 : 0)) * D + (D / 4) * t, at1 = ((size_t)u * T + (j1 < T ? j1 : 0)) * D + (D / 4) * t;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t a[4] = {j0 < T ? ld_pair(p.k_tree, at0 + 4 * k, p.f32) : 0u, j1 < T ? ld_pair(p.k_tree, at1 + 4 * k, p.f32) : 0u,
+                                           j0 < T ? ld_pair(p.k_tree, at0 + 4 * k + 2, p.f32) : 0u, j1 < T ? ld_pair(p.k_tree, at1 + 4 * k + 2, p.f32) : 0u};
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma_bf16(s[mt][nb], a, q[nb][k][0], q[nb][k][1]);
+                }
+            }
+        }
+        // visible keys of the chunk for queries 2t and 2t + 1 of the blocks
+        if (tree || P - k0 < C::KEYS) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t see;
+                    if (!tree) {
+                        see = (1u << (P - k0)) - 1u;
+                    } else {
+                        see = 0u;
+                        const int r = 8 * nb + 2 * t + e;
+                        for (int a = r < R ? r % T : -1; a >= k0;) {   // up the tree, strictly
+                            if (a - k0 < 32) see |= 1u << (a - k0);
+                            const int up = par[a];
+                            a = up < a ? up : -1;
+                        }
+                    }
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (!((see >> (16 * mt + 8 * h + g)) & 1u)) s[mt][nb][2 * h + e] = -INFINITY;
+                }
+            __syncwarp();
+        }
+        float mx[NB][2];
+        bool grows = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = fmaxf(fmaxf(s[0][nb][e], s[0][nb][2 + e]), fmaxf(s[1][nb][e], s[1][nb][2 + e]));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                mx[nb][e] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16)) * p.scale_log2;
+                grows |= mx[nb][e] > m[nb][e] + 8.f;
+            }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float nw = fmaxf(m[nb][e], mx[nb][e]);
+                    const float a = m[nb][e] == nw ? 1.f : ex2(m[nb][e] - nw);
+                    m[nb][e] = nw;
+                    l[nb][e] *= a;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) o[i][nb][e] *= a, o[i][nb][2 + e] *= a;
+                }
+        }
+        // P^T's fragments of 16 keys: the accumulators' 8 x 8 tiles transposed
+        uint32_t hi[2][NB][2], lo[2][NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            // a query that has seen no key yet: every score is -inf, every probability 0
+            const float n0 = m[nb][0] == -INFINITY ? 0.f : -m[nb][0], n1 = m[nb][1] == -INFINITY ? 0.f : -m[nb][1];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float p0 = ex2(fmaf(s[mt][nb][2 * h], p.scale_log2, n0)), p1 = ex2(fmaf(s[mt][nb][2 * h + 1], p.scale_log2, n1));
+                    l[nb][0] += p0;
+                    l[nb][1] += p1;
+                    uint32_t a, c2;
+                    split_bf16x2_fma(pack2(p0, p1), a, c2);
+                    hi[mt][nb][h] = movmatrix(a);
+                    lo[mt][nb][h] = movmatrix(c2);
+                }
+        }
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            auto add_pv = [&](int i, const uint32_t (&a)[4]) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    mma_bf16(o[i][nb], a, hi[mt][nb][0], hi[mt][nb][1]);
+                    mma_bf16(o[i][nb], a, lo[mt][nb][0], lo[mt][nb][1]);
+                }
+            };
+            if (!tree) {
+                uint32_t w[4][D / 64], s2[2], o2[2];   // rows 2t, 2t + 1 | 2t + 8, 2t + 9 of the 16
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t row = 16 * mt + 2 * t + (x & 1) + 8 * (x >> 1);
+                    if constexpr (D == 128) {
+                        const uint2 v = ld_shared_u64(src + C::CODES + ((row * 64u + g * 8u) ^ (uint32_t)(v_swizzle(row) * 16)));
+                        w[x][0] = v.x, w[x][1] = v.y;
+                    } else {
+                        w[x][0] = ld_shared_u32(src + C::CODES + ((row * 32u + g * 4u) ^ (uint32_t)(v_swizzle(row) * 16)));
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t sa = __shfl_sync(0xffffffffu, vs, 16 * kk + t + 8 * i);
-                    const uint32_t sb = __shfl_sync(0xffffffffu, vs, 16 * kk + t + 8 * i + 4);
-                    const uint32_t sh = D == 128 ? 8 * (g >> 1) : 8 * (g >> 2);
-                    s2[i] = kv4_scale2(((sa >> sh) & 0xFFu) | ((sb >> sh) & 0xFFu) << 16);
-                    o2[i] = kv4_offset2(s2[i]);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t row = 16 * mt + 2 * t + 8 * h;
+                    const uint32_t at = src + C::OFF_SC + 128 + row * 4u;
+                    const uint32_t a0 = D == 128 ? at + (g >> 1) : at + (((row ^ odd) & 1u) << 1) + (g >> 2);
+                    const uint32_t a1 = D == 128 ? at + 4 + (g >> 1) : at + 4 + ((((row + 1) ^ odd) & 1u) << 1) + (g >> 2);
+                    s2[h] = kv4_scale2(ld_shared_u8(a0) | ld_shared_u8(a1) << 16);
+                    o2[h] = kv4_offset2(s2[h]);
                 }
+                // channel i of a word is nibble i / 2 + 4 (i % 2): the low halves of two keys' words
+                // side by side hold the even channels, the high halves the odd ones
+                if constexpr (D == 128) {
 #pragma unroll
-                for (int x = 0; x < D / 64; ++x) {
+                    for (int odd_ch = 0; odd_ch < 2; ++odd_ch) {
+                        const uint32_t sel = odd_ch ? 0x7632u : 0x5410u;
+                        const uint32_t x0 = __byte_perm(w[0][0], w[1][0], sel), x1 = __byte_perm(w[0][1], w[1][1], sel);
+                        const uint32_t x2 = __byte_perm(w[2][0], w[3][0], sel), x3 = __byte_perm(w[2][1], w[3][1], sel);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {   // nibbles 0..3, then 4..7
-                        const uint32_t sel = half ? 0x7632u : 0x5410u;
-                        const uint32_t c0w = __byte_perm(w[0][x], w[1][x], sel), c1w = __byte_perm(w[2][x], w[3][x], sel);
+                        for (int n = 0; n < 4; ++n) {
+                            const uint32_t a[4] = {kv4_pair(x0 >> (4 * n), s2[0], o2[0]), kv4_pair(x1 >> (4 * n), s2[0], o2[0]),
+                                                   kv4_pair(x2 >> (4 * n), s2[1], o2[1]), kv4_pair(x3 >> (4 * n), s2[1], o2[1])};
+                            add_pv(2 * n + odd_ch, a);
+                        }
+                    }
+                } else {
+                    // eight channels a thread: 0..3 in the upper rows, 4..7 in the lower ones
+                    const uint32_t e0 = __byte_perm(w[0][0], w[1][0], 0x5410), d0 = __byte_perm(w[0][0], w[1][0], 0x7632);
+                    const uint32_t e1 = __byte_perm(w[2][0], w[3][0], 0x5410), d1 = __byte_perm(w[2][0], w[3][0], 0x7632);
 #pragma unroll
-                        for (int n = 0; n < 4; ++n)   // nibble n + 4 half: channel 2 n + half of the word
-                            add_pv(kk, o[8 * x + 2 * n + half], kv4_pair(c0w >> (4 * n), s2[0], o2[0]),
-                                   kv4_pair(c1w >> (4 * n), s2[1], o2[1]));
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t y0 = i & 1 ? d0 : e0, y1 = i & 1 ? d1 : e1;
+                        const uint32_t a[4] = {kv4_pair(y0 >> (4 * (i >> 1)), s2[0], o2[0]), kv4_pair(y0 >> (4 * (i >> 1) + 8), s2[0], o2[0]),
+                                               kv4_pair(y1 >> (4 * (i >> 1)), s2[1], o2[1]), kv4_pair(y1 >> (4 * (i >> 1) + 8), s2[1], o2[1])};
+                        add_pv(i, a);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 16; i += 2) {
+                    uint32_t v[2][4];   // channels i, i + 1 (and D / 16 on) of the four keys
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int j = k0 + 16 * mt + 2 * t + (x & 1) + 8 * (x >> 1);
+                            v[h][x] = j < T ? ld_pair(p.v_tree, ((size_t)u * T + j) * D + (D / 8) * g + (D / 16) * h + i, p.f32) : 0u;
+                        }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t sel = x ? 0x7632u : 0x5410u;
+                        const uint32_t a[4] = {__byte_perm(v[0][0], v[0][1], sel), __byte_perm(v[1][0], v[1][1], sel),
+                                               __byte_perm(v[0][2], v[0][3], sel), __byte_perm(v[1][2], v[1][3], sel)};
+                        add_pv(i + x, a);
                     }
                 }
             }
-        } else {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int i = 0; i < D / 8; i += 2) {   // channels i, i + 1 of g's
-                    uint32_t v[4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int j = k0 + 16 * kk + t + 4 * x;
-                        v[x] = j < T ? ld_pair(p.v_tree, ((size_t)u * T + j) * D + (D / 8) * g + i, p.f32) : 0u;
-                    }
-                    add_pv(kk, o[i], __byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410));
-                    add_pv(kk, o[i + 1], __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
-                }
         }
         __syncwarp();   // the stage is read: the next fetch may overwrite it
-        stage = (stage + 1) % C::STAGES;
+        stage = stage == C::STAGES - 1 ? 0 : stage + 1;
     }
     cp_async_wait<0>();
     __syncthreads();   // every warp is done with its ring: the states go over it
 
-    float *st = reinterpret_cast<float *>(smem) + (size_t)warp * 16 * D;
+    constexpr int ROWS = 8 * NB;
+    float *st = reinterpret_cast<float *>(smem) + (size_t)warp * ROWS * D;
     float2 *ml = reinterpret_cast<float2 *>(smem + C::OFF_ML);
-    if (HALF) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) o[i][0] += o[i][2], o[i][1] += o[i][3];
-    }
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        if (t == 0) ml[warp * 16 + g + 8 * h] = make_float2(m[h], l[h]);
+        for (int e = 0; e < 2; ++e) {
+            float x = l[nb][e];
+            x += __shfl_xor_sync(0xffffffffu, x, 4);
+            x += __shfl_xor_sync(0xffffffffu, x, 8);
+            x += __shfl_xor_sync(0xffffffffu, x, 16);
+            const int r = 8 * nb + 2 * t + e;
+            if (g == 0) ml[warp * ROWS + r] = make_float2(m[nb][e], x);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < D / 8; i += 4)
-                *reinterpret_cast<float4 *>(st + (g + 8 * h) * D + (2 * t + e) * (D / 8) + i) =
-                    make_float4(o[i][2 * h + e], o[i + 1][2 * h + e], o[i + 2][2 * h + e], o[i + 3][2 * h + e]);
-    }
-    __syncthreads();
-    // a thread merges D / 8 channels of a row
-    const int row = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (D / 8);
-    if (row >= 8 * NH || r0 + row >= R) return;
-    float M = -INFINITY, w[C::WARPS], L = 0.f;
-#pragma unroll
-    for (int i = 0; i < C::WARPS; ++i) M = fmaxf(M, ml[i * 16 + row].x);
-#pragma unroll
-    for (int i = 0; i < C::WARPS; ++i) {
-        const float2 x = ml[i * 16 + row];
-        w[i] = x.x == -INFINITY ? 0.f : ex2(x.x - M);
-        L += x.y * w[i];
-    }
-    const size_t r = q_row0 + r0 + row;
-    const bool whole = p.splits == 1;
-    const float inv = whole ? 1.f / L : 1.f;
-    const long long part = (u * p.splits + split) * R + r0 + row;
-    if (d0 == 0) {
-        if (whole) {
-            if (p.lse) p.lse[r] = (M + lg2(L)) * 0.69314718055994530942f;
-        } else {
-            p.part_ml[part] = make_float2(M, L);
+                for (int i = 0; i < D / 16; i += 4)
+                    *reinterpret_cast<float4 *>(st + r * D + g * (D / 8) + h * (D / 16) + i) =
+                        make_float4(o[i][nb][2 * h + e], o[i + 1][nb][2 * h + e], o[i + 2][nb][2 * h + e], o[i + 3][nb][2 * h + e]);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < D / 8; i += 4) {
+    __syncthreads();
+    // a thread merges four channels of a row at a time
+    const bool whole = p.splits == 1;
+    for (int i = threadIdx.x; i < R * (D / 4); i += C::THREADS) {
+        const int row = i / (D / 4), d = i % (D / 4) * 4;
+        float M = -INFINITY, L = 0.f;
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
+        for (int x = 0; x < C::WARPS; ++x) M = fmaxf(M, ml[x * ROWS + row].x);
+#pragma unroll
         for (int x = 0; x < C::WARPS; ++x) {
-            const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem) + (size_t)x * 16 * D + row * D + d0 + i);
-            a.x += w[x] * v.x, a.y += w[x] * v.y, a.z += w[x] * v.z, a.w += w[x] * v.w;
+            const float2 y = ml[x * ROWS + row];
+            const float w = y.x == -INFINITY ? 0.f : ex2(y.x - M);
+            const float4 v = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem) + (x * ROWS + row) * D + d);
+            L += y.y * w;
+            a.x += w * v.x, a.y += w * v.y, a.z += w * v.z, a.w += w * v.w;
         }
+        const size_t r = q_row0 + row, part = ((size_t)u * p.splits + split) * R + row;
         if (whole) {
-            const uint2 v = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
-            *reinterpret_cast<uint2 *>(p.out + r * D + d0 + i) = v;
+            const float inv = 1.f / L;
+            if (d == 0 && p.lse) p.lse[r] = (M + lg2(L)) * 0.69314718055994530942f;
+            *reinterpret_cast<uint2 *>(p.out + r * D + d) = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
         } else {
-            *reinterpret_cast<float4 *>(p.part_o + part * D + d0 + i) = a;
+            if (d == 0) p.part_ml[part] = make_float2(M, L);
+            *reinterpret_cast<float4 *>(p.part_o + part * D + d) = a;
         }
     }
 }
 
-// The parts of split slices: a thread merges four channels of a row.
-__global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnParams p, int D)
+// The parts of split slices: a thread merges four channels of a row, the loads of eight parts
+// in flight.
+__global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4AttnParams p, int D)
 {
     pdl_release();
     pdl_wait();
@@ -514,40 +540,53 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttnParams p, i
     const long long u = r / R, first = u * p.splits * R + (r - u * R);
     float M = -INFINITY, L = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < p.splits; ++s) M = fmaxf(M, p.part_ml[first + s * R].x);
-    for (int s = 0; s < p.splits; ++s) {
-        const float2 x = p.part_ml[first + s * R];
-        if (x.x == -INFINITY) continue;
-        const float w = ex2(x.x - M);
-        const float4 v = *reinterpret_cast<const float4 *>(p.part_o + (first + s * R) * D + d);
-        L += x.y * w;
-        a.x += w * v.x, a.y += w * v.y, a.z += w * v.z, a.w += w * v.w;
+    for (int s0 = 0; s0 < p.splits; s0 += 8) {
+        float2 x[8];
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const long long at = first + min(s0 + i, p.splits - 1) * R;
+            x[i] = __ldcg(p.part_ml + at);
+            v[i] = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + d));
+        }
+        float nw = M;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) nw = fmaxf(nw, x[i].x);
+        const float so = M == nw ? 1.f : ex2(M - nw);   // (no part with a key yet: both -inf)
+        M = nw;
+        L *= so, a.x *= so, a.y *= so, a.z *= so, a.w *= so;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float w = s0 + i >= p.splits || x[i].x == -INFINITY ? 0.f : ex2(x[i].x - M);
+            L = fmaf(w, x[i].y, L);
+            a.x = fmaf(w, v[i].x, a.x), a.y = fmaf(w, v[i].y, a.y), a.z = fmaf(w, v[i].z, a.z), a.w = fmaf(w, v[i].w, a.w);
+        }
     }
     const float inv = 1.f / L;
     if (d == 0 && p.lse) p.lse[r] = (M + lg2(L)) * 0.69314718055994530942f;
     *reinterpret_cast<uint2 *>(p.out + r * D + d) = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
 }
 
-template <int D, bool HALF>
+template <int D, int NB>
 static cudaError_t launch_few_t(const Kv4AttnParams &p, cudaStream_t stream)
 {
     using C = Kv4Few<D>;
     static std::atomic<uint64_t> configured{0};
-    const cudaError_t e = allow_smem(kv4_attention_few_kernel<D, HALF>, C::SMEM, configured);
+    const cudaError_t e = allow_smem(kv4_attention_few_kernel<D, NB>, C::SMEM, configured);
     if (e != cudaSuccess) return e;
-    return launch_chained_smem(kv4_attention_few_kernel<D, HALF>, dim3((unsigned)(p.slices * p.splits * p.row_blocks)),
-                               dim3(C::THREADS), dim3(1), C::SMEM, stream, p);
+    return launch_chained_smem(kv4_attention_few_kernel<D, NB>, dim3((unsigned)(p.slices * p.splits)), dim3(C::THREADS), dim3(1), C::SMEM,
+                               stream, p);
 }
 
 cudaError_t launch_kv4_attention(const Kv4AttnParams &p, int D, cudaStream_t stream)
 {
-    const bool half = p.G * p.T <= 8;
-    const cudaError_t e = D == 128 ? (half ? launch_few_t<128, true>(p, stream) : launch_few_t<128, false>(p, stream))
-                                   : (half ? launch_few_t<64, true>(p, stream) : launch_few_t<64, false>(p, stream));
+    const bool one = p.G * p.T <= 8;
+    const cudaError_t e = D == 128 ? (one ? launch_few_t<128, 1>(p, stream) : launch_few_t<128, 2>(p, stream))
+                                   : (one ? launch_few_t<64, 1>(p, stream) : launch_few_t<64, 2>(p, stream));
     if (e != cudaSuccess || p.splits == 1) return e;
-    const int rows = 256 / (D / 4);
+    const int rows = 128 / (D / 4);
     const long long n = p.slices * p.G * p.T;
-    return launch_chained(kv4_merge_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(256), dim3(1), stream, p, D);
+    return launch_chained(kv4_merge_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(128), dim3(1), stream, p, D);
 }
 
 }  // namespace ppd

@@ -71,6 +71,14 @@ PPD_DEV void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// An 8 x 8 tile of 16-bit values, row lane / 4, columns 2 (lane % 4) and the next: transposed.
+PPD_DEV uint32_t movmatrix(uint32_t x)
+{
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
+}
+
 // Asynchronous copies into shared memory; bytes beyond `n` of the 16 (or 4) read as zero.
 PPD_DEV void cp_async16(uint32_t dst, const void *src, uint32_t n)
 {
@@ -88,6 +96,12 @@ PPD_DEV uint32_t ld_shared_u32(uint32_t a)
 {
     uint32_t v;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+PPD_DEV uint32_t ld_shared_u8(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
 PPD_DEV uint2 ld_shared_u64(uint32_t a)
