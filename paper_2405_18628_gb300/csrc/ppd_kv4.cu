@@ -213,11 +213,12 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
         const int st = tree_status(parent, T, P_in, p.S_max, lane);
         if (lane == 0) p.dev_status[b] = st;
     }
-    int *par = reinterpret_cast<int *>(smem + C::OFF_PARENT);
-    for (int i = threadIdx.x; i < T; i += C::THREADS) par[i] = ld_input(parent + i);
-
     const int n_pref = (P + C::KEYS - 1) / C::KEYS, n_all = n_pref + (T + C::KEYS - 1) / C::KEYS;
     const int c0 = (int)((long long)n_all * split / p.splits), c1 = (int)((long long)n_all * (split + 1) / p.splits);
+
+    int *par = reinterpret_cast<int *>(smem + C::OFF_PARENT);
+    if (c1 > n_pref)   // this part has tree keys
+        for (int i = threadIdx.x; i < T; i += C::THREADS) par[i] = ld_input(parent + i);
 
     const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE;
     const size_t row0 = (size_t)u * p.S_max;
@@ -227,29 +228,38 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
         return D == 128 ? (((row >> 1) & 1) << 1) | (((row >> 2) & 1) << 2) : ((row >> 2) & 1) << 1;
     };
     constexpr int UPR = C::RB / 16;   // 16-byte pieces of a row; piece i of a lane is 512 bytes on from piece i - 1
-    const int f_row = lane / UPR;
+    const uint32_t to_v = (uint32_t)(lane ^ v_swizzle(lane / UPR)) * 16;   // (the swizzle repeats every 512 bytes)
     auto fetch = [&](int c, int stage) {
         if (c < min(c1, n_pref)) {
             const int k0 = c * C::KEYS, n = P - k0;
             const uint32_t dst = ring + stage * C::STAGE;
             const size_t at = (row0 + k0) * C::RB + lane * 16;
             const uint8_t *k = p.k_cache + at, *v = p.v_cache + at;
+            if (D == 128 && n >= C::KEYS) {
+                const size_t a = (row0 + k0 + lane) * C::SB;
 #pragma unroll
-            for (int i = 0; i < UPR; ++i) {
-                const int row = i * (32 / UPR) + f_row;
-                const uint32_t to = dst + i * 512 + lane * 16, to_v = dst + C::CODES + (uint32_t)((i * 32 + lane) ^ v_swizzle(row)) * 16;
-                const bool in = row < n;   // rows past the prefix arrive as zeros (finite: scale 2^-20)
-                cp_async16(to, in ? k + i * 512 : p.k_cache, in ? 16u : 0u);
-                cp_async16(to_v, in ? v + i * 512 : p.v_cache, in ? 16u : 0u);
+                for (int i = 0; i < UPR; ++i) {
+                    cp_async16(dst + lane * 16 + i * 512, k + i * 512, 16u);
+                    cp_async16(dst + C::CODES + to_v + i * 512, v + i * 512, 16u);
+                }
+                cp_async4(dst + C::OFF_SC + lane * 4, p.k_scale + a, 4u);
+                cp_async4(dst + C::OFF_SC + 128 + lane * 4, p.v_scale + a, 4u);
+            } else {
+#pragma unroll
+                for (int i = 0; i < UPR; ++i) {
+                    const bool in = i * (32 / UPR) + lane / UPR < n;   // rows past the prefix arrive as zeros (finite: scale 2^-20)
+                    cp_async16(dst + lane * 16 + i * 512, in ? k + i * 512 : p.k_cache, in ? 16u : 0u);
+                    cp_async16(dst + C::CODES + to_v + i * 512, in ? v + i * 512 : p.v_cache, in ? 16u : 0u);
+                }
+                // a word holds the row's scales (D = 64: those of an even and an odd row; the
+                // tensors' last word may be half one)
+                const bool in = lane < n;
+                const size_t a = ((row0 + (in ? k0 + lane : 0)) * C::SB) & ~(size_t)3;
+                const size_t left = p.scale_bytes - a;
+                const uint32_t m = in ? (left < 4 ? (uint32_t)left : 4u) : 0u;
+                cp_async4(dst + C::OFF_SC + lane * 4, p.k_scale + a, m);
+                cp_async4(dst + C::OFF_SC + 128 + lane * 4, p.v_scale + a, m);
             }
-            // a word holds the row's scales (D = 64: those of an even and an odd row; the
-            // tensors' last word may be half one)
-            const bool in = lane < n;
-            const size_t a = ((row0 + (in ? k0 + lane : 0)) * C::SB) & ~(size_t)3;
-            const size_t left = p.scale_bytes - a;
-            const uint32_t m = in ? (left < 4 ? (uint32_t)left : 4u) : 0u;
-            cp_async4(dst + C::OFF_SC + lane * 4, p.k_scale + a, m);
-            cp_async4(dst + C::OFF_SC + 128 + lane * 4, p.v_scale + a, m);
         }
         cp_async_commit();
     };
