@@ -1072,7 +1072,7 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
     p.slices = (long long)L * B * H;
     p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
-    p.splits = kv4_splits(p.slices, T, S_max, 3);
+    p.splits = kv4_splits(p.slices, T, S_max, 4);
     return cuda_status(ppd::launch_kv_weight(p, D, static_cast<cudaStream_t>(stream)));
 }
 

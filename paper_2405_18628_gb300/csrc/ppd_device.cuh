@@ -540,6 +540,13 @@ PPD_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return d;
 }
 
+PPD_DEV uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 PPD_DEV uint64_t add2(uint64_t a, uint64_t b)
 {
     uint64_t d;

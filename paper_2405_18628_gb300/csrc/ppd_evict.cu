@@ -6,156 +6,174 @@ namespace ppd {
 
 // ------------------------------------------------------------------ weight per cached row
 
-// A warp takes chunks of 32 keys of a slice: S = Q K^T by mma.sync for blocks of 16 of the
-// slice's G n accepted query rows, p = exp(scale S - lse), and each key's sum over the rows
-// by a halving exchange over the eight lanes that hold its column, which leaves one key
-// to each lane.  Keys are columns as in the attention of few rows: column c of a block of
-// eight is its row c / 2 + 4 (c % 2).  Tree keys come last: the path's own rows, each seen by
-// itself and the nodes after it.
+// A warp takes chunks of 32 keys of a slice: S^T = K Q^T by mma.sync for the slice's G n accepted
+// query rows in blocks of eight (their fragments in shared memory, up to 128 rows at a time),
+// p = exp(scale S - lse), and each key's sum over the rows: the columns of a thread, then a
+// halving exchange over a quad that leaves one key to each lane.  K's fragments are made from the
+// codes (or bf16 channels) a thread loads, the next chunk's on their way meanwhile; the order of
+// the channels in the sum is free as long as Q follows it.  Tree keys come last: the path's own
+// rows, each seen by itself and the nodes after it.
+constexpr int kWeightRows = 128;
+
 template <int D, bool KV4>
-__global__ void __launch_bounds__(128, 3) kv_weight_kernel(const KvWeightParams p)
+__global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams p)
 {
     __shared__ int path_s[kMaxTree];
+    __shared__ __align__(16) uint2 q_s[kWeightRows / 8][D / 16][32];
+    __shared__ __align__(16) float neg_lse[kWeightRows];
+    __shared__ int place[kWeightRows];   // of the rows on the path
     pdl_release();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int split = (int)(blockIdx.x % p.splits);
-    const long long u = blockIdx.x / p.splits;
-    const int b = (int)(u / p.H % p.B);
+    const uint32_t u = blockIdx.x / p.splits;
+    const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B);
     const int T = p.T;
     const int P = ld_input(p.prefix_len + b);
     const int n = min(ld_input(p.accept_len + b), T);
     if (n < 1 || P < 0 || P > p.S_max) return;   // uniform over the block
-    for (int i = threadIdx.x; i < n; i += 128) path_s[i] = ld_input(p.path + (size_t)b * T + i);
-    __syncthreads();
     const int n_pref = (P + 31) / 32, n_all = n_pref + (n + 31) / 32;
     const int c0 = (int)((long long)n_all * split / p.splits), c1 = (int)((long long)n_all * (split + 1) / p.splits);
-    const int rows = p.G * n, blocks = (rows + 15) / 16;
+    const int rows = p.G * n;
     const size_t row0 = (size_t)u * p.S_max;
-    const int perm = (g >> 1) + 4 * (g & 1);
     // first channel of step s of a quad's thread: as the thread's loads of K bring them
     auto channel = [&](int s) { return KV4 ? (D / 4) * t + 4 * s : 32 * (s >> 1) + 8 * t + 4 * (s & 1); };
 
-    uint32_t q[D / 16][4];
-    float neg_lse[2];
-    int at_a[2];   // the rows' places on the path
-    auto load_rows = [&](int block) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = block * 16 + g + 8 * h;
-            const int a = r % n, node = r < rows ? path_s[a] : -1;
-            const bool real = node >= 0 && node < T;
-            const size_t row = ((size_t)u * p.G + (real ? r / n : 0)) * T + (real ? node : 0);
-            at_a[h] = a;
-            neg_lse[h] = real ? -1.4426950408889634f * ld_input(p.lse + row) : -INFINITY;
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                q[s][h] = real ? ld_pair(p.q, row * D + channel(s), p.f32) : 0u;
-                q[s][2 + h] = real ? ld_pair(p.q, row * D + channel(s) + 2, p.f32) : 0u;
-            }
-        }
-    };
-    load_rows(0);
-
-    // K of a chunk in registers: the codes of four keys (and each lane's key's scales), or
-    // their bf16 channels
+    // K of a chunk in registers, rows g, g + 8 of 16 keys each: codes and the thread's scale
+    // bytes, or bf16 channels
     constexpr int KW = KV4 ? D / 32 : D / 8;   // words of a key in a thread
     struct Keys {
-        uint32_t w[4][KW];
-        uint32_t scale;
+        uint32_t w[4][KW], scale[4];
     };
     auto load_keys = [&](int c, Keys &k) {
-        const int k0 = c * 32;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int j = k0 + 8 * i + perm;
-            const size_t row = row0 + (j < P ? j : 0);
-            if constexpr (KV4 && D == 128) {
-                const uint4 v = j < P ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * 64) + t) : make_uint4(0, 0, 0, 0);
-                k.w[i][0] = v.x, k.w[i][1] = v.y, k.w[i][2] = v.z, k.w[i][3] = v.w;
-            } else if constexpr (KV4) {
-                uint2 v = make_uint2(0, 0);
-                if (j < P)
-                    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p.k_cache + row * 32 + t * 8) : "memory");
-                k.w[i][0] = v.x, k.w[i][1] = v.y;
+            const int j = c * 32 + 8 * i + g;
+            const bool in = j < P;
+            const size_t row = row0 + (in ? j : 0);
+            k.scale[i] = 0;
+            if constexpr (KV4) {
+                if constexpr (D == 128) {
+                    const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * 64) + t) : make_uint4(0, 0, 0, 0);
+                    k.w[i][0] = v.x, k.w[i][1] = v.y, k.w[i][2] = v.z, k.w[i][3] = v.w;
+                } else {
+                    uint2 v = make_uint2(0, 0);
+                    if (in) asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p.k_cache + row * 32 + t * 8) : "memory");
+                    k.w[i][0] = v.x, k.w[i][1] = v.y;
+                }
+                if (in)
+                    asm volatile("ld.global.u8 %0, [%1];" : "=r"(k.scale[i]) : "l"(p.k_scale + row * (D / kKv4Group) + t / (128 / D)) : "memory");
             } else {
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) {
-                    const uint4 v = j < P ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * D * 2) + 4 * x + t) : make_uint4(0, 0, 0, 0);
+                    const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * D * 2) + 4 * x + t) : make_uint4(0, 0, 0, 0);
                     k.w[i][4 * x] = v.x, k.w[i][4 * x + 1] = v.y, k.w[i][4 * x + 2] = v.z, k.w[i][4 * x + 3] = v.w;
                 }
             }
         }
-        k.scale = 0;
-        if (KV4 && k0 + lane < P) {
-            const uint8_t *s = p.k_scale + (row0 + k0 + lane) * (D / kKv4Group);
-            if constexpr (D == 128) k.scale = (uint32_t)ld_input(reinterpret_cast<const int *>(s));
-            else asm volatile("ld.global.u16 %0, [%1];" : "=r"(k.scale) : "l"(s) : "memory");
-        }
     };
-    // 4-bit keys a chunk ahead; bf16 ones fill the registers as they are
-    Keys cur, nxt;
-    int c = c0 + warp;
-    if (KV4 && c < min(c1, n_pref)) load_keys(c, nxt);
-    for (; c < c1; c += 4) {
-        const bool tree = c >= n_pref;
-        const int k0 = (tree ? c - n_pref : c) * 32;
-        if constexpr (KV4) {
-            cur = nxt;
-            if (c + 4 < min(c1, n_pref)) load_keys(c + 4, nxt);
-        } else if (!tree) {
-            load_keys(c, cur);
-        }
-        const int mine = k0 + 8 * (g >> 1) + t + 4 * (g & 1);   // this lane's key in the end
-        const bool stays = tree ? mine < n && P + mine < p.S_max : mine < P;
-        float *out = p.weight + row0 + (tree ? P : 0) + (stays ? mine : 0);
-        float old = 0.f;
-        if (stays && !tree) old = ld_input(out);
-        float sum[8] = {};
-        for (int block = 0; block < blocks; ++block) {
-            if (blocks > 1) load_rows(block);
+    Keys nxt;
+    if (KV4 && c0 + warp < min(c1, n_pref)) load_keys(c0 + warp, nxt);   // bf16 keys fill the registers as they are
+    for (int i = threadIdx.x; i < n; i += 128) path_s[i] = ld_input(p.path + (size_t)b * T + i);
+
+    for (int r0 = 0; r0 < rows; r0 += kWeightRows) {
+        __syncthreads();   // the path is there; the rows before these are done with
+        const int blocks = (min(kWeightRows, rows - r0) + 7) / 8;
+        for (int x = warp; x < blocks; x += 4) {
+            const int r = r0 + 8 * x + g, a = r % n, node = r < rows ? path_s[a] : -1;
+            const bool real = node >= 0 && node < T;
+            const size_t row = ((size_t)u * p.G + (real ? r / n : 0)) * T + (real ? node : 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-                if (tree) {
-                    const int a = k0 + 8 * i + perm, node = a < n ? path_s[a] : -1;
+            for (int s = 0; s < D / 16; ++s)
+                q_s[x][s][lane] = real ? make_uint2(ld_pair(p.q, row * D + channel(s), p.f32), ld_pair(p.q, row * D + channel(s) + 2, p.f32))
+                                       : make_uint2(0u, 0u);
+            if (t == 0) {
+                neg_lse[8 * x + g] = real ? -1.4426950408889634f * ld_input(p.lse + row) : -INFINITY;
+                place[8 * x + g] = a;
+            }
+        }
+        __syncthreads();
+        if (KV4 && r0 > 0 && c0 + warp < min(c1, n_pref)) load_keys(c0 + warp, nxt);
+        for (int c = c0 + warp; c < c1; c += 4) {
+            const bool tree = c >= n_pref;
+            const int k0 = (tree ? c - n_pref : c) * 32;
+            const int mine = k0 + 8 * t + g;   // this lane's key in the end
+            const bool stays = tree ? mine < n && P + mine < p.S_max : mine < P;
+            float *out = p.weight + row0 + (tree ? P : 0) + (stays ? mine : 0);
+            float old = 0.f;
+            if (stays && (!tree || r0 > 0)) old = ld_input(out);
+            uint32_t k[2][D / 16][4];   // K's fragments of 2 x 16 keys
+            if (tree) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int a = k0 + 8 * i + g, node = a < n ? path_s[a] : -1;
                     const bool real = node >= 0 && node < T;
                     const size_t row = ((size_t)u * T + (real ? node : 0)) * D;
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_bf16(s, q[x], real ? ld_pair(p.k_tree, row + channel(x), p.f32) : 0u,
-                                 real ? ld_pair(p.k_tree, row + channel(x) + 2, p.f32) : 0u);
-                } else if constexpr (KV4) {
-                    const uint32_t sw = __shfl_sync(0xffffffffu, cur.scale, 8 * i + perm);
-                    const uint32_t s2 = kv4_scale2(((sw >> (D == 128 ? 8 * t : 8 * (t >> 1))) & 0xFFu) * 0x10001u);
-                    const uint32_t o2 = kv4_offset2(s2);
+                    for (int s = 0; s < D / 16; ++s) {
+                        k[i >> 1][s][i & 1] = real ? ld_pair(p.k_tree, row + channel(s), p.f32) : 0u;
+                        k[i >> 1][s][2 + (i & 1)] = real ? ld_pair(p.k_tree, row + channel(s) + 2, p.f32) : 0u;
+                    }
+                }
+            } else {
+                if constexpr (!KV4) load_keys(c, nxt);
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        mma_bf16(s, q[x], kv4_pair(cur.w[i][x >> 1] >> (8 * (x & 1)), s2, o2),
-                                 kv4_pair(cur.w[i][x >> 1] >> (8 * (x & 1) + 4), s2, o2));
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (KV4) {
+                        const Kv4Scale sc = kv4_scales(nxt.scale[i] * 0x10001u);
+#pragma unroll
+                        for (int x = 0; x < D / 32; ++x) {
+                            uint32_t v[4];
+                            kv4_word(nxt.w[i][x], sc, v);
+                            k[i >> 1][2 * x][i & 1] = v[0], k[i >> 1][2 * x][2 + (i & 1)] = v[1];
+                            k[i >> 1][2 * x + 1][i & 1] = v[2], k[i >> 1][2 * x + 1][2 + (i & 1)] = v[3];
+                        }
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < D / 16; ++s) k[i >> 1][s][i & 1] = nxt.w[i][2 * s], k[i >> 1][s][2 + (i & 1)] = nxt.w[i][2 * s + 1];
+                    }
+                }
+                if constexpr (KV4)
+                    if (c + 4 < min(c1, n_pref)) load_keys(c + 4, nxt);
+            }
+            const float scale = KV4 && !tree ? p.scale_log2 * (1.f / kKv4Unit) : p.scale_log2;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};   // keys g, g + 8, g + 16, g + 24
+#pragma unroll 1
+            for (int x = 0; x < blocks; ++x) {
+                float s[2][4] = {};
+#pragma unroll
+                for (int y = 0; y < D / 16; ++y) {
+                    const uint2 q = q_s[x][y][lane];
+                    mma_bf16(s[0], k[0][y], q.x, q.y);
+                    mma_bf16(s[1], k[1][y], q.x, q.y);
+                }
+                const float2 nl = *reinterpret_cast<const float2 *>(neg_lse + 8 * x + 2 * t);
+                if (!tree) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1)], scale, nl.x)) + ex2(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, nl.y));
                 } else {
+                    const int2 at = *reinterpret_cast<const int2 *>(place + 8 * x + 2 * t);
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x) mma_bf16(s, q[x], cur.w[i][2 * x], cur.w[i][2 * x + 1]);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float w = ex2(fmaf(s[e], p.scale_log2, neg_lse[e >> 1]));
-                    if (tree && at_a[e >> 1] < k0 + 8 * i + t + 4 * (e & 1)) w = 0.f;   // a later node's row
-                    sum[2 * i + (e & 1)] += w;
+                    for (int i = 0; i < 4; ++i) {   // a later node's row is not seen
+                        const int key = k0 + 8 * i + g;
+                        if (at.x >= key) sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1)], scale, nl.x));
+                        if (at.y >= key) sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, nl.y));
+                    }
                 }
             }
-        }
-        // eight values over the eight lanes of equal t: lane (g, t) ends with value g
+            // four values over the four lanes of a quad: lane t ends with value t
 #pragma unroll
-        for (int half = 4; half >= 1; half >>= 1) {
-            const bool up = (g & half) != 0;
+            for (int half = 2; half >= 1; half >>= 1) {
+                const bool up = (t & half) != 0;
 #pragma unroll
-            for (int i = 0; i < half; ++i) {
-                const float send = up ? sum[i] : sum[i + half], keep = up ? sum[i + half] : sum[i];
-                sum[i] = keep + __shfl_xor_sync(0xffffffffu, send, 4 * half);
+                for (int i = 0; i < half; ++i) {
+                    const float send = up ? sum[i] : sum[i + half], keep = up ? sum[i + half] : sum[i];
+                    sum[i] = keep + __shfl_xor_sync(0xffffffffu, send, half);
+                }
             }
+            if (stays) *out = old + sum[0];
         }
-        if (stays) *out = old + sum[0];
     }
 }
 

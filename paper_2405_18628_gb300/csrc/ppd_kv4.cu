@@ -134,10 +134,10 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4ReadParams p)
     for (int k = 0; k < kReadDeep; ++k) {
         const uint32_t r = row0 + k * (256 / WORDS);
         if (r >= rows) return;
-        const uint32_t s2 = kv4_scale2(sb[k] * 0x10001u), o2 = kv4_offset2(s2);
         uint32_t v[4];
+        kv4_word(c[k], kv4_scales(sb[k] * 0x10001u), v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = kv4_pair(c[k] >> (4 * e), s2, o2);
+        for (int e = 0; e < 4; ++e) v[e] = kv4_whole(v[e]);
         const size_t at = (size_t)r * D + 8 * w;
         if (!p.f32) {
             *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(p.out) + at) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -173,7 +173,8 @@ cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream)
 //                    movmatrix; V^T's are made from the codes of two neighbouring keys at once,
 //                    thread g of a column holding channels [g D / 8, (g + 1) D / 8)
 //
-// with a running maximum that moves when a score passes it by 2^8, and P as bf16 hi + lo
+// with a running reference kKv4Shift below the maximum (what takes the values' unit up again),
+// which moves when a score passes the maximum by 2^8, and P as bf16 hi + lo
 // (2^-18: V's values are exact, so the output's own rounding is all that shows).  Each warp's
 // state is merged in shared memory, those of a split slice by kv4_merge_kernel.  A chunk's
 // codes and scales come by asynchronous copies into a ring of the warp's own: no barrier in the
@@ -188,7 +189,7 @@ struct Kv4Few {
     static constexpr uint32_t OFF_SC = 2 * CODES;            // scales, a word a key: K's, then V's
     static constexpr uint32_t STAGE = 2 * CODES + 2 * KEYS * 4;
     static constexpr uint32_t RING = WARPS * STAGES * STAGE; // merge: [WARPS][rows][D] over the ring
-    static constexpr uint32_t OFF_ML = RING;                 // [WARPS][16]: maximum, sum
+    static constexpr uint32_t OFF_ML = RING;                 // [WARPS][16]: reference, sum
     static constexpr uint32_t OFF_PARENT = OFF_ML + WARPS * 16 * 8;
     static constexpr uint32_t SMEM = OFF_PARENT + kMaxTree * 4;
     static_assert(WARPS * 16 * D * 4 <= RING, "the states fit over the ring");
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
 #pragma unroll
             for (int e = 0; e < 2; ++e) q[nb][s][e] = r < R ? ld_pair(p.q, at + 4 * s + 2 * e, p.f32) : 0u;
     }
-    float o[D / 16][NB][4] = {};   // channels g D / 8 + i and D / 16 on, queries 2t and 2t + 1
+    float o[D / 16][NB][4] = {};   // kKv4Unit times the sums: channels g D / 8 + i and D / 16 on, queries 2t and 2t + 1
     float m[NB][2], l[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) m[nb][0] = m[nb][1] = -INFINITY, l[nb][0] = l[nb][1] = 0.f;
@@ -299,7 +300,8 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             if (!tree) {
-                uint32_t w[2][D / 32], s2[2], o2[2];
+                uint32_t w[2][D / 32];
+                Kv4Scale sc[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t row = 16 * mt + 8 * h + g;
@@ -311,13 +313,12 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                         w[h][0] = v.x, w[h][1] = v.y;
                     }
                     const uint32_t at = D == 128 ? t : (((row ^ odd) & 1u) << 1) + (t >> 1);
-                    s2[h] = kv4_scale2(ld_shared_u8(src + C::OFF_SC + row * 4u + at) * 0x10001u);
-                    o2[h] = kv4_offset2(s2[h]);
+                    sc[h] = kv4_scales(ld_shared_u8(src + C::OFF_SC + row * 4u + at) * 0x10001u);
                 }
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t a[4] = {kv4_pair(w[0][k >> 1] >> (8 * (k & 1)), s2[0], o2[0]), kv4_pair(w[1][k >> 1] >> (8 * (k & 1)), s2[1], o2[1]),
-                                           kv4_pair(w[0][k >> 1] >> (8 * (k & 1) + 4), s2[0], o2[0]), kv4_pair(w[1][k >> 1] >> (8 * (k & 1) + 4), s2[1], o2[1])};
+                    const uint32_t x0 = w[0][k >> 1] >> (8 * (k & 1)), x1 = w[1][k >> 1] >> (8 * (k & 1));
+                    const uint32_t a[4] = {kv4_low(x0, sc[0]), kv4_low(x1, sc[1]), kv4_high(x0, sc[0]), kv4_high(x1, sc[1])};
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma_bf16(s[mt][nb], a, q[nb][k][0], q[nb][k][1]);
                 }
@@ -359,6 +360,7 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                 }
             __syncwarp();
         }
+        const float scale = tree ? p.scale_log2 : p.scale_log2 * (1.f / kKv4Unit);
         float mx[NB][2];
         bool grows = false;
 #pragma unroll
@@ -368,15 +370,15 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                 float x = fmaxf(fmaxf(s[0][nb][e], s[0][nb][2 + e]), fmaxf(s[1][nb][e], s[1][nb][2 + e]));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                mx[nb][e] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16)) * p.scale_log2;
-                grows |= mx[nb][e] > m[nb][e] + 8.f;
+                mx[nb][e] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16)) * scale;
+                grows |= mx[nb][e] > m[nb][e] + (kKv4Shift + 8.f);
             }
         if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float nw = fmaxf(m[nb][e], mx[nb][e]);
+                    const float nw = fmaxf(m[nb][e], mx[nb][e] - kKv4Shift);
                     const float a = m[nb][e] == nw ? 1.f : ex2(m[nb][e] - nw);
                     m[nb][e] = nw;
                     l[nb][e] *= a;
@@ -394,9 +396,10 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(fmaf(s[mt][nb][2 * h], p.scale_log2, n0)), p1 = ex2(fmaf(s[mt][nb][2 * h + 1], p.scale_log2, n1));
+                    float p0 = ex2(fmaf(s[mt][nb][2 * h], scale, n0)), p1 = ex2(fmaf(s[mt][nb][2 * h + 1], scale, n1));
                     l[nb][0] += p0;
                     l[nb][1] += p1;
+                    if (tree) p0 *= kKv4Unit, p1 *= kKv4Unit;   // the tree's values are whole: the sums of p v are in units
                     uint32_t a, c2;
                     split_bf16x2_fma(pack2(p0, p1), a, c2);
                     hi[mt][nb][h] = movmatrix(a);
@@ -413,7 +416,8 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                 }
             };
             if (!tree) {
-                uint32_t w[4][D / 64], s2[2], o2[2];   // rows 2t, 2t + 1 | 2t + 8, 2t + 9 of the 16
+                Kv4Scale sc[2];
+                uint32_t w[4][D / 64];   // rows 2t, 2t + 1 | 2t + 8, 2t + 9 of the 16
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t row = 16 * mt + 2 * t + (x & 1) + 8 * (x >> 1);
@@ -430,8 +434,7 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                     const uint32_t at = src + C::OFF_SC + 128 + row * 4u;
                     const uint32_t a0 = D == 128 ? at + (g >> 1) : at + (((row ^ odd) & 1u) << 1) + (g >> 2);
                     const uint32_t a1 = D == 128 ? at + 4 + (g >> 1) : at + 4 + ((((row + 1) ^ odd) & 1u) << 1) + (g >> 2);
-                    s2[h] = kv4_scale2(ld_shared_u8(a0) | ld_shared_u8(a1) << 16);
-                    o2[h] = kv4_offset2(s2[h]);
+                    sc[h] = kv4_scales(ld_shared_u8(a0) | ld_shared_u8(a1) << 16);
                 }
                 // channel i of a word is nibble i / 2 + 4 (i % 2): the low halves of two keys' words
                 // side by side hold the even channels, the high halves the odd ones
@@ -441,10 +444,11 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                         const uint32_t sel = odd_ch ? 0x7632u : 0x5410u;
                         const uint32_t x0 = __byte_perm(w[0][0], w[1][0], sel), x1 = __byte_perm(w[0][1], w[1][1], sel);
                         const uint32_t x2 = __byte_perm(w[2][0], w[3][0], sel), x3 = __byte_perm(w[2][1], w[3][1], sel);
+                        uint32_t v0[4], v1[4], v2[4], v3[4];
+                        kv4_word(x0, sc[0], v0), kv4_word(x1, sc[0], v1), kv4_word(x2, sc[1], v2), kv4_word(x3, sc[1], v3);
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
-                            const uint32_t a[4] = {kv4_pair(x0 >> (4 * n), s2[0], o2[0]), kv4_pair(x1 >> (4 * n), s2[0], o2[0]),
-                                                   kv4_pair(x2 >> (4 * n), s2[1], o2[1]), kv4_pair(x3 >> (4 * n), s2[1], o2[1])};
+                            const uint32_t a[4] = {v0[n], v1[n], v2[n], v3[n]};
                             add_pv(2 * n + odd_ch, a);
                         }
                     }
@@ -452,11 +456,11 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
                     // eight channels a thread: 0..3 in the upper rows, 4..7 in the lower ones
                     const uint32_t e0 = __byte_perm(w[0][0], w[1][0], 0x5410), d0 = __byte_perm(w[0][0], w[1][0], 0x7632);
                     const uint32_t e1 = __byte_perm(w[2][0], w[3][0], 0x5410), d1 = __byte_perm(w[2][0], w[3][0], 0x7632);
+                    uint32_t v0[2][4], v1[2][4];
+                    kv4_word(e0, sc[0], v0[0]), kv4_word(d0, sc[0], v0[1]), kv4_word(e1, sc[1], v1[0]), kv4_word(d1, sc[1], v1[1]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t y0 = i & 1 ? d0 : e0, y1 = i & 1 ? d1 : e1;
-                        const uint32_t a[4] = {kv4_pair(y0 >> (4 * (i >> 1)), s2[0], o2[0]), kv4_pair(y0 >> (4 * (i >> 1) + 8), s2[0], o2[0]),
-                                               kv4_pair(y1 >> (4 * (i >> 1)), s2[1], o2[1]), kv4_pair(y1 >> (4 * (i >> 1) + 8), s2[1], o2[1])};
+                        const uint32_t a[4] = {v0[i & 1][i >> 1], v0[i & 1][2 + (i >> 1)], v1[i & 1][i >> 1], v1[i & 1][2 + (i >> 1)]};
                         add_pv(i, a);
                     }
                 }
@@ -526,7 +530,7 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
         }
         const size_t r = q_row0 + row, part = ((size_t)u * p.splits + split) * R + row;
         if (whole) {
-            const float inv = 1.f / L;
+            const float inv = (1.f / kKv4Unit) / L;
             if (d == 0 && p.lse) p.lse[r] = (M + lg2(L)) * 0.69314718055994530942f;
             *reinterpret_cast<uint2 *>(p.out + r * D + d) = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
         } else {
@@ -572,7 +576,7 @@ __global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4AttnParams p, i
             a.x = fmaf(w, v[i].x, a.x), a.y = fmaf(w, v[i].y, a.y), a.z = fmaf(w, v[i].z, a.z), a.w = fmaf(w, v[i].w, a.w);
         }
     }
-    const float inv = 1.f / L;
+    const float inv = (1.f / kKv4Unit) / L;
     if (d == 0 && p.lse) p.lse[r] = (M + lg2(L)) * 0.69314718055994530942f;
     *reinterpret_cast<uint2 *>(p.out + r * D + d) = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
 }

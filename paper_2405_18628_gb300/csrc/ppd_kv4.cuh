@@ -17,12 +17,6 @@ namespace ppd {
 
 constexpr int kKv4Group = 32;   // channels of a scale
 
-// A scale byte as bf16 bits in both halves of a register: `two` holds the byte in bits
-// 0..7 and in bits 16..23.  The byte's exponent field counts from 2^-20, bf16's from 2^-127.
-PPD_DEV uint32_t kv4_scale2(uint32_t two) { return (two + 0x03580358u) << 4; }
-
-PPD_DEV float kv4_scale(uint32_t b) { return __uint_as_float((b + 856u) << 20); }
-
 PPD_DEV uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c)
 {
     uint32_t d;
@@ -30,17 +24,41 @@ PPD_DEV uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c)
     return d;
 }
 
-// -136 s for a pair of scales (17 times four significant bits: exact).
-PPD_DEV uint32_t kv4_offset2(uint32_t s2) { return bf16x2_fma(s2, 0xC308C308u, 0x80008000u); }
+// A scale as fp32.  The byte's exponent field counts from 2^-20, fp32's from 2^-127.
+PPD_DEV float kv4_scale(uint32_t b) { return __uint_as_float((b + 856u) << 20); }
 
-// The values of two codes, in bits 0..3 and 16..19 of `pair` (other bits ignored): the
-// codes become the low bits of 128 + c, and one fused multiply-add gives s (128 + c) - 136 s.
-PPD_DEV uint32_t kv4_pair(uint32_t pair, uint32_t s2, uint32_t o2)
+// Codes become bf16 values without a conversion: bits 0..7 of a bf16 number alone (seven of
+// the mantissa, the lowest of the exponent) stand for that byte times 2^-133, so a masked code in
+// bits 0..3 is c 2^-133 and one in bits 4..7 is 16 c 2^-133, where it lies.  One fused multiply-add
+// with 2^113 s (or a sixteenth of it) and -8 s 2^-20 then makes kKv4Unit s (c - 8): exact, and a
+// word of eight codes takes one shift instead of three.  What the unit leaves over is a power
+// of two: the softmax scale takes up K's, the outputs V's.
+constexpr float kKv4Unit = 1.f / (1 << 20), kKv4Shift = 20.f;
+struct Kv4Scale {
+    uint32_t s, s16, off;   // of a pair of codes, each
+};
+// `two` holds one scale byte in bits 0..7 and one in bits 16..23.
+PPD_DEV Kv4Scale kv4_scales(uint32_t two)
 {
-    uint32_t x;   // (pair & mask) | 128: one instruction, said so
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(pair), "r"(0x000F000Fu), "r"(0x43004300u));
-    return bf16x2_fma(x, s2, o2);
+    Kv4Scale r;
+    r.s = (two + 0x06E006E0u) << 4;             // 2^113 s as bf16 bits
+    r.s16 = r.s - 0x02000200u;
+    r.off = bf16x2_fma(r.s, 0x80088008u, 0x80008000u);   // times -2^-130
+    return r;
 }
+// kKv4Unit times the values of the pairs of codes in bits 0..3 and 16..19, and in 4..7 and 20..23.
+PPD_DEV uint32_t kv4_low(uint32_t w, const Kv4Scale &k) { return bf16x2_fma(w & 0x000F000Fu, k.s, k.off); }
+PPD_DEV uint32_t kv4_high(uint32_t w, const Kv4Scale &k) { return bf16x2_fma(w & 0x00F000F0u, k.s16, k.off); }
+// The four pairs of a word: channels (0, 1), (2, 3), (4, 5), (6, 7).
+PPD_DEV void kv4_word(uint32_t w, const Kv4Scale &k, uint32_t (&v)[4])
+{
+    v[0] = kv4_low(w, k);
+    v[1] = kv4_high(w, k);
+    v[2] = kv4_low(w >> 8, k);
+    v[3] = kv4_high(w >> 8, k);
+}
+// A pair of such values without the unit.
+PPD_DEV uint32_t kv4_whole(uint32_t v) { return bf16x2_fma(v, 0x49804980u, 0x80008000u); }
 
 // Two fp32 values as a bf16 pair, the first in the low half.
 PPD_DEV uint32_t bf16x2(float lo, float hi)

@@ -54,9 +54,9 @@ struct Kv4Wide {
                          NBAR = B_DRAIN + 1;
     static constexpr uint32_t OFF_TMEMPTR = OFF_BAR + NBAR * 8;
     static constexpr uint32_t OFF_ABORT = OFF_TMEMPTR + 4;
-    static constexpr uint32_t OFF_NM = (OFF_ABORT + 4 + 15) & ~15u;   // [TP] minus the running maxima
+    static constexpr uint32_t OFF_NM = (OFF_ABORT + 4 + 15) & ~15u;   // [TP] minus the running references
     static constexpr uint32_t OFF_L = OFF_NM + TP * 4;                // [OB][TP] row sums (1 / sum of a whole unit)
-    static constexpr uint32_t OFF_MX = OFF_L + OB * TP * 4;           // [OB][TP] maxima of a part
+    static constexpr uint32_t OFF_MX = OFF_L + OB * TP * 4;           // [OB][TP] references of a part
     static constexpr uint32_t OFF_RED = OFF_MX + OB * TP * 4;         // [NWG][4][NC]
     static constexpr uint32_t OFF_RANGE = (OFF_RED + NWG * 4 * NC * 4 + 15) & ~15u;
     static constexpr uint32_t SMEM_BYTES = OFF_RANGE + sizeof(WorkRange);
@@ -225,11 +225,15 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 tc_fence_after();
 #pragma unroll
                 for (int c = 0; c < UPR; ++c) {
-                    const uint32_t s2 = kv4_scale2(((sc >> (8 * c)) & 0xFFu) * 0x10001u), o2 = kv4_offset2(s2);
+                    const Kv4Scale k = kv4_scales(((sc >> (8 * c)) & 0xFFu) * 0x10001u);
                     const uint32_t u[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
                     uint32_t r[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) r[i] = kv4_pair(u[i >> 2] >> (4 * (i & 3)), s2, o2);
+                    for (int i = 0; i < 16; i += 4) {
+                        uint32_t v[4];
+                        kv4_word(u[i >> 2], k, v);
+                        r[i] = v[0], r[i + 1] = v[1], r[i + 2] = v[2], r[i + 3] = v[3];
+                    }
                     store(c, r);
                 }
             } else {
@@ -400,8 +404,8 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         const uint32_t p_row = smem_addr(smem) + Lay::OFF_P +
                                (uint32_t)(t >> 3) * 1024u + (uint32_t)(t & 7) * 128u;
         const uint32_t p_swz = (uint32_t)(t & 7);
-        const float sl2 = p.scale_log2;
-        const uint64_t sl2x2 = pack2(sl2, sl2);
+        float sl2 = 0.f;          // this tile's scores times it are log2 units: prefix keys come in kKv4Units
+        float p_unit = 1.f;       // and the tree's probabilities meet whole values: they go in as units
         float *nm = reinterpret_cast<float *>(smem + Lay::OFF_NM) + q0;           // [NC]
         float *red = reinterpret_cast<float *>(smem + Lay::OFF_RED) + wg * 4 * NC;   // [4][NC]
         float *linv = reinterpret_cast<float *>(smem + Lay::OFF_L) + q0;          // [OB][TP]
@@ -418,15 +422,19 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         // the range's first segment, bit 3 its O accumulator
         int pend_f = 0, pend_u = 0, pend_g = 0;
 
+        // The running references lie kKv4Shift below the maxima, which takes the values' unit up
+        // again: probabilities are up to 2^20, and one above 2^36 moves its column's reference.
+        constexpr float kTooLarge = 6.8719477e10f;
         // Probabilities of this thread's key row for its NC query columns from its raw
         // scores r, against the current running maxima: split into bf16 hi + lo, stored
         // into the probability tile at byte offset `pbuf`, and kept in pr for the row sums.
-        // Returns their sum: above 2^16 (or no number) where one of them is too large, and
+        // Returns their sum: above kTooLarge (or no number) where one of them is too large, and
         // the exact path then writes the tile again.  (Adding is the FMA pipe's work, a maximum
         // and a split by shifts and masks the integer pipe's, which bounds this loop.)
         auto emit = [&](auto bits_c, const Cols &r, uint32_t bits, uint32_t pbuf, Probs &pr) {
             constexpr bool BITS = decltype(bits_c)::value != 0;
             uint64_t total[2] = {0ull, 0ull};
+            const uint64_t sl2x2 = pack2(sl2, sl2);
 #pragma unroll
             for (int h = 0; h < NC; h += 8) {
                 const ulonglong2 na = *reinterpret_cast<const ulonglong2 *>(nm + h);
@@ -445,7 +453,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                     const uint64_t pp = pack2(ex2(d0), ex2(d1));
                     pr[(h + e) >> 1] = pp;
                     total[(e >> 1) & 1] = add2(total[(e >> 1) & 1], pp);
-                    split_bf16x2_fma(pp, hw[e >> 1], lw[e >> 1]);
+                    split_bf16x2_fma(BITS ? mul2(pp, pack2(p_unit, p_unit)) : pp, hw[e >> 1], lw[e >> 1]);
                 }
                 const int ch = q0 + h, cl = TP + q0 + h;   // hi and lo columns
                 const uint32_t ah = p_row + pbuf + (uint32_t)(ch >> 6) * Lay::GROUP_BYTES +
@@ -481,7 +489,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             if (t < NC) {
                 const float tm = fmaxf(fmaxf(red[t], red[NC + t]), fmaxf(red[2 * NC + t], red[3 * NC + t]));
                 const float old = -nm[t];
-                const float nw = fmaxf(old, tm);
+                const float nw = fmaxf(old, tm - kKv4Shift);
                 nm[t] = -nw;
                 red[t] = (nw == old) ? 1.f : ex2(old - nw);   // alpha
             }
@@ -566,6 +574,8 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             for (int j = sg.j0; j < sg.j1; ++j, ++g) {
                 const bool tree = j >= ui.n_pref;
                 const bool first = (j == sg.j0);
+                sl2 = tree ? p.scale_log2 : p.scale_log2 * (1.f / kKv4Unit);
+                p_unit = tree ? kKv4Unit : 1.f;
                 const int n_valid = tree ? Lay::KT : min(Lay::KT, ui.P - j * Lay::KT);
                 const bool masked = tree || n_valid < Lay::KT;
                 const int sb = g & 1;
@@ -604,7 +614,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                     if (t == 0) {
                         const bool all_see = j <= ui.n_pref;
 #pragma unroll
-                        for (int e = 0; e < NC; ++e) nm[e] = all_see ? -(__uint_as_float(r[e]) * sl2) : 1e30f;
+                        for (int e = 0; e < NC; ++e) nm[e] = all_see ? kKv4Shift - __uint_as_float(r[e]) * sl2 : 1e30f;
                     }
                     named_bar_sync(1 + wg, 128);
                 }
@@ -614,10 +624,10 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 Probs pr;
                 if (!masked) {
                     const float sum = emit(kind_t<0>{}, r, bits, pbuf, pr);
-                    if (named_bar_or(1 + wg, 128, !(sum <= 65536.f))) exact_tile(kind_t<0>{}, r, bits, pbuf, first, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<0>{}, r, bits, pbuf, first, pr);
                 } else {
                     const float sum = emit(kind_t<1>{}, r, bits, pbuf, pr);
-                    if (named_bar_or(1 + wg, 128, !(sum <= 65536.f))) exact_tile(kind_t<1>{}, r, bits, pbuf, first, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<1>{}, r, bits, pbuf, first, pr);
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
@@ -651,7 +661,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                     if (!SPLIT || seg_whole(sg)) {
                         const int row = ui.qb * TP + q0 + t;
                         if (x.lse && row < R) x.lse[(size_t)ui.lbh * R + row] = (m + lg2(l)) * 0.69314718055994530942f;
-                        linv[ob * TP + t] = 1.f / l;
+                        linv[ob * TP + t] = (1.f / kKv4Unit) / l;
                     } else {
                         linv[ob * TP + t] = l;
                         pmx[ob * TP + t] = m;
@@ -723,7 +733,7 @@ __global__ void __launch_bounds__(256) kv4_wide_merge_kernel(const AttnParams p,
             a.z = fmaf(a.z, so, w * v[i].z), a.w = fmaf(a.w, so, w * v[i].w);
         }
     }
-    const float inv = 1.f / L;
+    const float inv = (1.f / kKv4Unit) / L;
     const size_t at = (size_t)lbh * R + r0 + row;
     *reinterpret_cast<uint2 *>(x.out + at * D + c0) = make_uint2(bf16x2(a.x * inv, a.y * inv), bf16x2(a.z * inv, a.w * inv));
     if (c0 == 0 && x.lse) x.lse[at] = (M + lg2(L)) * 0.69314718055994530942f;
