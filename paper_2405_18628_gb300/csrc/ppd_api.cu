@@ -933,21 +933,22 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
     return cuda_status(ppd::launch_kv4_read(p, static_cast<cudaStream_t>(stream)));
 }
 
-// Parts that the keys of a slice are shared out to, blocks of which `per_sm` fit an SM.  Fewer
-// slices than that in all get one wave of parts; more are cut where whole slices would
-// leave over a tenth of the last wave idle.  A part has at least eight chunks of 32 keys,
-// two a warp.
+// Parts that the keys of a slice are shared out to, blocks of which `per_sm` fit an SM: the number
+// with the shortest time of all waves of blocks, a part counting as its chunks of 32 keys and
+// eight more for a block's start and end (8 us for parts of 66 chunks that take 60 in all).  A
+// part has at least eight chunks, two a warp.
 static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 {
     const long long slots = (long long)per_sm * num_sms();
     const long long chunks = (S_max + 31) / 32 + (T + 31) / 32;
-    long long n = 1;
-    if (slices < slots)
-        n = slots / slices;
-    else
-        while (n < 4 && 10 * ((slices * n + slots - 1) / slots) * slots > 11 * slices * n) ++n;
-    const long long most = chunks / 8 < 1 ? 1 : chunks / 8;
-    return (int)(n < most ? n : most);
+    long long best = -1, most = chunks / 8;
+    int splits = 1;
+    if (most > 8 * slots / slices) most = 8 * slots / slices;
+    for (long long n = 1; n <= most || n == 1; ++n) {
+        const long long cost = (slices * n + slots - 1) / slots * ((chunks + n - 1) / n + 8);
+        if (best < 0 || cost < best) best = cost, splits = (int)n;
+    }
+    return splits;
 }
 
 // How an attention call runs: up to 16 query rows of a slice in registers, its keys in
@@ -1072,7 +1073,8 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
     p.slices = (long long)L * B * H;
     p.B = B, p.H = H, p.G = G, p.T = T, p.S_max = S_max, p.f32 = dt == PPD_F32;
     p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
-    p.splits = kv4_splits(p.slices, T, S_max, 4);
+    p.scale_bytes = (size_t)p.slices * S_max * (D / 32);
+    p.splits = kv4_splits(p.slices, T, S_max, ppd::kv_weight_blocks(k_scale != nullptr));
     return cuda_status(ppd::launch_kv_weight(p, D, static_cast<cudaStream_t>(stream)));
 }
 

@@ -7,21 +7,33 @@ namespace ppd {
 // ------------------------------------------------------------------ weight per cached row
 
 // A warp takes chunks of 32 keys of a slice: S^T = K Q^T by mma.sync for the slice's G n accepted
-// query rows in blocks of eight (their fragments in shared memory, up to 128 rows at a time),
+// query rows in blocks of eight (their fragments in shared memory, up to 32 rows at a time),
 // p = exp(scale S - lse), and each key's sum over the rows: the columns of a thread, then a
 // halving exchange over a quad that leaves one key to each lane.  K's fragments are made from the
-// codes (or bf16 channels) a thread loads, the next chunk's on their way meanwhile; the order of
-// the channels in the sum is free as long as Q follows it.  Tree keys come last: the path's own
-// rows, each seen by itself and the nodes after it.
-constexpr int kWeightRows = 128;
+// codes (or bf16 channels) that asynchronous copies bring into a ring of the warp's own; the
+// order of the channels in the sum is free as long as Q follows it.  Tree keys come last: the
+// path's own rows, each seen by itself and the nodes after it.
+constexpr int kWeightRows = 32;
 
 template <int D, bool KV4>
-__global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams p)
+struct KvWeight {
+    static constexpr int BLOCKS = KV4 ? 4 : 3;                         // on an SM
+    static constexpr int STAGES = KV4 ? 4 : (D == 128 ? 2 : 4);
+    static constexpr uint32_t RB = KV4 ? D / 2 : 2 * D;                // bytes of a row
+    static constexpr uint32_t STAGE = 32 * RB + (KV4 ? 128 : 0);       // rows, then a word of scales each
+    static constexpr uint32_t OFF_Q = 4 * STAGES * STAGE;
+    static constexpr uint32_t SMEM = OFF_Q + kWeightRows / 8 * (D / 16) * 32 * 8;
+};
+
+template <int D, bool KV4>
+__global__ void __launch_bounds__(128, (KvWeight<D, KV4>::BLOCKS)) kv_weight_kernel(const KvWeightParams p)
 {
+    using C = KvWeight<D, KV4>;
+    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int path_s[kMaxTree];
-    __shared__ __align__(16) uint2 q_s[kWeightRows / 8][D / 16][32];
     __shared__ __align__(16) float neg_lse[kWeightRows];
-    __shared__ int place[kWeightRows];   // of the rows on the path
+    __shared__ __align__(8) int place[kWeightRows];   // of the rows on the path
+    uint2 (*q_s)[D / 16][32] = reinterpret_cast<uint2(*)[D / 16][32]>(smem + C::OFF_Q);
     pdl_release();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -39,45 +51,37 @@ __global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams 
     // first channel of step s of a quad's thread: as the thread's loads of K bring them
     auto channel = [&](int s) { return KV4 ? (D / 4) * t + 4 * s : 32 * (s >> 1) + 8 * t + 4 * (s & 1); };
 
-    // K of a chunk in registers, rows g, g + 8 of 16 keys each: codes and the thread's scale
-    // bytes, or bf16 channels
-    constexpr int KW = KV4 ? D / 32 : D / 8;   // words of a key in a thread
-    struct Keys {
-        uint32_t w[4][KW], scale[4];
-    };
-    auto load_keys = [&](int c, Keys &k) {
+    const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE;
+    constexpr int UPR = C::RB / 16;   // 16-byte pieces of a row; bf16: the odd rows' halves of 128 bytes change places
+    auto fetch = [&](int c, int stage) {
+        if (c < min(c1, n_pref)) {
+            const int k0 = c * 32;
+            const uint32_t dst = ring + stage * C::STAGE;
+            const uint8_t *src = p.k_cache + (row0 + k0) * C::RB + lane * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = c * 32 + 8 * i + g;
-            const bool in = j < P;
-            const size_t row = row0 + (in ? j : 0);
-            k.scale[i] = 0;
-            if constexpr (KV4) {
-                if constexpr (D == 128) {
-                    const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * 64) + t) : make_uint4(0, 0, 0, 0);
-                    k.w[i][0] = v.x, k.w[i][1] = v.y, k.w[i][2] = v.z, k.w[i][3] = v.w;
-                } else {
-                    uint2 v = make_uint2(0, 0);
-                    if (in) asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p.k_cache + row * 32 + t * 8) : "memory");
-                    k.w[i][0] = v.x, k.w[i][1] = v.y;
-                }
-                if (in)
-                    asm volatile("ld.global.u8 %0, [%1];" : "=r"(k.scale[i]) : "l"(p.k_scale + row * (D / kKv4Group) + t / (128 / D)) : "memory");
-            } else {
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(p.k_cache + row * D * 2) + 4 * x + t) : make_uint4(0, 0, 0, 0);
-                    k.w[i][4 * x] = v.x, k.w[i][4 * x + 1] = v.y, k.w[i][4 * x + 2] = v.z, k.w[i][4 * x + 3] = v.w;
-                }
+            for (int i = 0; i < UPR; ++i) {
+                const int row = (i * 32 + lane) / UPR;
+                const bool in = k0 + row < P;   // rows past the prefix arrive as zeros
+                const uint32_t to = (uint32_t)((i * 32 + lane) ^ (KV4 ? 0 : (row & 1) << 2)) * 16;
+                cp_async16(dst + to, in ? src + i * 512 : p.k_cache, in ? 16u : 0u);
+            }
+            if constexpr (KV4) {   // (D = 64: a word holds an even and an odd row's scales, the tensor's last perhaps one)
+                constexpr int SB = D / kKv4Group;
+                const bool in = k0 + lane < P;
+                const size_t a = ((row0 + (in ? k0 + lane : 0)) * SB) & ~(size_t)3;
+                const size_t left = p.scale_bytes - a;
+                cp_async4(dst + 32 * C::RB + lane * 4, p.k_scale + a, in ? (left < 4 ? (uint32_t)left : 4u) : 0u);
             }
         }
+        cp_async_commit();
     };
-    Keys nxt;
-    if (KV4 && c0 + warp < min(c1, n_pref)) load_keys(c0 + warp, nxt);   // bf16 keys fill the registers as they are
     for (int i = threadIdx.x; i < n; i += 128) path_s[i] = ld_input(p.path + (size_t)b * T + i);
 
     for (int r0 = 0; r0 < rows; r0 += kWeightRows) {
         __syncthreads();   // the path is there; the rows before these are done with
+        int next = c0 + warp;   // the next chunk to fetch
+#pragma unroll
+        for (int s = 0; s < C::STAGES - 1; ++s, next += 4) fetch(next, s);
         const int blocks = (min(kWeightRows, rows - r0) + 7) / 8;
         for (int x = warp; x < blocks; x += 4) {
             const int r = r0 + 8 * x + g, a = r % n, node = r < rows ? path_s[a] : -1;
@@ -93,8 +97,10 @@ __global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams 
             }
         }
         __syncthreads();
-        if (KV4 && r0 > 0 && c0 + warp < min(c1, n_pref)) load_keys(c0 + warp, nxt);
+        int stage = 0;
         for (int c = c0 + warp; c < c1; c += 4) {
+            fetch(next, stage == 0 ? C::STAGES - 1 : stage - 1);
+            next += 4;
             const bool tree = c >= n_pref;
             const int k0 = (tree ? c - n_pref : c) * 32;
             const int mine = k0 + 8 * t + g;   // this lane's key in the end
@@ -116,25 +122,40 @@ __global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams 
                     }
                 }
             } else {
-                if constexpr (!KV4) load_keys(c, nxt);
+                cp_async_wait<C::STAGES - 1>();
+                __syncwarp();
+                const uint32_t src = ring + stage * C::STAGE;
+                const uint32_t odd = D == 64 ? (uint32_t)(row0 + k0) & 1u : 0u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    const uint32_t row = 8 * i + g;
                     if constexpr (KV4) {
-                        const Kv4Scale sc = kv4_scales(nxt.scale[i] * 0x10001u);
+                        uint32_t w[D / 32];
+                        if constexpr (D == 128) {
+                            const uint4 v = ld_shared_u128(src + row * 64u + t * 16u);
+                            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+                        } else {
+                            const uint2 v = ld_shared_u64(src + row * 32u + t * 8u);
+                            w[0] = v.x, w[1] = v.y;
+                        }
+                        const uint32_t at = D == 128 ? t : (((row ^ odd) & 1u) << 1) + (t >> 1);
+                        const Kv4Scale sc = kv4_scales(ld_shared_u8(src + 32 * C::RB + row * 4u + at) * 0x10001u);
 #pragma unroll
                         for (int x = 0; x < D / 32; ++x) {
                             uint32_t v[4];
-                            kv4_word(nxt.w[i][x], sc, v);
+                            kv4_word(w[x], sc, v);
                             k[i >> 1][2 * x][i & 1] = v[0], k[i >> 1][2 * x][2 + (i & 1)] = v[1];
                             k[i >> 1][2 * x + 1][i & 1] = v[2], k[i >> 1][2 * x + 1][2 + (i & 1)] = v[3];
                         }
                     } else {
 #pragma unroll
-                        for (int s = 0; s < D / 16; ++s) k[i >> 1][s][i & 1] = nxt.w[i][2 * s], k[i >> 1][s][2 + (i & 1)] = nxt.w[i][2 * s + 1];
+                        for (int x = 0; x < D / 32; ++x) {
+                            const uint4 v = ld_shared_u128(src + row * C::RB + (uint32_t)((4 * x + t) ^ ((row & 1) << 2)) * 16);
+                            k[i >> 1][2 * x][i & 1] = v.x, k[i >> 1][2 * x][2 + (i & 1)] = v.y;
+                            k[i >> 1][2 * x + 1][i & 1] = v.z, k[i >> 1][2 * x + 1][2 + (i & 1)] = v.w;
+                        }
                     }
                 }
-                if constexpr (KV4)
-                    if (c + 4 < min(c1, n_pref)) load_keys(c + 4, nxt);
             }
             const float scale = KV4 && !tree ? p.scale_log2 * (1.f / kKv4Unit) : p.scale_log2;
             float sum[4] = {0.f, 0.f, 0.f, 0.f};   // keys g, g + 8, g + 16, g + 24
@@ -173,21 +194,29 @@ __global__ void __launch_bounds__(128, 4) kv_weight_kernel(const KvWeightParams 
                 }
             }
             if (stays) *out = old + sum[0];
+            __syncwarp();   // the stage is read: the next fetch may overwrite it
+            stage = stage == C::STAGES - 1 ? 0 : stage + 1;
         }
+        cp_async_wait<0>();
     }
 }
 
-template <int D>
+template <int D, bool KV4>
 static cudaError_t launch_weight_t(const KvWeightParams &p, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)(p.slices * p.splits));
-    return p.k_scale ? launch_chained(kv_weight_kernel<D, true>, grid, dim3(128), dim3(1), stream, p)
-                     : launch_chained(kv_weight_kernel<D, false>, grid, dim3(128), dim3(1), stream, p);
+    using C = KvWeight<D, KV4>;
+    static std::atomic<uint64_t> configured{0};
+    const cudaError_t e = allow_smem(kv_weight_kernel<D, KV4>, C::SMEM, configured);
+    if (e != cudaSuccess) return e;
+    return launch_chained_smem(kv_weight_kernel<D, KV4>, dim3((unsigned)(p.slices * p.splits)), dim3(128), dim3(1), C::SMEM, stream, p);
 }
+
+int kv_weight_blocks(bool kv4) { return kv4 ? 4 : 3; }
 
 cudaError_t launch_kv_weight(const KvWeightParams &p, int D, cudaStream_t stream)
 {
-    return D == 128 ? launch_weight_t<128>(p, stream) : launch_weight_t<64>(p, stream);
+    if (p.k_scale) return D == 128 ? launch_weight_t<128, true>(p, stream) : launch_weight_t<64, true>(p, stream);
+    return D == 128 ? launch_weight_t<128, false>(p, stream) : launch_weight_t<64, false>(p, stream);
 }
 
 // ------------------------------------------------------------------ the rows to keep

@@ -452,8 +452,10 @@ struct KvWeightParams {
     long long slices;
     int B, H, G, T, S_max, f32;
     float scale_log2;
+    size_t scale_bytes;              // of k_scale
     int splits;                      // blocks of a slice
 };
+int kv_weight_blocks(bool kv4);   // that an SM holds
 cudaError_t launch_kv_weight(const KvWeightParams &p, int D, cudaStream_t stream);
 
 // The rows kept of each slice, and the planes they are rows of.
