@@ -53,24 +53,31 @@ __global__ void __launch_bounds__(128, (KvWeight<D, KV4>::BLOCKS)) kv_weight_ker
 
     const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE;
     constexpr int UPR = C::RB / 16;   // 16-byte pieces of a row; bf16: the odd rows' halves of 128 bytes change places
+    // piece i of a lane is 512 bytes (an even number of rows) on from piece i - 1
+    const uint32_t to = (uint32_t)(lane ^ (KV4 ? 0 : (lane / UPR & 1) << 2)) * 16;
     auto fetch = [&](int c, int stage) {
         if (c < min(c1, n_pref)) {
-            const int k0 = c * 32;
+            const int k0 = c * 32, left_rows = P - k0;
             const uint32_t dst = ring + stage * C::STAGE;
             const uint8_t *src = p.k_cache + (row0 + k0) * C::RB + lane * 16;
+            constexpr int SB = D / kKv4Group;
+            if (left_rows >= 32 && !(KV4 && D == 64)) {
 #pragma unroll
-            for (int i = 0; i < UPR; ++i) {
-                const int row = (i * 32 + lane) / UPR;
-                const bool in = k0 + row < P;   // rows past the prefix arrive as zeros
-                const uint32_t to = (uint32_t)((i * 32 + lane) ^ (KV4 ? 0 : (row & 1) << 2)) * 16;
-                cp_async16(dst + to, in ? src + i * 512 : p.k_cache, in ? 16u : 0u);
-            }
-            if constexpr (KV4) {   // (D = 64: a word holds an even and an odd row's scales, the tensor's last perhaps one)
-                constexpr int SB = D / kKv4Group;
-                const bool in = k0 + lane < P;
-                const size_t a = ((row0 + (in ? k0 + lane : 0)) * SB) & ~(size_t)3;
-                const size_t left = p.scale_bytes - a;
-                cp_async4(dst + 32 * C::RB + lane * 4, p.k_scale + a, in ? (left < 4 ? (uint32_t)left : 4u) : 0u);
+                for (int i = 0; i < UPR; ++i) cp_async16(dst + to + i * 512, src + i * 512, 16u);
+                if (KV4) cp_async4(dst + 32 * C::RB + lane * 4, p.k_scale + (row0 + k0 + lane) * SB, 4u);
+            } else {
+#pragma unroll
+                for (int i = 0; i < UPR; ++i) {
+                    const int row = (i * 32 + lane) / UPR;
+                    const bool in = row < left_rows;   // rows past the prefix arrive as zeros
+                    cp_async16(dst + to + i * 512, in ? src + i * 512 : p.k_cache, in ? 16u : 0u);
+                }
+                if constexpr (KV4) {   // (D = 64: a word holds an even and an odd row's scales, the tensor's last perhaps one)
+                    const bool in = lane < left_rows;
+                    const size_t a = ((row0 + (in ? k0 + lane : 0)) * SB) & ~(size_t)3;
+                    const size_t left = p.scale_bytes - a;
+                    cp_async4(dst + 32 * C::RB + lane * 4, p.k_scale + a, in ? (left < 4 ? (uint32_t)left : 4u) : 0u);
+                }
             }
         }
         cp_async_commit();
@@ -231,19 +238,26 @@ PPD_DEV uint32_t weight_rank(float w)
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-// One block per slice: the rank of the last row kept by three rounds of counting (11, 11
-// and 10 bits), then one ordered pass that writes the kept rows' indices: all above that
-// rank, and of those equal to it the first ones.  The first and last rows rank above all.
+// One block per slice: the rank of the last row kept, by counting digits of 11, 11 and 10 bits
+// from the top, then the kept rows' indices in order: all above that rank, and of those equal
+// to it the first ones.  The first and last rows rank above all.  Ranks are read once and
+// stay in shared memory where they fit (CACHED); after the first digit the rows that share
+// it are a short list in most cases, which the other digits are counted on.  The indices need
+// no barrier in their loop: each warp counts its stretch of the rows, then writes it.
+constexpr int kSelList = 2048, kSelWarps = kSelThreads / 32;
+
+template <bool CACHED>
 __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvEvictParams p)
 {
-    __shared__ uint32_t hist[kSelBins];
-    __shared__ uint32_t warp_sum[2][kSelThreads / 32];
-    __shared__ uint32_t found[2];   // the bin, and how many rows rank above it
+    extern __shared__ uint32_t ranks[];
+    __shared__ uint32_t hist[kSelBins], list[kSelList];
+    __shared__ uint32_t warp_sum[kSelWarps], warp_eq[kSelWarps];
+    __shared__ uint32_t found[3], n_list;   // the bin, how many rows rank above it, how many share it
     pdl_release();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long u = blockIdx.x;
-    const int b = (int)(u / p.H % p.B);
+    const uint32_t u = blockIdx.x;
+    const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B);
     const int len = ld_input(p.length + b);
     const bool bad = len < 0 || len > p.S_max;
     if (u / p.H < p.B && u % p.H == 0 && tid == 0) {
@@ -256,20 +270,38 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvEvictPar
         return;
     }
     const float *w = p.weight + (size_t)u * p.S_max;
-    auto rank = [&](int j) {
+    auto rank_of = [&](int j) {
         return j < p.sink || j >= len - p.recent ? 0xFFFFFFFFu : weight_rank(ld_input(w + j));
     };
+    auto rank = [&](int j) { return CACHED ? ranks[j] : rank_of(j); };
+    for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+    for (int j0 = tid; j0 < len; j0 += 4 * kSelThreads) {   // four loads in flight
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = j0 + i * kSelThreads < len ? rank_of(j0 + i * kSelThreads) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (j0 + i * kSelThreads < len) {
+                if (CACHED) ranks[j0 + i * kSelThreads] = r[i];
+                atomicAdd(hist + (r[i] >> 21), 1u);
+            }
+    }
     uint32_t prefix = 0, need = (uint32_t)p.budget;   // of the rows with the digits found so far, `need` are kept
-    int shift = 32;
+    bool listed = false;
+#pragma unroll 1
     for (int round = 0; round < 3; ++round) {
-        const int bits = round < 2 ? 11 : 10, bins = 1 << bits;
-        const uint32_t above = shift == 32 ? 0u : 0xFFFFFFFFu << shift;
-        shift -= bits;
-        for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < len; j += kSelThreads) {
-            const uint32_t r = rank(j);
-            if ((r & above) == prefix) atomicAdd(hist + ((r >> shift) & (bins - 1)), 1u);
+        const int bits = round < 2 ? 11 : 10, bins = 1 << bits, shift = round == 0 ? 21 : round == 1 ? 10 : 0;
+        if (round > 0) {
+            const uint32_t above = 0xFFFFFFFFu << (shift + bits);
+            for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
+            __syncthreads();
+            const int n = listed ? (int)n_list : len;
+            for (int j = tid; j < n; j += kSelThreads) {
+                const uint32_t r = listed ? list[j] : rank(j);
+                if ((r & above) == prefix) atomicAdd(hist + ((r >> shift) & (bins - 1)), 1u);
+            }
         }
         __syncthreads();
         // rows ranking in a higher bin, from the top: thread i has bins 4 i .. of the order
@@ -287,47 +319,59 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvEvictPar
             const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
             if (lane >= o) inc += x;
         }
-        if (lane == 31) warp_sum[0][warp] = inc;
+        if (lane == 31) warp_sum[warp] = inc;
         __syncthreads();
         uint32_t before = inc - s;
-        for (int i = 0; i < warp; ++i) before += warp_sum[0][i];
+        for (int i = 0; i < warp; ++i) before += warp_sum[i];
 #pragma unroll
         for (int i = 0; i < per; ++i) {
             if (before < need && need <= before + c[i]) {
                 found[0] = (uint32_t)(bins - 1 - (tid * per + i));
                 found[1] = before;
+                found[2] = c[i];
             }
             before += c[i];
         }
         __syncthreads();
         prefix |= found[0] << shift;
         need -= found[1];
+        if (round == 0 && found[2] <= kSelList) {
+            listed = true;
+            for (int j = tid; j < len; j += kSelThreads) {
+                const uint32_t r = rank(j);
+                if (r >> 21 == prefix >> 21) list[atomicAdd(&n_list, 1u)] = r;
+            }
+        }
         __syncthreads();
     }
-    // rows ranking above `prefix`, and the first `need` that equal it, in order
-    uint32_t n_out = 0, n_eq = 0;
-    for (int j0 = 0; j0 < len; j0 += kSelThreads) {
-        const int j = j0 + tid;
-        const uint32_t r = j < len ? rank(j) : 0u;
-        const uint32_t gt = __ballot_sync(0xffffffffu, j < len && r > prefix);
-        const uint32_t eq = __ballot_sync(0xffffffffu, j < len && r == prefix);
-        if (lane == 0) warp_sum[0][warp] = __popc(gt) | (uint32_t)__popc(eq) << 16;
-        __syncthreads();
-        uint32_t g_before = 0, e_before = 0, g_all = 0, e_all = 0;
-#pragma unroll
-        for (int i = 0; i < kSelThreads / 32; ++i) {
-            const uint32_t x = warp_sum[0][i];
-            if (i < warp) g_before += x & 0xFFFFu, e_before += x >> 16;
-            g_all += x & 0xFFFFu, e_all += x >> 16;
-        }
+    // a warp's stretch of rows: how many rank above `prefix`, how many equal it
+    const int stretch = ((len + kSelThreads - 1) / kSelThreads) * 32;
+    const int j0 = min(len, warp * stretch), j1 = min(len, j0 + stretch);
+    uint32_t n_gt = 0, n_eq = 0;
+    for (int j = j0 + lane; j < j1; j += 32) {
+        const uint32_t r = rank(j);
+        n_gt += r > prefix;
+        n_eq += r == prefix;
+    }
+    n_gt = __reduce_add_sync(0xffffffffu, n_gt);
+    n_eq = __reduce_add_sync(0xffffffffu, n_eq);
+    if (lane == 0) warp_sum[warp] = n_gt, warp_eq[warp] = n_eq;
+    __syncthreads();
+    uint32_t out = 0, eq = 0;   // kept rows before this warp's, and equal ones before it
+    for (int i = 0; i < warp; ++i) out += warp_sum[i], eq += warp_eq[i];
+    out += min(eq, need);
+    for (int j = j0; j < j1; j += 32) {
+        const uint32_t r = j + lane < j1 ? rank(j + lane) : 0u;
+        const uint32_t is_gt = __ballot_sync(0xffffffffu, j + lane < j1 && r > prefix);
+        uint32_t is_eq = __ballot_sync(0xffffffffu, j + lane < j1 && r == prefix);
         const uint32_t low = (1u << lane) - 1u;
-        const uint32_t my_g = g_before + __popc(gt & low), my_e = n_eq + e_before + __popc(eq & low);
-        const bool is_g = (gt >> lane) & 1u, is_e = ((eq >> lane) & 1u) && my_e < need;
-        // kept rows before this one: those above, and the equal ones taken so far
-        if (is_g || is_e) kept[n_out + my_g + (min(my_e, need) - min(n_eq, need))] = j;
-        n_out += g_all + (min(n_eq + e_all, need) - min(n_eq, need));
-        n_eq += e_all;
-        __syncthreads();
+        // of the equal rows the first ones, until there are `need`
+        const uint32_t left = need > eq ? need - eq : 0u;
+        eq += __popc(is_eq);
+        is_eq = __ballot_sync(0xffffffffu, ((is_eq >> lane) & 1u) && __popc(is_eq & low) < left);
+        const uint32_t take = is_gt | is_eq;
+        if ((take >> lane) & 1u) kept[out + __popc(take & low)] = j + lane;
+        out += __popc(take);
     }
 }
 
@@ -343,37 +387,43 @@ template <> struct MoveUnit<1> { using T = uint8_t; };
 
 constexpr int kMoveThreads = 256, kMoveDeep = 4;
 
-// Kept row i goes to row i of the destination: each step of a block reads 1024 units (16
-// bytes where rows and addresses allow), then writes them.  In place a block takes its
-// columns of the whole slice alone, in order: the rows of a step lie at or above their places,
-// and so do those of every later step, so what a step overwrites has been read.
+// Kept row i goes to row i of the destination: each step of a block reads kMoveDeep units a thread
+// (16 bytes where rows and addresses allow), then writes them; the next step's row indices are on
+// their way meanwhile.  In place a block takes its columns of the whole slice alone, in order:
+// the rows of a step lie at or above their places, and so do those of every later step, so
+// what a step overwrites has been read.
 template <int BYTES>
-PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, long long u, int c0, int c1, int i0, int i1)
+PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, uint32_t u, int c0, int c1, int i0, int i1)
 {
     using T = typename MoveUnit<BYTES>::T;
-    const T *src = reinterpret_cast<const T *>(static_cast<const uint8_t *>(pl.src) + (size_t)u * p.S_max * pl.row_bytes);
-    T *dst = reinterpret_cast<T *>(static_cast<uint8_t *>(pl.dst) + (size_t)u * p.S_out * pl.row_bytes);
     const int per_row = pl.row_bytes / BYTES, w = c1 - c0;   // this block's units of a row
+    const T *src = reinterpret_cast<const T *>(static_cast<const uint8_t *>(pl.src) + (size_t)u * p.S_max * pl.row_bytes) + c0;
+    T *dst = reinterpret_cast<T *>(static_cast<uint8_t *>(pl.dst) + (size_t)u * p.S_out * pl.row_bytes) + c0;
     const bool in_place = pl.src == pl.dst;
-    const int rows = kMoveThreads * kMoveDeep / w;           // of a step (w divides the threads or is below)
+    const int rows = kMoveThreads * kMoveDeep / w;           // of a step
+    int row[kMoveDeep], col[kMoveDeep], from[kMoveDeep];
+#pragma unroll
+    for (int x = 0; x < kMoveDeep; ++x) {
+        const int unit = x * kMoveThreads + (int)threadIdx.x;
+        row[x] = unit / w;
+        col[x] = unit - row[x] * w;
+        if (row[x] >= rows) row[x] = i1;   // none
+        from[x] = i0 + row[x] < i1 ? ld_input(kept + i0 + row[x]) : -1;
+    }
     for (int r0 = i0; r0 < i1; r0 += rows) {
         T v[kMoveDeep];
         bool go[kMoveDeep];
 #pragma unroll
         for (int x = 0; x < kMoveDeep; ++x) {
-            const int unit = x * kMoveThreads + (int)threadIdx.x, row = unit / w;
-            const int i = r0 + row;
-            go[x] = row < rows && i < i1;
-            const int from = go[x] ? ld_input(kept + i) : -1;
-            go[x] = go[x] && from >= 0 && !(in_place && from == i);
-            if (go[x]) v[x] = src[(size_t)from * per_row + c0 + unit % w];
+            go[x] = from[x] >= 0 && !(in_place && from[x] == r0 + row[x]);
+            if (go[x]) v[x] = src[(size_t)from[x] * per_row + col[x]];
         }
+#pragma unroll
+        for (int x = 0; x < kMoveDeep; ++x) from[x] = r0 + rows + row[x] < i1 ? ld_input(kept + r0 + rows + row[x]) : -1;
         if (in_place) __syncthreads();
 #pragma unroll
-        for (int x = 0; x < kMoveDeep; ++x) {
-            const int unit = x * kMoveThreads + (int)threadIdx.x;
-            if (go[x]) dst[(size_t)(r0 + unit / w) * per_row + c0 + unit % w] = v[x];
-        }
+        for (int x = 0; x < kMoveDeep; ++x)
+            if (go[x]) dst[(size_t)(r0 + row[x]) * per_row + col[x]] = v[x];
     }
 }
 
@@ -383,11 +433,11 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const KvEvictPara
 {
     pdl_release();
     pdl_wait();
-    const long long u = blockIdx.x / p.move_blocks;
+    const uint32_t u = blockIdx.x / (uint32_t)p.move_blocks;
     int part = (int)(blockIdx.x % p.move_blocks), x = 0;
     while (part >= p.plane[x].parts) part -= p.plane[x++].parts;
     const KvPlane &pl = p.plane[x];
-    const int b = (int)(u / p.H % p.B);
+    const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B);
     const int len = ld_input(p.length + b);
     if (len < 0 || len > p.S_max) return;
     const int n = min(len, p.budget);
@@ -413,7 +463,18 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const KvEvictPara
 
 cudaError_t launch_kv_evict(const KvEvictParams &p, cudaStream_t stream)
 {
-    const cudaError_t e = launch_chained(kv_select_kernel, dim3((unsigned)p.slices), dim3(kSelThreads), dim3(1), stream, p);
+    // ranks in shared memory up to 40,000 rows (160 KB): read again instead, longer caches take
+    // twice the time a row
+    constexpr uint32_t most = 40000;
+    static std::atomic<uint64_t> configured{0};
+    cudaError_t e;
+    if ((uint32_t)p.S_max <= most) {
+        e = allow_smem(kv_select_kernel<true>, most * 4, configured);
+        if (e == cudaSuccess)
+            e = launch_chained_smem(kv_select_kernel<true>, dim3((unsigned)p.slices), dim3(kSelThreads), dim3(1), (uint32_t)p.S_max * 4u, stream, p);
+    } else {
+        e = launch_chained(kv_select_kernel<false>, dim3((unsigned)p.slices), dim3(kSelThreads), dim3(1), stream, p);
+    }
     if (e != cudaSuccess) return e;
     return launch_chained(kv_move_kernel, dim3((unsigned)(p.slices * p.move_blocks)), dim3(kMoveThreads), dim3(1), stream, p);
 }

@@ -164,3 +164,25 @@ def test_evict_reports_bad_lengths(cuda_device):
     E = ppd.PPD_ERR_CAPACITY
     assert status.tolist() == [E, E, 0] and new_len.tolist() == [-1, 21, 4]
     assert (kept[:, :2] == -1).all() and torch.equal(w[:, :2], before[:, :2])
+
+
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_of_long_caches(cuda_device, ties):
+    """More rows than a block's shared memory holds, and more equal ones than a short list."""
+    from paper_2405_18628_gb300 import ppd
+    dev, S, budget = cuda_device, 70001, 30011
+    g = torch.Generator(device=dev)
+    g.manual_seed(9)
+    for n in (S, 39999):
+        w = torch.rand(1, 1, 2, n, device=dev, generator=g)
+        if ties:
+            w = (w * 3).floor()
+        host = w.clone()
+        kept = torch.empty(1, 1, 2, min(budget, n // 2), dtype=torch.int32, device=dev)
+        i = [torch.empty(1, dtype=torch.int32, device=dev) for _ in range(2)]
+        ppd.ppd_kv_evict(w, [], _i32([n], dev), kept.shape[3], 5, 7, kept, *i)
+        key = host.clone()
+        key[..., :5] = key[..., n - 7:] = float("inf")
+        want = torch.sort(torch.sort(key, dim=-1, descending=True, stable=True).indices[..., :kept.shape[3]], -1).values
+        assert torch.equal(kept.long(), want)
+        assert torch.equal(w[..., :kept.shape[3]], torch.gather(host, 3, want))
