@@ -277,16 +277,30 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvEvictPar
     for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
     if (tid == 0) n_list = 0;
     __syncthreads();
-    for (int j0 = tid; j0 < len; j0 += 4 * kSelThreads) {   // four loads in flight
-        uint32_t r[4];
+    auto take = [&](int j, float x) {
+        const uint32_t r = j < p.sink || j >= len - p.recent ? 0xFFFFFFFFu : weight_rank(x);
+        if (CACHED) ranks[j] = r;
+        atomicAdd(hist + (r >> 21), 1u);
+    };
+    // 32 bytes or more a thread in flight
+    const int len4 = (reinterpret_cast<uintptr_t>(w) & 15) == 0 ? len / 4 : 0;
+    for (int i0 = tid; i0 < len4; i0 += 4 * kSelThreads) {
+        float4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = j0 + i * kSelThreads < len ? rank_of(j0 + i * kSelThreads) : 0u;
+        for (int i = 0; i < 4; ++i) x[i] = i0 + i * kSelThreads < len4 ? ld_input(reinterpret_cast<const float4 *>(w) + i0 + i * kSelThreads) : float4{};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (j0 + i * kSelThreads < len) {
-                if (CACHED) ranks[j0 + i * kSelThreads] = r[i];
-                atomicAdd(hist + (r[i] >> 21), 1u);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int j = 4 * (i0 + i * kSelThreads);
+            if (j < 4 * len4) take(j, x[i].x), take(j + 1, x[i].y), take(j + 2, x[i].z), take(j + 3, x[i].w);
+        }
+    }
+    for (int j0 = 4 * len4 + tid; j0 < len; j0 += 8 * kSelThreads) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = j0 + i * kSelThreads < len ? ld_input(w + j0 + i * kSelThreads) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j0 + i * kSelThreads < len) take(j0 + i * kSelThreads, x[i]);
     }
     uint32_t prefix = 0, need = (uint32_t)p.budget;   // of the rows with the digits found so far, `need` are kept
     bool listed = false;
