@@ -48,7 +48,7 @@ PPD_DEV float block_reduce(float v, float *warp_s, float none, Op op)
     return __shfl_sync(0xffffffffu, v, 0);
 }
 
-__global__ void __launch_bounds__(kSampleThreads) sample_accept_kernel(const SampleParams p, int cluster)
+__global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const SampleParams p, int cluster)
 {
     extern __shared__ __align__(16) float e[];   // this CTA's share of R
     __shared__ SampleShared s;
