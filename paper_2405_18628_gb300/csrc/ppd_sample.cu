@@ -20,37 +20,33 @@ namespace ppd {
 // one pass over its logits and one exchange of the CTAs' maxima and sums, its chosen
 // children none; a drawn child's rejection costs one pass over the share and its draft row,
 // and an exchange.  Every CTA takes the same decisions from the same numbers.
-constexpr int kSampleThreads = 512;
+//
+// Bound by the chain of a walk's passes, not by their bytes: a thread keeps to its own elements
+// of the share and a warp to its own maximum, so that a pass has one barrier of the block and
+// one of the cluster; what a pass will need next (the children's entries, the draft row) is asked
+// for while the row is on its way.
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 
 struct SampleShared {
     int par[kMaxTree], tok[kMaxTree], row[kMaxTree];   // parents, tokens, draft rows
-    float u[kMaxTree], value[kMaxTree], prob[kMaxTree];   // value: R at the node's token
+    float u[kMaxTree], prob[kMaxTree];
     int child[kMaxTree];      // children of the node, in order
+    float value[kMaxTree];    // R at their tokens
+    float draft[kMaxTree];    // q at their tokens
+    bool first[kMaxTree];     // a chosen child whose token no chosen one before it has
     int path[kMaxTree];
+    float2 warp[kSampleWarps];
     float2 part[2][kMaxCluster];
-    unsigned long long best[kMaxCluster];
-    float warp[kSampleThreads / 32];
-    unsigned long long warp_best[kSampleThreads / 32];
-    int n_child, verdict;
+    unsigned long long best[kMaxCluster], warp_best[kSampleWarps];
+    int n_child, verdict, next;
+    float z;
 };
 
-template <class Op>
-PPD_DEV float block_reduce(float v, float *warp_s, float none, Op op)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) warp_s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = threadIdx.x % 32 < kSampleThreads / 32 ? warp_s[threadIdx.x % 32] : none;
-#pragma unroll
-    for (int o = kSampleThreads / 64; o; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return __shfl_sync(0xffffffffu, v, 0);
-}
-
+// VEC: 16-byte accesses, which every row allows.
+template <bool VEC>
 __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const SampleParams p, int cluster)
 {
-    extern __shared__ __align__(16) float e[];   // this CTA's share of R
+    extern __shared__ __align__(16) float e[];   // this CTA's share: R over a factor of the warp
     __shared__ SampleShared s;
     pdl_release();
     pdl_wait();
@@ -58,14 +54,18 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     const int rank = (int)(blockIdx.x % cluster), b = (int)(blockIdx.x / cluster);
     const int T = p.T, V = p.V;
     const int lo = min(V, rank * p.chunk), n = min(V, lo + p.chunk) - lo;
-    const float *x0 = p.logits + (size_t)b * T * V;
-    const float *q0 = p.draft_probs ? p.draft_probs + (size_t)b * p.n_draft * V : nullptr;
+    const float *x0 = p.logits + (size_t)b * T * V + lo;
+    const float *q0 = p.draft_probs ? p.draft_probs + (size_t)b * p.n_draft * V + lo : nullptr;
+    // a thread's elements are its own throughout
+    constexpr int STEP = VEC ? 4 : 1, STRIDE = kSampleThreads * STEP;
+    const int own0 = tid * STEP;
+    auto owner = [&](int v) { return v / STEP % kSampleThreads; };
 
     // ------------------------------------------------ the tree
     bool bad = false;
     for (int i = tid; i < T; i += kSampleThreads) {
         const int pa = ld_input(p.parent + (size_t)b * T + i), tk = ld_input(p.cand + (size_t)b * T + i);
-        const int dr = q0 && p.draft_row ? ld_input(p.draft_row + (size_t)b * T + i) : -1;
+        const int dr = q0 ? ld_input(p.draft_row + (size_t)b * T + i) : -1;
         bad |= i == 0 ? (pa != -1 || tk < 0 || tk >= V) : (pa < 0 || pa >= i || tk < -1 || tk >= V);
         bad |= i > 0 && tk >= 0 && (dr < -1 || dr >= p.n_draft);
         s.par[i] = pa;
@@ -79,56 +79,78 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     int err = bad ? kErrTree : (P < 0 || P > p.S_max ? kErrCapacity : kOk);
 
     int phase = 0;
-    float M = 0.f, f = 1.f, Z = 0.f, rest = 0.f;   // R = f e; rest: the sum of R in the shares
-    // maxima and sums of the CTAs together: M, this CTA's factor and the sum
-    auto exchange = [&](float m_c, float s_c) {
-        if (tid < cluster) st_cluster_v2(cluster_map(smem_addr(&s.part[phase][rank]), (uint32_t)tid), m_c, s_c);
+    float M = 0.f, f = 1.f, rest = 0.f;   // R = f e; rest: the sum of R in the shares
+    // the warps' maxima and sums together: M, this warp's factor and the sum of all
+    auto combine = [&](float2 v) {   // over a warp's lanes
+        float m = v.x;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float y = v.x == -INFINITY ? v.y : v.y * ex2((v.x - m) * p.k);   // y: 0, or NaN
+#pragma unroll
+        for (int o = 16; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+        return make_float2(m, y);
+    };
+    auto exchange = [&](float m_w, float s_w) {   // (a lane's maximum is its warp's, a sum its own)
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s_w += __shfl_xor_sync(0xffffffffu, s_w, o);
+        if (lane == 0) s.warp[warp] = make_float2(m_w, s_w);
+        __syncthreads();
+        if (warp == 0) {
+            const float2 v = combine(lane < kSampleWarps ? s.warp[lane] : make_float2(-INFINITY, 0.f));
+            if (lane < cluster) st_cluster_v2(cluster_map(smem_addr(&s.part[phase][rank]), (uint32_t)lane), v.x, v.y);
+        }
         cluster_sync();
         M = -INFINITY;
         for (int r = 0; r < cluster; ++r) M = fmaxf(M, s.part[phase][r].x);
         rest = 0.f;
         for (int r = 0; r < cluster; ++r) {
             const float2 v = s.part[phase][r];
-            rest += v.x == -INFINITY ? v.y : v.y * ex2((v.x - M) * p.k);   // y: 0, or NaN
+            rest += v.x == -INFINITY ? v.y : v.y * ex2((v.x - M) * p.k);
         }
-        f = m_c == -INFINITY ? 1.f : ex2((m_c - M) * p.k);
+        f = m_w == -INFINITY ? 1.f : ex2((m_w - M) * p.k);
         phase ^= 1;
     };
-    auto fmax_op = [](float a, float c) { return fmaxf(a, c); };
-    // the node's logits into the share; `leave`: without the chosen children's tokens
-    auto load_row = [&](int node, bool leave) {
-        const float *x = x0 + (size_t)node * V + lo;
+    // the node's logits into the share, without the first `leave` children's chosen tokens
+    auto load_row = [&](int node, int leave) {
+        const float *x = x0 + (size_t)node * V;
         float m = -INFINITY;
-        if ((reinterpret_cast<uintptr_t>(x) & 15) == 0 && (n & 3) == 0) {
-            for (int v = tid; v < n / 4; v += kSampleThreads) {
-                const float4 a = ld_input(reinterpret_cast<const float4 *>(x) + v);
-                reinterpret_cast<float4 *>(e)[v] = a;
+        if constexpr (VEC) {
+#pragma unroll 4
+            for (int v = own0; v < n; v += STRIDE) {
+                const float4 a = ld_input(reinterpret_cast<const float4 *>(x + v));
+                *reinterpret_cast<float4 *>(e + v) = a;
                 m = fmaxf(m, fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)));
             }
         } else {
-            for (int v = tid; v < n; v += kSampleThreads) {
+#pragma unroll 4
+            for (int v = own0; v < n; v += STRIDE) {
                 const float a = ld_input(x + v);
                 e[v] = a;
                 m = fmaxf(m, a);
             }
         }
-        m = block_reduce(m, s.warp, -INFINITY, fmax_op);
-        if (leave) {
-            for (int i = tid; i < s.n_child; i += kSampleThreads) {
-                const int c = s.child[i], v = s.tok[c] - lo;
-                // (a NaN stays where it is: it is what the row is)
-                if (s.row[c] < 0 && v >= 0 && v < n && e[v] == e[v]) e[v] = -INFINITY;
-            }
-            __syncthreads();
+        for (int i = 0; i < leave; ++i) {
+            const int c = s.child[i], v = s.tok[c] - lo;
+            // (a NaN stays where it is: it is what the row is)
+            if (s.row[c] < 0 && v >= 0 && v < n && owner(v) == tid && e[v] == e[v]) e[v] = -INFINITY;
         }
-        float sum = 0.f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         const float mm = m == -INFINITY ? 0.f : m;
-        for (int v = tid; v < n; v += kSampleThreads) {
-            const float r = ex2((e[v] - mm) * p.k);
-            e[v] = r;
-            sum += r;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int v = own0; v < n; v += STRIDE) {
+            if constexpr (VEC) {
+                float4 a = *reinterpret_cast<const float4 *>(e + v);
+                a = make_float4(ex2((a.x - mm) * p.k), ex2((a.y - mm) * p.k), ex2((a.z - mm) * p.k), ex2((a.w - mm) * p.k));
+                *reinterpret_cast<float4 *>(e + v) = a;
+                sum += (a.x + a.y) + (a.z + a.w);
+            } else {
+                const float r = ex2((e[v] - mm) * p.k);
+                e[v] = r;
+                sum += r;
+            }
         }
-        sum = block_reduce(sum, s.warp, 0.f, OpAdd());
         exchange(m, sum);
     };
 
@@ -138,7 +160,6 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
         if (tid == 0) s.path[0] = 0;
         while (true) {
             // the node's children, in order
-            __syncthreads();
             if (warp == 0) {
                 int k = 0;
                 for (int i0 = cur + 1 - (cur + 1) % 32; i0 < T; i0 += 32) {
@@ -152,11 +173,28 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
             }
             __syncthreads();
             const int kids = s.n_child;
-            load_row(cur, true);
+            // their entries of the row and of their draft rows (one each, from thread i), and
+            // the first one's draft row, which a rejection reads, into L2
+            float kid_x = 0.f, kid_q = 1.f;
+            if (tid < kids) {
+                const int c = s.child[tid], t = s.tok[c], r = s.row[c];
+                kid_x = ld_input(x0 - lo + (size_t)cur * V + t);
+                if (r >= 0) kid_q = ld_input(q0 - lo + (size_t)r * V + t);
+                bool first = r < 0;
+                for (int h = 0; first && h < tid; ++h) first = s.row[s.child[h]] >= 0 || s.tok[s.child[h]] != t;
+                s.first[tid] = first;
+            }
+            if (kids > 0 && s.row[s.child[0]] >= 0) {
+                const float *q = q0 + (size_t)s.row[s.child[0]] * V;
+                for (int v = 32 * tid; v < n; v += 32 * kSampleThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + v));
+            }
+            load_row(cur, kids);
             // R at the children's tokens; a chosen token counts once, at its first child
             flat = !(M > -INFINITY && M < INFINITY) || rest != rest;
-            for (int i = tid; i < kids; i += kSampleThreads)
-                s.value[i] = ex2((ld_input(x0 + (size_t)cur * V + s.tok[s.child[i]]) - M) * p.k);
+            if (tid < kids) {
+                s.value[tid] = ex2((kid_x - M) * p.k);
+                s.draft[tid] = kid_q;
+            }
             __syncthreads();
             int next = -1, at = 0;
             while (at < kids) {
@@ -164,25 +202,18 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
                     // Z: the shares and what is left of the chosen children's tokens
                     auto chosen_sum = [&]() {
                         float z = 0.f;
-                        for (int i = lane; i < kids; i += 32) {
-                            const int c = s.child[i];
-                            bool first = s.row[c] < 0;
-                            for (int h = 0; first && h < i; ++h) first = s.row[s.child[h]] >= 0 || s.tok[s.child[h]] != s.tok[c];
-                            if (first) z += s.value[i];
-                        }
+                        for (int i = lane; i < kids; i += 32)
+                            if (s.first[i]) z += s.value[i];
 #pragma unroll
                         for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
                         return z;
                     };
                     int verdict = -1;   // all rejected; i: child i accepted; kMaxTree + i: drawn child i rejected
+                    float z = rest + chosen_sum();
                     for (; at < kids; ++at) {
                         const int c = s.child[at], t = s.tok[c];
-                        const float z = rest + chosen_sum();
                         float a = s.value[at] / z;
-                        if (s.row[c] >= 0) {
-                            const float q = ld_input(q0 + (size_t)s.row[c] * V + t);
-                            a = q > 0.f ? a / q : 0.f;
-                        }
+                        if (s.row[c] >= 0) a = s.draft[at] > 0.f ? a / s.draft[at] : 0.f;
                         a = flat || !(z > 0.f) ? 0.f : fminf(a, 1.f);
                         if (lane == 0) s.prob[c] = a;
                         if (s.u[c] < a) {
@@ -198,37 +229,47 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
                         for (int i = lane; i < kids; i += 32)
                             if (s.tok[s.child[i]] == t) s.value[i] = 0.f;
                         __syncwarp();
+                        z = rest + chosen_sum();
                     }
-                    const float z = rest + chosen_sum();
                     if (lane == 0) {
                         s.verdict = verdict;
-                        s.warp[0] = z;
+                        if (verdict >= 0 && verdict < kMaxTree) s.next = s.child[verdict];   // (the list is the next node's soon)
+                        s.z = z;
                     }
                 }
                 __syncthreads();
                 const int verdict = s.verdict;
-                Z = s.warp[0];
+                const float Z = s.z;
                 if (verdict < 0) break;
                 if (verdict < kMaxTree) {
-                    next = s.child[verdict];
+                    next = s.next;
                     break;
                 }
                 // a drawn child's rejection: what its distribution covers is taken away
+                // (e is 0 at the chosen children's tokens, and stays it)
                 at = verdict - kMaxTree + 1;
                 const float *q = q0 + (size_t)s.row[s.child[at - 1]] * V;
+                if (tid < kids) kid_q = ld_input(q - lo + s.tok[s.child[tid]]);
                 const float zf = f / Z;
                 float sum = 0.f;
-                for (int v = tid; v < n; v += kSampleThreads) {
-                    const float r = fmaxf(e[v] * zf - ld_input(q + lo + v), 0.f);
-                    e[v] = r;
-                    sum += r;
+                if constexpr (VEC) {
+#pragma unroll 4
+                    for (int v = own0; v < n; v += STRIDE) {
+                        const float4 y = ld_input(reinterpret_cast<const float4 *>(q + v)), a = *reinterpret_cast<const float4 *>(e + v);
+                        const float4 r = make_float4(fmaxf(a.x * zf - y.x, 0.f), fmaxf(a.y * zf - y.y, 0.f), fmaxf(a.z * zf - y.z, 0.f), fmaxf(a.w * zf - y.w, 0.f));
+                        *reinterpret_cast<float4 *>(e + v) = r;
+                        sum += (r.x + r.y) + (r.z + r.w);
+                    }
+                } else {
+#pragma unroll 4
+                    for (int v = own0; v < n; v += STRIDE) {
+                        const float r = fmaxf(e[v] * zf - ld_input(q + v), 0.f);
+                        e[v] = r;
+                        sum += r;
+                    }
                 }
-                for (int i = tid; i < kids; i += kSampleThreads)
-                    s.value[i] = fmaxf(s.value[i] / Z - ld_input(q + s.tok[s.child[i]]), 0.f);
-                // (e is 0 at the chosen children's tokens, and stays it)
-                sum = block_reduce(sum, s.warp, 0.f, OpAdd());
+                if (tid < kids) s.value[tid] = fmaxf(s.value[tid] / Z - kid_q, 0.f);
                 exchange(0.f, sum);
-                __syncthreads();
             }
             if (next < 0) break;
             cur = next;
@@ -242,20 +283,32 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     if (err == kOk) {
         // every child was rejected: the shares hold what is left
         const bool none = !flat && !(rest > 0.f);
-        if (none) load_row(cur, false);   // nothing left: the node's own distribution
-        const float *x = x0 + (size_t)cur * V + lo, *noise = p.noise + (size_t)b * V + lo;
+        if (none) load_row(cur, 0);   // nothing left: the node's own distribution
+        const float *x = x0 + (size_t)cur * V, *noise = p.noise + (size_t)b * V + lo;
         unsigned long long best = 0;
-        for (int v = tid; v < n; v += kSampleThreads) {
-            float r;
-            if (flat) {   // the first NaN, or the first of the largest
-                const float a = ld_input(x + v);
-                r = a != a ? 2.f : a == M ? 1.f : 0.f;
+#pragma unroll 1
+        for (int v0 = own0; v0 < n; v0 += STRIDE) {   // a thread's own elements: the warp's factor is theirs
+            float4 y = make_float4(1.f, 1.f, 1.f, 1.f);
+            if (!VEC || (reinterpret_cast<uintptr_t>(noise) & 15)) {
+                y.x = ld_input(noise + v0);
+                if (VEC) y.y = ld_input(noise + v0 + 1), y.z = ld_input(noise + v0 + 2), y.w = ld_input(noise + v0 + 3);
             } else {
-                r = f * e[v] / ld_input(noise + v);
-                if (!(r >= 0.f)) r = 0.f;
+                y = ld_input(reinterpret_cast<const float4 *>(noise + v0));
             }
-            const unsigned long long key = (unsigned long long)__float_as_uint(r) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + v));
-            if (key > best) best = key;
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const int v = v0 + i;
+                float r;
+                if (flat) {   // the first NaN, or the first of the largest
+                    const float a = ld_input(x + v);
+                    r = a != a ? 2.f : a == M ? 1.f : 0.f;
+                } else {
+                    r = f * e[v] / (i == 0 ? y.x : i == 1 ? y.y : i == 2 ? y.z : y.w);
+                    if (!(r >= 0.f)) r = 0.f;
+                }
+                const unsigned long long key = (unsigned long long)__float_as_uint(r) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + v));
+                if (key > best) best = key;
+            }
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
@@ -265,7 +318,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
         if (lane == 0) s.warp_best[warp] = best;
         __syncthreads();
         if (tid == 0) {
-            for (int w = 1; w < kSampleThreads / 32; ++w)
+            for (int w = 1; w < kSampleWarps; ++w)
                 if (s.warp_best[w] > best) best = s.warp_best[w];
             st_cluster_u64(cluster_map(smem_addr(&s.best[rank]), 0), best);
         }
@@ -291,13 +344,20 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     }
 }
 
-cudaError_t launch_sample_accept(const SampleParams &p, int cluster, cudaStream_t stream)
+template <bool VEC>
+static cudaError_t launch_sample_t(const SampleParams &p, int cluster, cudaStream_t stream)
 {
     static std::atomic<uint64_t> configured{0};
-    const cudaError_t e = allow_smem(sample_accept_kernel, kSampleMaxChunk * 4, configured);
+    const cudaError_t e = allow_smem(sample_accept_kernel<VEC>, kSampleMaxChunk * 4, configured);
     if (e != cudaSuccess) return e;
-    return launch_chained_smem(sample_accept_kernel, dim3((unsigned)(p.B * cluster)), dim3(kSampleThreads),
-                               dim3((unsigned)cluster), (uint32_t)p.chunk * 4u, stream, p, cluster);
+    return launch_chained_smem(sample_accept_kernel<VEC>, dim3((unsigned)(p.B * cluster)), dim3(kSampleThreads), dim3((unsigned)cluster),
+                               (uint32_t)p.chunk * 4u, stream, p, cluster);
+}
+
+cudaError_t launch_sample_accept(const SampleParams &p, int cluster, cudaStream_t stream)
+{
+    const bool vec = p.V % 4 == 0 && (reinterpret_cast<uintptr_t>(p.logits) & 15) == 0 && (reinterpret_cast<uintptr_t>(p.draft_probs) & 15) == 0;
+    return vec ? launch_sample_t<true>(p, cluster, stream) : launch_sample_t<false>(p, cluster, stream);
 }
 
 }  // namespace ppd
