@@ -1,9 +1,10 @@
 // ppd_sample.cu -- drafted tokens of a tree verified against the target's probabilities
 // with given random numbers, and the token after the last accepted one drawn from what the
 // rejections left.
-#include "ppd_device.cuh"
+#include "ppd_kv4.cuh"
 
 #include <cmath>
+#include <type_traits>
 
 namespace ppd {
 
@@ -58,6 +59,8 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     const float *q0 = p.draft_probs ? p.draft_probs + (size_t)b * p.n_draft * V + lo : nullptr;
     // a thread's elements are its own throughout
     constexpr int STEP = VEC ? 4 : 1, STRIDE = kSampleThreads * STEP;
+    constexpr int AHEAD = VEC ? 2 : 8;
+    using Own = std::conditional_t<VEC, float4, float>;
     const int own0 = tid * STEP;
     auto owner = [&](int v) { return v / STEP % kSampleThreads; };
 
@@ -113,20 +116,22 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     // the node's logits into the share, without the first `leave` children's chosen tokens
     auto load_row = [&](int node, int leave) {
         const float *x = x0 + (size_t)node * V;
+        const uint32_t to = smem_addr(e);
+#pragma unroll 4
+        for (int v = own0; v < n; v += STRIDE) {   // all of a thread's elements on their way at once
+            if constexpr (VEC) cp_async16(to + v * 4, x + v, 16u);
+            else cp_async4(to + v * 4, x + v, 4u);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
         float m = -INFINITY;
-        if constexpr (VEC) {
 #pragma unroll 4
-            for (int v = own0; v < n; v += STRIDE) {
-                const float4 a = ld_input(reinterpret_cast<const float4 *>(x + v));
-                *reinterpret_cast<float4 *>(e + v) = a;
+        for (int v = own0; v < n; v += STRIDE) {
+            if constexpr (VEC) {
+                const float4 a = *reinterpret_cast<const float4 *>(e + v);
                 m = fmaxf(m, fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)));
-            }
-        } else {
-#pragma unroll 4
-            for (int v = own0; v < n; v += STRIDE) {
-                const float a = ld_input(x + v);
-                e[v] = a;
-                m = fmaxf(m, a);
+            } else {
+                m = fmaxf(m, e[v]);
             }
         }
         for (int i = 0; i < leave; ++i) {
@@ -252,20 +257,26 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
                 if (tid < kids) kid_q = ld_input(q - lo + s.tok[s.child[tid]]);
                 const float zf = f / Z;
                 float sum = 0.f;
-                if constexpr (VEC) {
-#pragma unroll 4
-                    for (int v = own0; v < n; v += STRIDE) {
-                        const float4 y = ld_input(reinterpret_cast<const float4 *>(q + v)), a = *reinterpret_cast<const float4 *>(e + v);
-                        const float4 r = make_float4(fmaxf(a.x * zf - y.x, 0.f), fmaxf(a.y * zf - y.y, 0.f), fmaxf(a.z * zf - y.z, 0.f), fmaxf(a.w * zf - y.w, 0.f));
-                        *reinterpret_cast<float4 *>(e + v) = r;
-                        sum += (r.x + r.y) + (r.z + r.w);
-                    }
-                } else {
-#pragma unroll 4
-                    for (int v = own0; v < n; v += STRIDE) {
-                        const float r = fmaxf(e[v] * zf - ld_input(q + v), 0.f);
-                        e[v] = r;
-                        sum += r;
+                for (int v0 = own0; v0 < n; v0 += AHEAD * STRIDE) {
+                    Own y[AHEAD];   // the loads of several elements in flight
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i)
+                        if (v0 + i * STRIDE < n) y[i] = ld_input(reinterpret_cast<const Own *>(q + v0 + i * STRIDE));
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) {
+                        const int v = v0 + i * STRIDE;
+                        if (v >= n) break;
+                        if constexpr (VEC) {
+                            const float4 x = *reinterpret_cast<const float4 *>(e + v);
+                            const float4 r = make_float4(fmaxf(x.x * zf - y[i].x, 0.f), fmaxf(x.y * zf - y[i].y, 0.f), fmaxf(x.z * zf - y[i].z, 0.f),
+                                                         fmaxf(x.w * zf - y[i].w, 0.f));
+                            *reinterpret_cast<float4 *>(e + v) = r;
+                            sum += (r.x + r.y) + (r.z + r.w);
+                        } else {
+                            const float r = fmaxf(e[v] * zf - y[i], 0.f);
+                            e[v] = r;
+                            sum += r;
+                        }
                     }
                 }
                 if (tid < kids) s.value[tid] = fmaxf(s.value[tid] / Z - kid_q, 0.f);
@@ -286,29 +297,39 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
         if (none) load_row(cur, 0);   // nothing left: the node's own distribution
         const float *x = x0 + (size_t)cur * V, *noise = p.noise + (size_t)b * V + lo;
         unsigned long long best = 0;
-#pragma unroll 1
-        for (int v0 = own0; v0 < n; v0 += STRIDE) {   // a thread's own elements: the warp's factor is theirs
-            float4 y = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (!VEC || (reinterpret_cast<uintptr_t>(noise) & 15)) {
-                y.x = ld_input(noise + v0);
-                if (VEC) y.y = ld_input(noise + v0 + 1), y.z = ld_input(noise + v0 + 2), y.w = ld_input(noise + v0 + 3);
+        auto consider = [&](int v, float noise_v) {
+            float r;
+            if (flat) {   // the first NaN, or the first of the largest
+                const float a = ld_input(x + v);
+                r = a != a ? 2.f : a == M ? 1.f : 0.f;
             } else {
-                y = ld_input(reinterpret_cast<const float4 *>(noise + v0));
+                r = f * e[v] / noise_v;
+                if (!(r >= 0.f)) r = 0.f;
+            }
+            const unsigned long long key = (unsigned long long)__float_as_uint(r) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + v));
+            if (key > best) best = key;
+        };
+        // a thread's own elements: the warp's factor is theirs
+        const bool wide = VEC && (reinterpret_cast<uintptr_t>(noise) & 15) == 0;
+        for (int v0 = own0; v0 < n; v0 += AHEAD * STRIDE) {
+            float y[AHEAD * STEP];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int v = v0 + i * STRIDE;
+                if (v >= n) break;
+                if (wide) {
+                    const float4 a = ld_input(reinterpret_cast<const float4 *>(noise + v));
+                    y[i * STEP] = a.x, y[(i * STEP + 1) % (AHEAD * STEP)] = a.y, y[(i * STEP + 2) % (AHEAD * STEP)] = a.z, y[(i * STEP + 3) % (AHEAD * STEP)] = a.w;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < STEP; ++k) y[i * STEP + k] = ld_input(noise + v + k);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < STEP; ++i) {
-                const int v = v0 + i;
-                float r;
-                if (flat) {   // the first NaN, or the first of the largest
-                    const float a = ld_input(x + v);
-                    r = a != a ? 2.f : a == M ? 1.f : 0.f;
-                } else {
-                    r = f * e[v] / (i == 0 ? y.x : i == 1 ? y.y : i == 2 ? y.z : y.w);
-                    if (!(r >= 0.f)) r = 0.f;
-                }
-                const unsigned long long key = (unsigned long long)__float_as_uint(r) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + v));
-                if (key > best) best = key;
-            }
+            for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (int k = 0; k < STEP; ++k)
+                    if (v0 + i * STRIDE < n) consider(v0 + i * STRIDE + k, y[i * STEP + k]);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
