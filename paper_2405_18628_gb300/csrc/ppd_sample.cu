@@ -24,8 +24,8 @@ namespace ppd {
 //
 // Bound by the chain of a walk's passes, not by their bytes: a thread keeps to its own elements
 // of the share and a warp to its own maximum, so that a pass has one barrier of the block and
-// one of the cluster; what a pass will need next (the children's entries, the draft row) is asked
-// for while the row is on its way.
+// one of the cluster; the children's entries are asked for before the row.  (Asking L2 for
+// the draft row or the noise ahead of their passes made 80 sequences 42 -> 56 us.)
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 
 struct SampleShared {
@@ -178,8 +178,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
             }
             __syncthreads();
             const int kids = s.n_child;
-            // their entries of the row and of their draft rows (one each, from thread i), and
-            // the first one's draft row, which a rejection reads, into L2
+            // their entries of the row and of their draft rows (one each, from thread i)
             float kid_x = 0.f, kid_q = 1.f;
             if (tid < kids) {
                 const int c = s.child[tid], t = s.tok[c], r = s.row[c];
@@ -188,10 +187,6 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
                 bool first = r < 0;
                 for (int h = 0; first && h < tid; ++h) first = s.row[s.child[h]] >= 0 || s.tok[s.child[h]] != t;
                 s.first[tid] = first;
-            }
-            if (kids > 0 && s.row[s.child[0]] >= 0) {
-                const float *q = q0 + (size_t)s.row[s.child[0]] * V;
-                for (int v = 32 * tid; v < n; v += 32 * kSampleThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + v));
             }
             load_row(cur, kids);
             // R at the children's tokens; a chosen token counts once, at its first child
@@ -297,21 +292,23 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
         if (none) load_row(cur, 0);   // nothing left: the node's own distribution
         const float *x = x0 + (size_t)cur * V, *noise = p.noise + (size_t)b * V + lo;
         unsigned long long best = 0;
-        auto consider = [&](int v, float noise_v) {
-            float r;
-            if (flat) {   // the first NaN, or the first of the largest
-                const float a = ld_input(x + v);
-                r = a != a ? 2.f : a == M ? 1.f : 0.f;
-            } else {
-                r = f * e[v] / noise_v;
-                if (!(r >= 0.f)) r = 0.f;
-            }
-            const unsigned long long key = (unsigned long long)__float_as_uint(r) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + v));
-            if (key > best) best = key;
+        // a thread's best so far; its elements come in ascending order, so the first of equals stays
+        float top = -1.f;
+        int at = 0;
+        auto consider = [&](int v, float r) {
+            if (r > top) top = r, at = v;
         };
         // a thread's own elements: the warp's factor is theirs
         const bool wide = VEC && (reinterpret_cast<uintptr_t>(noise) & 15) == 0;
-        for (int v0 = own0; v0 < n; v0 += AHEAD * STRIDE) {
+        if (flat)   // the first NaN, or the first of the largest
+            for (int v = own0; v < n; v += STRIDE)
+                for (int k = 0; k < STEP; ++k) {
+                    const float a = ld_input(x + v + k);
+                    consider(v + k, a != a ? 2.f : a == M ? 1.f : 0.f);
+                }
+        // a quotient to two units in the last place, equal for equal sides: an IEEE one took a
+        // tenth of a batch's time.  (One that is no number never wins: 0 does where nothing else.)
+        for (int v0 = own0; v0 < n && !flat; v0 += AHEAD * STRIDE) {
             float y[AHEAD * STEP];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
@@ -329,7 +326,11 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
             for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
                 for (int k = 0; k < STEP; ++k)
-                    if (v0 + i * STRIDE < n) consider(v0 + i * STRIDE + k, y[i * STEP + k]);
+                    if (v0 + i * STRIDE < n) consider(v0 + i * STRIDE + k, __fdividef(f * e[v0 + i * STRIDE + k], y[i * STEP + k]));
+        }
+        if (own0 < n) {
+            if (top < 0.f) top = 0.f, at = own0;
+            best = (unsigned long long)__float_as_uint(top) << 32 | (0xFFFFFFFFu - (uint32_t)(lo + at));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
