@@ -68,13 +68,62 @@ struct Kv4Wide {
     static_assert(T_O + OB * 2 * TP <= TMEM_COLS, "tensor memory budget");
 };
 
+// This CTA's units one by one, as SegIter hands them out: whole ones round-robin, or (SPLIT) those
+// of its range of tiles.  The sequence of a unit comes by adding where SegIter divides: every
+// role does this between two units, and short contexts feel it (2000 cycles a unit).
+template <bool SPLIT>
+struct UnitIter {
+    int u, j0, left;
+    int r, b;                         // u = x d + r, d units a (layer, sequence); b = x % B
+    int d, step_r, step_b;
+    PPD_DEV UnitIter(const AttnParams &p, const WorkRange &w)
+    {
+        u = SPLIT ? w.u_first : (int)blockIdx.x;
+        j0 = SPLIT ? w.j_first : 0;
+        left = SPLIT ? w.n_tiles : 0;
+        const int step = SPLIT ? 1 : (int)gridDim.x;
+        d = p.H * p.n_qb;
+        r = u % d;
+        b = u / d % p.B;
+        step_r = step % d;
+        step_b = step / d % p.B;
+    }
+    PPD_DEV bool next(const AttnParams &p, Seg &s)
+    {
+        if ((SPLIT && left <= 0) || u >= p.n_units) return false;
+        s.u = u;
+        s.ui.lbh = p.n_qb == 1 ? u : u / p.n_qb;
+        s.ui.qb = u - s.ui.lbh * p.n_qb;
+        s.ui.b = b;
+        s.ui.P_raw = ld_input(p.prefix_len + b);
+        s.ui.P = min(max(s.ui.P_raw, 0), p.S_max);
+        s.ui.n_pref = (s.ui.P + 127) >> 7;
+        s.ui.n_tiles = s.ui.n_pref + p.n_tt;
+        s.j0 = j0;
+        s.j1 = SPLIT ? min(s.ui.n_tiles, j0 + left) : s.ui.n_tiles;
+        if (s.j1 <= s.j0) {   // cannot happen with a consistent plan; never loop on it
+            left = 0;
+            u = p.n_units;
+            return false;
+        }
+        left -= s.j1 - s.j0;
+        j0 = 0;
+        u += SPLIT ? 1 : (int)gridDim.x;
+        r += step_r;
+        b += step_b;
+        if (r >= d) r -= d, ++b;
+        if (b >= p.B) b -= p.B;
+        return true;
+    }
+};
+
 // The tiles of a CTA's range one by one.
 template <bool SPLIT>
 struct TileWalk {
-    SegIter<SPLIT> it;
+    UnitIter<SPLIT> it;
     Seg sg;
     int j = 0, end = 0;
-    PPD_DEV explicit TileWalk(const WorkRange &w) : it(w) {}
+    PPD_DEV TileWalk(const AttnParams &p, const WorkRange &w) : it(p, w) {}
     PPD_DEV bool next(const AttnParams &p)   // sg and j then name a tile
     {
         if (++j >= end) {
@@ -149,7 +198,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         const uint32_t k_mem = tmem_base + ((uint32_t)(wq * 32) << 16) + Lay::T_K;
         const uint32_t v_row = smem_addr(smem) + Lay::OFF_V + (uint32_t)(t >> 3) * 1024u + (uint32_t)(t & 7) * 128u;
         constexpr int UPR = Lay::RB / 16;        // 16-byte pieces of a row's codes, 32 channels each
-        TileWalk<SPLIT> ahead(wr), at(wr);
+        TileWalk<SPLIT> ahead(p, wr), at(p, wr);
         bool more = true;
         // piece i of this lane: row i * 32 / UPR + lane / UPR of the warp's 32, 512 bytes on from
         // piece i - 1 on both sides.  A thread reads one row: eight rows' equal pieces lie in
@@ -282,7 +331,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         reg_dec<Lay::OTHER_REGS>();
         status_warp(p, lane);
         int k = 0;
-        SegIter<SPLIT> it(wr);
+        UnitIter<SPLIT> it(p, wr);
         for (Seg sg; it.next(p, sg); ++k) {
             const int qs = k & 1;
             mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
@@ -354,7 +403,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         int g = 0, k = 0;
         bool prev_first = false;
         uint32_t prev_to = 0;
-        SegIter<SPLIT> it(wr);
+        UnitIter<SPLIT> it(p, wr);
         for (Seg sg;; ++k) {
             const int n = warp_uniform(it.next(p, sg) ? sg.j1 - sg.j0 : 0);
             if (n == 0) break;
@@ -565,7 +614,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         };
 
         int k = 0;
-        SegIter<SPLIT> it(wr);
+        UnitIter<SPLIT> it(p, wr);
         for (Seg sg; it.next(p, sg); ++k) {
             const UnitInfo &ui = sg.ui;
             const int u = sg.u;
