@@ -1157,10 +1157,11 @@ ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, co
     if (!aligned(logits, 4) || !aligned(draft_probs, 4) || !aligned(u, 4) || !aligned(noise, 4) || !aligned(accept_prob, 4))
         return PPD_ERR_INVALID_ARG;
     // as many CTAs a sequence as the GPU holds for all of them at once (three an SM, by threads and
-    // by a share of up to 50 KB)
+    // by a share of up to 50 KB), and none for less than four elements a thread: a small
+    // vocabulary's passes are their barriers (80 sequences of 1024 tokens: 24 us with four CTAs each)
     int cluster = ppd::kMaxCluster;
     auto share = [&](int c) { return ((V + c - 1) / c + 3) & ~3; };
-    while (cluster > 1 && (long long)B * cluster > 3ll * num_sms() && share(cluster / 2) <= 12800) cluster /= 2;
+    while (cluster > 1 && (((long long)B * cluster > 3ll * num_sms() && share(cluster / 2) <= 12800) || share(cluster) < 2048)) cluster /= 2;
     const int chunk = share(cluster);
     if (chunk > ppd::kSampleMaxChunk) return PPD_ERR_UNSUPPORTED;
     ppd::SampleParams p{logits, cand_tokens, parent, prefix_len, draft_probs, draft_row, u, noise, accept_len, path,

@@ -406,23 +406,23 @@ constexpr int kMoveThreads = 256, kMoveDeep = 4;
 // their way meanwhile.  In place a block takes its columns of the whole slice alone, in order:
 // the rows of a step lie at or above their places, and so do those of every later step, so
 // what a step overwrites has been read.
-template <int BYTES>
-PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, uint32_t u, int c0, int c1, int i0, int i1)
+template <int BYTES, int THREADS>   // 32: a warp, else a block
+PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, uint32_t u, int c0, int c1, int i0, int i1, int tid)
 {
     using T = typename MoveUnit<BYTES>::T;
     const int per_row = pl.row_bytes / BYTES, w = c1 - c0;   // this block's units of a row
     const T *src = reinterpret_cast<const T *>(static_cast<const uint8_t *>(pl.src) + (size_t)u * p.S_max * pl.row_bytes) + c0;
     T *dst = reinterpret_cast<T *>(static_cast<uint8_t *>(pl.dst) + (size_t)u * p.S_out * pl.row_bytes) + c0;
     const bool in_place = pl.src == pl.dst;
-    const int rows = kMoveThreads * kMoveDeep / w;           // of a step
+    const int rows = THREADS * kMoveDeep / w;           // of a step
     int row[kMoveDeep], col[kMoveDeep], from[kMoveDeep];
 #pragma unroll
     for (int x = 0; x < kMoveDeep; ++x) {
-        const int unit = x * kMoveThreads + (int)threadIdx.x;
+        const int unit = x * THREADS + tid;
         row[x] = unit / w;
         col[x] = unit - row[x] * w;
         if (row[x] >= rows) row[x] = i1;   // none
-        from[x] = i0 + row[x] < i1 ? ld_input(kept + i0 + row[x]) : -1;
+        from[x] = i0 + row[x] < i1 ? kept[i0 + row[x]] : -1;
     }
     for (int r0 = i0; r0 < i1; r0 += rows) {
         T v[kMoveDeep];
@@ -433,11 +433,26 @@ PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t 
             if (go[x]) v[x] = src[(size_t)from[x] * per_row + col[x]];
         }
 #pragma unroll
-        for (int x = 0; x < kMoveDeep; ++x) from[x] = r0 + rows + row[x] < i1 ? ld_input(kept + r0 + rows + row[x]) : -1;
-        if (in_place) __syncthreads();
+        for (int x = 0; x < kMoveDeep; ++x) from[x] = r0 + rows + row[x] < i1 ? kept[r0 + rows + row[x]] : -1;
+        if (in_place) {
+            if (THREADS == 32) __syncwarp();
+            else __syncthreads();
+        }
 #pragma unroll
         for (int x = 0; x < kMoveDeep; ++x)
             if (go[x]) dst[(size_t)(r0 + row[x]) * per_row + col[x]] = v[x];
+    }
+}
+
+template <int THREADS>
+PPD_DEV void move_plane(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, uint32_t u, int c0, int c1, int i0, int i1, int tid)
+{
+    switch (pl.unit) {
+    case 16: move_rows<16, THREADS>(p, pl, kept, u, c0, c1, i0, i1, tid); break;
+    case 8: move_rows<8, THREADS>(p, pl, kept, u, c0, c1, i0, i1, tid); break;
+    case 4: move_rows<4, THREADS>(p, pl, kept, u, c0, c1, i0, i1, tid); break;
+    case 2: move_rows<2, THREADS>(p, pl, kept, u, c0, c1, i0, i1, tid); break;
+    default: move_rows<1, THREADS>(p, pl, kept, u, c0, c1, i0, i1, tid); break;
     }
 }
 
@@ -466,17 +481,78 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(const KvEvictPara
         i0 = (int)((long long)p.budget * part / pl.parts);
         i1 = min(n, (int)((long long)p.budget * (part + 1) / pl.parts));
     }
-    switch (pl.unit) {
-    case 16: move_rows<16>(p, pl, kept, u, c0, c1, i0, i1); break;
-    case 8: move_rows<8>(p, pl, kept, u, c0, c1, i0, i1); break;
-    case 4: move_rows<4>(p, pl, kept, u, c0, c1, i0, i1); break;
-    case 2: move_rows<2>(p, pl, kept, u, c0, c1, i0, i1); break;
-    default: move_rows<1>(p, pl, kept, u, c0, c1, i0, i1); break;
+    move_plane<kMoveThreads>(p, pl, kept, u, c0, c1, i0, i1, (int)threadIdx.x);
+}
+
+// Short caches: a warp a slice.  A lane holds four rows' ranks and counts, for each, the rows that
+// come before it in order of weight; then the warp moves its planes' rows.  (2,700 slices of
+// 31 rows: a block each and the moves in a second grid took 94 us.)
+constexpr int kShortRows = 128;
+__global__ void __launch_bounds__(128) kv_evict_short_kernel(const KvEvictParams p)
+{
+    __shared__ int32_t kept_s[4][kShortRows];
+    pdl_release();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t u = blockIdx.x * 4 + warp;
+    if (u >= p.slices) return;
+    const int b = (int)(u / (uint32_t)p.H % (uint32_t)p.B);
+    const int len = ld_input(p.length + b);
+    const bool bad = len < 0 || len > p.S_max;
+    if (u / p.H < p.B && u % p.H == 0 && lane == 0) {
+        p.dev_status[b] = bad ? kErrCapacity : kOk;
+        p.new_len[b] = bad ? len : min(len, p.budget);
+    }
+    const float *w = p.weight + (size_t)u * p.S_max;
+    int32_t *kept = p.kept + (size_t)u * p.budget;
+    constexpr int PER = kShortRows / 32;
+    uint32_t r[PER];
+    int before[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int j = lane + 32 * k;
+        const bool in = !bad && j < len;
+        r[k] = !in ? 0u : j < p.sink || j >= len - p.recent ? 0xFFFFFFFFu : weight_rank(ld_input(w + j));
+        before[k] = in ? 0 : kShortRows;   // rows past the length are not kept
+    }
+    if (!bad && len > p.budget) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            for (int i = 0; i < min(32, len - 32 * k); ++i) {
+                const uint32_t x = __shfl_sync(0xffffffffu, r[k], i);
+#pragma unroll
+                for (int m = 0; m < PER; ++m) before[m] += x > r[m] || (x == r[m] && 32 * k + i < lane + 32 * m);
+            }
+    }
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const bool take = before[k] < p.budget && lane + 32 * k < len;
+        const uint32_t all = __ballot_sync(0xffffffffu, take);
+        if (take) {
+            const int i = n + __popc(all & ((1u << lane) - 1u));
+            kept_s[warp][i] = lane + 32 * k;
+            kept[i] = lane + 32 * k;
+        }
+        n += __popc(all);
+    }
+    for (int i = n + lane; i < p.budget; i += 32) kept[i] = -1;
+    if (bad) return;
+    __syncwarp();
+    for (int x = 0; x < p.planes; ++x) {
+        const KvPlane &pl = p.plane[x];
+        if (pl.src == pl.dst && len <= p.budget) continue;   // every row is in its place
+        // a row of up to 1024 bytes in pieces that a step holds
+        const int per_row = pl.row_bytes / pl.unit, most = 32 * kMoveDeep;
+        for (int c = 0; c < per_row; c += most) move_plane<32>(p, pl, kept_s[warp], u, c, min(per_row, c + most), 0, n, lane);
+        __syncwarp();
     }
 }
 
 cudaError_t launch_kv_evict(const KvEvictParams &p, cudaStream_t stream)
 {
+    if (p.S_max <= kShortRows)
+        return launch_chained(kv_evict_short_kernel, dim3((unsigned)((p.slices + 3) / 4)), dim3(128), dim3(1), stream, p);
     // ranks in shared memory up to 40,000 rows (160 KB): read again instead, longer caches take
     // twice the time a row
     constexpr uint32_t most = 40000;

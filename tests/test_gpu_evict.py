@@ -186,3 +186,34 @@ def test_evict_of_long_caches(cuda_device, ties):
         want = torch.sort(torch.sort(key, dim=-1, descending=True, stable=True).indices[..., :kept.shape[3]], -1).values
         assert torch.equal(kept.long(), want)
         assert torch.equal(w[..., :kept.shape[3]], torch.gather(host, 3, want))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("S,lens,budget,sink,recent", [(128, [128, 0, 77, 33], 31, 1, 2), (31, [31, 30, 10, 1], 10, 0, 0), (127, [127, 126, 2, 96], 96, 33, 40)])
+def test_evict_of_short_caches(cuda_device, in_place, S, lens, budget, sink, recent):
+    """Many heads of a few rows, more than one of them ending anywhere in a warp's rows; rows of 1 to
+    1024 bytes."""
+    from paper_2405_18628_gb300 import ppd
+    dev, L, H = cuda_device, 3, 5
+    g = torch.Generator(device=dev)
+    g.manual_seed(S)
+    weight = (torch.rand(L, 4, H, S, device=dev, generator=g) * 6).floor()
+    weight[0, 0, 0, 3] = float("nan")
+    planes = [torch.randint(0, 256, (L, 4, H, S, w), dtype=torch.uint8, device=dev, generator=g) for w in (1, 64, 1024, 1000, 38)]
+    host = [p.clone() for p in planes] + [weight.clone()]
+    outs = planes if in_place else [torch.zeros(L, 4, H, budget, p.shape[4], dtype=torch.uint8, device=dev) for p in planes]
+    out_w = weight if in_place else torch.zeros(L, 4, H, budget, device=dev)
+    kept = torch.empty(L, 4, H, budget, dtype=torch.int32, device=dev)
+    new_len, status = (torch.empty(4, dtype=torch.int32, device=dev) for _ in range(2))
+    ppd.ppd_kv_evict(weight, planes, _i32(lens, dev), budget, sink, recent, kept, new_len, status, out_planes=None if in_place else outs,
+                     out_weight=None if in_place else out_w)
+    assert new_len.tolist() == [min(x, budget) for x in lens] and status.tolist() == [0] * 4
+    for l in range(L):
+        for b in range(4):
+            for h in range(H):
+                want = O.evict(host[-1][l, b, h].tolist(), lens[b], budget, sink, recent)
+                assert kept[l, b, h].tolist() == want + [-1] * (budget - len(want))
+                at = torch.tensor(want, dtype=torch.long, device=dev)
+                for src, dst in zip(host, outs + [out_w]):
+                    assert torch.equal(dst[l, b, h, :len(want)].nan_to_num(9.0) if dst.is_floating_point() else dst[l, b, h, :len(want)],
+                                       src[l, b, h][at].nan_to_num(9.0) if src.is_floating_point() else src[l, b, h][at])
