@@ -31,7 +31,7 @@ struct Kv4Wide {
     static constexpr int SW = 8, KW = SW, VW = KW + 4, QW = VW + 4, IW = QW + 1;
     static constexpr int THREADS = (QW + 4) * 32;
     // registers a thread: 20 warps start with 96 and share the same total out anew
-    static constexpr int SOFTMAX_REGS = 144, CONVERT_REGS = 72, OTHER_REGS = 48;
+    static constexpr int SOFTMAX_REGS = 168, CONVERT_REGS = 56, OTHER_REGS = 32;
     static_assert(2 * SOFTMAX_REGS + 2 * CONVERT_REGS + OTHER_REGS <= 5 * 96, "register shares");
     static constexpr int STAGES = 3;              // tiles of codes in a converting warp's ring
     static constexpr int QS = 2, PS = 2, VS = 2, OB = 2;
@@ -263,10 +263,6 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 cp_async_wait<Lay::STAGES - 1>();
                 __syncwarp();
                 const uint32_t src = ring + stage * Lay::STAGE;
-                uint4 w[UPR];
-#pragma unroll
-                for (int c = 0; c < UPR; ++c)
-                    w[c] = ld_shared_u128(src + (uint32_t)(lane * UPR + (UPR == 4 ? c ^ ((lane >> 1) & 3) : c ^ ((lane >> 2) & 1))) * 16);
                 // (D = 64: a word of scales holds an even and an odd row's)
                 const uint32_t odd = D == 64 ? (uint32_t)(((size_t)at.sg.ui.lbh * p.S_max + (size_t)at.j * Lay::KT + t) & 1) * 16u : 0u;
                 const uint32_t sc = ld_shared_u32(src + Lay::CODES + lane * 4) >> odd;
@@ -274,8 +270,9 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 tc_fence_after();
 #pragma unroll
                 for (int c = 0; c < UPR; ++c) {
+                    const uint4 w = ld_shared_u128(src + (uint32_t)(lane * UPR + (UPR == 4 ? c ^ ((lane >> 1) & 3) : c ^ ((lane >> 2) & 1))) * 16);
                     const Kv4Scale k = kv4_scales(((sc >> (8 * c)) & 0xFFu) * 0x10001u);
-                    const uint32_t u[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
                     uint32_t r[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
@@ -292,21 +289,19 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 if (g >= 2) mbar_wait(free_bar, ((g >> 1) - 1) & 1, abort_flag);
                 tc_fence_after();
                 if (!x.f32) {
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t r[16];
 #pragma unroll
-                    for (int c = 0; c < D / 32; c += 2) {   // 64 channels' loads in flight
-                        uint32_t r[2][16];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             const uint4 v = in ? ld_input(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(tree_rows) + row + 32 * c) + i)
                                                : make_uint4(0, 0, 0, 0);
-                            uint32_t *to = &r[i >> 2][4 * (i & 3)];
-                            to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+                            r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
                         }
-                        store(c, r[0]);
-                        store(c + 1, r[1]);
+                        store(c, r);
                     }
                 } else {
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t r[16];
 #pragma unroll
@@ -460,6 +455,16 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         float *linv = reinterpret_cast<float *>(smem + Lay::OFF_L) + q0;          // [OB][TP]
         float *pmx = reinterpret_cast<float *>(smem + Lay::OFF_MX) + q0;          // [OB][TP]
 
+        // the columns' entries of nm, in registers: read by every thread for every tile they were a
+        // sixth of shared memory's traffic (a 16-byte load takes four wavefronts, broadcast or not)
+        Probs nmr;
+        auto load_nm = [&]() {
+#pragma unroll
+            for (int h = 0; h < NC; h += 4) {
+                const ulonglong2 x2 = *reinterpret_cast<const ulonglong2 *>(nm + h);
+                nmr[h / 2] = x2.x, nmr[h / 2 + 1] = x2.y;
+            }
+        };
         uint64_t lacc[NC / 2];   // this key row's share of every owned query's row sum, in pairs
 #pragma unroll
         for (int c = 0; c < NC / 2; ++c) lacc[c] = 0ull;
@@ -486,14 +491,11 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             const uint64_t sl2x2 = pack2(sl2, sl2);
 #pragma unroll
             for (int h = 0; h < NC; h += 8) {
-                const ulonglong2 na = *reinterpret_cast<const ulonglong2 *>(nm + h);
-                const ulonglong2 nb = *reinterpret_cast<const ulonglong2 *>(nm + h + 4);
-                const uint64_t nmv[4] = {na.x, na.y, nb.x, nb.y};
                 uint32_t hw[4], lw[4];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     float d0, d1;
-                    unpack2(fma2(pack2(__uint_as_float(r[h + e]), __uint_as_float(r[h + e + 1])), sl2x2, nmv[e >> 1]),
+                    unpack2(fma2(pack2(__uint_as_float(r[h + e]), __uint_as_float(r[h + e + 1])), sl2x2, nmr[(h + e) >> 1]),
                             d0, d1);
                     if (BITS) {
                         d0 = ((bits >> (h + e)) & 1u) ? d0 : -INFINITY;
@@ -525,9 +527,12 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         // A score jumped past its column's maximum by about 2^16: every column's maximum
         // over the 128 key rows is a warp max (redux) combined across the four warps; the row
         // sums, and O unless this is the unit's first tile, are rescaled; the probabilities are
-        // computed again.
-        auto exact_tile = [&](auto bits_c, const Cols &r, uint32_t bits, uint32_t pbuf, bool first, Probs &pr) {
+        // computed again, from the scores, which the buffer holds until then.
+        auto exact_tile = [&](auto bits_c, uint32_t t_s, uint32_t bits, uint32_t pbuf, bool first, Probs &pr) {
             constexpr bool BITS = decltype(bits_c)::value != 0;
+            Cols r;
+            load_cols(t_s, r);
+            tmem_wait_ld(r);
 #pragma unroll
             for (int e = 0; e < NC; ++e) {
                 const bool vis = !BITS || ((bits >> e) & 1u) != 0;
@@ -572,6 +577,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 }
             }
             if (!first) tmem_wait_st();
+            load_nm();
             (void)emit(bits_c, r, bits, pbuf, pr);
         };
 
@@ -666,6 +672,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                         for (int e = 0; e < NC; ++e) nm[e] = all_see ? kKv4Shift - __uint_as_float(r[e]) * sl2 : 1e30f;
                     }
                     named_bar_sync(1 + wg, 128);
+                    load_nm();
                 }
                 // Done optimistically with the current running maxima; when a score
                 // exceeds its maximum by more than 2^16, again by the exact path.
@@ -673,10 +680,10 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 Probs pr;
                 if (!masked) {
                     const float sum = emit(kind_t<0>{}, r, bits, pbuf, pr);
-                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<0>{}, r, bits, pbuf, first, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<0>{}, t_s, bits, pbuf, first, pr);
                 } else {
                     const float sum = emit(kind_t<1>{}, r, bits, pbuf, pr);
-                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<1>{}, r, bits, pbuf, first, pr);
+                    if (named_bar_or(1 + wg, 128, !(sum <= kTooLarge))) exact_tile(kind_t<1>{}, t_s, bits, pbuf, first, pr);
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
