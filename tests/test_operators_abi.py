@@ -72,6 +72,17 @@ def test_evict(lib):
     assert lib.ppd_kv_evict(F, F, None, None, None, 1, F, 1, 1, 1, 10, 10, 4, 1, 1, F, F, F, S) == INVALID
 
 
+def test_evict_over_its_own_lengths(lib):
+    """Every block reads the lengths: an output over them would race."""
+    at = [ctypes.c_void_p(0x1000000 * (i + 1)) for i in range(5)]
+    weight, length, kept, new_len, status = at
+    for over in (dict(new_len=length), dict(status=length), dict(kept=length), dict(kept=ctypes.c_void_p(length.value - 8)),
+                 dict(new_len=ctypes.c_void_p(length.value + 4))):
+        a = dict(kept=kept, new_len=new_len, status=status) | over
+        assert lib.ppd_kv_evict(weight, weight, None, None, None, 0, length, 1, 2, 1, 10, 10, 4, 1, 1, a["kept"], a["new_len"], a["status"],
+                                S) == INVALID, over
+
+
 def test_sample(lib):
     #       logits cand parent prefix probs row  u  noise B T V nd S temp  outputs ...
     args = [F] * 4 + [None, None] + [F] * 2 + [1, 4, 100, 0, 10, 0.7] + [F] * 7
