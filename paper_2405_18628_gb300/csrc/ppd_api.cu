@@ -935,8 +935,9 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
 
 // Parts that the keys of a slice are shared out to, blocks of which `per_sm` fit an SM: the number
 // with the shortest time of all waves of blocks, a part counting as its chunks of 32 keys and
-// eight more for a block's start and end (8 us for parts of 66 chunks that take 60 in all).  A
-// part has at least eight chunks, two a warp.
+// eight more for a block's start and end (960 slices of 1024 keys: 47 us, and 58 us with none
+// for them; 32 slices of 10,000 keys: 22 us, and 82 us as whole slices).  A part has at least
+// eight chunks, two a warp.
 static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 {
     const long long slots = (long long)per_sm * num_sms();
@@ -951,9 +952,13 @@ static int kv4_splits(long long slices, int T, int S_max, int per_sm)
     return splits;
 }
 
-// How an attention call runs: up to 16 query rows of a slice in registers, its keys in
-// `splits` parts; more on the tensor cores in blocks of tp rows, all key tiles shared out
-// (`share`; a batch that the sharing's plan holds).
+// How an attention call runs: few query rows of a slice in registers, its keys in `splits`
+// parts; more on the tensor cores in blocks of tp rows, all key tiles shared out (`share`; a batch
+// that the sharing's plan holds).  Registers / tensor cores, 2048 keys, 64 x 32 slices and 32:
+//   8 rows, D = 128    178 / 240 us    14 / 15 us
+//   12 rows            235 / 240 us    21 / 16 us   (two blocks of eight; shorter contexts alike)
+//   16 rows, D = 64     79 /  97 us    (64 x 16 slices)
+// Blocks of 32 rows against 64 where 32 hold them all: 129 and 146 us (32 x 32 slices).
 struct Kv4Ws {
     size_t o, ml, rec, total;
     int row_blocks, splits, tp, share;
@@ -963,11 +968,12 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
     Kv4Ws w{};
     const long long slices = (long long)L * B * H, rows = (long long)G * T;
     w.splits = 1;
-    if (rows > 16) {
+    if (rows > (D == 64 ? 16 : 8)) {
         w.tp = rows <= 32 ? 32 : 64;
         w.row_blocks = (int)((rows + w.tp - 1) / w.tp);
         // whole units where sharing their tiles out would save less than it costs (about six tiles'
-        // time: the merge grid and the parts' way through memory)
+        // time: the merge grid and the parts' way through memory).  Whole / shared, 64 tokens: 23 / 20 us
+        // (8 slices of 2048 keys), 29 / 40 us (256 of 1024), 149 / 163 us (1024 of 2048)
         const long long units = slices * w.row_blocks, t_u = (S_max + 127) / 128 + (T + 127) / 128, sms = split_grid();
         w.share = B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + 6 < (units + sms - 1) / sms * t_u;
         if (w.share) {
@@ -1092,6 +1098,11 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
         n_recent > budget - n_sink)
         return PPD_ERR_INVALID_ARG;
     if (!aligned(weight, 4) || !aligned(out_weight, 4) || slices * S_max * 1024 > 9.0e15 || slices * S_out * 1024 > 9.0e15)
+        return PPD_ERR_INVALID_ARG;
+    // every block reads the lengths: none may be written meanwhile
+    const size_t nb = (size_t)B * 4;
+    if (overlaps(new_len, nb, length, nb) || overlaps(dev_status, nb, length, nb) ||
+        overlaps(kept, (size_t)slices * budget * 4, length, nb))
         return PPD_ERR_INVALID_ARG;
     ppd::KvEvictParams p{};
     p.weight = weight;

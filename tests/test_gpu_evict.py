@@ -217,3 +217,39 @@ def test_evict_of_short_caches(cuda_device, in_place, S, lens, budget, sink, rec
                 for src, dst in zip(host, outs + [out_w]):
                     assert torch.equal(dst[l, b, h, :len(want)].nan_to_num(9.0) if dst.is_floating_point() else dst[l, b, h, :len(want)],
                                        src[l, b, h][at].nan_to_num(9.0) if src.is_floating_point() else src[l, b, h][at])
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("S,budget,sink,recent", [(1, 1, 0, 0), (31, 10, 2, 3), (64, 63, 0, 0), (100, 40, 0, 40), (128, 31, 1, 2)])
+def test_evict_of_many_short_caches(cuda_device, in_place, S, budget, sink, recent):
+    """Slices by the hundred, of every length up to the capacity and one outside it."""
+    from paper_2405_18628_gb300 import ppd
+    dev, L, B, H = cuda_device, 2, 33, 9
+    g = torch.Generator(device=dev)
+    g.manual_seed(S)
+    lens = [int(x) for x in np.linspace(0, S, B - 1)] + [S + 1]
+    weight = (torch.rand(L, B, H, S, device=dev, generator=g) * 9).floor()
+    planes = [torch.randint(0, 256, (L, B, H, S, w), dtype=torch.uint8, device=dev, generator=g) for w in (64, 4, 1024, 7)]
+    host = [p.clone() for p in planes] + [weight.clone()]
+    outs = planes if in_place else [torch.zeros(L, B, H, budget, p.shape[4], dtype=torch.uint8, device=dev) for p in planes]
+    out_w = weight if in_place else torch.zeros(L, B, H, budget, device=dev)
+    before = [x.clone() for x in outs + [out_w]]
+    kept = torch.full((L, B, H, budget), 77, dtype=torch.int32, device=dev)
+    new_len, status = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
+    ppd.ppd_kv_evict(weight, planes, _i32(lens, dev), budget, sink, recent, kept, new_len, status, out_planes=None if in_place else outs,
+                     out_weight=None if in_place else out_w)
+    assert new_len.tolist() == [min(x, budget) for x in lens[:-1]] + [S + 1]
+    assert status.tolist() == [0] * (B - 1) + [status[-1].item()] and status[-1] != 0
+    ranks, got, b = host[-1].tolist(), kept.tolist(), B - 1
+    for l in range(L):
+        for h in range(H):
+            assert got[l][b][h] == [-1] * budget
+            for b_ in range(B - 1):
+                want = O.evict(ranks[l][b_][h], lens[b_], budget, sink, recent)
+                assert got[l][b_][h] == want + [-1] * (budget - len(want))
+    at = kept.long().clamp(min=0)
+    for src, dst, old in zip(host, outs + [out_w], before):
+        rows = torch.take_along_dim(src, at.reshape(*at.shape, *[1] * (src.dim() - 4)), 3)
+        live = (kept >= 0).reshape(*kept.shape, *[1] * (src.dim() - 4))
+        assert torch.equal(dst[..., :budget, :] if src.dim() == 5 else dst[..., :budget],
+                           torch.where(live, rows, old[..., :budget, :] if src.dim() == 5 else old[..., :budget]))
