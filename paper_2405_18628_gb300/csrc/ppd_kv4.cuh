@@ -34,6 +34,7 @@ PPD_DEV float kv4_scale(uint32_t b) { return __uint_as_float((b + 856u) << 20); 
 // word of eight codes takes one shift instead of three.  What the unit leaves over is a power
 // of two: the softmax scale takes up K's, the outputs V's.
 constexpr float kKv4Unit = 1.f / (1 << 20), kKv4Shift = 20.f;
+constexpr int kKv4UnitLog2 = -20;
 struct Kv4Scale {
     uint32_t s, s16, off;   // of a pair of codes, each
 };

@@ -26,10 +26,9 @@ struct Kv4Wide {
     static constexpr int KT = 128;                // keys per tile
     static constexpr int DCH = D / 64;
     static constexpr int NWG = 2, NC = TP / NWG;  // softmax warpgroups, columns of each
-    // softmax warps, four warps converting K, four converting V, then the Q warp, the issuer and
-    // two that fill up the warpgroup
-    static constexpr int SW = 8, KW = SW, VW = KW + 4, QW = VW + 4, IW = QW + 1;
-    static constexpr int THREADS = (QW + 4) * 32;
+    // softmax warps, four warps converting K, four converting V, then three that bring Q and the issuer
+    static constexpr int SW = 8, KW = SW, VW = KW + 4, QW = VW + 4, NQ = 3, IW = QW + NQ;
+    static constexpr int THREADS = (IW + 1) * 32;
     // registers a thread: 20 warps start with 96 and share the same total out anew
     static constexpr int SOFTMAX_REGS = 168, CONVERT_REGS = 56, OTHER_REGS = 32;
     static_assert(2 * SOFTMAX_REGS + 2 * CONVERT_REGS + OTHER_REGS <= 5 * 96, "register shares");
@@ -59,7 +58,8 @@ struct Kv4Wide {
     static constexpr uint32_t OFF_MX = OFF_L + OB * TP * 4;           // [OB][TP] references of a part
     static constexpr uint32_t OFF_RED = OFF_MX + OB * TP * 4;         // [NWG][4][NC]
     static constexpr uint32_t OFF_RANGE = (OFF_RED + NWG * 4 * NC * 4 + 15) & ~15u;
-    static constexpr uint32_t SMEM_BYTES = OFF_RANGE + sizeof(WorkRange);
+    static constexpr uint32_t OFF_PARENT = (OFF_RANGE + sizeof(WorkRange) + 15) & ~15u;   // [NWG][kMaxTree]
+    static constexpr uint32_t SMEM_BYTES = OFF_PARENT + NWG * kMaxTree * 4;
     // tensor memory: K0 | K1 | S0 | S1 | O0 (hi | lo) | O1
     static constexpr uint32_t T_K = 0, T_S = D, T_O = T_S + 2 * TP, TMEM_COLS = 512;
 
@@ -158,7 +158,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Lay::NBAR; ++i) {
-            uint32_t count = 1;
+            uint32_t count = i < Lay::B_QEMPTY ? Lay::NQ : 1;
             if (i >= Lay::B_KFULL && i < Lay::B_SFULL) count = 4;   // K and V tiles
             if (i >= Lay::B_PFULL && i < Lay::B_PFULL + 2) count = Lay::SW;
             mbar_init(bars + i, count);
@@ -303,9 +303,16 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 } else {
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
+                        const float4 *src = reinterpret_cast<const float4 *>(tree_rows) + (row >> 2) + 8 * c;
                         uint32_t r[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) r[i] = in ? ld_pair(tree_rows, row + 32 * c + 2 * i, true) : 0u;
+                        for (int h = 0; h < 8; h += 4) {
+                            float4 v[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = in ? ld_input(src + h + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) r[2 * (h + i)] = bf16x2(v[i].x, v[i].y), r[2 * (h + i) + 1] = bf16x2(v[i].z, v[i].w);
+                        }
                         store(c, r);
                     }
                 }
@@ -321,10 +328,11 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             stage = (stage + 1) % Lay::STAGES;
         }
         cp_async_wait<0>();
-    } else if (warp == Lay::QW) {
-        // ------------------------------------------------------------ Q warp, statuses
+    } else if (warp < Lay::IW && warp >= Lay::QW) {
+        // ------------------------------------------------------------ Q warps, statuses
         reg_dec<Lay::OTHER_REGS>();
-        status_warp(p, lane);
+        if (warp == Lay::QW) status_warp(p, lane);
+        const int i0 = (warp - Lay::QW) * 32 + lane;
         int k = 0;
         UnitIter<SPLIT> it(p, wr);
         for (Seg sg; it.next(p, sg); ++k) {
@@ -340,21 +348,30 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             };
             if (!x.f32) {   // every chunk on its way at once
                 const uint8_t *src = reinterpret_cast<const uint8_t *>(x.q) + row0 * D * 2;
-#pragma unroll 8
-                for (int i = lane; i < TP * CPR; i += 32) {
+#pragma unroll 4
+                for (int i = i0; i < TP * CPR; i += Lay::NQ * 32) {
                     const bool in = r0 + i / CPR < R;
                     cp_async16(chunk_at(i / CPR, i % CPR), in ? src + (size_t)i * 16 : reinterpret_cast<const uint8_t *>(x.q), in ? 16u : 0u);
                 }
                 cp_async_commit();
                 cp_async_wait<0>();
-            } else {
-#pragma unroll 4
-                for (int i = lane; i < TP * CPR; i += 32) {
-                    const int row = i / CPR, c = i % CPR;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    const size_t a = (row0 + row) * D + 8 * c;
-                    if (r0 + row < R) v = make_uint4(ld_pair(x.q, a, true), ld_pair(x.q, a + 2, true), ld_pair(x.q, a + 4, true), ld_pair(x.q, a + 6, true));
-                    st_shared_v4(chunk_at(row, c), v.x, v.y, v.z, v.w);
+            } else {   // two chunks' loads in flight
+                const float4 *src = reinterpret_cast<const float4 *>(x.q) + row0 * (D / 4);
+#pragma unroll 1
+                for (int i = i0; i < TP * CPR; i += 2 * Lay::NQ * 32) {
+                    float4 v[4];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int c = i + (h >> 1) * Lay::NQ * 32;
+                        v[h] = c < TP * CPR && r0 + c / CPR < R ? ld_input(src + 2 * c + (h & 1)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 4; h += 2) {
+                        const int c = i + (h >> 1) * Lay::NQ * 32;
+                        if (c < TP * CPR)
+                            st_shared_v4(chunk_at(c / CPR, c % CPR), bf16x2(v[h].x, v[h].y), bf16x2(v[h].z, v[h].w),
+                                         bf16x2(v[h + 1].x, v[h + 1].y), bf16x2(v[h + 1].z, v[h + 1].w));
+                    }
                 }
             }
             fence_proxy_async_smem();
@@ -433,8 +450,6 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         if (elect_one()) umma_commit(bars + Lay::B_DRAIN);
         __syncwarp();
         mbar_wait_drain(bars + Lay::B_DRAIN, 0);
-    } else if (warp > Lay::IW) {
-        reg_dec<Lay::OTHER_REGS>();
     } else {
         // ------------------------------------------------------------ softmax warpgroups
         reg_inc<Lay::SOFTMAX_REGS>();
@@ -454,6 +469,7 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
         float *red = reinterpret_cast<float *>(smem + Lay::OFF_RED) + wg * 4 * NC;   // [4][NC]
         float *linv = reinterpret_cast<float *>(smem + Lay::OFF_L) + q0;          // [OB][TP]
         float *pmx = reinterpret_cast<float *>(smem + Lay::OFF_MX) + q0;          // [OB][TP]
+        int *parent_s = reinterpret_cast<int *>(smem + Lay::OFF_PARENT) + wg * kMaxTree;
 
         // the columns' entries of nm, in registers: read by every thread for every tile they were a
         // sixth of shared memory's traffic (a 16-byte load takes four wavefronts, broadcast or not)
@@ -631,6 +647,10 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 const bool first = (j == sg.j0);
                 sl2 = tree ? p.scale_log2 : p.scale_log2 * (1.f / kKv4Unit);
                 p_unit = tree ? kKv4Unit : 1.f;
+                if (first && sg.j1 > ui.n_pref) {   // the sequence's parents, for the tree's tiles
+                    for (int i = t; i < T; i += 128) cp_async4(smem_addr(parent_s + i), p.parent + (size_t)ui.b * T + i, 4);
+                    cp_async_commit();
+                }
                 const int n_valid = tree ? Lay::KT : min(Lay::KT, ui.P - j * Lay::KT);
                 const bool masked = tree || n_valid < Lay::KT;
                 const int sb = g & 1;
@@ -638,18 +658,22 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
                 uint32_t dbits = 0;   // bit c: this thread's tree key is visible to row q0 + c
                 if (tree) {
                     // lane c walks up from row q0 + c's node and marks its ancestors among the
-                    // warp's 32 keys; then every lane collects its key's bit of each row
+                    // warp's 32 keys; the 32 x 32 bits turned over, every lane has its key's
+                    cp_async_wait<0>();
+                    named_bar_sync(1 + wg, 128);
                     const int key0 = (j - ui.n_pref) * Lay::KT + wq * 32, row = ui.qb * TP + q0 + lane;
-                    const int32_t *par = p.parent + (size_t)ui.b * T;
-                    uint32_t seen = 0;
                     for (int a = lane < NC && row < R ? row % T : -1; a >= key0;) {
-                        if (a - key0 < 32) seen |= 1u << (a - key0);
-                        const int up = ld_input(par + a);
+                        if (a - key0 < 32) dbits |= 1u << (a - key0);
+                        const int up = parent_s[a];
                         a = up < a ? up : -1;   // strictly upwards: ends
                     }
                     __syncwarp();
+                    uint32_t m = 0xFFFFu;
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) dbits |= ((__shfl_sync(0xffffffffu, seen, c) >> lane) & 1u) << c;
+                    for (int o = 16; o; o >>= 1, m ^= m << o) {
+                        const uint32_t y = __shfl_xor_sync(0xffffffffu, dbits, o);
+                        dbits = (lane & o) ? (dbits & ~m) | ((y >> o) & m) : (dbits & m) | ((y << o) & ~m);
+                    }
                 }
                 mbar_wait(bars + Lay::B_SFULL + sb, (g >> 1) & 1, abort_flag);
                 tc_fence_after();
