@@ -936,7 +936,7 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
 // Parts that the keys of a slice are shared out to, blocks of which `per_sm` fit an SM: the number
 // with the shortest time of all waves of blocks, a part counting as its chunks of 32 keys and
 // eight more for a block's start and end (960 slices of 1024 keys: 47 us, and 58 us with none
-// for them; 32 slices of 10,000 keys: 22 us, and 82 us as whole slices).  A part has at least
+// for them; 32 slices of 10,000 keys: 20 us, and 82 us as whole slices).  A part has at least
 // eight chunks, two a warp.
 static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 {
@@ -955,8 +955,8 @@ static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 // How an attention call runs: few query rows of a slice in registers, its keys in `splits`
 // parts; more on the tensor cores in blocks of tp rows, all key tiles shared out (`share`; a batch
 // that the sharing's plan holds).  Registers / tensor cores, 2048 keys, 64 x 32 slices and 32:
-//   8 rows, D = 128    178 / 240 us    14 / 15 us
-//   12 rows            235 / 240 us    21 / 16 us   (two blocks of eight; shorter contexts alike)
+//   8 rows, D = 128    170 / 250 us    13 / 15 us
+//   12 rows            235 / 250 us    21 / 15 us   (two blocks of eight; of short contexts the latter alike)
 //   16 rows, D = 64     79 /  97 us    (64 x 16 slices)
 // Blocks of 32 rows against 64 where 32 hold them all: 129 and 146 us (32 x 32 slices).
 struct Kv4Ws {

@@ -181,8 +181,8 @@ cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream)
 // loop.
 //
 // Bound by instruction issue: some 735 instructions for a chunk of 32 keys (D = 128), of them 384
-// cycles of the tensor pipe; 64 x 32 slices of 2048 keys 168 us, 3.4 TB/s.  Few slices are bound by
-// a block's start and end and by the merge: 32 slices of 10,000 keys 21.7 us, 1.8 TB/s.
+// cycles of the tensor pipe; 64 x 32 slices of 2048 keys 163 us, 3.5 TB/s.  Few slices are bound by
+// a block's start and end and by the merge: 32 slices of 10,000 keys 20.4 us, 1.7 TB/s.
 template <int D>
 struct Kv4Few {
     static constexpr int WARPS = 4, THREADS = 128, KEYS = 32;
@@ -222,8 +222,14 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
     const int c0 = (int)((long long)n_all * split / p.splits), c1 = (int)((long long)n_all * (split + 1) / p.splits);
 
     int *par = reinterpret_cast<int *>(smem + C::OFF_PARENT);
-    if (c1 > n_pref)   // this part has tree keys
+    if (c1 > n_pref) {   // this part has tree keys: their rows are read when their turn comes
         for (int i = threadIdx.x; i < T; i += C::THREADS) par[i] = ld_input(parent + i);
+        const size_t bytes = (size_t)T * D * (p.f32 ? 4 : 2);
+        for (size_t i = (size_t)threadIdx.x * 128; i < bytes; i += C::THREADS * 128) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const uint8_t *>(p.k_tree) + u * bytes + i));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const uint8_t *>(p.v_tree) + u * bytes + i));
+        }
+    }
 
     const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE;
     const size_t row0 = (size_t)u * p.S_max;
@@ -279,10 +285,21 @@ __global__ void __launch_bounds__(Kv4Few<D>::THREADS, NB == 1 ? 4 : 3) kv4_atten
     for (int nb = 0; nb < NB; ++nb) {
         const int r = 8 * nb + g;
         const size_t at = (q_row0 + (r < R ? r : 0)) * D + (D / 4) * t;
+        if (!p.f32) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(p.q) + at);
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s)
+            for (int i = 0; i < D / 32; ++i) {
+                const uint4 v = r < R ? ld_input(src + i) : make_uint4(0, 0, 0, 0);
+                q[nb][2 * i][0] = v.x, q[nb][2 * i][1] = v.y, q[nb][2 * i + 1][0] = v.z, q[nb][2 * i + 1][1] = v.w;
+            }
+        } else {
+            const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(p.q) + at);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) q[nb][s][e] = r < R ? ld_pair(p.q, at + 4 * s + 2 * e, p.f32) : 0u;
+            for (int i = 0; i < D / 16; ++i) {
+                const float4 v = r < R ? ld_input(src + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+                q[nb][i][0] = bf16x2(v.x, v.y), q[nb][i][1] = bf16x2(v.z, v.w);
+            }
+        }
     }
     float o[D / 16][NB][4] = {};   // kKv4Unit times the sums: channels g D / 8 + i and D / 16 on, queries 2t and 2t + 1
     float m[NB][2], l[NB][2];
