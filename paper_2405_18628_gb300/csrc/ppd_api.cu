@@ -958,7 +958,7 @@ static int kv4_splits(long long slices, int T, int S_max, int per_sm)
 //   8 rows, D = 128    170 / 250 us    13 / 15 us
 //   12 rows            235 / 250 us    21 / 15 us   (two blocks of eight; of short contexts the latter alike)
 //   16 rows, D = 64     79 /  97 us    (64 x 16 slices)
-// Blocks of 32 rows against 64 where 32 hold them all: 129 and 146 us (32 x 32 slices).
+// Blocks of 32 rows against 64 where 32 hold them all: 128 and 145 us (32 x 32 slices).
 struct Kv4Ws {
     size_t o, ml, rec, total;
     int row_blocks, splits, tp, share;
@@ -973,7 +973,7 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
         w.row_blocks = (int)((rows + w.tp - 1) / w.tp);
         // whole units where sharing their tiles out would save less than it costs (about six tiles'
         // time: the merge grid and the parts' way through memory).  Whole / shared, 64 tokens: 23 / 20 us
-        // (8 slices of 2048 keys), 29 / 40 us (256 of 1024), 149 / 163 us (1024 of 2048)
+        // (8 slices of 2048 keys), 29 / 40 us (256 of 1024)
         const long long units = slices * w.row_blocks, t_u = (S_max + 127) / 128 + (T + 127) / 128, sms = split_grid();
         w.share = B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + 6 < (units + sms - 1) / sms * t_u;
         if (w.share) {

@@ -13,6 +13,10 @@ namespace ppd {
 // codes (or bf16 channels) that asynchronous copies bring into a ring of the warp's own; the
 // order of the channels in the sum is free as long as Q follows it.  Tree keys come last: the
 // path's own rows, each seen by itself and the nodes after it.
+//
+// A bf16 cache: bound by HBM, 1.38 GB (B = 8, up to 16,384 keys, 16 heads of two) 208 us, 6.6 TB/s.
+// 4 bits: by instruction issue and the second wave of blocks, half empty: 1024 slices of 2048 keys 51
+// us, 3.2 TB/s (the bf16 cache 95 us).
 constexpr int kWeightRows = 32;
 
 template <int D, bool KV4>
@@ -244,6 +248,8 @@ PPD_DEV uint32_t weight_rank(float w)
 // stay in shared memory where they fit (CACHED); after the first digit the rows that share
 // it are a short list in most cases, which the other digits are counted on.  The indices need
 // no barrier in their loop: each warp counts its stretch of the rows, then writes it.
+// Bound by the chain of digits and barriers: 1024 slices of up to 16,384 rows, seven waves of
+// blocks, are a fifth of an eviction's 285 us.
 constexpr int kSelList = 2048, kSelWarps = kSelThreads / 32;
 
 template <bool CACHED>
@@ -405,7 +411,9 @@ constexpr int kMoveThreads = 256, kMoveDeep = 4;
 // (16 bytes where rows and addresses allow), then writes them; the next step's row indices are on
 // their way meanwhile.  In place a block takes its columns of the whole slice alone, in order:
 // the rows of a step lie at or above their places, and so do those of every later step, so
-// what a step overwrites has been read.
+// what a step overwrites has been read.  Bound by HBM, which brings 128 bytes for a row of 64 that
+// lies alone: 4096 of 16,384 rows kept, 1024 slices of a 4-bit cache, four fifths of the call's 285 us,
+// in which 1.5 GB are read and written for 1.2 that are needed.
 template <int BYTES, int THREADS>   // 32: a warp, else a block
 PPD_DEV void move_rows(const KvEvictParams &p, const KvPlane &pl, const int32_t *kept, uint32_t u, int c0, int c1, int i0, int i1, int tid)
 {

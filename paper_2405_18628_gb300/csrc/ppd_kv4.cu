@@ -36,6 +36,8 @@ PPD_DEV int append_status(int start, int n, int T, int S_max)
 // an fp32 reciprocal rounded to nearest, and a fused residual); halves are then exact, and
 // adding 1.5 * 2^23 + 8 rounds to the nearest integer, half to even, and leaves the code in the low
 // bits.  Divisions in their place were 43 of a prompt's 67 us.  Four rows' loads a thread in flight.
+// Bound by instruction issue, then by HBM: 256 slices of 1003 fp32 rows into the cache and out of it
+// (D = 64, 232 MB) 56 us, 4.2 TB/s.
 constexpr int kAppendRows = 64, kAppendDeep = 4;
 template <int D>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4AppendParams p)

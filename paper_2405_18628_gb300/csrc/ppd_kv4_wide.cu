@@ -13,6 +13,13 @@
 //
 // The converting warps fetch their own rows by asynchronous copies, two tiles ahead, so the
 // codes pass shared memory once and meet no barrier on their way in.
+//
+// Bound by the softmax warps, which the scores never wait for: some 1100 of a tile's 1780 cycles (64
+// query rows, D = 128) are the probabilities' instructions, the rest their way from and to the
+// tensor cores and the tile's vote; shared memory's loads and stores take some 800 cycles beside
+// the products' own reads, the products a third.  A unit's first scores, its tree, row sums and output
+// cost four tiles more: 1024 slices of 2048 keys 141 us, 2.5 TB/s, 0.49 PFLOP/s; eight sequences of
+// up to 16,384 keys (4 x 32 slices each) 648 us, 2.3 TB/s, 0.53 PFLOP/s.
 #include "ppd_attention_common.cuh"
 #include "ppd_kv4.cuh"
 
@@ -29,7 +36,8 @@ struct Kv4Wide {
     // softmax warps, four warps converting K, four converting V, then three that bring Q and the issuer
     static constexpr int SW = 8, KW = SW, VW = KW + 4, QW = VW + 4, NQ = 3, IW = QW + NQ;
     static constexpr int THREADS = (IW + 1) * 32;
-    // registers a thread: 20 warps start with 96 and share the same total out anew
+    // registers a thread: 20 warps start with 96 and share the same total out anew (144 to 176 for the
+    // softmax, which changes little: 141 to 148 us, 634 to 652)
     static constexpr int SOFTMAX_REGS = 168, CONVERT_REGS = 56, OTHER_REGS = 32;
     static_assert(2 * SOFTMAX_REGS + 2 * CONVERT_REGS + OTHER_REGS <= 5 * 96, "register shares");
     static constexpr int STAGES = 3;              // tiles of codes in a converting warp's ring

@@ -22,7 +22,8 @@ namespace ppd {
 // children none; a drawn child's rejection costs one pass over the share and its draft row,
 // and an exchange.  Every CTA takes the same decisions from the same numbers.
 //
-// Bound by the chain of a walk's passes, not by their bytes: a thread keeps to its own elements
+// Bound by the chain of a walk's passes, not by their bytes (one sequence, 32,000 tokens, chosen
+// guesses: 9 us; 80 sequences, 50,257 tokens, drawn: 39 us, some 3 us a pass): a thread keeps to its own elements
 // of the share and a warp to its own maximum, so that a pass has one barrier of the block and
 // one of the cluster; the children's entries are asked for before the row.  (Asking L2 for
 // the draft row or the noise ahead of their passes made 80 sequences 42 -> 56 us.)
