@@ -14,12 +14,12 @@
 // The converting warps fetch their own rows by asynchronous copies, two tiles ahead, so the
 // codes pass shared memory once and meet no barrier on their way in.
 //
-// Bound by the softmax warps, which the scores never wait for: some 1100 of a tile's 1780 cycles (64
+// Bound by the softmax warps, which the scores never wait for: some 1100 of a tile's 1760 cycles (64
 // query rows, D = 128) are the probabilities' instructions, the rest their way from and to the
 // tensor cores and the tile's vote; shared memory's loads and stores take some 800 cycles beside
 // the products' own reads, the products a third.  A unit's first scores, its tree, row sums and output
-// cost four tiles more: 1024 slices of 2048 keys 141 us, 2.5 TB/s, 0.49 PFLOP/s; eight sequences of
-// up to 16,384 keys (4 x 32 slices each) 648 us, 2.3 TB/s, 0.53 PFLOP/s.
+// cost four tiles more: 1024 slices of 2048 keys 140 us, 2.5 TB/s, 0.49 PFLOP/s; eight sequences of
+// up to 16,384 keys (4 x 32 slices each) 604 us, 2.5 TB/s, 0.57 PFLOP/s.
 #include "ppd_attention_common.cuh"
 #include "ppd_kv4.cuh"
 
@@ -37,7 +37,8 @@ struct Kv4Wide {
     static constexpr int SW = 8, KW = SW, VW = KW + 4, QW = VW + 4, NQ = 3, IW = QW + NQ;
     static constexpr int THREADS = (IW + 1) * 32;
     // registers a thread: 20 warps start with 96 and share the same total out anew (144 to 176 for the
-    // softmax, which changes little: 141 to 148 us, 634 to 652)
+    // softmax: 140 to 148 us and 604 to 652 for those below, the compiler's order of the loop more
+    // than the registers)
     static constexpr int SOFTMAX_REGS = 168, CONVERT_REGS = 56, OTHER_REGS = 32;
     static_assert(2 * SOFTMAX_REGS + 2 * CONVERT_REGS + OTHER_REGS <= 5 * 96, "register shares");
     static constexpr int STAGES = 3;              // tiles of codes in a converting warp's ring
@@ -650,15 +651,15 @@ kv4_attention_wide_kernel(const AttnParams p, const Kv4AttnParams x)
             const int u = sg.u;
             cur_k = k;
             const int ob = k & 1;
+            if (sg.j1 > ui.n_pref) {   // the sequence's parents, for the tree's tiles
+                for (int i = t; i < T; i += 128) cp_async4(smem_addr(parent_s + i), p.parent + (size_t)ui.b * T + i, 4);
+                cp_async_commit();
+            }
             for (int j = sg.j0; j < sg.j1; ++j, ++g) {
                 const bool tree = j >= ui.n_pref;
                 const bool first = (j == sg.j0);
                 sl2 = tree ? p.scale_log2 : p.scale_log2 * (1.f / kKv4Unit);
                 p_unit = tree ? kKv4Unit : 1.f;
-                if (first && sg.j1 > ui.n_pref) {   // the sequence's parents, for the tree's tiles
-                    for (int i = t; i < T; i += 128) cp_async4(smem_addr(parent_s + i), p.parent + (size_t)ui.b * T + i, 4);
-                    cp_async_commit();
-                }
                 const int n_valid = tree ? Lay::KT : min(Lay::KT, ui.P - j * Lay::KT);
                 const bool masked = tree || n_valid < Lay::KT;
                 const int sb = g & 1;
