@@ -82,6 +82,9 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     bad = __syncthreads_or(bad);
     const int P = ld_input(p.prefix_len + b);
     int err = bad ? kErrTree : (P < 0 || P > p.S_max ? kErrCapacity : kOk);
+    // every CTA of the cluster has started, and has read its inputs per node, before one stores into
+    // another's shared memory, or writes an output
+    cluster_sync();
 
     int phase = 0;
     float M = 0.f, f = 1.f, rest = 0.f;   // R = f e; rest: the sum of R in the shares

@@ -65,3 +65,21 @@ def test_no_load_assumes_that_its_data_never_changes():
     for name, text in _sources().items():
         for word in ("__ldg", "global.nc", "__restrict__"):
             assert word not in text, (name, word)
+
+
+def test_no_store_into_a_peer_before_every_cta_of_the_cluster_runs():
+    """Shared memory of another CTA may be touched once that CTA has started, which only a
+    barrier of the cluster shows: a kernel that stores into its peers passes one first, outside
+    any branch or loop."""
+    found = 0
+    for name, text in _sources().items():
+        if name == "ppd_device.cuh":
+            continue
+        for body in re.findall(r"__global__.*?^\}$", text, flags=re.S | re.M):
+            store = body.find("st_cluster_")
+            if store < 0:
+                continue
+            found += 1
+            barrier = re.search(r"^    cluster_sync\(\);", body, flags=re.M)
+            assert barrier and barrier.start() < store, name
+    assert found
