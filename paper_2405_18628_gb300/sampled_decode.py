@@ -36,6 +36,7 @@ class LongContext:
         i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
         self.length, self.new_length = i32(B), i32(B)
         self.longest = 0                       # no sequence is longer (host)
+        self.row = torch.arange(S_max, dtype=torch.int32, device=device)
         self.out = torch.empty((L, B, H * G, T, D), dtype=torch.bfloat16, device=device)
         self.lse = torch.empty((L, B, H * G, T), device=device)
         self.accept_len, self.next_token, self.path = i32(B), i32(B), i32(B, T)
@@ -46,10 +47,12 @@ class LongContext:
         self.workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
     def prompt(self, k, v):
-        """A prompt's rows of every layer, k and v [L,B,H,n,D], enter the caches."""
+        """A prompt's rows of every layer, k and v [L,B,H,n,D], enter the caches, without weight yet."""
         B, n = k.shape[1], k.shape[3]
         count = torch.full((B,), n, dtype=torch.int32, device=k.device)
         ppd.ppd_kv4_append(k, v, self.k, self.k_scale, self.v, self.v_scale, self.length, count, self.append_status)
+        # an eviction leaves the weights of other rows past the new length: the prompt's start at 0
+        self.weight.masked_fill_((self.row >= self.length[:, None])[:, None], 0.0)
         self.length += count
         self.longest += n
 

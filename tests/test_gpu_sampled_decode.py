@@ -77,3 +77,47 @@ def test_the_command(cuda_device, capsys):
     from paper_2405_18628_gb300 import sampled_decode as S
     assert S.main(["--steps", "24", "--layers", "2"]) == 0
     assert "statuses [0, 0, 0, 0]" in capsys.readouterr().out
+
+
+def test_a_prompt_after_an_eviction(cuda_device):
+    """A second turn's prompt: its rows have no weight, whatever rows an eviction left behind them,
+    and the next eviction ranks them by what steps gave them."""
+    from paper_2405_18628_gb300 import sampled_decode as S
+    dev, L, B, H, G, T, D, V = cuda_device, 2, 3, 2, 1, 8, 64, 100
+    g = torch.Generator(device=dev)
+    g.manual_seed(6)
+    n = lambda *s: torch.randn(s, dtype=torch.bfloat16, device=dev, generator=g)  # noqa: E731
+    ctx = S.LongContext(L, B, H, G, T, D, V, 64, 20, n_sink=2, n_recent=3, device=dev)
+    parent = torch.tensor([[-1, 0, 1, 2, 3, 4, 5, 6]] * B, dtype=torch.int32, device=dev)
+
+    def step():
+        q, kt, vt = n(L, B, H * G, T, D), n(L, B, H, T, D), n(L, B, H, T, D)
+        for l in range(L):
+            ctx.attend(l, q[l], kt[l], vt[l], parent)
+        logits = 3 * torch.randn(B, T, V, device=dev, generator=g)
+        cand = logits.argmax(-1).gather(1, parent.long().clamp(min=0)).int()
+        ctx.accept(logits, cand, parent, 1.0, torch.rand(B, T, device=dev, generator=g),
+                   torch.empty(B, V, device=dev).exponential_(generator=g).clamp_(min=1e-12))
+        ctx.commit(q, kt, vt)
+
+    ctx.prompt(n(L, B, H, 40, D), n(L, B, H, 40, D))
+    step()
+    ctx.weight[:, :, :, 20:] += 1000.0        # heavy rows where the next turn's will be
+    ctx.evict()
+    assert ctx.length.tolist() == [20] * B
+    old = ctx.weight[..., :20].clone()
+    assert (ctx.weight[..., 20:28] > 0).all()
+    ctx.prompt(n(L, B, H, 11, D), n(L, B, H, 11, D))
+    assert torch.equal(ctx.weight[..., :20], old) and (ctx.weight[..., 20:31] == 0).all()
+    step()
+    # a step's weight: less than its accepted nodes' for each row
+    assert (ctx.weight[..., 20:31] < T).all() and (ctx.weight[..., 20:31].sum((0, 1, 2)) > 0).all()
+    lens = ctx.length.tolist()
+    weight = ctx.weight.tolist()
+    ctx.evict()
+    for l in range(L):
+        for b in range(B):
+            for h in range(H):
+                assert ctx.kept[l, b, h].tolist() == O.evict(weight[l][b][h], lens[b], 20, 2, 3)
+    for st in (ctx.attend_status, ctx.accept_status, ctx.append_status, ctx.evict_status):
+        assert (st == 0).all()

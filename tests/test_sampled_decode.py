@@ -1,0 +1,80 @@
+"""The decode loop's own bookkeeping (lengths, weights, room in the caches), with plain forms
+in the place of the kernels: no GPU needed."""
+import pytest
+import torch
+
+import oracle.operators as O
+
+
+def _append(k_new, v_new, k_cache, k_scale, v_cache, v_scale, start, n_new, dev_status, rows=None, stream=None):
+    L, B, H, T, D = k_new.shape
+    for b in range(B):
+        s, n = int(start[b]), int(n_new[b])
+        dev_status[b] = 0 if s >= 0 and 0 <= n <= T and s + n <= k_cache.shape[3] else 4
+        if dev_status[b] or n == 0:
+            continue
+        at = list(range(n)) if rows is None else rows[b, :n].tolist()
+        for x, c, sc in ((k_new, k_cache, k_scale), (v_new, v_cache, v_scale)):
+            c[:, b, :, s:s + n], sc[:, b, :, s:s + n] = O.kv4_quantise(x[:, b][:, :, at])
+
+
+def _evict(weight, planes, length, budget, n_sink, n_recent, kept, new_len, dev_status, out_weight=None, out_planes=None, stream=None):
+    L, B, H, S = weight.shape
+    for b in range(B):
+        n = int(length[b])
+        dev_status[b] = 0 if 0 <= n <= S else 4
+        new_len[b] = n if dev_status[b] else min(n, budget)
+        for l in range(L):
+            for h in range(H):
+                at = [] if dev_status[b] else O.evict(weight[l, b, h].tolist(), n, budget, n_sink, n_recent)
+                kept[l, b, h] = torch.tensor(at + [-1] * (budget - len(at)))
+                for x in (*planes, weight):
+                    x[l, b, h, :len(at)] = x[l, b, h][at].clone()
+
+
+def _weight_add(q, lse, k_cache, k_tree, path, accept_len, prefix_len, weight, k_scale=None, scale=0.0, stream=None):
+    """Every cached row gets 1 from a step, an accepted one too."""
+    for b in range(weight.shape[1]):
+        P, n = int(prefix_len[b]), int(accept_len[b])
+        weight[:, b, :, :P] += 1
+        weight[:, b, :, P:P + n] = 1
+
+
+@pytest.fixture
+def decode(monkeypatch):
+    from paper_2405_18628_gb300 import build, ppd, sampled_decode
+    build.build()
+    monkeypatch.setattr(ppd, "ppd_kv4_append", _append)
+    monkeypatch.setattr(ppd, "ppd_kv_evict", _evict)
+    monkeypatch.setattr(ppd, "ppd_kv_weight_add", _weight_add)
+    return sampled_decode
+
+
+def _rows(n, seed=0, L=2, B=2, H=1, D=64):
+    return torch.randn(L, B, H, n, D, generator=torch.Generator().manual_seed(seed))
+
+
+def _step(ctx, n, **commit):
+    """A step that accepts n[b] nodes."""
+    L, B, H, G, T, D = ctx.sizes[:6]
+    for b in range(B):
+        ctx.accept_len[b] = n[b]
+        ctx.path[b] = torch.tensor(list(range(n[b])) + [-1] * (T - n[b]))
+    ctx.new_length.copy_(ctx.length + ctx.accept_len)
+    ctx.commit(torch.zeros(L, B, H * G, T, D), _rows(T, 1, L, B, H, D), _rows(T, 2, L, B, H, D), **commit)
+
+
+def test_a_prompt_after_an_eviction_starts_without_weight(decode):
+    ctx = decode.LongContext(2, 2, 1, 1, 4, 64, 50, 40, 16, n_sink=1, n_recent=2, device="cpu")
+    ctx.prompt(_rows(30), _rows(30))
+    assert (ctx.weight == 0).all()
+    _step(ctx, [3, 1])
+    ctx.weight[:, :, :, :30] += torch.arange(30.0)   # unlike weights, large ones at the end
+    ctx.evict()
+    assert ctx.length.tolist() == [16, 16]
+    old = ctx.weight[..., :16].clone()
+    ctx.prompt(_rows(5, 3), _rows(5, 4))
+    assert ctx.length.tolist() == [21, 21]
+    assert torch.equal(ctx.weight[..., :16], old) and (ctx.weight[..., 16:] == 0).all()
+    _step(ctx, [1, 2])
+    assert (ctx.weight[..., 16:22] == 1).all()
