@@ -24,8 +24,8 @@ class LongContext:
     and the buffers of a step.  H K/V heads of G query heads each, trees of T tokens, a
     vocabulary of V.  A cache holds S_max rows per head and is cut to `budget` rows (the first
     n_sink, the last n_recent, and the heaviest between) when a step might not fit any more.
-    Nothing here waits for the GPU: lengths stay on the device, and the host counts the most
-    that they can be."""
+    Nothing here waits for the GPU but a prompt that might not fit: lengths stay on the device,
+    and the host counts the most that they can be."""
 
     def __init__(self, L, B, H, G, T, D, V, S_max, budget, n_sink=4, n_recent=32, device="cuda"):
         self.sizes = L, B, H, G, T, D, V, S_max
@@ -47,8 +47,13 @@ class LongContext:
         self.workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
     def prompt(self, k, v):
-        """A prompt's rows of every layer, k and v [L,B,H,n,D], enter the caches, without weight yet."""
-        B, n = k.shape[1], k.shape[3]
+        """A prompt's rows of every layer, k and v [L,B,H,n,D], enter the caches, without weight yet.
+        One that does not fit is refused."""
+        B, n, S_max = k.shape[1], k.shape[3], self.sizes[7]
+        if self.longest + n > S_max:           # perhaps: what steps accepted decides (waits for the GPU)
+            self.longest = int(self.length.max())
+        if self.longest + n > S_max:
+            raise ValueError(f"a prompt of {n} rows after {self.longest}: the caches hold {S_max}")
         count = torch.full((B,), n, dtype=torch.int32, device=k.device)
         ppd.ppd_kv4_append(k, v, self.k, self.k_scale, self.v, self.v_scale, self.length, count, self.append_status)
         # an eviction leaves the weights of other rows past the new length: the prompt's start at 0

@@ -78,3 +78,29 @@ def test_a_prompt_after_an_eviction_starts_without_weight(decode):
     assert torch.equal(ctx.weight[..., :16], old) and (ctx.weight[..., 16:] == 0).all()
     _step(ctx, [1, 2])
     assert (ctx.weight[..., 16:22] == 1).all()
+
+
+def test_a_prompt_that_does_not_fit_is_refused(decode):
+    """Nothing is written and no length moves; what does fit still enters."""
+    ctx = decode.LongContext(1, 2, 1, 1, 4, 64, 50, 40, 36, n_sink=1, n_recent=2, device="cpu")
+    with pytest.raises(ValueError, match="41 rows"):
+        ctx.prompt(_rows(41, L=1), _rows(41, L=1))
+    assert ctx.length.tolist() == [0, 0] and ctx.longest == 0 and (ctx.k == 0).all()
+    ctx.prompt(_rows(25, L=1), _rows(25, L=1))
+    with pytest.raises(ValueError, match="16 rows"):
+        ctx.prompt(_rows(16, L=1), _rows(16, L=1))
+    assert ctx.length.tolist() == [25, 25] and ctx.append_status.tolist() == [0, 0]
+    ctx.prompt(_rows(10, L=1), _rows(10, L=1))
+    assert ctx.length.tolist() == [35, 35] and ctx.append_status.tolist() == [0, 0]
+
+
+def test_a_prompt_fits_by_what_steps_accepted(decode):
+    """The host counts the most that steps can accept; where that leaves no room for a prompt, what
+    they did accept decides."""
+    ctx = decode.LongContext(1, 2, 1, 1, 4, 64, 50, 40, 30, n_sink=1, n_recent=2, device="cpu")
+    ctx.prompt(_rows(20, L=1), _rows(20, L=1))
+    for _ in range(3):
+        _step(ctx, [1, 2])
+    assert ctx.longest == 32 and ctx.length.tolist() == [23, 26]
+    ctx.prompt(_rows(10, L=1), _rows(10, L=1))
+    assert ctx.length.tolist() == [33, 36] and ctx.longest == 36 and ctx.append_status.tolist() == [0, 0]
