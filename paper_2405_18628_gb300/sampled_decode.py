@@ -23,13 +23,20 @@ class LongContext:
     """The 4-bit caches of B sequences over L layers, the attention weight of every cached row,
     and the buffers of a step.  H K/V heads of G query heads each, trees of T tokens, a
     vocabulary of V.  A cache holds S_max rows per head and is cut to `budget` rows (the first
-    n_sink, the last n_recent, and the heaviest between) when a step might not fit any more.
+    n_sink, the last n_recent, and the heaviest between) when a prompt does not fit, or a step of
+    `most` accepted nodes (T where not given) might not fit any more.  Rows without weight yet
+    (a prompt's, before a step) count as the lightest, the earlier ones first.
     Nothing here waits for the GPU but a prompt that might not fit: lengths stay on the device,
     and the host counts the most that they can be."""
 
-    def __init__(self, L, B, H, G, T, D, V, S_max, budget, n_sink=4, n_recent=32, device="cuda"):
+    def __init__(self, L, B, H, G, T, D, V, S_max, budget, n_sink=4, n_recent=32, device="cuda", most=None):
+        most = T if most is None else most
+        if most < 1 or budget < 1 or budget + most > S_max:
+            raise ValueError(f"a budget of {budget} rows and a step of {most} in caches of {S_max}")
+        if n_sink < 0 or n_recent < 0 or n_sink + n_recent > budget:
+            raise ValueError(f"{n_sink} first and {n_recent} last rows in a budget of {budget}")
         self.sizes = L, B, H, G, T, D, V, S_max
-        self.budget, self.n_sink, self.n_recent = budget, n_sink, n_recent
+        self.budget, self.n_sink, self.n_recent, self.most = budget, n_sink, n_recent, most
         self.k, self.k_scale = ppd.kv4_cache(L, B, H, S_max, D, device)
         self.v, self.v_scale = ppd.kv4_cache(L, B, H, S_max, D, device)
         self.weight = torch.zeros((L, B, H, S_max), device=device)
@@ -48,18 +55,22 @@ class LongContext:
 
     def prompt(self, k, v):
         """A prompt's rows of every layer, k and v [L,B,H,n,D], enter the caches, without weight yet.
-        One that does not fit is refused."""
+        One that does not fit, even after an eviction, is refused."""
         B, n, S_max = k.shape[1], k.shape[3], self.sizes[7]
         if self.longest + n > S_max:           # perhaps: what steps accepted decides (waits for the GPU)
             self.longest = int(self.length.max())
+        if min(self.longest, self.budget) + n > S_max:
+            raise ValueError(f"a prompt of {n} rows after {min(self.longest, self.budget)}: the caches hold {S_max}")
         if self.longest + n > S_max:
-            raise ValueError(f"a prompt of {n} rows after {self.longest}: the caches hold {S_max}")
+            self.evict()
         count = torch.full((B,), n, dtype=torch.int32, device=k.device)
         ppd.ppd_kv4_append(k, v, self.k, self.k_scale, self.v, self.v_scale, self.length, count, self.append_status)
         # an eviction leaves the weights of other rows past the new length: the prompt's start at 0
         self.weight.masked_fill_((self.row >= self.length[:, None])[:, None], 0.0)
         self.length += count
         self.longest += n
+        if self.longest + self.most > S_max:
+            self.evict()
 
     def attend(self, layer, q, k_tree, v_tree, parent):
         """One layer's attention: q [B,H*G,T,D], k_tree and v_tree [B,H,T,D] -> bf16 [B,H*G,T,D]."""
@@ -79,9 +90,9 @@ class LongContext:
 
     def commit(self, q, k_tree, v_tree, most=None):
         """The accepted nodes' attention weight and rows (of every layer: q [L,B,H*G,T,D], k_tree and
-        v_tree [L,B,H,T,D]) enter the caches; `most`: nodes that a step accepts at most."""
-        T, S_max = self.sizes[4], self.sizes[7]
-        most = T if most is None else most
+        v_tree [L,B,H,T,D]) enter the caches; `most`: nodes that this step and the next accept at most."""
+        S_max = self.sizes[7]
+        most = self.most if most is None else most
         ppd.ppd_kv_weight_add(q, self.lse, self.k, k_tree, self.path, self.accept_len, self.length, self.weight, k_scale=self.k_scale)
         ppd.ppd_kv4_append(k_tree, v_tree, self.k, self.k_scale, self.v, self.v_scale, self.length, self.accept_len, self.append_status,
                            rows=self.path)
@@ -111,9 +122,9 @@ def main(argv=None):
     g = torch.Generator(device="cuda")
     g.manual_seed(a.seed)
     n = lambda *s: torch.randn(s, dtype=torch.bfloat16, device="cuda", generator=g)  # noqa: E731
-    ctx = LongContext(L, B, H, G, T, D, V, a.capacity, a.capacity * 3 // 4)
-    ctx.prompt(n(L, B, H, a.prompt, D), n(L, B, H, a.prompt, D))
     w = W.Workload("demo", L=1, B=1, H=1, D=64, P=0, T=T, V=1, n_cand=T // 4, max_depth=4, chains="fill3", match_rate=0.6)
+    ctx = LongContext(L, B, H, G, T, D, V, a.capacity, a.capacity * 3 // 4, most=w.max_depth + 1)
+    ctx.prompt(n(L, B, H, a.prompt, D), n(L, B, H, a.prompt, D))
     emitted = 0
     t0 = time.perf_counter()
     for step in range(a.steps):
@@ -128,7 +139,7 @@ def main(argv=None):
         cand = torch.where(prompt, -1, logits.argmax(-1).gather(1, parent.long().clamp(min=0))).int()
         u, noise = torch.rand(B, T, device="cuda", generator=g), torch.empty(B, V, device="cuda").exponential_(generator=g).clamp_(min=1e-20)
         ctx.accept(logits, cand, parent, 0.7, u, noise)
-        ctx.commit(q, k_tree, v_tree, most=w.max_depth + 1)
+        ctx.commit(q, k_tree, v_tree)
         emitted += int(ctx.accept_len.sum())
     torch.cuda.synchronize()
     bad = [int(x.abs().sum()) for x in (ctx.attend_status, ctx.accept_status, ctx.append_status, ctx.evict_status)]

@@ -104,3 +104,35 @@ def test_a_prompt_fits_by_what_steps_accepted(decode):
     assert ctx.longest == 32 and ctx.length.tolist() == [23, 26]
     ctx.prompt(_rows(10, L=1), _rows(10, L=1))
     assert ctx.length.tolist() == [33, 36] and ctx.longest == 36 and ctx.append_status.tolist() == [0, 0]
+
+
+def test_room_is_made_for_a_prompt_and_for_the_step_after_it(decode):
+    ctx = decode.LongContext(1, 2, 1, 1, 4, 64, 50, 40, 16, n_sink=1, n_recent=2, device="cpu")
+    ctx.prompt(_rows(36, L=1), _rows(36, L=1))              # a step of four nodes still fits
+    assert ctx.length.tolist() == [36, 36]
+    ctx.weight[:, :, :, :36] += torch.arange(36.0)
+    ctx.prompt(_rows(10, L=1), _rows(10, L=1))              # after an eviction by weight
+    assert ctx.length.tolist() == [26, 26] and ctx.append_status.tolist() == [0, 0]
+    assert ctx.weight[0, 0, 0, :16].tolist() == [0.0] + [float(x) for x in range(21, 36)]
+    assert (ctx.weight[..., 16:] == 0).all()
+    ctx.prompt(_rows(12, L=1), _rows(12, L=1))              # it fits, a step after it would not
+    assert ctx.length.tolist() == [16, 16] and ctx.longest == 16
+    assert ctx.kept[0, 0, 0, -2:].tolist() == [36, 37]
+    _step(ctx, [4, 4])
+    assert ctx.length.tolist() == [20, 20] and ctx.append_status.tolist() == [0, 0]
+    with pytest.raises(ValueError, match="25 rows"):        # no eviction makes room for it: none happens
+        ctx.prompt(_rows(25, L=1), _rows(25, L=1))
+    assert ctx.length.tolist() == [20, 20]
+
+
+def test_budgets_that_leave_no_room_are_refused(decode):
+    sizes = (1, 1, 1, 1, 4, 64, 50, 40)
+    for bad in (dict(budget=37), dict(budget=41), dict(budget=35, most=6), dict(budget=10, n_sink=5, n_recent=6), dict(budget=0, n_sink=0, n_recent=0),
+                dict(budget=10, most=0), dict(budget=20, n_sink=-1)):
+        with pytest.raises(ValueError):
+            decode.LongContext(*sizes, **{**dict(n_sink=1, n_recent=2, device="cpu"), **bad})
+    decode.LongContext(*sizes, 36, n_sink=1, n_recent=2, device="cpu")
+    ctx = decode.LongContext(*sizes, 38, n_sink=1, n_recent=2, device="cpu", most=2)   # steps of two nodes
+    ctx.prompt(_rows(38, L=1, B=1), _rows(38, L=1, B=1))
+    _step(ctx, [2])
+    assert ctx.length.tolist() == [38]                      # cut as the step ended
