@@ -22,7 +22,7 @@ from . import workloads as W
 class LongContext:
     """The 4-bit caches of B sequences over L layers, the attention weight of every cached row,
     and the buffers of a step.  H K/V heads of G query heads each, trees of T tokens, a
-    vocabulary of V.  A cache holds S_max rows per head and is cut to `budget` rows (the first
+    vocabulary of V.  A cache holds S_max rows per head (rounded up to eight) and is cut to `budget` rows (the first
     n_sink, the last n_recent, and the heaviest between) when a prompt does not fit, or a step of
     `most` accepted nodes (T where not given) might not fit any more.  Rows without weight yet
     (a prompt's, before a step) count as the lightest, the earlier ones first.
@@ -35,6 +35,7 @@ class LongContext:
             raise ValueError(f"a budget of {budget} rows and a step of {most} in caches of {S_max}")
         if n_sink < 0 or n_recent < 0 or n_sink + n_recent > budget:
             raise ValueError(f"{n_sink} first and {n_recent} last rows in a budget of {budget}")
+        S_max = (S_max + 7) // 8 * 8           # a layer's scales, H S_max D / 32 bytes, start on 16 of them
         self.sizes = L, B, H, G, T, D, V, S_max
         self.budget, self.n_sink, self.n_recent, self.most = budget, n_sink, n_recent, most
         self.k, self.k_scale = ppd.kv4_cache(L, B, H, S_max, D, device)

@@ -121,3 +121,21 @@ def test_a_prompt_after_an_eviction(cuda_device):
                 assert ctx.kept[l, b, h].tolist() == O.evict(weight[l][b][h], lens[b], 20, 2, 3)
     for st in (ctx.attend_status, ctx.accept_status, ctx.append_status, ctx.evict_status):
         assert (st == 0).all()
+
+
+def test_layers_of_odd_capacities(cuda_device):
+    from paper_2405_18628_gb300 import sampled_decode as S
+    dev, D = cuda_device, 64
+    g = torch.Generator(device=dev)
+    g.manual_seed(7)
+    n = lambda *s: torch.randn(s, dtype=torch.bfloat16, device=dev, generator=g)  # noqa: E731
+    ctx = S.LongContext(3, 1, 1, 1, 4, D, 50, 97, 50, n_sink=1, n_recent=2, device=dev)
+    kp, vp, q, kt, vt = n(3, 1, 1, 60, D), n(3, 1, 1, 60, D), n(3, 1, 1, 4, D), n(3, 1, 1, 4, D), n(3, 1, 1, 4, D)
+    ctx.prompt(kp, vp)
+    parent = [-1, 0, 0, 1]
+    for l in range(3):
+        out = ctx.attend(l, q[l], kt[l], vt[l], torch.tensor([parent], dtype=torch.int32, device=dev))
+        k, v = (O.kv4_values(*O.kv4_quantise(x[l, 0, 0])) for x in (kp, vp))
+        want, _, mass, size = O.attention_kv4(q[l, 0], k, v, kt[l, 0, 0], vt[l, 0, 0], 60, parent)
+        assert ((out[0].double() - want).abs() <= (2.0 ** -8 + 1e-4 + 2 * D * 2.0 ** -24 * size) * mass + 1e-36).all()
+    assert (ctx.attend_status == 0).all()

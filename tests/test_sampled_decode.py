@@ -136,3 +136,14 @@ def test_budgets_that_leave_no_room_are_refused(decode):
     ctx.prompt(_rows(38, L=1, B=1), _rows(38, L=1, B=1))
     _step(ctx, [2])
     assert ctx.length.tolist() == [38]                      # cut as the step ended
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S_max", [41, 44, 97, 1001])
+def test_every_layers_tensors_are_aligned(decode, S_max, D):
+    """Attention is called one layer at a time, with 16-byte aligned tensors, whatever the capacity."""
+    ctx = decode.LongContext(3, 1, 1, 1, 4, D, 50, S_max, 16, n_sink=1, n_recent=2, device="cpu")
+    assert S_max <= ctx.sizes[7] == ctx.weight.shape[3] < S_max + 8
+    for layer in range(3):
+        for x in (ctx.k, ctx.k_scale, ctx.v, ctx.v_scale, ctx.out):
+            assert x[layer:layer + 1].data_ptr() % 16 == 0
