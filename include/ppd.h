@@ -337,6 +337,7 @@ ppd_status ppd_node_argmax_noalloc(const float *logits, int B, int T, int V, int
  * c = 8 + min(max(round(x / s), -7), 7), half to even; a NaN becomes 0.
  * start or n_new outside the cache or n_new > T: PPD_ERR_CAPACITY, nothing
  * written for that sequence.  A row index outside [0, T) writes nothing.
+ * The caches and dev_status share no memory with each other or with what is read.
  */
 ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache, uint8_t *k_scale,
                           uint8_t *v_cache, uint8_t *v_scale, const int32_t *rows,

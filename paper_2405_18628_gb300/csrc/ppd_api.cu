@@ -12,6 +12,7 @@
 #include <cstdint>
 #include <atomic>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 
 namespace {
@@ -32,6 +33,25 @@ bool overlaps(const void *a, size_t na, const void *b, size_t nb)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
+}
+
+// Memory that a call reads or writes (null: none).
+struct Mem {
+    const void *p;
+    size_t n;
+};
+
+// Blocks of a grid write `out` while others still read `in`: true where an output shares bytes
+// with an input or with another output.
+bool share_memory(std::initializer_list<Mem> out, std::initializer_list<Mem> in)
+{
+    for (const Mem *a = out.begin(); a != out.end(); ++a) {
+        for (const Mem *b = a + 1; b != out.end(); ++b)
+            if (a->p && b->p && overlaps(a->p, a->n, b->p, b->n)) return true;
+        for (const Mem &b : in)
+            if (a->p && b.p && overlaps(a->p, a->n, b.p, b.n)) return true;
+    }
+    return false;
 }
 
 int num_sms()
@@ -915,6 +935,10 @@ ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache
     if (!kv4_dims_ok(L, B, H, 1, T, D, S_max) || (dt != PPD_BF16 && dt != PPD_F32)) return PPD_ERR_INVALID_ARG;
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
         !aligned(k_scale, 16) || !aligned(v_scale, 16))
+        return PPD_ERR_INVALID_ARG;
+    const size_t cached = (size_t)L * B * H * S_max, fresh = (size_t)L * B * H * T * D * (dt == PPD_F32 ? 4 : 2), nb = (size_t)B * 4;
+    if (share_memory({{k_cache, cached * (D / 2)}, {k_scale, cached * (D / 32)}, {v_cache, cached * (D / 2)}, {v_scale, cached * (D / 32)}, {dev_status, nb}},
+                     {{k_new, fresh}, {v_new, fresh}, {rows, nb * T}, {start, nb}, {n_new, nb}}))
         return PPD_ERR_INVALID_ARG;
     if (T > 65535 * 64) return PPD_ERR_UNSUPPORTED;
     ppd::Kv4AppendParams p{k_new, v_new, k_cache, v_cache, k_scale, v_scale, rows, start, n_new, dev_status,
