@@ -347,7 +347,7 @@ ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache
 /*
  * Rows out of a 4-bit cache (K or V): out [L,B,H,N,D] (PPD_BF16 or PPD_F32, exact
  * in both) row j is the value of cache row start[b] + j for j < n[b], zero for
- * the other j < N and for rows outside the cache.
+ * the other j < N and for rows outside the cache.  out shares no memory with what is read.
  */
 ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_t *start,
                         const int32_t *n, int L, int B, int H, int N, int D, int S_max, void *out,

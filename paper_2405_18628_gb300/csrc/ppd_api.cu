@@ -953,6 +953,10 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
     if (!cache || !scale || !start || !n || !out) return PPD_ERR_INVALID_ARG;
     if (!kv4_dims_ok(L, B, H, 1, N, D, S_max) || (dt != PPD_BF16 && dt != PPD_F32)) return PPD_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(scale, 16) || !aligned(out, 16)) return PPD_ERR_INVALID_ARG;
+    const size_t cached = (size_t)L * B * H * S_max, nb = (size_t)B * 4;
+    if (share_memory({{out, (size_t)L * B * H * N * D * (dt == PPD_F32 ? 4 : 2)}},
+                     {{cache, cached * (D / 2)}, {scale, cached * (D / 32)}, {start, nb}, {n, nb}}))
+        return PPD_ERR_INVALID_ARG;
     ppd::Kv4ReadParams p{cache, scale, start, n, out, (long long)L * B * H, B, H, N, D, S_max, dt == PPD_F32};
     return cuda_status(ppd::launch_kv4_read(p, static_cast<cudaStream_t>(stream)));
 }

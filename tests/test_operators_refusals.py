@@ -54,3 +54,11 @@ def test_append(lib):
             dict(D=96), dict(S=0), dict(dt=2))
     assert call(rows=None) == CUDA
     assert call(k_new=at(0), v_new=at(0)) == CUDA      # the same rows as K and V are read alone
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+def test_read(lib, dt):
+    def call(cache=at(0), scale=at(1), start=at(2), n=at(3), L=2, B=8, H=3, N=16, D=64, S=40, out=at(4), dt=dt):
+        return lib.ppd_kv4_read(cache, scale, start, n, L, B, H, N, D, S, out, dt, None)
+    refused(call, [("out", i) for i in ("cache", "scale", "start", "n")], *(dict([(x, None)]) for x in ("cache", "scale", "start", "n", "out")),
+            *(dict([(x, at(20, 8))]) for x in ("cache", "scale", "out")), dict(L=0), dict(B=0), dict(H=0), dict(N=0), dict(D=256), dict(S=0), dict(dt=5))
