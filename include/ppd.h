@@ -360,7 +360,8 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
  * decoding.  out is bf16 [L,B,H*G,T,D]: products and sums are fp32, and the
  * probabilities meet V as two bf16 terms (2^-18), so that the output's rounding is
  * all that shows; lse fp32 [L,B,H*G,T] or NULL.  parent, prefix_len, dev_status as in ppd_tree_attention.  A NaN or
- * an infinity in a tree row may reach every query of the tree.
+ * an infinity in a tree row may reach every query of the tree.  Outputs and workspace share no
+ * memory with each other or with what is read; out may be q itself where q is bf16.
  * Workspace: ppd_kv4_attention_workspace_bytes(...) bytes (0 where none is
  * used); without one the keys of a slice are not shared out to several SMs.
  */

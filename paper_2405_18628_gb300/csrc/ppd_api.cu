@@ -1043,6 +1043,13 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
     const long long slices = (long long)L * B * H;
     const Kv4Ws w = kv4_workspace(L, B, H, G, T, D, S_max);
     const bool ws_ok = workspace && ws_bytes >= w.total && aligned(workspace, kAlign);
+    const size_t cached = (size_t)slices * S_max, rows = (size_t)slices * G * T, nb = (size_t)B * 4, elem = dt == PPD_F32 ? 4 : 2;
+    const Mem scratch{ws_ok && w.total ? workspace : nullptr, w.total}, o{out, rows * D * 2}, l{lse, rows * 4}, st{dev_status, nb}, q_rows{q, rows * D * elem};
+    if (share_memory({o, l, st, scratch},
+                     {{k_cache, cached * (D / 2)}, {k_scale, cached * (D / 32)}, {v_cache, cached * (D / 2)}, {v_scale, cached * (D / 32)},
+                      {k_tree, (size_t)slices * T * D * elem}, {v_tree, (size_t)slices * T * D * elem}, {prefix_len, nb}, {parent, nb * T}}) ||
+        share_memory({l, st, scratch}, {q_rows}) || (!(q == out && dt == PPD_BF16) && share_memory({o}, {q_rows})))
+        return PPD_ERR_INVALID_ARG;
     ppd::Kv4AttnParams p{};
     p.q = q;
     p.k_cache = k_cache, p.k_scale = k_scale, p.v_cache = v_cache, p.v_scale = v_scale;

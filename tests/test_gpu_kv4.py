@@ -279,3 +279,21 @@ def test_workloads_trees_run(cuda_device):
         c.parent = [W.make_tree(np.random.default_rng(1), w)[0].tolist()]
         c.run(ppd)
         c.check()
+
+
+@pytest.mark.parametrize("T", [1, 24, 90])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_attention_into_its_queries(cuda_device, T, workspace):
+    """The output may take the queries' place, and a call repeats itself bit for bit."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 2, 3, 2, 2, 128, T, [1500, 0, 333], 1501, seed=T)
+    c.run(ppd, workspace=workspace)
+    first, lse = c.out.clone(), c.lse.clone()
+    c.run(ppd, workspace=workspace)
+    assert torch.equal(c.out, first) and torch.equal(c.lse, lse)
+    q = c.q.clone()
+    c.out = c.q
+    c.run(ppd, workspace=workspace)
+    assert torch.equal(c.out, first) and torch.equal(c.lse, lse)
+    c.q = q
+    c.check()

@@ -62,3 +62,28 @@ def test_read(lib, dt):
         return lib.ppd_kv4_read(cache, scale, start, n, L, B, H, N, D, S, out, dt, None)
     refused(call, [("out", i) for i in ("cache", "scale", "start", "n")], *(dict([(x, None)]) for x in ("cache", "scale", "start", "n", "out")),
             *(dict([(x, at(20, 8))]) for x in ("cache", "scale", "out")), dict(L=0), dict(B=0), dict(H=0), dict(N=0), dict(D=256), dict(S=0), dict(dt=5))
+
+
+@pytest.mark.parametrize("T,S", [(2, 40), (16, 9000), (40, 90)])
+def test_attention(lib, T, S):
+    L, B, H, G, D = 1, 8, 3, 2, 64
+    n = lib.ppd_kv4_attention_workspace_bytes(L, B, H, G, T, D, S)
+    assert (n > 0) == (S == 9000)
+
+    def call(q=at(0), k=at(1), ks=at(2), v=at(3), vs=at(4), kt=at(5), vt=at(6), prefix=at(7), parent=at(8), L=L, B=B, H=H, G=G, T=T, D=D, S=S, dt=0,
+             scale=0.0, out=at(9), lse=at(10), status=at(11), ws=at(12), n=n):
+        return lib.ppd_tree_attention_kv4(q, k, ks, v, vs, kt, vt, prefix, parent, L, B, H, G, T, D, S, dt, scale, out, lse, status, ws, n, None)
+    inputs = ("k", "ks", "v", "vs", "kt", "vt", "prefix", "parent")
+    outs = ("out", "lse", "status")
+    pairs = [(o, i) for o in outs for i in inputs] + [(o, "q") for o in outs[1:]] + [("out", "lse"), ("out", "status"), ("lse", "status")]
+    refused(call, pairs, *(dict([(x, None)]) for x in ("q", *inputs, "out", "status")),
+            *(dict([(x, at(20, 8))]) for x in ("q", "k", "ks", "v", "vs", "kt", "vt", "out")), *(dict([(x, 0)]) for x in "LBHGTDS"), dict(T=513),
+            dict(D=80), dict(dt=3), dict(scale=float("nan")), dict(lse=at(20, 2)), dict(out=at(0, 16)), dict(q=at(9, 16)), dict(dt=1, out=at(0)))
+    if n:      # a workspace that the call uses
+        for p in (*inputs, "q", *outs):
+            given = inspect.signature(call).parameters[p].default
+            assert call(ws=given) == INVALID, p
+        assert call(ws=None, n=0) == CUDA
+    assert call(out=at(0)) == CUDA         # a block writes the rows that it alone has read
+    assert call(lse=None) == CUDA
+    assert call(k=at(1), v=at(1), ks=at(2), vs=at(2)) == CUDA
