@@ -386,6 +386,7 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
  *   k_cache: with k_scale the codes of a 4-bit cache, without (NULL) bf16
  *   [L,B,H,S_max,D].  Run it before or after the rows enter the cache.
  * accept_len < 1 (a failed sequence) or a prefix outside the cache: nothing.
+ * weight shares no memory with what is read.
  */
 ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cache,
                              const uint8_t *k_scale, const void *k_tree, const int32_t *path,

@@ -1103,6 +1103,11 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(k_scale, 16) || !aligned(k_tree, 16) || !aligned(lse, 4) ||
         !aligned(weight, 4))
         return PPD_ERR_INVALID_ARG;
+    const size_t slices = (size_t)L * B * H, rows = slices * G * T, cached = slices * S_max, nb = (size_t)B * 4, elem = dt == PPD_F32 ? 4 : 2;
+    if (share_memory({{weight, cached * 4}},
+                     {{q, rows * D * elem}, {lse, rows * 4}, {k_cache, cached * (k_scale ? D / 2 : 2 * D)}, {k_scale, cached * (D / 32)},
+                      {k_tree, slices * T * D * elem}, {path, nb * T}, {accept_len, nb}, {prefix_len, nb}}))
+        return PPD_ERR_INVALID_ARG;
     ppd::KvWeightParams p{};
     p.q = q;
     p.lse = lse;

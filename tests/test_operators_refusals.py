@@ -87,3 +87,18 @@ def test_attention(lib, T, S):
     assert call(out=at(0)) == CUDA         # a block writes the rows that it alone has read
     assert call(lse=None) == CUDA
     assert call(k=at(1), v=at(1), ks=at(2), vs=at(2)) == CUDA
+
+
+@pytest.mark.parametrize("kv4", [True, False])
+def test_weight_add(lib, kv4):
+    def call(q=at(0), lse=at(1), k=at(2), ks=at(3) if kv4 else None, kt=at(4), path=at(5), accept=at(6), prefix=at(7), L=2, B=8, H=3, G=2, T=16, D=64,
+             S=40, dt=0, scale=0.0, weight=at(8)):
+        return lib.ppd_kv_weight_add(q, lse, k, ks, kt, path, accept, prefix, L, B, H, G, T, D, S, dt, scale, weight, None)
+    inputs = ("q", "lse", "k", "kt", "path", "accept", "prefix")
+    refused(call, [("weight", i) for i in (*inputs, *(("ks",) if kv4 else ()))], *(dict([(x, None)]) for x in (*inputs, "weight")),
+            *(dict([(x, at(20, 8))]) for x in ("q", "k", "ks", "kt")), dict(lse=at(20, 2)), dict(weight=at(20, 2)), *(dict([(x, 0)]) for x in "LBHGTDS"),
+            dict(T=513), dict(D=100), dict(dt=7), dict(scale=float("inf")))
+    # the whole extent of the cache counts: rows of D / 2 bytes with scales, of 2 D without
+    rows = 2 * 8 * 3 * 40
+    assert call(weight=at(2, rows * (32 if kv4 else 128) - 16)) == INVALID
+    assert call(weight=at(2, rows * (32 if kv4 else 128))) == CUDA
