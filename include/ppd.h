@@ -409,7 +409,8 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
  *   new_len int32 [B] = min(length, budget); rows beyond it are not written
  *   dev_status int32 [B]: PPD_ERR_CAPACITY for a length outside [0, S_max]
  *   (nothing moves, kept -1, new_len = length)
- * kept, new_len and dev_status are no part of length's memory.
+ * kept, new_len and dev_status share no memory with each other, with length or with a plane
+ * or the weights; destinations share none with length.
  * planes, out_planes and row_bytes are host arrays, read before the call returns.
  * budget <= S_max and S_out, n_sink + n_recent <= budget.
  */

@@ -1141,9 +1141,8 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
         return PPD_ERR_INVALID_ARG;
     // every block reads the lengths: none may be written meanwhile
     const size_t nb = (size_t)B * 4;
-    if (overlaps(new_len, nb, length, nb) || overlaps(dev_status, nb, length, nb) ||
-        overlaps(kept, (size_t)slices * budget * 4, length, nb))
-        return PPD_ERR_INVALID_ARG;
+    const Mem kept_m{kept, (size_t)slices * budget * 4}, new_len_m{new_len, nb}, status_m{dev_status, nb}, length_m{length, nb};
+    if (share_memory({kept_m, new_len_m, status_m}, {length_m})) return PPD_ERR_INVALID_ARG;
     ppd::KvEvictParams p{};
     p.weight = weight;
     p.length = length;
@@ -1163,8 +1162,11 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
         pl.unit = 16;
         while (pl.row_bytes % pl.unit || !aligned(pl.src, pl.unit) || !aligned(pl.dst, pl.unit)) pl.unit /= 2;
     }
-    // a destination may be its own source, and shares no byte with another plane
-    for (int i = 0; i < p.planes; ++i)
+    // a destination may be its own source, and shares no byte with another plane; the other outputs
+    // share none with a plane
+    for (int i = 0; i < p.planes; ++i) {
+        const Mem src{p.plane[i].src, (size_t)p.slices * S_max * p.plane[i].row_bytes}, dst{p.plane[i].dst, (size_t)p.slices * S_out * p.plane[i].row_bytes};
+        if (share_memory({dst}, {length_m}) || share_memory({kept_m, new_len_m, status_m}, {src, dst})) return PPD_ERR_INVALID_ARG;
         for (int j = 0; j < p.planes; ++j) {
             const size_t ni = (size_t)p.slices * S_out * p.plane[i].row_bytes;
             const size_t ns = (size_t)p.slices * S_max * p.plane[j].row_bytes;
@@ -1173,6 +1175,7 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
             if (!(i == j && p.plane[i].src == p.plane[i].dst) && overlaps(p.plane[i].dst, ni, p.plane[j].src, ns))
                 return PPD_ERR_INVALID_ARG;
         }
+    }
     for (int i = 0; i < p.planes; ++i) {
         ppd::KvPlane &pl = p.plane[i];
         const int per_row = pl.row_bytes / pl.unit;

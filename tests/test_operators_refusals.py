@@ -102,3 +102,33 @@ def test_weight_add(lib, kv4):
     rows = 2 * 8 * 3 * 40
     assert call(weight=at(2, rows * (32 if kv4 else 128) - 16)) == INVALID
     assert call(weight=at(2, rows * (32 if kv4 else 128))) == CUDA
+
+
+def test_evict(lib):
+    def call(budget=4, sink=1, recent=1, S_max=10, S_out=10, planes=(at(0).value, at(1).value), outs=(at(2).value, at(3).value), rows=(16, 3), n=None,
+             weight=at(4), out_w=at(5), length=at(6), kept=at(7), new_len=at(8), status=at(9), L=1, B=8, H=2):
+        k = len(planes)
+        src, dst = (ctypes.c_void_p * k)(*planes), (ctypes.c_void_p * k)(*outs)
+        return lib.ppd_kv_evict(weight, out_w, src, dst, (ctypes.c_int * k)(*rows), k if n is None else n, length, L, B, H, S_max, S_out, budget,
+                                sink, recent, kept, new_len, status, None)
+    p0, p1, o0, o1 = (at(i).value for i in range(4))
+    own = ("kept", "new_len", "status")
+    refused(call, [(o, i) for o in (*own, "out_w") for i in ("length",)] + [(o, w) for o in own for w in ("weight", "out_w")] +
+            [("kept", "new_len"), ("kept", "status"), ("new_len", "status")],
+            *(dict([(x, None)]) for x in ("weight", "out_w", "length", *own)), dict(budget=0), dict(budget=11), dict(budget=9, S_out=8), dict(sink=-1),
+            dict(recent=-1), dict(sink=3, recent=2), dict(sink=5, recent=0), dict(sink=0, recent=5), dict(rows=(0, 3)), dict(rows=(16, 1025)),
+            dict(planes=(None, p1)), dict(outs=(o0, None)), dict(n=-1), dict(L=0), dict(B=0), dict(H=0), dict(S_max=0), dict(S_out=0),
+            dict(planes=tuple(at(20 + i).value for i in range(9)), outs=tuple(at(30 + i).value for i in range(9)), rows=(4,) * 9),
+            dict(outs=(p0 + 16, o1)),                         # over its own source, not in place
+            dict(outs=(p0, o1), S_out=8),                     # in place with another capacity
+            dict(out_w=at(4), S_out=8),
+            dict(outs=(p1, o1)), dict(outs=(o0, p0)),         # over the other's source
+            dict(outs=(o0, o0 + 16)), dict(outs=(o0, at(5).value)), dict(outs=(at(4).value, o1)),   # two destinations; the weights'
+            *(dict([(x, ctypes.c_void_p(p))]) for x in own for p in (p0, p1, o0, o1)), dict(outs=(at(6).value, o1)), dict(weight=at(20, 2)),
+            dict(out_w=at(20, 2)))
+    assert lib.ppd_kv_evict(at(4), at(5), None, None, None, 1, at(6), 1, 8, 2, 10, 10, 4, 1, 1, at(7), at(8), at(9), None) == INVALID
+    assert call(planes=(), outs=(), rows=()) == CUDA
+    assert call(outs=(p0, p1), out_w=at(4)) == CUDA           # in place
+    assert call(outs=(p0, o1)) == CUDA
+    assert call(budget=8, S_out=8, sink=8, recent=0) == CUDA
+    assert call(rows=(1, 1024)) == CUDA
