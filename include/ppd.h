@@ -440,6 +440,8 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
  *   accept_prob fp32 [B,T] or NULL: a of the tested nodes, -1 elsewhere
  * Other arguments, outputs and errors as in ppd_accept_path (a draft_row outside
  * [-1, n_draft) of a candidate: PPD_ERR_TREE).  temperature > 0; V <= 393,216.
+ * Outputs share no memory with each other; one of [B] may take the place of prefix_len, one
+ * of [B,T] that of cand_tokens, parent, draft_row or u, and they share none with inputs else.
  * A test whose sides agree to within float rounding, and a draw between tokens that
  * do, may go either way against a higher-precision evaluation.
  */

@@ -1218,6 +1218,16 @@ ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, co
     while (cluster > 1 && (((long long)B * cluster > 3ll * num_sms() && share(cluster / 2) <= 12800) || share(cluster) < 2048)) cluster /= 2;
     const int chunk = share(cluster);
     if (chunk > ppd::kSampleMaxChunk) return PPD_ERR_UNSUPPORTED;
+    // the CTAs of a sequence read its entries before one of them writes there, those of another may not have
+    const size_t nb = (size_t)B * 4, nodes = nb * T;
+    const Mem outs[] = {{accept_len, nb}, {next_token, nb}, {new_prefix_len, nb}, {dev_status, nb}, {path, nodes}, {accept_prob, nodes}};
+    const Mem ins[] = {{prefix_len, nb}, {cand_tokens, nodes}, {parent, nodes}, {draft_row, nodes}, {u, nodes}};
+    for (const Mem &o : outs) {
+        if (share_memory({o}, {{logits, nodes * V}, {noise, nb * V}, {draft_probs, nb * V * (draft_probs ? n_draft : 0)}})) return PPD_ERR_INVALID_ARG;
+        for (const Mem &i : ins)
+            if (!(o.p == i.p && o.n == i.n) && share_memory({o}, {i})) return PPD_ERR_INVALID_ARG;
+    }
+    if (share_memory({outs[0], outs[1], outs[2], outs[3], outs[4], outs[5]}, {})) return PPD_ERR_INVALID_ARG;
     ppd::SampleParams p{logits, cand_tokens, parent, prefix_len, draft_probs, draft_row, u, noise, accept_len, path,
                         next_token, new_prefix_len, dev_status, accept_prob, B, T, V, S_max, draft_probs ? n_draft : 0,
                         1.4426950408889634f / temperature, chunk};

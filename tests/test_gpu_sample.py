@@ -192,3 +192,26 @@ def test_emitted_tokens_have_the_targets_distribution(cuda_device):
         count = torch.bincount(tok, minlength=V).double()
         sd = (B * p * (1 - p)).sqrt()
         assert ((count - B * p).abs() < 4 * sd).all(), (count.tolist(), (B * p).tolist())
+
+
+@pytest.mark.parametrize("V", [700, 32000])
+def test_outputs_in_the_place_of_inputs(cuda_device, V):
+    """New lengths over the lengths, the path over the candidates, probabilities over the random
+    numbers: what separate memory gives, failed sequences among them."""
+    from paper_2405_18628_gb300 import ppd
+    dev, B, T = cuda_device, 9, 16
+    logits, cand, parent, u, noise, probs, row = _case(B, T, V, "some", 5, 0.7)
+    prefix = [10 + b for b in range(B)]
+    prefix[2], prefix[5], parent[7][3] = -1, 5001, 3
+    want, prob = _outputs(B, T, dev)
+    lg, noise, probs, row = logits.to(dev), noise.to(dev), probs.to(dev), _i32(row, dev)
+    ppd.ppd_sample_accept(lg, _i32(cand, dev), _i32(parent, dev), _i32(prefix, dev), 5000, 0.7, u.to(dev), noise, accept_prob=prob, draft_probs=probs,
+                          draft_row=row, **want)
+    assert [x != 0 for x in want["dev_status"].tolist()] == [b in (2, 5, 7) for b in range(B)]
+    o, _ = _outputs(B, T, dev)
+    length, c, w = _i32(prefix, dev), _i32(cand, dev), u.to(dev)
+    o.update(new_prefix_len=length, path=c)
+    ppd.ppd_sample_accept(lg, c, _i32(parent, dev), length, 5000, 0.7, w, noise, accept_prob=w, draft_probs=probs, draft_row=row, **o)
+    for k in want:
+        assert torch.equal(o[k], want[k]), k
+    assert torch.equal(w, prob)

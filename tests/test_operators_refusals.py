@@ -132,3 +132,29 @@ def test_evict(lib):
     assert call(outs=(p0, o1)) == CUDA
     assert call(budget=8, S_out=8, sink=8, recent=0) == CUDA
     assert call(rows=(1, 1024)) == CUDA
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_sample(lib, drawn):
+    def call(logits=at(0), cand=at(1), parent=at(2), prefix=at(3), probs=at(4) if drawn else None, row=at(5) if drawn else None, u=at(6), noise=at(7),
+             B=8, T=4, V=100, n_draft=3, S=10, temp=0.7, accept_len=at(8), path=at(9), nxt=at(10), new_len=at(11), prob=at(12), status=at(13)):
+        return lib.ppd_sample_accept(logits, cand, parent, prefix, probs, row, u, noise, B, T, V, n_draft, S, temp, accept_len, path, nxt, new_len, prob,
+                                     status, None)
+    outs = ("accept_len", "path", "nxt", "new_len", "prob", "status")
+    required = ("logits", "cand", "parent", "prefix", "u", "noise", *outs[:4], "status")
+    given = {k: v.default for k, v in inspect.signature(call).parameters.items()}
+    refused(call, [(a, b) for a in outs for b in outs if a < b], *(dict([(x, None)]) for x in required), dict(B=0), dict(T=0), dict(T=513), dict(V=0),
+            dict(S=0), dict(temp=0.0), dict(temp=-1.0), dict(temp=float("nan")), dict(temp=float("inf")), dict(temp=1e-39),
+            *(dict([(x, at(20, 2))]) for x in ("logits", "u", "noise", "prob")),
+            *((dict(probs=None), dict(row=None), dict(n_draft=0), dict(probs=at(20, 2))) if drawn else (dict(probs=at(4)), dict(row=at(5)))))
+    # an output per sequence or per node may take the whole place of an input of that size (a
+    # sequence's CTAs have all read it by then), and share no other bytes with what is read
+    inputs = ("logits", "cand", "parent", "prefix", "u", "noise", *(("probs", "row") if drawn else ()))
+    for o in outs:
+        for i in inputs:
+            same = (o in ("path", "prob") and i in ("cand", "parent", "row", "u")) or (o not in ("path", "prob") and i == "prefix")
+            assert call(**{o: given[i]}) == (CUDA if same else INVALID), (o, i)
+            assert call(**{o: shifted(given[i], 16)}) == INVALID, (o, i)
+            assert call(**{i: shifted(given[o], 16)}) == INVALID, (o, i)
+    assert call(prob=None) == CUDA
+    assert call(V=8 * 48 * 1024 + 1) == UNSUPPORTED
