@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(128, (KvWeight<D, KV4>::BLOCKS)) kv_weight_ker
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int path_s[kMaxTree];
     __shared__ __align__(16) float neg_lse[kWeightRows];
-    __shared__ __align__(8) int place[kWeightRows];   // of the rows on the path
+    __shared__ __align__(8) int place[kWeightRows];   // of the rows on the path; -1: none, no row of its own
     uint2 (*q_s)[D / 16][32] = reinterpret_cast<uint2(*)[D / 16][32]>(smem + C::OFF_Q);
     pdl_release();
     pdl_wait();
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(128, (KvWeight<D, KV4>::BLOCKS)) kv_weight_ker
                                        : make_uint2(0u, 0u);
             if (t == 0) {
                 neg_lse[8 * x + g] = real ? -1.4426950408889634f * ld_input(p.lse + row) : -INFINITY;
-                place[8 * x + g] = a;
+                place[8 * x + g] = real ? a : -1;
             }
         }
         __syncthreads();
@@ -180,15 +180,15 @@ __global__ void __launch_bounds__(128, (KvWeight<D, KV4>::BLOCKS)) kv_weight_ker
                     mma_bf16(s[1], k[1][y], q.x, q.y);
                 }
                 const float2 nl = *reinterpret_cast<const float2 *>(neg_lse + 8 * x + 2 * t);
-                if (!tree) {
+                if (KV4 && !tree) {   // (a row that is none: products of zeros and finite values)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1)], scale, nl.x)) + ex2(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, nl.y));
                 } else {
                     const int2 at = *reinterpret_cast<const int2 *>(place + 8 * x + 2 * t);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {   // a later node's row is not seen
-                        const int key = k0 + 8 * i + g;
+                    for (int i = 0; i < 4; ++i) {   // a later node's row is not seen, and a row that is none sees nothing (0 times an infinity)
+                        const int key = tree ? k0 + 8 * i + g : 0;
                         if (at.x >= key) sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1)], scale, nl.x));
                         if (at.y >= key) sum[i] += ex2(fmaf(s[i >> 1][2 * (i & 1) + 1], scale, nl.y));
                     }

@@ -253,3 +253,37 @@ def test_evict_of_many_short_caches(cuda_device, in_place, S, budget, sink, rece
         live = (kept >= 0).reshape(*kept.shape, *[1] * (src.dim() - 4))
         assert torch.equal(dst[..., :budget, :] if src.dim() == 5 else dst[..., :budget],
                            torch.where(live, rows, old[..., :budget, :] if src.dim() == 5 else old[..., :budget]))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "kv4"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,n", [(1, 1), (1, 3), (2, 4), (3, 7), (5, 9)])
+def test_weights_of_infinite_rows(cuda_device, cache, D, G, n):
+    """Rows whose every score is -inf get no weight, of +inf infinite weight, of NaN NaN, however many
+    queries there are; all others what they get without such rows."""
+    from paper_2405_18628_gb300 import ppd
+    dev, T, P = cuda_device, 12, 70
+    g = torch.Generator(device=dev)
+    g.manual_seed(G * 10 + n)
+    r = lambda *s: torch.randn(s, device=dev, generator=g)  # noqa: E731
+    q, kt = r(1, 1, G, T, D).to(torch.bfloat16), r(1, 1, 1, T, D).to(torch.bfloat16)
+    q[..., 0] = q[..., 0].abs() + 1                # the scores' sign is that of the rows' first channel
+    lse = 4 + 0.3 * r(1, 1, G, T)
+    path = sorted(np.random.default_rng(n).permutation(T)[:n].tolist())
+    rest = dict(path=_i32([path + [-1] * (T - n)], dev), accept_len=_i32([n], dev), prefix_len=_i32([P], dev))
+    if cache == "kv4":
+        kc, ks = O.kv4_quantise(r(1, 1, 1, P + T, D))
+    else:
+        kc, ks = r(1, 1, 1, P + T, D).to(torch.bfloat16), None
+    start = r(1, 1, 1, P + T).abs()
+    plain, weight = start.clone(), start.clone()
+    ppd.ppd_kv_weight_add(q, lse, kc, kt, weight=plain, k_scale=ks, **rest)
+    kt[0, 0, 0, path[n // 2], 0] = -math.inf
+    want = plain.clone()
+    want[..., P + n // 2] = 0
+    if cache == "bf16":
+        for row, x, w in ((5, -math.inf, start[..., 5]), (31, -math.inf, start[..., 31]), (9, math.inf, math.inf), (66, math.nan, math.nan)):
+            kc[..., row, 0] = x
+            want[..., row] = w
+    ppd.ppd_kv_weight_add(q, lse, kc, kt, weight=weight, k_scale=ks, **rest)
+    assert torch.equal(weight.nan_to_num(-7.0), want.nan_to_num(-7.0))
