@@ -320,7 +320,7 @@ ppd_status ppd_node_argmax_noalloc(const float *logits, int B, int T, int V, int
  * 2 (p % 4) + p / 4 of the eight.  A scale byte b stands for
  * s = (1 + (b % 8) / 8) * 2^(b / 8 - 20), a code c for s * (c - 8): 4.25 bits a
  * channel; every value is a bf16 number and any bytes are finite values.  All
- * tensors are 16-byte aligned.
+ * tensors are 16-byte aligned.  S_max is 2^31 - 65,537 at most in what follows.
  * ---------------------------------------------------------------------------
  */
 

@@ -917,6 +917,9 @@ ppd_status ppd_selftest_umma(const void *a, const void *b, float *d, int mode, i
 
 // ------------------------------------------------------------------ 4-bit cache, eviction, sampling
 
+// Rows that a slice holds at most: kernels count rows in 32 bits, and steps pass the last one.
+constexpr int kMaxRows = 2147483647 - 65536;
+
 // Shapes of a 4-bit cache's slices; G query heads share a K/V head.
 static bool kv4_dims_ok(int L, int B, int H, int G, int T, int D, int S_max)
 {
@@ -940,7 +943,7 @@ ppd_status ppd_kv4_append(const void *k_new, const void *v_new, uint8_t *k_cache
     if (share_memory({{k_cache, cached * (D / 2)}, {k_scale, cached * (D / 32)}, {v_cache, cached * (D / 2)}, {v_scale, cached * (D / 32)}, {dev_status, nb}},
                      {{k_new, fresh}, {v_new, fresh}, {rows, nb * T}, {start, nb}, {n_new, nb}}))
         return PPD_ERR_INVALID_ARG;
-    if (T > 65535 * 64) return PPD_ERR_UNSUPPORTED;
+    if (T > 65535 * 64 || S_max > kMaxRows) return PPD_ERR_UNSUPPORTED;
     ppd::Kv4AppendParams p{k_new, v_new, k_cache, v_cache, k_scale, v_scale, rows, start, n_new, dev_status,
                            (long long)L * B * H, B, H, T, D, S_max, dt == PPD_F32};
     return cuda_status(ppd::launch_kv4_append(p, static_cast<cudaStream_t>(stream)));
@@ -957,6 +960,7 @@ ppd_status ppd_kv4_read(const uint8_t *cache, const uint8_t *scale, const int32_
     if (share_memory({{out, (size_t)L * B * H * N * D * (dt == PPD_F32 ? 4 : 2)}},
                      {{cache, cached * (D / 2)}, {scale, cached * (D / 32)}, {start, nb}, {n, nb}}))
         return PPD_ERR_INVALID_ARG;
+    if (S_max > kMaxRows) return PPD_ERR_UNSUPPORTED;
     ppd::Kv4ReadParams p{cache, scale, start, n, out, (long long)L * B * H, B, H, N, D, S_max, dt == PPD_F32};
     return cuda_status(ppd::launch_kv4_read(p, static_cast<cudaStream_t>(stream)));
 }
@@ -1003,7 +1007,7 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
         // time: the merge grid and the parts' way through memory).  Whole / shared, 64 tokens: 23 / 20 us
         // (8 slices of 2048 keys), 29 / 40 us (256 of 1024)
         const long long units = slices * w.row_blocks, t_u = (S_max + 127) / 128 + (T + 127) / 128, sms = split_grid();
-        w.share = B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + 6 < (units + sms - 1) / sms * t_u;
+        w.share = B <= ppd::kSplitMaxB && units * t_u <= 2147483647 && (units * t_u + sms - 1) / sms + 6 < (units + sms - 1) / sms * t_u;
         if (w.share) {
             w.rec = align_up((size_t)2 * split_grid() * ppd::kv4_slot_floats(D, w.tp) * 4);
             w.total = align_up(w.rec + (size_t)split_grid() * sizeof(ppd::SplitRecord));
@@ -1021,7 +1025,7 @@ static Kv4Ws kv4_workspace(int L, int B, int H, int G, int T, int D, int S_max)
 
 size_t ppd_kv4_attention_workspace_bytes(int L, int B, int H, int G, int T, int D, int S_max)
 {
-    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT) return 0;
+    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT || S_max > kMaxRows) return 0;
     return kv4_workspace(L, B, H, G, T, D, S_max).total;
 }
 
@@ -1040,6 +1044,7 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(k_scale, 16) || !aligned(v_cache, 16) ||
         !aligned(v_scale, 16) || !aligned(k_tree, 16) || !aligned(v_tree, 16) || !aligned(out, 16) || !aligned(lse, 4))
         return PPD_ERR_INVALID_ARG;
+    if (S_max > kMaxRows) return PPD_ERR_UNSUPPORTED;
     const long long slices = (long long)L * B * H;
     const Kv4Ws w = kv4_workspace(L, B, H, G, T, D, S_max);
     const bool ws_ok = workspace && ws_bytes >= w.total && aligned(workspace, kAlign);
@@ -1108,6 +1113,7 @@ ppd_status ppd_kv_weight_add(const void *q, const float *lse, const void *k_cach
                      {{q, rows * D * elem}, {lse, rows * 4}, {k_cache, cached * (k_scale ? D / 2 : 2 * D)}, {k_scale, cached * (D / 32)},
                       {k_tree, slices * T * D * elem}, {path, nb * T}, {accept_len, nb}, {prefix_len, nb}}))
         return PPD_ERR_INVALID_ARG;
+    if (S_max > kMaxRows) return PPD_ERR_UNSUPPORTED;
     ppd::KvWeightParams p{};
     p.q = q;
     p.lse = lse;
@@ -1143,6 +1149,7 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
     const size_t nb = (size_t)B * 4;
     const Mem kept_m{kept, (size_t)slices * budget * 4}, new_len_m{new_len, nb}, status_m{dev_status, nb}, length_m{length, nb};
     if (share_memory({kept_m, new_len_m, status_m}, {length_m})) return PPD_ERR_INVALID_ARG;
+    if (S_max > kMaxRows || S_out > kMaxRows) return PPD_ERR_UNSUPPORTED;
     ppd::KvEvictParams p{};
     p.weight = weight;
     p.length = length;

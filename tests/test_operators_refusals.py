@@ -158,3 +158,22 @@ def test_sample(lib, drawn):
             assert call(**{i: shifted(given[o], 16)}) == INVALID, (o, i)
     assert call(prob=None) == CUDA
     assert call(V=8 * 48 * 1024 + 1) == UNSUPPORTED
+
+
+def test_capacities_that_counters_cannot_hold(lib):
+    """Row numbers are 32-bit, with room for the tiles that pass the last row; a call whose tiles are
+    past 32 bits in all takes its units whole."""
+    most = 2 ** 31 - 1 - 65536
+    ws = lib.ppd_kv4_attention_workspace_bytes
+    assert ws(1, 1, 1, 1, 1, 64, most) > 0
+    assert ws(1, 1, 1, 1, 1, 64, most + 1) == 0
+    assert ws(1, 1, 1, 2, 512, 64, 2 ** 20) > 0
+    assert ws(1, 1, 1, 128, 512, 64, most) == 0     # 1024 blocks of rows, 16 million tiles each
+    far = [ctypes.c_void_p(i << 44) for i in range(1, 14)]
+    for S, want in ((most, CUDA), (most + 1, UNSUPPORTED), (2 ** 31 - 1, UNSUPPORTED)):
+        assert lib.ppd_kv4_append(*far[:9], 1, 1, 1, 4, 64, S, 0, far[9], None) == want
+        assert lib.ppd_kv4_read(*far[:4], 1, 1, 1, 4, 64, S, far[4], 0, None) == want
+        assert lib.ppd_tree_attention_kv4(*far[:9], 1, 1, 1, 1, 4, 64, S, 0, 0.0, far[9], None, far[10], None, 0, None) == want
+        assert lib.ppd_kv_weight_add(*far[:8], 1, 1, 1, 1, 4, 64, S, 0, 0.0, far[8], None) == want
+        assert lib.ppd_kv_evict(far[0], far[1], None, None, None, 0, far[2], 1, 1, 1, S, 10, 4, 1, 1, far[3], far[4], far[5], None) == want
+        assert lib.ppd_kv_evict(far[0], far[1], None, None, None, 0, far[2], 1, 1, 1, 10, S, 4, 1, 1, far[3], far[4], far[5], None) == want
