@@ -287,3 +287,39 @@ def test_weights_of_infinite_rows(cuda_device, cache, D, G, n):
             want[..., row] = w
     ppd.ppd_kv_weight_add(q, lse, kc, kt, weight=weight, k_scale=ks, **rest)
     assert torch.equal(weight.nan_to_num(-7.0), want.nan_to_num(-7.0))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("B,H,S,budget,sink,recent", [(12, 22, 31, 10, 2, 3), (12, 43, 128, 77, 0, 5), (9, 15, 33, 32, 0, 0), (7, 3, 127, 40, 3, 2)])
+def test_evict_of_short_caches_of_any_weights(cuda_device, in_place, B, H, S, budget, sink, recent):
+    """NaN, zeros of both signs, negative, tiny and infinite weights, and rows in more pieces than a warp moves at
+    once; hundreds of slices, and (the last) too few for a warp each."""
+    from paper_2405_18628_gb300 import ppd
+    dev, L = cuda_device, 2
+    g = torch.Generator(device=dev)
+    g.manual_seed(S)
+    lens = [int(x) for x in np.linspace(0, S, B)]
+    odd = torch.tensor([math.nan, -math.nan, 0.0, -0.0, -1.0, 1.0, math.inf, -math.inf, 1e-42, -1e-42, 3.4e38, 0.5], device=dev)
+    weight = odd[torch.randint(0, len(odd), (L, B, H, S), device=dev, generator=g)]
+    planes = [torch.randint(0, 256, (L, B, H, S, w), dtype=torch.uint8, device=dev, generator=g) for w in (1023, 64, 513)]
+    host = [p.clone() for p in planes] + [weight.clone()]
+    outs = planes if in_place else [torch.full((L, B, H, budget, p.shape[4]), 3, dtype=torch.uint8, device=dev) for p in planes]
+    out_w = weight if in_place else torch.full((L, B, H, budget), 3.0, device=dev)
+    before = [x.clone() for x in outs + [out_w]]
+    kept = torch.full((L, B, H, budget), 77, dtype=torch.int32, device=dev)
+    new_len, status = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
+    ppd.ppd_kv_evict(weight, planes, _i32(lens, dev), budget, sink, recent, kept, new_len, status, out_planes=None if in_place else outs,
+                     out_weight=None if in_place else out_w)
+    assert new_len.tolist() == [min(x, budget) for x in lens] and (status == 0).all()
+    ranks, got = host[-1].tolist(), kept.tolist()
+    for l in range(L):
+        for b in range(B):
+            for h in range(H):
+                want = O.evict(ranks[l][b][h], lens[b], budget, sink, recent)
+                assert got[l][b][h] == want + [-1] * (budget - len(want)), (l, b, h)
+    at, live = kept.long().clamp(min=0), kept >= 0
+    raw = lambda x: x.view(torch.int32) if x.dtype == torch.float32 else x  # noqa: E731
+    for src, dst, old in zip(host, outs + [out_w], before):
+        src, dst, old = (raw(x).reshape(L, B, H, x.shape[3], -1) for x in (src, dst, old))
+        rows = torch.take_along_dim(src, at[..., None], 3)
+        assert torch.equal(dst[..., :budget, :], torch.where(live[..., None], rows, old[..., :budget, :]))

@@ -297,3 +297,44 @@ def test_attention_into_its_queries(cuda_device, T, workspace):
     assert torch.equal(c.out, first) and torch.equal(c.lse, lse)
     c.q = q
     c.check()
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,G", [(1, 1), (1, 8), (2, 8), (24, 1), (64, 1), (40, 2), (200, 1)])
+def test_attention_of_maxima_that_come_late(cuda_device, T, G, D, dtype, workspace):
+    """Keys that outweigh all before them by far, after many tiles: a prefix row, the root, and the last
+    node (which only itself sees), for references that move when sums have been added up."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 1, 2, 2, G, D, T, [1000, 931], 1003, dtype=dtype, seed=T + G)
+    c.q[..., :4] = c.q[..., :4].abs() + 1
+    for b, row in ((0, 900), (1, 930)):
+        k = torch.randn(2, D, device=cuda_device, generator=torch.Generator(device=cuda_device).manual_seed(b))
+        k[:, :4] = 40.0
+        c.kc[0, b, :, row], c.ks[0, b, :, row] = O.kv4_quantise(k)
+    c.kt[0, :, :, 0, :4] = 80.0
+    if T > 1:
+        c.kt[0, :, :, T - 1, :4] = 160.0
+    c.run(ppd, workspace=workspace)
+    c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,G", [(1, 1), (1, 8), (24, 1), (64, 1), (90, 1)])
+def test_attention_fp32_operands_of_both_head_sizes(cuda_device, T, G, D):
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 1, 2, 2, G, D, T, [300, 299], 301, dtype=torch.float32, seed=T, size=4.0)
+    c.run(ppd, scale=0.5)
+    c.check(scale=0.5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T", [1, 7, 30, 64, 100])
+@pytest.mark.parametrize("L,B,H", [(1, 4, 8), (2, 3, 1)])
+def test_attention_of_capacities_far_above_the_lengths(cuda_device, L, B, H, T, D):
+    """Parts of a slice's keys without any: planned by the capacity, which a program allocates once."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, L, B, H, 1, D, T, [500, 0, 33, 1][:B], 16384, seed=T)
+    c.run(ppd)
+    c.check()
