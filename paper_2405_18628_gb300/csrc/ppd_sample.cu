@@ -51,6 +51,7 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
 {
     extern __shared__ __align__(16) float e[];   // this CTA's share: R over a factor of the warp
     __shared__ SampleShared s;
+    cluster_sync();   // every CTA of the cluster has started before one stores into another's shared memory
     pdl_release();
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -82,9 +83,6 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
     bad = __syncthreads_or(bad);
     const int P = ld_input(p.prefix_len + b);
     int err = bad ? kErrTree : (P < 0 || P > p.S_max ? kErrCapacity : kOk);
-    // every CTA of the cluster has started, and has read its inputs per node, before one stores into
-    // another's shared memory, or writes an output
-    cluster_sync();
 
     int phase = 0;
     float M = 0.f, f = 1.f, rest = 0.f;   // R = f e; rest: the sum of R in the shares
@@ -356,6 +354,8 @@ __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const 
             p.next_token[b] = (int)(0xFFFFFFFFu - (uint32_t)best);
         }
     }
+    // (a failed sequence: every CTA has read its inputs before one writes an output in their place)
+    if (err != kOk) cluster_sync();
     if (rank != 0) return;
     __syncthreads();
     const int n_out = err == kOk ? len : 0;
