@@ -382,7 +382,8 @@ ppd_status ppd_tree_attention_kv4(const void *q, const uint8_t *k_cache, const u
  * i.e. the probabilities that the step's attention gave (lse from
  * ppd_tree_attention or ppd_tree_attention_kv4), the new rows' counted from the
  * step that accepts them.  weight fp32 [L,B,H,S_max]; other entries stay.
- *   q [L,B,H*G,T,D] and k_tree [L,B,H,T,D] of dtype dt; lse fp32 [L,B,H*G,T];
+ *   q [L,B,H*G,T,D] and k_tree [L,B,H,T,D] of dtype dt (PPD_F32 rounded to bf16 on
+ *   load); lse fp32 [L,B,H*G,T];
  *   k_cache: with k_scale the codes of a 4-bit cache, without (NULL) bf16
  *   [L,B,H,S_max,D].  Run it before or after the rows enter the cache.
  * accept_len < 1 (a failed sequence) or a prefix outside the cache: nothing.
@@ -428,7 +429,8 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
  *     a = min(1, R_t / (q_t sum R)),  accepted when u[b][c] < a
  * with q = draft_probs[b][draft_row[b][c]] for a child drawn from that
  * distribution, and q_t = 1 for one that was chosen (draft_row -1, or no drafts:
- * the top guesses of ppd_next_tree).  A rejected child leaves
+ * the top guesses of ppd_next_tree); a drawn child of q_t = 0, which no draw gives, is
+ * rejected.  A rejected child leaves
  * R <- max(R / sum R - q, 0) (drawn) or R_t <- 0 (chosen); an accepted one
  * becomes the current node.  After the last node, next_token = the first v of
  * the largest R_v / noise[b][v]: with exponentially distributed noise a draw from R.
@@ -443,7 +445,8 @@ ppd_status ppd_kv_evict(const float *weight, float *out_weight, const void *cons
  * Outputs share no memory with each other; one of [B] may take the place of prefix_len, one
  * of [B,T] that of cand_tokens, parent, draft_row or u, and they share none with inputs else.
  * A test whose sides agree to within float rounding, and a draw between tokens that
- * do, may go either way against a higher-precision evaluation.
+ * do (its quotients are good to two units in the last place), may go either way against
+ * a higher-precision evaluation.
  */
 ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, const int32_t *parent,
                              const int32_t *prefix_len, const float *draft_probs,

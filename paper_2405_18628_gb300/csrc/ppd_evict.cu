@@ -15,8 +15,8 @@ namespace ppd {
 // path's own rows, each seen by itself and the nodes after it.
 //
 // A bf16 cache: bound by HBM, 1.38 GB (B = 8, up to 16,384 keys, 16 heads of two) 208 us, 6.6 TB/s.
-// 4 bits: by instruction issue and the second wave of blocks, half empty: 1024 slices of 2048 keys 51
-// us, 3.2 TB/s (the bf16 cache 95 us).
+// 4 bits: by a warp's chain from codes to products (issue slots 50 % used, the tensor pipe 15 %) and by
+// the second wave of blocks, two thirds full: 1024 slices of 2048 keys 51 us, 3.2 TB/s (the bf16 cache 95 us).
 constexpr int kWeightRows = 32;
 
 template <int D, bool KV4>

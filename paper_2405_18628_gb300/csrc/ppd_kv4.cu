@@ -182,9 +182,11 @@ cudaError_t launch_kv4_read(const Kv4ReadParams &p, cudaStream_t stream)
 // codes and scales come by asynchronous copies into a ring of the warp's own: no barrier in the
 // loop.
 //
-// Bound by instruction issue: some 735 instructions for a chunk of 32 keys (D = 128), of them 384
-// cycles of the tensor pipe; 64 x 32 slices of 2048 keys 163 us, 3.5 TB/s.  Few slices are bound by
-// a block's start and end and by the merge: 32 slices of 10,000 keys 20.4 us, 1.7 TB/s.
+// Bound by the latency of a warp's chain from codes to products, which four blocks an SM do not
+// hide: issue slots are 56 % used, the tensor pipe 29 %, and a warp waits most for results of fixed
+// latency (some 735 instructions for a chunk of 32 keys, D = 128); 64 x 32 slices of 2048 keys 163 us,
+// 3.5 TB/s.  Few slices are bound by a block's start and end and by the merge (issue 41 %): 32 slices
+// of 10,000 keys 20.4 to 21.5 us, 1.7 TB/s.
 template <int D>
 struct Kv4Few {
     static constexpr int WARPS = 4, THREADS = 128, KEYS = 32;

@@ -23,7 +23,8 @@ namespace ppd {
 // and an exchange.  Every CTA takes the same decisions from the same numbers.
 //
 // Bound by the chain of a walk's passes, not by their bytes (one sequence, 32,000 tokens, chosen
-// guesses: 9 us; 80 sequences, 50,257 tokens, drawn: 39 us, some 3 us a pass): a thread keeps to its own elements
+// guesses: 9 us; 80 sequences, 50,257 tokens, drawn: 44 us, the longest of their walks seven or eight
+// passes): a thread keeps to its own elements
 // of the share and a warp to its own maximum, so that a pass has one barrier of the block and
 // one of the cluster; the children's entries are asked for before the row.  (Asking L2 for
 // the draft row or the noise ahead of their passes made 80 sequences 42 -> 56 us.)
@@ -44,8 +45,8 @@ struct SampleShared {
     float z;
 };
 
-// VEC: 16-byte accesses, which every row allows (80 sequences of 50,256 tokens: 34 us, by elements
-// 37).
+// VEC: 16-byte accesses, which every row allows (80 sequences of 50,256 tokens: 38 us, by elements
+// 42).
 template <bool VEC>
 __global__ void __launch_bounds__(kSampleThreads, 3) sample_accept_kernel(const SampleParams p, int cluster)
 {
