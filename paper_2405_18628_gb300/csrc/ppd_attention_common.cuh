@@ -1,5 +1,5 @@
 // ppd_attention_common.cuh -- pieces shared by the two tree-attention kernels
-// (ppd_attention.cu for trees of up to 64 tokens, ppd_attention_rows.cu for
+// (ppd_attention_key.cuh for trees of up to 64 tokens, ppd_attention_rows.cuh for
 // 65..512): the unit walk and the two ways to share a unit among CTAs (work split
 // and clusters) with their merges, drain waits and the fused step's side warp.
 #pragma once

@@ -223,7 +223,7 @@ cudaError_t launch_split_merge(const AttnParams &p, int D, int grid, cudaStream_
 constexpr int kFusedMaxB = 64;
 
 // Dispatches on the padded tree size: up to 64 tokens the key-row kernel
-// (ppd_attention.cu), 65..512 the query-row kernel (ppd_attention_rows.cu).
+// (ppd_attention_key.cuh), 65..512 the query-row kernel (ppd_attention_rows.cuh).
 cudaError_t launch_tree_attention(const AttnMaps &m, const AttnParams &p, int D, int num_sms,
                                   bool programmatic, cudaStream_t stream);
 cudaError_t launch_tree_attention_rows(const AttnMaps &m, const AttnParams &p, int D, int num_sms,

@@ -8,7 +8,7 @@
 //   K     four warps make a tile's values from its codes, a key row a thread, and store
 //         them into tensor memory: the A operand of S^T = K Q^T needs no shared memory
 //   V     the same rows into shared memory, the A operand of O^T += V^T [P_hi | P_lo]^T
-//   P     by eight softmax warps as in the bf16 key-row kernel (ppd_attention.cu): a key row a
+//   P     by eight softmax warps as in the bf16 key-row kernel (ppd_attention_key.cuh): a key row a
 //         thread, lazy maxima, probabilities in two bf16 terms
 //
 // The converting warps fetch their own rows by asynchronous copies, two tiles ahead, so the
