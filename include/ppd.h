@@ -456,6 +456,104 @@ ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, co
                              float *accept_prob, int32_t *dev_status, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Many requests over one pool of pages (no paper counterpart): instead of S_max cache
+ * rows for every sequence, pages of a pool that sequences take as they grow.
+ *
+ * A pool is bf16 [L,n_pages,H,page,D], one for K and one for V; page is a power of two, 8 to 256.
+ * Row r of sequence b is row r % page of page table[b][r / page], in every layer; its slot is
+ * table[b][r / page] * page + r % page.  table int32 [B,max_pages]: entries past a sequence's
+ * pages may hold anything.  Sequences may name the same pages (a shared prefix).  Rows that a
+ * sequence or a pool can hold end at 2^31 - 65,537.  H counts K/V heads, G query heads share each.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Block tables and slots from lengths: sequence b holds old_len[b] rows, ceil(old_len / page)
+ * pages, and is to hold new_len[b] (0: a request that has ended; more: a path's or a prompt's
+ * rows, or room that is reserved).  With S the stack of free pages (free_pages[0 .. n_free-1]),
+ * first all pages that are not needed any more are pushed, in order of sequence and index, then
+ * the pages that are needed are taken: the top K of the stack for K pages, kept in that order,
+ * in order of sequence and index.  (So a call with the lengths exchanged restores tables and
+ * stack.)  Sequences are served in order while the pages, and max_slots, last: b gains rows where the pages
+ * needed by sequences up to b are no more than there are, and the rows gained no more than
+ * max_slots.  Others, and lengths outside [0, max_pages * page], get PPD_ERR_CAPACITY and stay as they are.
+ *   table, free_pages int32 [B,max_pages], [n_pages]   in place; only entries that are taken or
+ *                     pushed are written
+ *   n_free, new_n_free int32 [1]   entries of the stack before and after
+ *   out_len int32 [B]              new_len where served, else old_len
+ *   slots int32 [max_slots]        the slots of rows old_len .. new_len - 1 of the sequences that grow, one
+ *                                  sequence after the other: b's are slots[slot_start[b] .. slot_start[b+1] - 1];
+ *                                  entries past the last are not written
+ *   slot_start int32 [B+1]
+ * Tables and stack must hold what earlier calls left there (or, at the start, old_len 0 and every page
+ * once on the stack); other contents are not checked, but nothing is read or written outside the arrays.
+ * Pages that two sequences name are given back once only (by the caller's lengths).  B <= 8192.
+ * Outputs share no memory with each other or with what is read.
+ */
+ppd_status ppd_page_assign(const int32_t *old_len, const int32_t *new_len, int B, int page, int n_pages,
+                           int max_pages, int max_slots, int32_t *table, int32_t *free_pages,
+                           const int32_t *n_free, int32_t *new_n_free, int32_t *out_len, int32_t *slots,
+                           int32_t *slot_start, int32_t *dev_status, void *stream);
+
+/*
+ * Rows into pages: for every l, b, h and j < n = slot_start[b+1] - slot_start[b]
+ *     pool row slots[slot_start[b] + j]  <-  new row rows[b][j], or j without rows
+ * of K and V: an accepted path (rows = path) or prompts of several lengths (rows NULL; T as long as
+ * the longest, it may exceed the 512 of a tree).
+ *   k_new, v_new [L,B,H,T,D] PPD_BF16, or PPD_F32 (rounded to nearest even); rows int32 [B,T] or NULL
+ *   slots int32 [max_slots], slot_start int32 [B+1] as ppd_page_assign leaves them
+ * A slot outside the pool (-1) or a row index outside [0, T) writes nothing.  n < 0, n > T or slots
+ * outside [0, max_slots): PPD_ERR_CAPACITY, nothing written for that sequence.  Of a slot named twice
+ * either row stays, or parts of both.  Outputs share no memory with each other or with what is read.
+ */
+ppd_status ppd_page_append(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
+                           const int32_t *rows, const int32_t *slots, const int32_t *slot_start, int L,
+                           int B, int H, int T, int D, int page, int n_pages, int max_slots, ppd_dtype dt,
+                           int32_t *dev_status, void *stream);
+
+/*
+ * Tree-masked attention over pages: as ppd_tree_attention, the prefix rows being those of the
+ * sequence's pages.  T = 1 is plain decoding: the new token's own K/V row is its tree.
+ *   q [L,B,H*G,T,D], k_tree, v_tree [L,B,H,T,D] PPD_BF16 or PPD_F32 (rounded to bf16 on load);
+ *   out bf16 [L,B,H*G,T,D] (fp32 products and sums, one rounding); lse fp32 [L,B,H*G,T] or NULL
+ *   dev_status: PPD_ERR_TREE, or PPD_ERR_CAPACITY for a prefix outside [0, max_pages * page] or a
+ *   page of it that is not in [0, n_pages); outputs of a failed sequence are unspecified
+ * Rows of a page at or beyond prefix_len[b] are never used and may hold anything, NaN included.  A NaN or
+ * an infinity in a row that is used may reach every query of its sequence.
+ * Outputs and workspace share no memory with each other or with what is read.
+ * Workspace: ppd_paged_attention_workspace_bytes(...) bytes (S_max = max_pages * page; 0 where none is
+ * used); a bf16 call may pass none, its slices are then not cut where clusters of SMs do not fit.
+ */
+size_t ppd_paged_attention_workspace_bytes(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt);
+ppd_status ppd_tree_attention_paged(const void *q, const void *k_pages, const void *v_pages,
+                                    const int32_t *table, const void *k_tree, const void *v_tree,
+                                    const int32_t *prefix_len, const int32_t *parent, int L, int B, int H,
+                                    int G, int T, int D, int page, int n_pages, int max_pages, ppd_dtype dt,
+                                    float scale, void *out, float *lse, int32_t *dev_status, void *workspace,
+                                    size_t ws_bytes, void *stream);
+
+/*
+ * Log probabilities of given tokens: item i of sequence b asks the logits row rows[b][i] (or i,
+ * without rows) about token tokens[b][i], with p = softmax(row / temperature):
+ *   logprob fp32 [B,n]       ln p of the token
+ *   entropy fp32 [B,n]       -sum_v p_v ln p_v
+ *   rank int32 [B,n]         entries that rank before the token (NaN first, then the larger
+ *                            value, then the lower index): 0 for the best
+ *   top_tokens int32 [B,n,K], top_logprobs fp32 [B,n,K]   the K first and their ln p
+ * logits PPD_F32 or PPD_BF16 [B,T,V], any alignment of rows; temperature > 0; 0 <= K <= 32, K <= V.
+ * Token -1: logprob 0 and rank -1, the rest as asked.  Row -1 (a path's padding): as well entropy 0,
+ * top_tokens -1, top_logprobs 0.  Other tokens outside [0, V) or rows outside [0, T): as row -1, and
+ * PPD_ERR_TREE in dev_status[b].  A row that holds a NaN or +inf, or only -inf, has no distribution: NaN for
+ * logprob, entropy and top_logprobs.  A token of probability 0 has -inf.
+ * Outputs share no memory with each other or with what is read.
+ */
+ppd_status ppd_token_logprobs(const void *logits, const int32_t *tokens, const int32_t *rows, int B,
+                              int T, int V, int n, int K, ppd_dtype dt, float temperature, float *logprob,
+                              float *entropy, int32_t *rank, int32_t *top_tokens, float *top_logprobs,
+                              int32_t *dev_status, void *stream);
+
+/*
  * Kernel launches one ppd_verify_step call (typical == 0) or
  * ppd_verify_step_typical call (typical != 0) enqueues for these sizes, with
  * a workspace of ppd_workspace_bytes(...) bytes and the whole GPU available.

@@ -288,15 +288,13 @@ bool attn_dims_ok(int L, int B, int H, int T, int D, int S_max, ppd_dtype dt)
 struct AttnPlan {
     int split, cluster;
 };
-constexpr long long kClusterCostTiles = 2, kSplitCostTiles = 6;
+constexpr long long kClusterCostTiles = 2, kSplitCostTiles = 6, kPagedSplitCostTiles = 10;
 
-AttnPlan plan_attention(int L, int B, int H, int T, int S_max, bool workspace, bool clusters)
+AttnPlan plan_units(long long units, long long t_u, int B, bool workspace, bool clusters)
 {
     AttnPlan plan{0, 1};
-    const int n_tt = T > 64 ? (T + 127) / 128 : 1;
-    const long long units = (long long)L * B * H * n_tt, sms = split_grid();
+    const long long sms = split_grid();
     if (units >= sms) return plan;
-    const long long t_u = (S_max + 127) / 128 + n_tt;
     long long best = t_u;
     for (int c = 2; clusters && c <= ppd::kMaxCluster && c <= t_u && units * c <= sms; ++c) {
         const long long cost = (t_u + c - 1) / c + kClusterCostTiles;
@@ -307,6 +305,12 @@ AttnPlan plan_attention(int L, int B, int H, int T, int S_max, bool workspace, b
     }
     if (workspace && B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + kSplitCostTiles < best) plan = {1, 1};
     return plan;
+}
+
+AttnPlan plan_attention(int L, int B, int H, int T, int S_max, bool workspace, bool clusters)
+{
+    const int n_tt = T > 64 ? (T + 127) / 128 : 1;   // also the blocks of queries
+    return plan_units((long long)L * B * H * n_tt, (S_max + 127) / 128 + n_tt, B, workspace, clusters);
 }
 
 // Enqueue the attention of all L*B*H slices (bf16 operands).
@@ -1239,6 +1243,202 @@ ppd_status ppd_sample_accept(const float *logits, const int32_t *cand_tokens, co
                         next_token, new_prefix_len, dev_status, accept_prob, B, T, V, S_max, draft_probs ? n_draft : 0,
                         1.4426950408889634f / temperature, chunk};
     return cuda_status(ppd::launch_sample_accept(p, cluster, static_cast<cudaStream_t>(stream)));
+}
+
+// ------------------------------------------------------------------ a pool of pages
+
+// log2 of a page's rows, or -1 where such pages are not supported: powers of two from 8 (a box of
+// the attention's copies starts on eight rows) to 256.
+static int page_shift(int page)
+{
+    for (int s = 3; s <= 8; ++s)
+        if (page == 1 << s) return s;
+    return -1;
+}
+
+static bool pool_dims_ok(int L, int H, int D, int page, int n_pages)
+{
+    if (L < 1 || H < 1 || (D != 64 && D != 128) || page < 1 || n_pages < 1) return false;
+    return (double)n_pages * page <= (double)kMaxRows && (double)L * n_pages * H < 2147483647.0;
+}
+
+ppd_status ppd_page_assign(const int32_t *old_len, const int32_t *new_len, int B, int page, int n_pages, int max_pages,
+                           int max_slots, int32_t *table, int32_t *free_pages, const int32_t *n_free, int32_t *new_n_free,
+                           int32_t *out_len, int32_t *slots, int32_t *slot_start, int32_t *dev_status, void *stream)
+{
+    if (!old_len || !new_len || !table || !free_pages || !n_free || !new_n_free || !out_len || !slots || !slot_start || !dev_status)
+        return PPD_ERR_INVALID_ARG;
+    if (B < 1 || page < 1 || n_pages < 1 || max_pages < 1 || max_slots < 1) return PPD_ERR_INVALID_ARG;
+    const size_t nb = (size_t)B * 4;
+    if (share_memory({{table, nb * max_pages}, {free_pages, (size_t)n_pages * 4}, {new_n_free, 4}, {out_len, nb}, {slots, (size_t)max_slots * 4},
+                      {slot_start, nb + 4}, {dev_status, nb}},
+                     {{old_len, nb}, {new_len, nb}, {n_free, 4}}))
+        return PPD_ERR_INVALID_ARG;
+    if (page_shift(page) < 0 || B > ppd::kMaxAssign || (double)n_pages * page > kMaxRows || (double)max_pages * page > kMaxRows ||
+        (double)B * max_pages > 2147483647.0 || max_slots > kMaxRows)
+        return PPD_ERR_UNSUPPORTED;
+    ppd::PageAssignParams p{old_len, new_len, n_free, table, free_pages, new_n_free, out_len, slots, slot_start, dev_status,
+                            B, page_shift(page), n_pages, max_pages, max_slots, aligned(slots, 16)};
+    return cuda_status(ppd::launch_page_assign(p, num_sms(), static_cast<cudaStream_t>(stream)));
+}
+
+ppd_status ppd_page_append(const void *k_new, const void *v_new, void *k_pages, void *v_pages, const int32_t *rows,
+                           const int32_t *slots, const int32_t *slot_start, int L, int B, int H, int T, int D, int page,
+                           int n_pages, int max_slots, ppd_dtype dt, int32_t *dev_status, void *stream)
+{
+    if (!k_new || !v_new || !k_pages || !v_pages || !slots || !slot_start || !dev_status) return PPD_ERR_INVALID_ARG;
+    if (B < 1 || T < 1 || max_slots < 1 || (dt != PPD_BF16 && dt != PPD_F32) || !pool_dims_ok(L, H, D, page, n_pages))
+        return PPD_ERR_INVALID_ARG;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16)) return PPD_ERR_INVALID_ARG;
+    const double slices = (double)L * B * H;
+    if (slices * T * D > 9.0e15) return PPD_ERR_INVALID_ARG;
+    const size_t pool = (size_t)L * n_pages * H * page * D * 2, fresh = (size_t)L * B * H * T * D * (dt == PPD_F32 ? 4 : 2), nb = (size_t)B * 4;
+    if (share_memory({{k_pages, pool}, {v_pages, pool}, {dev_status, nb}},
+                     {{k_new, fresh}, {v_new, fresh}, {rows, nb * T}, {slots, (size_t)max_slots * 4}, {slot_start, nb + 4}}))
+        return PPD_ERR_INVALID_ARG;
+    if (page_shift(page) < 0 || slices * ppd::page_append_chunks(T) > 2147483647.0) return PPD_ERR_UNSUPPORTED;
+    ppd::PageAppendParams p{k_new, v_new, k_pages, v_pages, slots, slot_start, rows, dev_status, (long long)L * B * H, B, H, T, D, n_pages,
+                            page_shift(page), max_slots, dt == PPD_F32, 0};
+    return cuda_status(ppd::launch_page_append(p, static_cast<cudaStream_t>(stream)));
+}
+
+// How an attention call over pages runs: blocks of query rows, how they are shared out, and where
+// the bf16 copies of fp32 operands and the work split's states lie in the workspace.
+struct PagedWs {
+    int rows, n_qb, n_tt;
+    AttnPlan plan;
+    size_t rec, part, total;
+};
+
+static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt, bool workspace)
+{
+    PagedWs w{};
+    const long long slices = (long long)L * B * H;
+    w.rows = G * T;
+    w.n_qb = w.rows > 64 ? (w.rows + 127) / 128 : 1;
+    w.n_tt = w.rows > 64 ? (T + 127) / 128 : 1;
+    const long long units = slices * w.n_qb, t_u = (S_max + 127) / 128 + w.n_tt, sms = split_grid();
+    w.plan = plan_units(units, t_u, B, workspace && units * t_u <= 2147483647ll, true);
+    // (a last, partial round of whole units weighs more here: requests' lengths are seldom alike)
+    if (workspace && units >= sms && B <= ppd::kSplitMaxB && units * t_u <= 2147483647ll &&
+        (units * t_u + sms - 1) / sms + kPagedSplitCostTiles < (units + sms - 1) / sms * t_u)
+        w.plan = {1, 1};
+    size_t off = dt == PPD_F32 ? align_up((size_t)slices * (w.rows + 2 * (size_t)T) * D * 2) : 0;
+    if (w.plan.split) {
+        w.rec = off;
+        off = align_up(off + (size_t)split_grid() * sizeof(ppd::SplitRecord));
+        w.part = off;
+        off = align_up(off + (size_t)2 * split_grid() * ppd::kSplitRows * (D + 2) * sizeof(float));
+    }
+    w.total = off;
+    return w;
+}
+
+static bool paged_dims_ok(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt)
+{
+    if (!kv4_dims_ok(L, B, H, G, T, D, S_max) || T > kMaxT || (dt != PPD_BF16 && dt != PPD_F32)) return false;
+    return (double)G * T <= 1 << 20;
+}
+
+size_t ppd_paged_attention_workspace_bytes(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt)
+{
+    if (!paged_dims_ok(L, B, H, G, T, D, S_max, dt) || S_max > kMaxRows) return 0;
+    return paged_workspace(L, B, H, G, T, D, S_max, dt, true).total;
+}
+
+ppd_status ppd_tree_attention_paged(const void *q, const void *k_pages, const void *v_pages, const int32_t *table,
+                                    const void *k_tree, const void *v_tree, const int32_t *prefix_len,
+                                    const int32_t *parent, int L, int B, int H, int G, int T, int D, int page, int n_pages,
+                                    int max_pages, ppd_dtype dt, float scale, void *out, float *lse, int32_t *dev_status,
+                                    void *workspace, size_t ws_bytes, void *stream)
+{
+    if (!q || !k_pages || !v_pages || !table || !k_tree || !v_tree || !prefix_len || !parent || !out || !dev_status)
+        return PPD_ERR_INVALID_ARG;
+    if (max_pages < 1 || !pool_dims_ok(L, H, D, page, n_pages) || !std::isfinite(scale)) return PPD_ERR_INVALID_ARG;
+    if ((double)max_pages * page > kMaxRows || page_shift(page) < 0) return PPD_ERR_UNSUPPORTED;
+    const int S_max = max_pages * page;
+    if (!paged_dims_ok(L, B, H, G, T, D, S_max, dt)) return PPD_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(k_tree, 16) || !aligned(v_tree, 16) ||
+        !aligned(out, 16) || !aligned(lse, 4))
+        return PPD_ERR_INVALID_ARG;
+    PagedWs w = paged_workspace(L, B, H, G, T, D, S_max, dt, true);
+    bool ws_ok = workspace && ws_bytes >= w.total && aligned(workspace, kAlign);
+    if (dt == PPD_F32 && !ws_ok) return PPD_ERR_INVALID_ARG;
+    if (!ws_ok) w = paged_workspace(L, B, H, G, T, D, S_max, dt, false);
+    const size_t slices = (size_t)L * B * H, rows = slices * w.rows, tree = slices * T * D * (dt == PPD_F32 ? 4 : 2), nb = (size_t)B * 4;
+    const size_t pool = (size_t)L * n_pages * H * page * D * 2;
+    if (share_memory({{out, rows * D * 2}, {lse, rows * 4}, {dev_status, nb}, {ws_ok && w.total ? workspace : nullptr, w.total}},
+                     {{q, rows * D * (dt == PPD_F32 ? 4 : 2)}, {k_pages, pool}, {v_pages, pool}, {table, nb * max_pages}, {k_tree, tree},
+                      {v_tree, tree}, {prefix_len, nb}, {parent, nb * T}}))
+        return PPD_ERR_INVALID_ARG;
+    if ((double)slices * w.n_qb > 2147483647.0) return PPD_ERR_UNSUPPORTED;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    if (dt == PPD_F32) {
+        uint16_t *bq = reinterpret_cast<uint16_t *>(ws), *bk = bq + rows * D, *bv = bk + slices * T * D;
+        ppd::RoundArgs r{};
+        r.t[0] = {static_cast<const float *>(q), bq, w.rows, 0};
+        r.t[1] = {static_cast<const float *>(k_tree), bk, T, 0};
+        r.t[2] = {static_cast<const float *>(v_tree), bv, T, 0};
+        r.n = 3, r.B = B, r.H = H, r.D = D, r.prefix_len = prefix_len;
+        const cudaError_t e = ppd::launch_round_bf16(r, (int64_t)slices, true, s);
+        if (e != cudaSuccess) return cuda_status(e);
+        q = bq, k_tree = bk, v_tree = bv;
+    }
+    const int T_pad = (w.rows + 31) & ~31, shift = page_shift(page);
+    AttnMaps m;
+    if (!encode_3d(&m.q, q, D, w.rows, slices, T_pad > 64 ? 128u : (uint32_t)T_pad) ||
+        !encode_3d(&m.kc, k_pages, D, page, (uint64_t)L * n_pages * H, page < 128 ? page : 128) ||
+        !encode_3d(&m.vc, v_pages, D, page, (uint64_t)L * n_pages * H, page < 128 ? page : 128) ||
+        !encode_3d(&m.kt, k_tree, D, T, slices, 128) || !encode_3d(&m.vt, v_tree, D, T, slices, 128))
+        return PPD_ERR_CUDA;
+    ppd::PagedParams p{};
+    p.prefix_len = prefix_len, p.parent = parent;
+    p.out = static_cast<float *>(out);
+    p.lse = lse;
+    p.dev_status = dev_status;
+    p.L = L, p.B = B, p.H = H, p.T = T, p.T_pad = T_pad, p.S_max = S_max;
+    p.n_qb = w.n_qb, p.n_tt = w.n_tt;
+    p.n_units = (int)(slices * w.n_qb);
+    p.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)D)) * 1.4426950408889634f;
+    p.table = table;
+    p.max_pages = max_pages, p.n_pages = n_pages, p.n_depth = L * n_pages * H;
+    p.page_shift = shift, p.box_shift = shift < 7 ? shift : 7;
+    p.rows = w.rows;
+    ppd::plan_rows(p, split_grid());
+    p.cluster = w.plan.cluster;
+    if (w.plan.split) {
+        p.split = 1;
+        p.split_rec = reinterpret_cast<ppd::SplitRecord *>(ws + w.rec);
+        p.split_part = reinterpret_cast<float *>(ws + w.part);
+    }
+    p.set_status = 1;
+    p.pdl_wait = 1;
+    return cuda_status(ppd::launch_paged_attention(m, p, D, split_grid(), s));
+}
+
+ppd_status ppd_token_logprobs(const void *logits, const int32_t *tokens, const int32_t *rows, int B, int T, int V, int n, int K,
+                              ppd_dtype dt, float temperature, float *logprob, float *entropy, int32_t *rank,
+                              int32_t *top_tokens, float *top_logprobs, int32_t *dev_status, void *stream)
+{
+    if (!logits || !tokens || !logprob || !entropy || !rank || !dev_status || (K > 0 && (!top_tokens || !top_logprobs)))
+        return PPD_ERR_INVALID_ARG;
+    if (B < 1 || T < 1 || V < 1 || n < 1 || K < 0 || K > V || (!rows && n > T) || (dt != PPD_BF16 && dt != PPD_F32) ||
+        (double)B * T * V > 9.0e15)
+        return PPD_ERR_INVALID_ARG;
+    if (!std::isfinite(temperature) || temperature <= 0.f || !std::isfinite(1.4426950408889634f / temperature))
+        return PPD_ERR_INVALID_ARG;
+    const size_t eb = dt == PPD_F32 ? 4 : 2, nb = (size_t)B * 4, items = nb * n;
+    if (!aligned(logits, eb) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(top_logprobs, 4)) return PPD_ERR_INVALID_ARG;
+    const Mem none{nullptr, 0};
+    if (share_memory({{logprob, items}, {entropy, items}, {rank, items}, K ? Mem{top_tokens, items * K} : none,
+                      K ? Mem{top_logprobs, items * K} : none, {dev_status, nb}},
+                     {{logits, (size_t)B * T * V * eb}, {tokens, items}, {rows, items}}))
+        return PPD_ERR_INVALID_ARG;
+    if (K > ppd::kLogMaxK || (double)B * n * ppd::kMaxCluster > 2147483647.0 || V > kMaxRows) return PPD_ERR_UNSUPPORTED;
+    ppd::LogprobParams p{logits, tokens, rows, logprob, entropy, rank, top_tokens, top_logprobs, dev_status, B, T, V, n, K, dt == PPD_BF16,
+                         1.4426950408889634f / temperature, 1};
+    return cuda_status(ppd::launch_token_logprobs(p, num_sms(), static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

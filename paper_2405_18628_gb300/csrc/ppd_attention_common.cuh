@@ -336,7 +336,8 @@ PPD_DEV size_t split_slot_floats(int D) { return (size_t)kSplitRows * (D + 2); }
 // weighted sum of the parts' O rows over the weighted sum of their row sums.
 // The parts are read eight at a time, every load of a batch issued before any
 // is used, so a batch costs one round trip to L2.
-static __device__ __forceinline__ void split_merge_chunk(const float *split_part, float *out, float *lse,
+template <class Out>
+static __device__ __forceinline__ void split_merge_chunk(const float *split_part, Out *out, float *lse,
                                                          const SplitParts &sp, long long N, int G,
                                                          size_t out_row0, int r, int c0, int D)
 {
@@ -379,8 +380,11 @@ static __device__ __forceinline__ void split_merge_chunk(const float *split_part
         }
     }
     const float inv = 1.f / Ls;
-    float *dst = out + (out_row0 + r) * D + c0;
-    if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
+    Out *dst = out + (out_row0 + r) * D + c0;
+    if constexpr (!std::is_same<Out, float>::value) {   // bf16, 16-byte aligned rows
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv),
+                                                     pack_bf16(acc[4] * inv, acc[5] * inv), pack_bf16(acc[6] * inv, acc[7] * inv));
+    } else if ((reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
         reinterpret_cast<float4 *>(dst)[0] = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
         reinterpret_cast<float4 *>(dst)[1] = make_float4(acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv);
     } else {
@@ -403,7 +407,7 @@ static __device__ __forceinline__ void split_merge_chunk(const float *split_part
 // values, unused, may still be on their way.  X = 2 pays with many rows (the query-row
 // kernel: 16 calls of 64 units, 200 tokens, 343 -> 326 us), X = 1 keeps more threads
 // busy with few.
-template <int X>
+template <int X, class Out = float>
 PPD_DEV bool cluster_merge(const AttnParams &p, int parts, uint32_t o, uint32_t pitch, uint32_t ml, int D,
                            int rank, int n_rows, size_t out_row0, int tid, int n_threads)
 {
@@ -455,8 +459,13 @@ PPD_DEV bool cluster_merge(const AttnParams &p, int parts, uint32_t o, uint32_t 
             }
         }
         const float inv = 1.f / Ls;
-        float *dst = p.out + (out_row0 + row) * D + col;
-        if (vec_out) {
+        Out *dst = reinterpret_cast<Out *>(p.out) + (out_row0 + row) * D + col;
+        if constexpr (!std::is_same<Out, float>::value) {   // bf16, 16-byte aligned rows
+#pragma unroll
+            for (int x = 0; x < 4 * X; x += 4)
+                *reinterpret_cast<uint2 *>(dst + x / 4 * (D / X)) =
+                    make_uint2(pack_bf16(acc[x] * inv, acc[x + 1] * inv), pack_bf16(acc[x + 2] * inv, acc[x + 3] * inv));
+        } else if (vec_out) {
 #pragma unroll
             for (int x = 0; x < 4 * X; x += 4)
                 *reinterpret_cast<float4 *>(dst + x / 4 * (D / X)) =
@@ -849,10 +858,10 @@ static __device__ __noinline__ void fused_side_warp(const AttnParams &p, const W
 // resident at once, or the launch fails) when the fused step's side warps
 // compute the argmax in-grid.  The shared-memory opt-in is set once per
 // device.
-template <class Kern>
+template <class Kern, class Params>
 cudaError_t launch_attention_grid(Kern kern, uint32_t smem, int threads,
                                   std::atomic<uint64_t> &configured,
-                                  const AttnMaps &m, const AttnParams &p, int num_sms,
+                                  const AttnMaps &m, const Params &p, int num_sms,
                                   bool programmatic, cudaStream_t stream)
 {
     int dev = 0;

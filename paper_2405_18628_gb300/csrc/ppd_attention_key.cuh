@@ -51,6 +51,7 @@
 #pragma once
 
 #include "ppd_attention_common.cuh"
+#include "ppd_paged.cuh"
 
 #include <cmath>
 #include <type_traits>
@@ -119,14 +120,16 @@ struct AttnLayout {
 };
 
 // MODE: whole units round-robin (0), the work split (1), the cluster split (2),
-// whole units with the longest sequences first (3).
-template <int D, int TP, int MODE>
+// whole units with the longest sequences first (3).  PAGED: the prefix's rows are in the
+// pages that the sequence's table names (ppd_paged.cuh), G query heads share a K/V head
+// (column c is tree node c mod T), and the output is bf16.
+template <int D, int TP, int MODE, bool PAGED = false>
 __global__ void __launch_bounds__(AttnLayout<D, TP>::THREADS, 1)
 tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                       const __grid_constant__ CUtensorMap map_kc,
                       const __grid_constant__ CUtensorMap map_vc,
                       const __grid_constant__ CUtensorMap map_kt,
-                      const __grid_constant__ CUtensorMap map_vt, const AttnParams p)
+                      const __grid_constant__ CUtensorMap map_vt, const AttnParamsOf<PAGED> p)
 {
     using Lay = AttnLayout<D, TP>;
     using KPos = RingPos<Lay::KS>;
@@ -149,7 +152,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
 
     const int warp = warp_uniform((int)threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    const int T = p.T;
+    const int T = p.T, R = query_rows<PAGED>(p);   // tree tokens, query columns
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < Lay::NBAR; ++i) {
@@ -176,7 +179,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     // grid: everything above overlapped it, nothing below reads before it is done
     // (the first K/V tiles are only asked of L2 before)
     if (p.pdl_wait) {
-        if (warp == Lay::SW) prefetch_first_tiles<RANGE>(p, lane, &map_kc, &map_vc, Lay::DCH, 3);
+        if (warp == Lay::SW) {
+            if constexpr (PAGED) {
+                const WorkRange w = plan_range<true>(p, lane);
+                prefetch_pages<Lay::DCH>(p, lane, &map_kc, &map_vc, RANGE ? w.u_first : (int)blockIdx.x, RANGE ? w.j_first : 0,
+                                         RANGE ? min(w.n_tiles, 3) : 3);
+            } else {
+                prefetch_first_tiles<RANGE>(p, lane, &map_kc, &map_vc, Lay::DCH, 3);
+            }
+        }
         asm volatile("griddepcontrol.wait;" ::: "memory");
     }
     WorkRange *wr_s = reinterpret_cast<WorkRange *>(smem + Lay::OFF_RANGE);
@@ -198,9 +209,73 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
 
     if (warp == Lay::SW + 2) {
         // ------------------------------------------------------------ fused-step side work
-        if (p.fused) fused_side_warp<true>(p, wr, lane, abort_flag);
-        else if (p.set_status) status_warp(p, lane);
-        if (p.late_wait) pdl_wait();
+        if constexpr (PAGED) {
+            paged_status_warp(p, lane);
+        } else {
+            if (p.fused) fused_side_warp<true>(p, wr, lane, abort_flag);
+            else if (p.set_status) status_warp(p, lane);
+            if (p.late_wait) pdl_wait();
+        }
+    } else if (PAGED && warp == Lay::SW) {
+        if constexpr (PAGED) {
+            // -------------------------------------------------------- TMA producer, page by page
+            // the whole warp: a lane copies one box, 64 columns of a page's rows of the tile
+            const uint64_t pol = l2_policy_evict_first();
+            KPos kp;
+            VPos vp;
+            int g = 0, k = 0;
+            SegIter<RANGE, RAGGED> it(wr);
+            auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, uint32_t off, uint64_t *full, bool tree, int z,
+                            const UnitInfo &ui, int row) {
+                if (warp_uniform(*abort_flag)) return;
+                if (!tree) {
+                    load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, lane, pol);
+                } else if (lane == 0) {
+                    mbar_arrive_expect_tx(full, Lay::TILE_BYTES);
+#pragma unroll
+                    for (int c = 0; c < Lay::DCH; ++c)
+                        tma_load_3d(smem + off + c * Lay::GROUP_BYTES, tree_map, full, c * 64, 0, ui.lbh, pol);
+                }
+                __syncwarp();
+            };
+            for (Seg sg; it.next(p, sg); ++k) {
+                const UnitInfo &ui = sg.ui;
+                const int qs = k & 1;
+                const PageUnit pu(p, ui.lbh, ui.b);
+                int z = page_coord<Lay::DCH>(p, pu, sg.j0 * Lay::KT, ui.P, lane);
+                mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
+                if (!warp_uniform(*abort_flag) && lane == 0) {
+                    mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
+#pragma unroll
+                    for (int c = 0; c < Lay::DCH; ++c)
+                        tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::Q_GROUP_BYTES,
+                                    &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
+                }
+                __syncwarp();
+                for (int j = sg.j0; j < sg.j1; ++j, ++g) {
+                    const bool tree = (j == ui.n_pref);
+                    const int row = j * Lay::KT;
+                    // the next tile's page numbers are asked for a tile ahead
+                    const int z_next = page_coord<Lay::DCH>(p, pu, row + Lay::KT, ui.P, lane);
+                    mbar_wait(bars + Lay::B_KEMPTY + kp.slot, kp.phase ^ 1u, abort_flag);
+                    load(&map_kc, &map_kt, Lay::OFF_K + kp.slot * Lay::TILE_BYTES, bars + Lay::B_KFULL + kp.slot, tree, z, ui, row);
+                    kp.advance();
+                    mbar_wait(bars + Lay::B_VEMPTY + vp.slot, vp.phase ^ 1u, abort_flag);
+                    load(&map_vc, &map_vt, Lay::OFF_V + vp.slot * Lay::TILE_BYTES, bars + Lay::B_VFULL + vp.slot, tree, z, ui, row);
+                    vp.advance();
+                    z = z_next;
+                }
+            }
+            if (*abort_flag) {
+                // let every copy already issued land before the CTA can exit
+                for (int i = max(0, g - Lay::KS); i < g; ++i)
+                    mbar_wait_drain(bars + Lay::B_KFULL + i % Lay::KS, (i / Lay::KS) & 1);
+                for (int i = max(0, g - Lay::VS); i < g; ++i)
+                    mbar_wait_drain(bars + Lay::B_VFULL + i % Lay::VS, (i / Lay::VS) & 1);
+                for (int i = max(0, k - Lay::QS); i < k; ++i)
+                    mbar_wait_drain(bars + Lay::B_QFULL + i % Lay::QS, (i / Lay::QS) & 1);
+            }
+        }
     } else if (warp == Lay::SW) {
         // ------------------------------------------------------------ TMA producer
         if (lane == 0) {
@@ -510,7 +585,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                 tmem_wait_ld(rl);
 #pragma unroll
                 for (int e = 0; e < NC; ++e)
-                    if (q0 + e < T) put(e, __uint_as_float(rh[e]) + __uint_as_float(rl[e]));
+                    if (q0 + e < R) put(e, __uint_as_float(rh[e]) + __uint_as_float(rl[e]));
             }
             tc_fence_before();
         };
@@ -523,12 +598,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             const int ob = (pend_f >> 3) & 1;
             if (!SPLIT || !(pend_f & 2)) {
                 const float *li = linv + ob * TP;
-                float *orow = p.out + ((size_t)pend_u * T + q0) * D + t;
-                read_o(ob, pend_g, [&](int e, float v) { orow[(size_t)e * D] = v * li[e]; });
+                OutOf<PAGED> *orow = reinterpret_cast<OutOf<PAGED> *>(p.out) + ((size_t)pend_u * R + q0) * D + t;
+                read_o(ob, pend_g, [&](int e, float v) { orow[(size_t)e * D] = OutOf<PAGED>(v * li[e]); });
             } else {
                 float *base = p.split_part + (size_t)(2 * (int)blockIdx.x + ((pend_f & 4) ? 0 : 1)) * slot_floats;
                 read_o(ob, pend_g, [&](int e, float v) { base[(size_t)(q0 + e) * D + t] = v; });
-                if (t < NC && q0 + t < T) {
+                if (t < NC && q0 + t < R) {
                     base[(size_t)kSplitRows * D + q0 + t] = pmx[ob * TP + t];
                     base[(size_t)kSplitRows * D + kSplitRows + q0 + t] = linv[ob * TP + t];
                 }
@@ -564,7 +639,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                     // ancestor sets by shuffles: lane c walks up from query q0 + c, then every
                     // lane collects its key's bit of each set
                     uint64_t anc = 0;
-                    int a = lane < NC && q0 + lane < T ? q0 + lane : -1;
+                    int a = lane < NC && q0 + lane < R ? (PAGED ? (q0 + lane) % T : q0 + lane) : -1;
                     while (__any_sync(0xffffffffu, a >= 0)) {
                         if (a >= 0) anc |= 1ull << a;
                         const int i = a < 0 ? 0 : a;
@@ -657,7 +732,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                     const float l = red[t] + red[NC + t] + red[2 * NC + t] + red[3 * NC + t];
                     const float m = -nm[t];
                     if (!RANGE || (SPLIT && seg_whole(sg))) {
-                        if (p.lse && q0 + t < T) p.lse[(size_t)u * T + q0 + t] = (m + lg2(l)) * 0.69314718055994530942f;
+                        if (p.lse && q0 + t < R) p.lse[(size_t)u * R + q0 + t] = (m + lg2(l)) * 0.69314718055994530942f;
                         linv[ob * TP + t] = rcp(l);
                     } else if (MODE == 2) {
                         ml[t] = make_float2(m, l);
@@ -699,8 +774,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
         bool unused = false;
         if (warp < Lay::SW) {
             const int u = (int)blockIdx.x / p.cluster;
-            unused = cluster_merge<1>(p, wr.parts, smem_addr(smem) + Lay::OFF_K, D * 4, smem_addr(smem) + Lay::OFF_PMX,
-                          D, (int)blockIdx.x - u * p.cluster, T, (size_t)u * T, threadIdx.x, Lay::SW * 32);
+            unused = cluster_merge<1, OutOf<PAGED>>(p, wr.parts, smem_addr(smem) + Lay::OFF_K, D * 4, smem_addr(smem) + Lay::OFF_PMX,
+                          D, (int)blockIdx.x - u * p.cluster, R, (size_t)u * R, threadIdx.x, Lay::SW * 32);
         }
         __syncwarp();
         cluster_leave(unused);

@@ -62,6 +62,7 @@
 #pragma once
 
 #include "ppd_attention_common.cuh"
+#include "ppd_paged.cuh"
 
 #include <cmath>
 
@@ -122,15 +123,15 @@ struct RowsJob {
 template <bool RANGE>
 PPD_DEV bool rows_pair_cta(const AttnParams &p)
 {
-    return !RANGE && p.pairs && (p.n_qb != 3 || (int)blockIdx.x < p.pair_grid);
+    return !RANGE && p.pairs && ((p.n_qb & 1) == 0 || (int)blockIdx.x < p.pair_grid);
 }
 
 // Walks a CTA's jobs in order (every role walks the same sequence).  Whole
-// jobs round-robin: single jobs (n_qb 1), pair jobs (n_qb 2, or 4 with two a
-// slice); with n_qb 3 the first p.pair_grid CTAs take the slices' pairs and
-// the others their third blocks.  RANGE (either split): single jobs, the CTA's range
+// jobs round-robin: single jobs, or n_qb / 2 pair jobs a slice; with an odd n_qb
+// the first p.pair_grid CTAs take the slices' pairs and
+// the others their last blocks.  RANGE (either split): single jobs, the CTA's range
 // of tiles.
-template <bool RANGE, bool RAGGED = false>
+template <bool RANGE, bool RAGGED = false, bool PAGED = false>
 struct RowsIter {
     SegIter<RANGE, RAGGED> seg;
     int x, step, n, per;
@@ -143,15 +144,15 @@ struct RowsIter {
         step = G;
         per = p.n_qb;   // jobs a slice
         if (p.pairs) {
-            per = p.n_qb == 4 ? 2 : 1;
-            if (p.n_qb == 3) {
+            per = pair ? p.n_qb / 2 : 1;
+            if (p.n_qb & 1) {
                 x = pair ? c : c - p.pair_grid;
                 step = pair ? p.pair_grid : G - p.pair_grid;
             }
         }
         n = p.n_units / p.n_qb * per;
     }
-    PPD_DEV bool next(const AttnParams &p, RowsJob &j)
+    PPD_DEV bool next(const AttnParamsOf<PAGED> &p, RowsJob &j)
     {
         if (RANGE) {
             Seg s;
@@ -169,8 +170,9 @@ struct RowsIter {
         const int slice = job / per, i = job - slice * per;
         const int qb = pair ? 2 * i : (p.pairs ? p.n_qb - 1 : i);
         j.ui = unit_info(p, slice * p.n_qb + qb);
-        // a query's ancestors come before it: no tree tile past the job's last block
-        j.ui.n_tiles = j.ui.n_pref + qb + (pair ? 2 : 1);
+        // a query's ancestors come before it: no tree tile past the job's last block (a block
+        // of several heads' rows may hold any node)
+        j.ui.n_tiles = j.ui.n_pref + (PAGED ? p.n_tt : qb + (pair ? 2 : 1));
         j.j0 = 0;
         j.j1 = j.ui.n_tiles;
         j.pair = pair;
@@ -201,15 +203,30 @@ PPD_DEV void rows_prefetch(const AttnParams &p, int lane, const CUtensorMap *kc,
     }
 }
 
+// The same over pages.
+template <bool RANGE, int DCH>
+PPD_DEV void rows_prefetch_pages(const PagedParams &p, int lane, const CUtensorMap *kc, const CUtensorMap *vc, int n)
+{
+    const WorkRange w = plan_range<true>(p, lane);
+    if (RANGE) {
+        prefetch_pages<DCH>(p, lane, kc, vc, w.u_first, w.j_first, min(w.n_tiles, n));
+        return;
+    }
+    const RowsIter<RANGE> it(p, w);
+    if (it.x < it.n) prefetch_pages<DCH>(p, lane, kc, vc, it.x / it.per * p.n_qb, 0, n);
+}
+
 // MODE: whole jobs round-robin (0), the work split (1), the cluster split (2),
-// whole jobs with the longest sequences first (3).
-template <int D, int MODE>
+// whole jobs with the longest sequences first (3).  PAGED: the prefix's rows are in the
+// pages that the sequence's table names (ppd_paged.cuh), G query heads share a K/V head
+// (row r is tree node r mod T), and the output is bf16.
+template <int D, int MODE, bool PAGED = false>
 __global__ void __launch_bounds__(384, 1)
 tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                            const __grid_constant__ CUtensorMap map_kc,
                            const __grid_constant__ CUtensorMap map_vc,
                            const __grid_constant__ CUtensorMap map_kt,
-                           const __grid_constant__ CUtensorMap map_vt, const AttnParams p)
+                           const __grid_constant__ CUtensorMap map_vt, const AttnParamsOf<PAGED> p)
 {
     using Lay = RowsLayout<D>;
     using Pos = RingPos<Lay::RS>;
@@ -229,7 +246,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
 
     const int warp = warp_uniform((int)threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    const int T = p.T;
+    const int T = p.T, R = query_rows<PAGED>(p);   // tree tokens, query rows of a slice
 
     const bool pair_cta = rows_pair_cta<RANGE>(p);
     if (threadIdx.x == 0) {
@@ -262,7 +279,10 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
     // grid: everything above overlapped it, nothing below reads before it is done
     // (the first K/V tiles are only asked of L2 before)
     if (p.pdl_wait) {
-        if (warp == 8) rows_prefetch<RANGE>(p, lane, &map_kc, &map_vc, Lay::DCH, 3);
+        if (warp == 8) {
+            if constexpr (PAGED) rows_prefetch_pages<RANGE, Lay::DCH>(p, lane, &map_kc, &map_vc, 3);
+            else rows_prefetch<RANGE>(p, lane, &map_kc, &map_vc, Lay::DCH, 3);
+        }
         asm volatile("griddepcontrol.wait;" ::: "memory");
     }
     WorkRange *wr_s = reinterpret_cast<WorkRange *>(smem + Lay::OFF_RANGE);
@@ -284,9 +304,99 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
 
     if (warp == 11) {
         // ------------------------------------------------------------ fused-step side work
-        if (p.fused) fused_side_warp<false>(p, wr, lane, abort_flag);
-        else if (p.set_status) status_warp(p, lane);
-        if (p.late_wait) pdl_wait();
+        if constexpr (PAGED) {
+            paged_status_warp(p, lane);
+        } else {
+            if (p.fused) fused_side_warp<false>(p, wr, lane, abort_flag);
+            else if (p.set_status) status_warp(p, lane);
+            if (p.late_wait) pdl_wait();
+        }
+    } else if (PAGED && warp == 8) {
+        if constexpr (PAGED) {
+            // -------------------------------------------------------- TMA producer, page by page
+            // the whole warp: a lane copies one box, 64 columns of a page's rows of the tile
+            const uint64_t pol = p.n_qb > 2 ? l2_policy_evict_normal() : l2_policy_evict_first();
+            Pos pos;
+            int n_tiles = 0, n_q0 = 0, n_q1 = 0;   // copies issued: ring tiles, Q blocks per slot
+            struct Tile {
+                int row, lbh, P, depth;   // first key, slice, keys below this; this lane's page
+                bool tree;
+            };
+            auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, const Tile &t) {
+                mbar_wait(bars + Lay::B_EMPTY + pos.slot, pos.phase ^ 1u, abort_flag);
+                if (!warp_uniform(*abort_flag)) {
+                    uint64_t *full = bars + Lay::B_FULL + pos.slot;
+                    uint8_t *dst = smem + Lay::OFF_R + pos.slot * Lay::TILE_BYTES;
+                    if (!t.tree) {
+                        load_page_tile<Lay::DCH>(p, pages, dst, Lay::GROUP_BYTES, full, t.depth, t.row, t.P, lane, pol);
+                    } else if (lane == 0) {
+                        mbar_arrive_expect_tx(full, Lay::TILE_BYTES);
+#pragma unroll
+                        for (int c = 0; c < Lay::DCH; ++c)
+                            tma_load_3d(dst + c * Lay::GROUP_BYTES, tree_map, full, c * 64, t.row, t.lbh, pol);
+                    }
+                    __syncwarp();
+                    ++n_tiles;
+                }
+                pos.advance();
+            };
+            auto load_q = [&](int qs, uint32_t parity, int qb, int lbh) {
+                mbar_wait(bars + Lay::B_QEMPTY + qs, parity ^ 1u, abort_flag);
+                if (!warp_uniform(*abort_flag)) {
+                    if (lane == 0) {
+                        // rows past the slice's last lie beyond the tensor and arrive as zeros
+                        mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
+#pragma unroll
+                        for (int c = 0; c < Lay::DCH; ++c)
+                            tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::GROUP_BYTES, &map_q,
+                                        bars + Lay::B_QFULL + qs, c * 64, qb * Lay::M, lbh, pol);
+                    }
+                    __syncwarp();
+                    n_q0 += qs == 0;
+                    n_q1 += qs == 1;
+                }
+            };
+            // V tiles of a single job trail their K tiles by two
+            Tile v0{}, v1{};
+            int g = 0, k = 0;
+            RowsIter<RANGE, RAGGED, PAGED> it(p, wr);
+            for (RowsJob jb; it.next(p, jb); ++k) {
+                const UnitInfo &ui = jb.ui;
+                const PageUnit pu(p, ui.lbh, ui.b);
+                int depth = page_coord<Lay::DCH>(p, pu, jb.j0 * Lay::KT, ui.P, lane);
+                if (!jb.pair) load_q(k & 1, (uint32_t)(k >> 1) & 1u, ui.qb, ui.lbh);
+                for (int j = jb.j0; j < jb.j1; ++j, ++g) {
+                    const bool tree = (j >= ui.n_pref);
+                    const Tile t{(tree ? j - ui.n_pref : j) * Lay::KT, ui.lbh, ui.P, depth, tree};
+                    // the next tile's page numbers are asked for a tile ahead
+                    depth = page_coord<Lay::DCH>(p, pu, (j + 1) * Lay::KT, ui.P, lane);
+                    if (jb.pair) {
+                        load(&map_kc, &map_kt, t);
+                        load(&map_vc, &map_vt, t);
+                        // the Q slots are free once the job before has its last scores:
+                        // its first tiles are queued ahead of that wait
+                        if (j == jb.j0) {
+                            load_q(0, (uint32_t)k & 1u, ui.qb, ui.lbh);
+                            load_q(1, (uint32_t)k & 1u, ui.qb + 1, ui.lbh);
+                        }
+                        continue;
+                    }
+                    if (g >= 2) load(&map_vc, &map_vt, g & 1 ? v1 : v0);
+                    if (g & 1) v1 = t;
+                    else v0 = t;
+                    load(&map_kc, &map_kt, t);
+                }
+            }
+            if (!it.pair)
+                for (int e = max(0, g - 2); e < g; ++e) load(&map_vc, &map_vt, e & 1 ? v1 : v0);
+            if (*abort_flag) {
+                // let every copy already issued land before the CTA can exit
+                for (int i = max(0, n_tiles - Lay::RS); i < n_tiles; ++i)
+                    mbar_wait_drain(bars + Lay::B_FULL + i % Lay::RS, (i / Lay::RS) & 1);
+                if (n_q0 > 0) mbar_wait_drain(bars + Lay::B_QFULL + 0, (n_q0 - 1) & 1);
+                if (n_q1 > 0) mbar_wait_drain(bars + Lay::B_QFULL + 1, (n_q1 - 1) & 1);
+            }
+        }
     } else if (warp == 8) {
         // ------------------------------------------------------------ TMA producer
         if (lane == 0) {
@@ -477,7 +587,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             if (first) ++p_job;
         };
 
-        RowsIter<RANGE, RAGGED> it(p, wr);
+        RowsIter<RANGE, RAGGED, PAGED> it(p, wr);
         const bool pair = it.pair;
         int g = 0, k = 0;   // tiles and jobs of the CTA so far
         for (RowsJob jb;; ++k) {
@@ -485,11 +595,12 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             if (n == 0) break;
             if (pair) {
                 // K0 V0 K1 V1 ...; the job's last tile holds no key that a query of its first
-                // block may see (n >= 2), so stream A stops one tile earlier
+                // block may see (n >= 2), so stream A stops one tile earlier (with shared K/V
+                // heads either block may hold any node)
                 for (int i = 0; i < n; ++i) {
                     if (pend) issue_pv(false);
                     else take_turn();
-                    if (s == 0 && i == n - 1) {
+                    if (!PAGED && s == 0 && i == n - 1) {
                         if (elect_one()) mbar_arrive(bars + Lay::B_TURN + 1);
                         __syncwarp();
                         pass();
@@ -500,7 +611,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                         mbar_wait(bars + Lay::B_QFULL + s, (uint32_t)k & 1u, abort_flag);
                         dead = warp_uniform(*abort_flag) != 0;
                     }
-                    issue_s((int)s, i == 0, i == (s == 0 ? n - 2 : n - 1));
+                    issue_s((int)s, i == 0, i == (!PAGED && s == 0 ? n - 2 : n - 1));
                 }
             } else {
                 // K0 K1 V0 K2 V1 ...: tile e of all jobs is preceded by the V of tile e - 2
@@ -668,8 +779,17 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
         };
 
         // 32 output values of row `orow` at `scale`.
-        auto store32 = [&](float *dst, const uint32_t (&r)[32], float scale) {
-            if (out32) {
+        auto store32 = [&](auto *dst, const uint32_t (&r)[32], float scale) {
+            if constexpr (!std::is_same<decltype(dst), float *>::value) {   // bf16, 16-byte aligned rows
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        w[x] = pack_bf16(__uint_as_float(r[e + 2 * x]) * scale, __uint_as_float(r[e + 2 * x + 1]) * scale);
+                    *reinterpret_cast<uint4 *>(dst + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else if (PAGED || out32) {   // (partial states are aligned)
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, r + e, scale);
             } else if (vec_out) {
@@ -695,9 +815,9 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
         // End of a pair job: this stream's block of 128 rows.
         auto finish_pair = [&](const RowsJob &jb) {
             const int qg = (jb.ui.qb + s) * Lay::M + q;
-            if (qg < T && p.lse) p.lse[(size_t)jb.ui.lbh * T + qg] = (m + lg2(l)) * 0.69314718055994530942f;
+            if (qg < R && p.lse) p.lse[(size_t)jb.ui.lbh * R + qg] = (m + lg2(l)) * 0.69314718055994530942f;
             const float linv = rcp(l);
-            float *orow = p.out + ((size_t)jb.ui.lbh * T + qg) * D;
+            OutOf<PAGED> *orow = reinterpret_cast<OutOf<PAGED> *>(p.out) + ((size_t)jb.ui.lbh * R + qg) * D;
             wait_done(s);
             tc_fence_after();
 #pragma unroll
@@ -712,7 +832,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                     __syncwarp();
                     o_free(s, 2);
                 }
-                if (qg < T) {
+                if (qg < R) {
                     store32(orow + c, r0, linv);
                     store32(orow + c + 32, r1, linv);
                 }
@@ -738,9 +858,9 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             const float inv = whole ? rcp(lt) : 1.f;
             float *dst;
             if (whole) {
-                if (s == 0 && qg < T && p.lse)
-                    p.lse[(size_t)jb.ui.lbh * T + qg] = (mt + lg2(lt)) * 0.69314718055994530942f;
-                dst = p.out + ((size_t)jb.ui.lbh * T + qg) * D;
+                if (s == 0 && qg < R && p.lse)
+                    p.lse[(size_t)jb.ui.lbh * R + qg] = (mt + lg2(lt)) * 0.69314718055994530942f;
+                dst = p.out + ((size_t)jb.ui.lbh * R + qg) * (PAGED ? D / 2 : D);   // (bf16: a row is D / 2 words)
             } else if (MODE == 2) {
                 // this CTA's part for the cluster: rows over the ring (every copy has landed,
                 // and the waits below cover every product that reads it)
@@ -749,14 +869,14 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             } else {
                 // a part of a cut unit: the unnormalised row, its maximum and its sum
                 float *base = p.split_part + (size_t)slot * split_slot_floats(D);
-                if (s == 0 && qg < T) {
+                if (s == 0 && qg < R) {
                     base[(size_t)kSplitRows * D + q] = mt;
                     base[(size_t)kSplitRows * D + kSplitRows + q] = lt;
                 }
                 dst = base + (size_t)q * D;
             }
-            dst += s * (D / 2);
-            const bool live = qg < T;
+            dst += s * (PAGED && whole ? D / 4 : D / 2);
+            const bool live = qg < R;
             const float fa = (s == 0 ? w_own : w_oth) * inv, fb = (s == 0 ? w_oth : w_own) * inv;
             const bool has_a = both || st0 == 0, has_b = both || st0 == 1;
             if (has_a) wait_done(0);
@@ -786,6 +906,8 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
                             st_shared_v4(smem_addr(dst + c + e), r0[e], r0[e + 1], r0[e + 2], r0[e + 3]);
+                    } else if (PAGED && whole) {
+                        store32(reinterpret_cast<OutOf<PAGED> *>(dst) + c, r0, 1.f);
                     } else {
                         store32(dst + c, r0, 1.f);
                     }
@@ -793,17 +915,17 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             }
         };
 
-        RowsIter<RANGE, RAGGED> it(p, wr);
+        RowsIter<RANGE, RAGGED, PAGED> it(p, wr);
         int k = 0;
         for (RowsJob jb; it.next(p, jb); ++k) {
             const UnitInfo &ui = jb.ui;
             const int qb = ui.qb + (jb.pair ? s : 0);
-            const int qg = qb * Lay::M + q;   // this thread's tree token
+            const int qg = qb * Lay::M + q;   // this thread's row: tree token qg (of a head: qg mod T)
             if (ui.b * p.n_qb + qb != cur_key) {
 #pragma unroll
                 for (int w = 0; w < NW; ++w) anc[w] = 0;
-                if (qg < T) {
-                    int a = qg;
+                if (qg < R) {
+                    int a = PAGED ? qg % T : qg;
                     while (true) {
                         anc[a >> 5] |= 1u << (a & 31);
                         const int pa = ld_input(p.parent + (size_t)ui.b * T + a);
@@ -818,7 +940,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             const int st0 = g & 1;   // single job: the stream of its first tile
             // this stream's tiles of the job: all of a pair's, every other one of a single's
             // (stream A's queries see nothing of a pair's last tree tile)
-            const int n_s = jb.pair && s == 0 ? n - 1 : n;
+            const int n_s = !PAGED && jb.pair && s == 0 ? n - 1 : n;
             for (int i = jb.pair ? 0 : (s ^ st0); i < n_s; i += jb.pair ? 1 : 2) {
                 const int j = jb.j0 + i;
                 const bool tree = (j >= ui.n_pref);
@@ -888,9 +1010,9 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
         if (warp < 8) {
             const int u = (int)blockIdx.x / p.cluster;
             const int lbh = u / p.n_qb, qb = u - lbh * p.n_qb;
-            unused = cluster_merge<2>(p, wr.parts, smem_addr(smem) + Lay::OFF_R, Lay::C_PITCH * 4, smem_addr(cs), D,
-                          (int)blockIdx.x - u * p.cluster, min(Lay::M, T - qb * Lay::M),
-                          (size_t)lbh * T + (size_t)qb * Lay::M, threadIdx.x, 256);
+            unused = cluster_merge<2, OutOf<PAGED>>(p, wr.parts, smem_addr(smem) + Lay::OFF_R, Lay::C_PITCH * 4, smem_addr(cs), D,
+                          (int)blockIdx.x - u * p.cluster, min(Lay::M, R - qb * Lay::M),
+                          (size_t)lbh * R + (size_t)qb * Lay::M, threadIdx.x, 256);
         }
         __syncwarp();
         cluster_leave(unused);

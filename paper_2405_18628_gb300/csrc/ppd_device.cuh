@@ -554,6 +554,13 @@ PPD_DEV uint64_t add2(uint64_t a, uint64_t b)
     return d;
 }
 
+// Two values rounded to bf16, the first in the low half.
+PPD_DEV uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 // The pair pp = (p0, p1) as bf16 hi + lo: hi the nearest bf16, lo the nearest to
 // what is left, together within 2^-18 of each value (hi truncated: 2^-17).
 PPD_DEV void split_bf16x2(uint64_t pp, float p0, float p1, uint32_t &hi, uint32_t &lo)

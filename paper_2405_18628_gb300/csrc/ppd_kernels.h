@@ -85,7 +85,7 @@ struct AttnParams {
     int n_qb;                   // query blocks of 128 per (layer, sequence, head) slice
     int n_tt;                   // tree-key tiles of 128 per slice
     int pairs;                  // query-row kernel: two blocks of queries of a slice are one job
-    int pair_grid;              // with n_qb 3: the CTAs that take the slices' pairs
+    int pair_grid;              // with an odd n_qb: the CTAs that take the slices' pairs
     float scale_log2;           // softmax scale * log2(e)
     // Work split: split != 0 shares all units out by their key tiles (launches with
     // fewer units than CTAs, B <= kSplitMaxB); units cut by a range
@@ -109,6 +109,16 @@ struct AttnParams {
     // (a step of more than 64 sequences): a spare warp waits for them, so that this
     // grid's completion says that they are complete too.
     int late_wait;
+};
+
+// Attention over pages (ppd_paged.cuh): G query heads share a K/V head, `out` is bf16, S_max
+// the rows that a sequence's table can name.
+struct PagedParams : AttnParams {
+    const int32_t *table;       // [B][max_pages]
+    int max_pages, n_pages;
+    int n_depth;                // L * n_pages * H
+    int page_shift, box_shift;  // log2 of a page's rows, and of min(128, those)
+    int rows;                   // query rows of a slice: its G heads' T tokens
 };
 
 // Work split limits: batch size (the per-CTA range search holds the batch in
@@ -145,17 +155,17 @@ struct SplitRecord {
     int u, n_tiles;
 };
 
-// Jobs of a launch without a split: its units, or with p.pairs (n_qb 2 to 4)
-// one, two -- a pair and a single block -- and two jobs a slice.
+// Jobs of a launch without a split: its units, or with p.pairs a slice's pairs of
+// blocks and, where their number is odd, a single one.
 inline long long whole_jobs(const AttnParams &p)
 {
     if (!p.pairs) return p.n_units;
     const long long slices = p.n_units / p.n_qb;
-    return p.n_qb == 2 ? slices : 2 * slices;
+    return (p.n_qb + 1) / 2 * slices;
 }
 
 // Whether the query-row kernel's whole jobs are pairs of query blocks, and for
-// n_qb 3 the split of the CTAs between pairs and single blocks: the choice with
+// an odd n_qb the split of the CTAs between pairs and single blocks: the choice with
 // the shortest longest queue.  A pair counts as 2 n + 4 and a single block next
 // to it as n + 4.5 tiles of 128 x 128 with n prefix tiles (S_max standing in for
 // the device-side prefix lengths): three tree tiles each, and the end of a job,
@@ -171,10 +181,10 @@ inline void plan_rows(AttnParams &p, int num_sms)
     const long long single_all = (23 * (2 * n + 9)) * ((p.n_units + G - 1) / G);   // in 1/40 tiles
     long long best = -1;
     int grid = 0;
-    if (p.n_qb == 3) {
-        const long long Gp = G < 2 * S ? G : 2 * S;
+    if (p.n_qb & 1) {
+        const long long pairs = S * (p.n_qb / 2), Gp = G < pairs + S ? G : pairs + S;
         for (long long g = 1; g < Gp; ++g) {
-            const long long a = (4 * n + 8) * ((S + g - 1) / g), b = (2 * n + 9) * ((S + Gp - g - 1) / (Gp - g));
+            const long long a = (4 * n + 8) * ((pairs + g - 1) / g), b = (2 * n + 9) * ((S + Gp - g - 1) / (Gp - g));
             const long long t = a > b ? a : b;
             if (best < 0 || t <= best) {
                 best = t;
@@ -182,7 +192,7 @@ inline void plan_rows(AttnParams &p, int num_sms)
             }
         }
     } else {
-        const long long jobs = p.n_qb == 2 ? S : 2 * S;
+        const long long jobs = S * (p.n_qb / 2);
         best = (4 * n + 8) * ((jobs + G - 1) / G);
     }
     if (best < 0 || 20 * best > single_all) return;
@@ -228,6 +238,10 @@ cudaError_t launch_tree_attention(const AttnMaps &m, const AttnParams &p, int D,
                                   bool programmatic, cudaStream_t stream);
 cudaError_t launch_tree_attention_rows(const AttnMaps &m, const AttnParams &p, int D, int num_sms,
                                        bool programmatic, cudaStream_t stream);
+
+// The same over pages, on the padded number of a slice's query rows.
+cudaError_t launch_paged_attention(const AttnMaps &m, const PagedParams &p, int D, int num_sms, cudaStream_t stream);
+cudaError_t launch_paged_attention_rows(const AttnMaps &m, const PagedParams &p, int D, int num_sms, cudaStream_t stream);
 
 // A kernel launch as a programmatic dependent of the stream's previous grid (it
 // may start before that grid completes; the kernel waits with pdl_wait()), in
@@ -496,6 +510,49 @@ struct SampleParams {
 // Logits of a CTA at most (its shared memory).
 constexpr int kSampleMaxChunk = 48 * 1024;
 cudaError_t launch_sample_accept(const SampleParams &p, int cluster, cudaStream_t stream);
+
+// ---- a pool of pages
+// Sequences of one ppd_page_assign call (their sums lie in shared memory).
+constexpr int kMaxAssign = 8192;
+struct PageAssignParams {
+    const int32_t *old_len, *new_len, *n_free;   // [B], [B], [1]
+    int32_t *table;                  // [B][max_pages]
+    int32_t *free_pages;             // [n_pages]
+    int32_t *new_n_free, *out_len;   // [1], [B]
+    int32_t *slots, *slot_start;     // [max_slots], [B + 1]
+    int32_t *dev_status;             // [B]
+    int B, page_shift, n_pages, max_pages, max_slots;
+    int vec;                         // slots is 16-byte aligned
+};
+cudaError_t launch_page_assign(const PageAssignParams &p, int num_sms, cudaStream_t stream);
+
+struct PageAppendParams {
+    const void *k_new, *v_new;       // [slices][T][D] bf16 or (f32) fp32
+    void *k_pages, *v_pages;         // bf16 [L][n_pages][H][page][D]
+    const int32_t *slots, *slot_start, *rows;   // rows [B,T] or null
+    int32_t *dev_status;             // [B]
+    long long slices;
+    int B, H, T, D, n_pages, page_shift, max_slots, f32;
+    int chunks;                      // blocks of a slice
+};
+int page_append_chunks(int T);
+cudaError_t launch_page_append(PageAppendParams p, cudaStream_t stream);
+
+// ---- log probabilities of given tokens
+constexpr int kLogMaxK = 32;
+struct LogprobParams {
+    const void *logits;              // [B,T,V] fp32 or bf16
+    const int32_t *tokens, *rows;    // [B,n]; rows null: row i
+    float *logprob, *entropy;        // [B,n]
+    int32_t *rank;                   // [B,n]
+    int32_t *top_tokens;             // [B,n,K]
+    float *top_logprobs;
+    int32_t *dev_status;             // [B]
+    int B, T, V, n, K, bf16;
+    float k;                         // log2(e) / temperature
+    int cluster;                     // CTAs of a row
+};
+cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t stream);
 
 cudaError_t launch_selftest_umma(const CUtensorMap &ma, const CUtensorMap &mb, const void *a_raw,
                                  const void *b_raw, float *d, int mode, int N, cudaStream_t stream);

@@ -74,6 +74,11 @@ def load() -> ctypes.CDLL:
             "ppd_kv_weight_add": ([vp] * 8 + [i32] * 8 + [f32, vp, vp], i32),
             "ppd_kv_evict": ([vp] * 5 + [i32, vp] + [i32] * 8 + [vp] * 4, i32),
             "ppd_sample_accept": ([vp] * 8 + [i32] * 5 + [f32] + [vp] * 7, i32),
+            "ppd_page_assign": ([vp] * 2 + [i32] * 5 + [vp] * 9, i32),
+            "ppd_page_append": ([vp] * 7 + [i32] * 9 + [vp, vp], i32),
+            "ppd_paged_attention_workspace_bytes": ([i32] * 8, sz),
+            "ppd_tree_attention_paged": ([vp] * 8 + [i32] * 10 + [f32, vp, vp, vp, vp, sz, vp], i32),
+            "ppd_token_logprobs": ([vp] * 3 + [i32] * 6 + [f32] + [vp] * 7, i32),
             "ppd_verify_step_typical": ([vp] * 9 + [i32] * 8 + [f32] * 4 + [vp] * 8 +
                                         [vp, sz, vp], i32),
         }
@@ -421,6 +426,82 @@ def ppd_sample_accept(logits, cand_tokens, parent, prefix_len, S_max, temperatur
               ("new_prefix_len", new_prefix_len, i32, one), ("accept_prob", accept_prob, f32, tree), ("dev_status", dev_status, i32, one))
     st = load().ppd_sample_accept(*a[:8], B, T, V, n_draft, int(S_max), float(temperature), *a[8:], _stream(stream))
     _check(st, "ppd_sample_accept")
+
+
+def page_pool(L, n_pages, H, page, D, device="cuda"):
+    """An empty pool of pages of K, or of V: bf16 [L,n_pages,H,page,D]."""
+    return torch.zeros((L, n_pages, H, page, D), dtype=torch.bfloat16, device=device)
+
+
+def ppd_page_assign(old_len, new_len, page: int, table, free_pages, n_free, new_n_free, out_len, slots, slot_start,
+                    dev_status, stream=None):
+    """Pages of `page` rows for sequences that grow from old_len to new_len [B], back from those that shrink: table
+    [B,max_pages] and the stack free_pages [n_pages] (n_free [1] entries, then new_n_free) in place; the new rows'
+    slots [max_slots], b's from slot_start [B+1] on; out_len [B] the lengths that sequences have then."""
+    (B, max_pages), n_pages, max_slots = table.shape, free_pages.numel(), slots.numel()
+    i32, one = torch.int32, (B,)
+    a = _take(("old_len", old_len, i32, one), ("new_len", new_len, i32, one), ("table", table, i32, (B, max_pages)),
+              ("free_pages", free_pages, i32, (n_pages,)), ("n_free", n_free, i32, (1,)), ("new_n_free", new_n_free, i32, (1,)),
+              ("out_len", out_len, i32, one), ("slots", slots, i32, (max_slots,)), ("slot_start", slot_start, i32, (B + 1,)),
+              ("dev_status", dev_status, i32, one))
+    st = load().ppd_page_assign(a[0], a[1], B, int(page), n_pages, max_pages, max_slots, *a[2:], _stream(stream))
+    _check(st, "ppd_page_assign")
+
+
+def ppd_page_append(k_new, v_new, k_pages, v_pages, slots, slot_start, dev_status, rows=None, stream=None):
+    """Rows k_new, v_new [L,B,H,T,D] (those of rows [B,T], or all in order) into their slots of the pools
+    [L,n_pages,H,page,D]; sequence b's slots are slots[slot_start[b] .. slot_start[b+1] - 1]."""
+    L, B, H, T, D = new = k_new.shape
+    n_pages, page, max_slots = k_pages.shape[1], k_pages.shape[3], slots.numel()
+    pool, i32, dt, bf = (L, n_pages, H, page, D), torch.int32, k_new.dtype, torch.bfloat16
+    a = _take(("k_new", k_new, dt, new), ("v_new", v_new, dt, new), ("k_pages", k_pages, bf, pool), ("v_pages", v_pages, bf, pool),
+              ("rows", rows, i32, (B, T)), ("slots", slots, i32, (max_slots,)), ("slot_start", slot_start, i32, (B + 1,)),
+              ("dev_status", dev_status, i32, (B,)))
+    st = load().ppd_page_append(*a[:7], L, B, H, T, D, page, n_pages, max_slots, _dtype(k_new), a[7], _stream(stream))
+    _check(st, "ppd_page_append")
+
+
+def ppd_paged_attention_workspace_bytes(L, B, H, G, T, D, S_max, dtype=PPD_BF16) -> int:
+    return int(load().ppd_paged_attention_workspace_bytes(L, B, H, G, T, D, S_max, dtype))
+
+
+def ppd_tree_attention_paged(q, k_pages, v_pages, table, k_tree, v_tree, prefix_len, parent, out, dev_status, lse=None,
+                             scale: float = 0.0, workspace=None, stream=None):
+    """Tree attention over pages: q [L,B,H*G,T,D] (bf16 or fp32), k_tree/v_tree [L,B,H,T,D], pools bf16
+    [L,n_pages,H,page,D], table [B,max_pages], out bf16 [L,B,H*G,T,D].  fp32 operands need a workspace; without
+    one a bf16 call's slices are not cut where clusters of SMs do not fit."""
+    L, B, Hq, T, D = rows = q.shape
+    n_pages, H, page = k_pages.shape[1:4]
+    max_pages = table.shape[1]
+    if H < 1 or Hq % H:
+        raise ValueError(f"{Hq} query heads over {H} K/V heads")
+    i32, dt, bf, pool, tree = torch.int32, q.dtype, torch.bfloat16, (L, n_pages, H, page, D), (L, B, H, T, D)
+    a = _take(("q", q, dt, rows), ("k_pages", k_pages, bf, pool), ("v_pages", v_pages, bf, pool), ("table", table, i32, (B, max_pages)),
+              ("k_tree", k_tree, dt, tree), ("v_tree", v_tree, dt, tree), ("prefix_len", prefix_len, i32, (B,)), ("parent", parent, i32, (B, T)),
+              ("out", out, bf, rows), ("lse", lse, torch.float32, (L, B, Hq, T)), ("dev_status", dev_status, i32, (B,)))
+    ws, ws_n = None, 0
+    if workspace is not None:
+        (ws,), ws_n = _ptrs(workspace), workspace.nbytes
+    st = load().ppd_tree_attention_paged(*a[:8], L, B, H, Hq // H, T, D, page, n_pages, max_pages, _dtype(q), float(scale), *a[8:], ws, ws_n,
+                                         _stream(stream))
+    _check(st, "ppd_tree_attention_paged")
+
+
+def ppd_token_logprobs(logits, tokens, temperature: float, logprob, entropy, rank, dev_status, rows=None, top_tokens=None,
+                       top_logprobs=None, stream=None):
+    """Log probabilities of tokens [B,n] under softmax(row / temperature) of rows [B,n] (or row i) of logits [B,T,V] (fp32 or
+    bf16), the rows' entropies, the tokens' ranks, and with top_tokens and top_logprobs [B,n,K] the K best."""
+    B, T, V = all_rows = logits.shape
+    n = tokens.shape[1]
+    if (top_tokens is None) != (top_logprobs is None):
+        raise ValueError("top_tokens and top_logprobs are given together")
+    K = top_tokens.shape[2] if top_tokens is not None else 0
+    i32, f32, each = torch.int32, torch.float32, (B, n)
+    a = _take(("logits", logits, logits.dtype, all_rows), ("tokens", tokens, i32, each), ("rows", rows, i32, each), ("logprob", logprob, f32, each),
+              ("entropy", entropy, f32, each), ("rank", rank, i32, each), ("top_tokens", top_tokens, i32, (B, n, K)),
+              ("top_logprobs", top_logprobs, f32, (B, n, K)), ("dev_status", dev_status, i32, (B,)))
+    st = load().ppd_token_logprobs(*a[:3], B, T, V, n, K, _dtype(logits), float(temperature), *a[3:], _stream(stream))
+    _check(st, "ppd_token_logprobs")
 
 
 def ppd_selftest_umma(a, b, d, mode: int, N: int, stream=None):
