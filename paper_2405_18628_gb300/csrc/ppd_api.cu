@@ -1437,7 +1437,7 @@ ppd_status ppd_token_logprobs(const void *logits, const int32_t *tokens, const i
         return PPD_ERR_INVALID_ARG;
     if (K > ppd::kLogMaxK || (double)B * n * ppd::kMaxCluster > 2147483647.0 || V > kMaxRows) return PPD_ERR_UNSUPPORTED;
     ppd::LogprobParams p{logits, tokens, rows, logprob, entropy, rank, top_tokens, top_logprobs, dev_status, B, T, V, n, K, dt == PPD_BF16,
-                         1.4426950408889634f / temperature, 1};
+                         1.4426950408889634f / temperature, 138.62943611198906f * temperature, 1};
     return cuda_status(ppd::launch_token_logprobs(p, num_sms(), static_cast<cudaStream_t>(stream)));
 }
 

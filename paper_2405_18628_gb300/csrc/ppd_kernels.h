@@ -550,6 +550,7 @@ struct LogprobParams {
     int32_t *dev_status;             // [B]
     int B, T, V, n, K, bf16;
     float k;                         // log2(e) / temperature
+    float span;                      // 200 / k
     int cluster;                     // CTAs of a row
 };
 cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t stream);

@@ -9,11 +9,19 @@
 // each streaming its columns in batches of 16-byte loads, the next batch's on their way while
 // one is worked on.
 //
-// The K best: `list` holds the best entries of the batches before, `least` the last of them.  A
-// batch in which no thread sees a better entry costs one barrier.  Where up to kFewThreads see
-// some, these push all of theirs; where more do (the first batch; rows that rise), the K-th best
-// of the maxima of groups of four threads bounds the batch's K-th best from below, and the K
-// groups above it push.  A pushed entry's place is the number of better ones.
+// Bound: HBM for many rows, once an entry costs few enough instructions: 6 of them for bf16, which
+// takes its maxima, clamps and comparisons two entries at a time (eight cost 1.4 times the time of
+// the bytes).  So the running maximum, NaN and candidates of a batch come from one maximum that
+// propagates NaN; entries are compared with the token as numbers, against the next number below it in
+// columns before it (where equals rank better); and no key is made but of what is pushed.
+//
+// The K best: entries that beat the K-th best so far are pushed onto a list, without a barrier; after
+// 1, 2, 4, 8, ... batches the list and the best so far are ranked by counting (an entry's place
+// is the number of better ones).  As many batches as there were before bring about K that beat the
+// K-th best of those, so few are ever pushed.  Where there is no such bound (the first batch), or more
+// than fit were pushed (rows that rise: their batches are gone through again), a batch's K-th
+// best is bounded from below by the K-th best of the maxima of pairs of threads: K pairs hold
+// all that are better.
 #include "ppd_device.cuh"
 #include "ppd_kernels.h"
 
@@ -22,10 +30,9 @@
 
 namespace ppd {
 
-constexpr int kLogThreads = 256, kLogWarps = kLogThreads / 32;
+constexpr int kLogThreads = 128, kLogWarps = kLogThreads / 32;
 constexpr int kLogLoads = 4;                   // 16-byte loads of a batch and thread
-constexpr int kGroups = kLogThreads / 4;
-constexpr int kFewThreads = 64;
+constexpr int kGroups = kLogThreads / 2;       // of two threads each
 static_assert(kLogMaxK <= kGroups, "the K-th best group exists");
 
 PPD_DEV uint32_t order_key(float x)
@@ -47,12 +54,25 @@ struct RowStats {
     int better, bad;
 };
 
+// k (x - m).  m k is rounded once and is then what all sums refer to, so that the products
+// below need one fused operation; numbers of the size of fp32's limits are subtracted first.
+constexpr float kPlain = 1e30f;
+PPD_DEV float exponent(float x, float m, float k)
+{
+    return fabsf(x) < kPlain && fabsf(m) < kPlain ? fmaf(x, k, -__fmul_rn(m, k)) : (x - m) * k;
+}
+// The same between two maxima (each m k rounded).
+PPD_DEV float exponent_of_max(float a, float m, float k)
+{
+    return fmaxf(fabsf(a) < kPlain && fabsf(m) < kPlain ? __fsub_rn(__fmul_rn(a, k), __fmul_rn(m, k)) : (a - m) * k, -200.f);
+}
+
 PPD_DEV void merge_stats(RowStats &a, const RowStats &o, float k)
 {
     const float nm = fmaxf(a.m, o.m);
     if (nm > -INFINITY) {
         // 2^d (s, u + d s) with d = k (m - nm) <= 0; nothing where there was no entry
-        const float da = fmaxf((a.m - nm) * k, -200.f), db = fmaxf((o.m - nm) * k, -200.f);
+        const float da = exponent_of_max(a.m, nm, k), db = exponent_of_max(o.m, nm, k);
         const float wa = a.m > -INFINITY ? ex2(da) : 0.f, wb = o.m > -INFINITY ? ex2(db) : 0.f;
         a.u = wa * fmaf(da, a.s, a.u) + wb * fmaf(db, o.s, o.u);
         a.s = wa * a.s + wb * o.s;
@@ -62,16 +82,36 @@ PPD_DEV void merge_stats(RowStats &a, const RowStats &o, float k)
     a.bad |= o.bad;
 }
 
+PPD_DEV __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); }
+PPD_DEV float max3_nan(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// The largest number below x (of the logits' type); NaN below -inf, which nothing is <= to.
 template <bool BF16>
-__global__ void __launch_bounds__(kLogThreads, 3) token_logprobs_kernel(const LogprobParams p)
+PPD_DEV float below(float x)
+{
+    constexpr uint32_t one = BF16 ? 0x10000u : 1u;
+    if (x == 0.f) return __uint_as_float(0x80000000u | one);
+    const uint32_t u = __float_as_uint(x);
+    if (u == 0xFF800000u) return NAN;
+    return __uint_as_float((u & 0x80000000u) ? u + one : u - one);
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kernel(const LogprobParams p)
 {
     constexpr int E = BF16 ? 8 : 4;            // entries of a load
     constexpr int NV = E * kLogLoads;          // of a batch and thread
-    constexpr int kMaxPush = (4 * kLogMaxK > kFewThreads ? 4 * kLogMaxK : kFewThreads) * NV;
+    constexpr int kMaxPush = 2 * kLogMaxK * NV;
     constexpr int eb = BF16 ? 2 : 4;
+    constexpr uint32_t kAbsent = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
     __shared__ unsigned long long s_push[kMaxPush], s_list[2][kLogMaxK], s_group[kGroups], s_bound;
     __shared__ RowStats s_stats[kLogWarps], s_cta;
-    __shared__ int s_n;
+    __shared__ int s_n, s_over;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, V = p.V;
     const int rank = (int)blockIdx.x % p.cluster;
@@ -112,118 +152,29 @@ __global__ void __launch_bounds__(kLogThreads, 3) token_logprobs_kernel(const Lo
         return ld_input(reinterpret_cast<const float *>(x0) + c);
     };
     const float xt = token >= 0 ? entry_at(token) : 0.f;
-    const uint32_t kt = order_key(xt);
+    const unsigned long long et = order_entry(order_key(xt), token);
+    // entries that are not <= this rank before the token: in columns before it, and after it
+    const float th0 = token < 0 ? INFINITY : below<BF16>(xt), th1 = token < 0 ? INFINITY : xt;
+    const bool odd_token = xt != xt;   // (a NaN is compared as an entry)
 
-    // ---- groups of E entries on 16 bytes: group g holds columns [g E - skew, ...)
+    // ---- groups of E entries on 16 bytes: group g holds columns [g E - skew, ...), groups
+    // [f0, f1) of the CTA's [g0, g1) lie inside the row
     const int skew = (int)(reinterpret_cast<uintptr_t>(x0) & 15) / eb;
     const int groups = (int)(((long long)V + skew + E - 1) / E);
     const int g0 = (int)((long long)groups * rank / p.cluster), g1 = (int)((long long)groups * (rank + 1) / p.cluster);
-    auto load = [&](int g, uint4 &r) {
-        if (g >= g1) return;
-        const long long c = (long long)g * E - skew;
-        if (c >= 0 && c + E <= V) {
-            r = ld_input(reinterpret_cast<const uint4 *>(x0 + c * eb));
-            return;
-        }
-        uint32_t w[4] = {0u, 0u, 0u, 0u};   // a row's ends: the entries that it has
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (c + e < 0 || c + e >= V) continue;
-            const uint32_t v = __float_as_uint(entry_at((int)(c + e)));
-            if (BF16) w[e / 2] |= (e & 1) ? v : v >> 16;
-            else w[e] = v;
-        }
-        r = make_uint4(w[0], w[1], w[2], w[3]);
-    };
+    const int f0 = max(g0, skew ? 1 : 0), f1 = min(g1, (int)(((long long)V + skew) / E));
+    const char *xg = x0 - skew * eb;
 
     RowStats st{-INFINITY, 0.f, 0.f, 0, 0};
-    int cur = 0;   // the list in use
+    float x_low = 0.f;             // no entry below it adds to s: 2^-200 of m
+    int cur = 0;                   // the list in use
+    float least = 0.f;             // the list's last entry, once it has K
+    bool full = false;
     if (tid < kLogMaxK) s_list[0][tid] = s_list[1][tid] = 0;
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-    unsigned long long least = 0;   // the list's last: entries must be better
+    if (tid == 0) s_n = s_over = 0;
 
-    uint4 next[kLogLoads];
-#pragma unroll
-    for (int q = 0; q < kLogLoads; ++q) load(g0 + q * kLogThreads + tid, next[q]);
-    for (int base = g0; base < g1; base += kLogLoads * kLogThreads) {
-        float x[NV];
-        // entry e of this thread: column col(e), absent outside [0, V) or past the CTA's groups
-        auto col = [&](int e) { return (long long)(base + (e / E) * kLogThreads + tid) * E - skew + e % E; };
-        auto live = [&](int e) { return base + (e / E) * kLogThreads + tid < g1 && col(e) >= 0 && col(e) < V; };
-#pragma unroll
-        for (int q = 0; q < kLogLoads; ++q) {
-            const uint32_t w[4] = {next[q].x, next[q].y, next[q].z, next[q].w};
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                x[q * E + e] = BF16 ? __uint_as_float((e & 1) ? (w[e / 2] & 0xFFFF0000u) : (w[e / 2] << 16)) : __uint_as_float(w[e]);
-        }
-#pragma unroll
-        for (int q = 0; q < kLogLoads; ++q) load(base + (kLogLoads + q) * kLogThreads + tid, next[q]);
-
-        // ---- statistics
-        float mb = -INFINITY;
-        unsigned long long top = 0;
-#pragma unroll
-        for (int e = 0; e < NV; ++e) {
-            if (!live(e)) {
-                x[e] = -INFINITY;
-                continue;
-            }
-            const uint32_t key = order_key(x[e]);
-            const unsigned long long en = order_entry(key, (int)col(e));
-            top = en > top ? en : top;
-            st.bad |= x[e] != x[e] || x[e] == INFINITY;
-            st.better += en > order_entry(kt, token);
-            mb = fmaxf(mb, x[e]);
-        }
-        if (mb > st.m) {
-            RowStats to{mb, 0.f, 0.f, 0, 0};
-            merge_stats(st, to, p.k);
-        }
-        const float m = st.m > -INFINITY ? st.m : 0.f;
-#pragma unroll
-        for (int e = 0; e < NV; ++e) {
-            const float d = fmaxf((x[e] - m) * p.k, -200.f);   // (2^-200 is 0; nothing times an infinity)
-            const float v = ex2(d);
-            st.s += v;
-            st.u = fmaf(v, d, st.u);
-        }
-        if (K == 0) continue;
-
-        // ---- the K best
-        unsigned long long bound = least + 1;
-        const int seeing = __syncthreads_count(top >= bound);
-        if (seeing == 0) continue;
-        if (seeing > kFewThreads) {
-            unsigned long long gm = top;
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                const unsigned long long y = __shfl_xor_sync(0xffffffffu, gm, o);
-                gm = y > gm ? y : gm;
-            }
-            if ((lane & 3) == 0) s_group[tid >> 2] = gm;
-            if (tid == 0) s_bound = 0;
-            __syncthreads();
-            if (tid < kGroups) {
-                const unsigned long long g = s_group[tid];
-                int place = 0;
-                for (int y = 0; y < kGroups; ++y) place += s_group[y] > g;
-                if (g != 0 && place == K - 1) s_bound = g;   // (fewer groups than K: no bound)
-            }
-            __syncthreads();
-            bound = s_bound > bound ? s_bound : bound;
-        }
-        if (top >= bound) {
-#pragma unroll
-            for (int e = 0; e < NV; ++e) {
-                if (!live(e)) continue;
-                const unsigned long long en = order_entry(order_key(x[e]), (int)col(e));
-                if (en >= bound) s_push[atomicAdd(&s_n, 1)] = en;
-            }
-        }
-        if (tid < kLogMaxK) s_list[cur ^ 1][tid] = 0;
-        __syncthreads();
+    // The list and the pushed entries together, by the whole block (after a barrier).
+    auto rank_pushed = [&]() {
         const int n = s_n;
         for (int y = tid; y < n + K; y += kLogThreads) {
             const unsigned long long mine = y < n ? s_push[y] : s_list[cur][y - n];
@@ -233,48 +184,319 @@ __global__ void __launch_bounds__(kLogThreads, 3) token_logprobs_kernel(const Lo
             if (mine != 0 && place < K) s_list[cur ^ 1][place] = mine;
         }
         __syncthreads();
+        if (tid < kLogMaxK) s_list[cur][tid] = 0;   // (for the ranking after the next)
         cur ^= 1;
-        least = s_list[cur][K - 1];
+        const unsigned long long last = s_list[cur][K - 1];
+        full = last != 0;
+        least = key_value((uint32_t)(last >> 32));
         if (tid == 0) s_n = 0;
+        __syncthreads();
+    };
+
+    // Rare work (a row's ends, the token's own group, numbers near the type's ends, pushes) is
+    // done in rolled loops that pick a load's words by selects: the code of a batch is a
+    // few hundred instructions, which the instruction cache holds.
+    constexpr int kStep = kLogLoads * kLogThreads;
+    uint4 next[kLogLoads];
+    bool fill = true;              // nothing but loads of the batch after
+    bool bounded = true;           // batch by batch, with a bound of its own
+    bool again = false;            // ... of batches whose sums are taken
+    int from = g0, to = g0 + kStep;   // the batches that are ranked together
+    for (int base = g0 - kStep; base < g1; base += kStep) {
+        uint4 w[kLogLoads];
+#pragma unroll
+        for (int q = 0; q < kLogLoads; ++q) w[q] = next[q];
+        auto group = [&](int q) { return base + q * kLogThreads + tid; };
+        // the next batch's loads
+        if (base + kStep >= f0 && base + 2 * kStep <= f1) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(xg) + group(0) + kStep;
+#pragma unroll
+            for (int q = 0; q < kLogLoads; ++q) next[q] = ld_input(src + q * kLogThreads);
+        } else if (base + kStep < g1) {
+#pragma unroll
+            for (int q = 0; q < kLogLoads; ++q) {
+                const int g = group(q) + kStep;
+                next[q] = make_uint4(kAbsent, kAbsent, kAbsent, kAbsent);
+                if (g >= f0 && g < f1) next[q] = ld_input(reinterpret_cast<const uint4 *>(xg + (size_t)g * 16));
+            }
+#pragma unroll 1
+            for (int q = 0; q < kLogLoads; ++q) {
+                const int g = group(q) + kStep;
+                if (g >= g1 || (g >= f0 && g < f1)) continue;
+                // a row's end: the entries that it has
+                uint32_t v[4] = {kAbsent, kAbsent, kAbsent, kAbsent};
+                const long long c = (long long)g * E - skew;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (c + e < 0 || c + e >= V) continue;
+                    const uint32_t y = __float_as_uint(entry_at((int)(c + e)));
+                    if (!BF16) v[e & 3] = y;
+                    else if (e & 1) v[e / 2] = (v[e / 2] & 0xFFFFu) | y;
+                    else v[e / 2] = (v[e / 2] & 0xFFFF0000u) | y >> 16;
+                }
+#pragma unroll
+                for (int x = 0; x < kLogLoads; ++x)
+                    if (x == q) next[x] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+        }
+        if (fill) {
+            fill = false;
+            continue;
+        }
+        auto word = [&](const uint4 &r, int x) { return x == 0 ? r.x : x == 1 ? r.y : x == 2 ? r.z : r.w; };
+        auto value = [&](const uint4 &r, int e) {   // entry e of a load's E
+            if (!BF16) return __uint_as_float(word(r, e));
+            return __uint_as_float((e & 1) ? (word(r, e / 2) & 0xFFFF0000u) : (word(r, e / 2) << 16));
+        };
+        auto pick = [&](int q) {
+            uint4 r = w[0];
+#pragma unroll
+            for (int x = 1; x < kLogLoads; ++x)
+                if (x == q) r = w[x];
+            return r;
+        };
+        auto column = [&](int q, int e) { return (long long)group(q) * E - skew + e; };
+        auto live = [&](int q, int e) { return group(q) < g1 && column(q, e) >= 0 && column(q, e) < V; };
+
+        // ---- the batch's maximum, NaN where there is one
+        float mb;
+        if (BF16) {
+            __nv_bfloat162 a = as_bf162(w[0].x), c = as_bf162(w[0].y);
+            a = __hmax2_nan(a, as_bf162(w[0].z)), c = __hmax2_nan(c, as_bf162(w[0].w));
+#pragma unroll
+            for (int q = 1; q < kLogLoads; ++q) {
+                a = __hmax2_nan(__hmax2_nan(a, as_bf162(w[q].x)), as_bf162(w[q].z));
+                c = __hmax2_nan(__hmax2_nan(c, as_bf162(w[q].y)), as_bf162(w[q].w));
+            }
+            a = __hmax2_nan(a, c);
+            mb = max3_nan(__low2float(a), __high2float(a), -INFINITY);
+        } else {
+            float a = -INFINITY, c = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < kLogLoads; ++q) {
+                a = max3_nan(a, value(w[q], 0), value(w[q], 1));
+                c = max3_nan(c, value(w[q], E > 2 ? 2 : 0), value(w[q], E > 2 ? 3 : 1));
+            }
+            mb = max3_nan(a, c, -INFINITY);
+        }
+        if (!again) {
+        st.bad |= !(mb < INFINITY);
+        if (mb > st.m) {
+            const float d = exponent_of_max(st.m, mb, p.k), f = ex2(d);   // (s is 0 where m was -inf)
+            st.u = f * fmaf(d, st.s, st.u);
+            st.s *= f;
+            st.m = mb;
+            x_low = __fsub_rd(mb, p.span);
+        }
+        // ---- sums
+        if (mb == -INFINITY) {
+            // nothing to add
+        } else if (fabsf(st.m) < kPlain && p.span < kPlain && p.span > 0.02f) {
+            const uint64_t nm2 = pack2(-__fmul_rn(st.m, p.k), -__fmul_rn(st.m, p.k)), k2 = pack2(p.k, p.k);
+            uint64_t s2 = 0ull, u2 = 0ull;
+            const __nv_bfloat162 low2 = __bfloat162bfloat162(__float2bfloat16_rd(x_low));
+#pragma unroll
+            for (int q = 0; q < kLogLoads; ++q) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float a, c;
+                    if (BF16) {
+                        const __nv_bfloat162 v = __hmax2(as_bf162(word(w[q], e / 2)), low2);
+                        const uint32_t x = *reinterpret_cast<const uint32_t *>(&v);
+                        a = __uint_as_float(x << 16), c = __uint_as_float(x & 0xFFFF0000u);
+                    } else {
+                        a = fmaxf(value(w[q], e), x_low), c = fmaxf(value(w[q], e + 1), x_low);
+                    }
+                    const uint64_t d2 = fma2(pack2(a, c), k2, nm2);
+                    unpack2(d2, a, c);
+                    const uint64_t v2 = pack2(ex2(a), ex2(c));
+                    s2 = add2(s2, v2);
+                    u2 = fma2(v2, d2, u2);
+                }
+            }
+            float a, c;
+            unpack2(s2, a, c);
+            st.s += a + c;
+            unpack2(u2, a, c);
+            st.u += a + c;
+        } else {   // numbers whose differences may overflow
+#pragma unroll 1
+            for (int q = 0; q < kLogLoads; ++q) {
+                const uint4 r = pick(q);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float d = fmaxf(exponent(value(r, e), st.m, p.k), -200.f);   // (2^-200 is 0; nothing times an infinity)
+                    const float v = ex2(d);
+                    st.s += v;
+                    st.u = fmaf(v, d, st.u);
+                }
+            }
+        }
+        // ---- entries that rank before the token
+        const long long c0 = (long long)base * E - skew;   // the batch's first column
+        if (base >= f0 && base + kStep <= f1 && !odd_token && (token < c0 || token >= c0 + (long long)kStep * E)) {
+            const float th = c0 < token ? th0 : th1;
+            if (BF16) {
+                const __nv_bfloat162 th2 = __bfloat162bfloat162(__float2bfloat16_rn(th));
+                __nv_bfloat162 n2 = __hgtu2(as_bf162(w[0].x), th2);
+#pragma unroll
+                for (int x = 1; x < 4 * kLogLoads; ++x) n2 = __hadd2(n2, __hgtu2(as_bf162(word(w[x / 4], x % 4)), th2));
+                st.better += (int)(__low2float(n2) + __high2float(n2));
+            } else {
+#pragma unroll
+                for (int q = 0; q < kLogLoads; ++q)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) st.better += !(value(w[q], e) <= th);
+            }
+        } else {   // the batch of the token, or a row's end: the loads that hold them entry by entry
+#pragma unroll 1
+            for (int q = 0; q < kLogLoads; ++q) {
+                const uint4 r = pick(q);
+                const int g = group(q);
+                const long long c = column(q, 0);
+                if (g >= g1) continue;
+                if (odd_token || (c <= token && token < c + E) || g < f0 || g >= f1) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        st.better += live(q, e) && order_entry(order_key(value(r, e)), (int)c + e) > et;
+                } else {
+                    const float th = c < token ? th0 : th1;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) st.better += !(value(r, e) <= th);
+                }
+            }
+        }
+        }
+        if (K == 0) continue;
+
+        // ---- the K best
+        const bool sees = full ? !(mb <= least) && least == least : group(0) < g1;
+        unsigned long long bound = full ? (unsigned long long)(order_key(least) + 1) << 32 : 1;   // (equal ones come later)
+        if (bounded) {
+            // this thread's best entry: the first of the batch's largest
+            int at = 0;
+#pragma unroll
+            for (int q = kLogLoads - 1; q >= 0; --q)
+#pragma unroll
+                for (int e = E - 1; e >= 0; --e) {
+                    const float v = value(w[q], e);
+                    if (!(v < mb) && (v == mb || v != v) && (mb > -INFINITY || mb != mb)) at = q * E + e;
+                }
+            unsigned long long gm = 0;
+            if (sees) {
+                int q = at / E, e = at % E;
+                if (mb == -INFINITY)   // only -inf: the first entry that there is
+                    while (q < kLogLoads && !live(q, e)) e = e + 1 < E ? e + 1 : 0, q += e == 0;
+                if (q < kLogLoads) gm = order_entry(order_key(mb), (int)column(q, e));
+            }
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, gm, 1);
+            gm = other > gm ? other : gm;
+            if ((lane & 1) == 0) s_group[tid >> 1] = gm;
+            if (tid == 0) s_bound = 0;
+            __syncthreads();
+            if (tid < kGroups) {
+                const unsigned long long g = s_group[tid];
+                int place = 0;
+#pragma unroll 4
+                for (int y = 0; y < kGroups; ++y) place += s_group[y] > g;
+                if (g != 0 && place == K - 1) s_bound = g;   // (fewer pairs than K: no bound)
+            }
+            __syncthreads();
+            bound = s_bound > bound ? s_bound : bound;
+        }
+        if (sees && order_entry(order_key(mb), 0) >= bound) {
+            // the entries that may be among the best, one bit each (few threads have more than
+            // one or two), read again from the row
+            const float t0 = key_value((uint32_t)(bound >> 32)), t = bound > 1 ? below<false>(t0) : NAN;   // those that are not <= t
+            uint32_t some = 0;
+            if (BF16) {
+                const __nv_bfloat162 t2 = __bfloat162bfloat162(__float2bfloat16_rd(t));
+#pragma unroll
+                for (int x = 0; x < 4 * kLogLoads; ++x) some |= __hgtu2_mask(as_bf162(word(w[x / 4], x % 4)), t2) & 0x10001u << x;
+            } else {
+#pragma unroll
+                for (int q = 0; q < kLogLoads; ++q)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) some |= (value(w[q], e) <= t ? 0u : 1u) << (q * E + e);
+            }
+            while (some) {
+                const int bit = __ffs(some) - 1;
+                some &= some - 1;
+                const int at = BF16 ? 2 * (bit & 15) + (bit >> 4) : bit;
+                const int q = at / E, e = at % E;
+                if (!live(q, e)) continue;
+                const unsigned long long en = order_entry(order_key(entry_at((int)column(q, e))), (int)column(q, e));
+                if (en < bound) continue;
+                const int place = atomicAdd(&s_n, 1);
+                if (place < kMaxPush) s_push[place] = en;
+                else s_over = 1;   // (not where the batch has a bound)
+            }
+        }
+        if (bounded || base + kStep >= to || base + kStep >= g1) {
+            __syncthreads();
+            if (s_over) {
+                // more than fit: the same batches again, one by one
+                __syncthreads();
+                if (tid == 0) s_n = s_over = 0;   // (barriers before the next push)
+                to = min(to, base + kStep);
+                base = from - 2 * kStep;
+                fill = bounded = again = true;
+                continue;
+            }
+            rank_pushed();
+            if (base + kStep >= to) {
+                from = base + kStep;
+                to = from + max(from - g0, kStep);
+                bounded = again = false;
+            }
+        }
     }
 
     // ---- the CTA's statistics, then the cluster's
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        RowStats y;
-        y.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-        y.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-        y.u = __shfl_xor_sync(0xffffffffu, st.u, o);
-        y.better = __shfl_xor_sync(0xffffffffu, st.better, o);
-        y.bad = __shfl_xor_sync(0xffffffffu, st.bad, o);
-        merge_stats(st, y, p.k);
-    }
+    auto merge_lanes = [&](int most) {
+#pragma unroll 1
+        for (int o = most; o > 0; o >>= 1) {
+            RowStats y;
+            y.m = __shfl_xor_sync(0xffffffffu, st.m, o);
+            y.s = __shfl_xor_sync(0xffffffffu, st.s, o);
+            y.u = __shfl_xor_sync(0xffffffffu, st.u, o);
+            y.better = __shfl_xor_sync(0xffffffffu, st.better, o);
+            y.bad = __shfl_xor_sync(0xffffffffu, st.bad, o);
+            merge_stats(st, y, p.k);
+        }
+    };
+    const RowStats empty{-INFINITY, 0.f, 0.f, 0, 0};
+    merge_lanes(16);
     if (lane == 0) s_stats[warp] = st;
     if (cur == 1 && tid < K) s_list[0][tid] = s_list[1][tid];
     __syncthreads();
-    if (tid == 0) {
-        st = s_stats[0];
-        for (int w = 1; w < kLogWarps; ++w) merge_stats(st, s_stats[w], p.k);
-        s_cta = st;
+    if (warp == 0) {
+        st = lane < kLogWarps ? s_stats[lane] : empty;
+        merge_lanes(kLogWarps / 2);
+        if (lane == 0) s_cta = st;
     }
     if (p.cluster > 1) cluster_sync();
     else __syncthreads();
     if (rank == 0) {
-        // every thread the whole row's statistics
-        st = s_cta;
-        for (int c = 1; c < p.cluster; ++c) {
-            const uint32_t a = cluster_map(smem_addr(&s_cta), c);
-            RowStats y;
-            y.m = ld_cluster_f32(a);
-            y.s = ld_cluster_f32(a + 4);
-            y.u = ld_cluster_f32(a + 8);
-            y.better = __float_as_int(ld_cluster_f32(a + 12));
-            y.bad = __float_as_int(ld_cluster_f32(a + 16));
-            merge_stats(st, y, p.k);
+        // every warp the whole row's statistics
+        st = empty;
+        if (lane < p.cluster) {
+            const uint32_t a = cluster_map(smem_addr(&s_cta), lane);
+            st.m = ld_cluster_f32(a);
+            st.s = ld_cluster_f32(a + 4);
+            st.u = ld_cluster_f32(a + 8);
+            st.better = __float_as_int(ld_cluster_f32(a + 12));
+            st.bad = __float_as_int(ld_cluster_f32(a + 16));
         }
+        merge_lanes(kMaxCluster / 2);   // lane 0's (lanes 0 to 7 agree)
+        st.m = __shfl_sync(0xffffffffu, st.m, 0);
+        st.s = __shfl_sync(0xffffffffu, st.s, 0);
+        st.u = __shfl_sync(0xffffffffu, st.u, 0);
+        st.better = __shfl_sync(0xffffffffu, st.better, 0);
+        st.bad = __shfl_sync(0xffffffffu, st.bad, 0);
         const bool bad = st.bad || st.m == -INFINITY;
         const float lg = lg2(st.s), ln2 = 0.69314718055994530942f;
-        auto logprob = [&](float x) { return bad ? NAN : ((x - st.m) * p.k - lg) * ln2; };
+        auto logprob = [&](float x) { return bad ? NAN : (exponent(x, st.m, p.k) - lg) * ln2; };
         if (tid == 0) {
             p.logprob[item] = token < 0 ? 0.f : logprob(xt);
             p.entropy[item] = bad ? NAN : (lg - st.u / st.s) * ln2;
