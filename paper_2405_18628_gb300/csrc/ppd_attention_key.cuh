@@ -219,7 +219,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     } else if (PAGED && warp == Lay::SW) {
         if constexpr (PAGED) {
             // -------------------------------------------------------- TMA producer, page by page
-            // the whole warp: a lane copies one box, 64 columns of a page's rows of the tile
+            // the whole warp walks the tiles, a lane looks up a box's page, one elected lane copies
             const uint64_t pol = l2_policy_evict_first();
             KPos kp;
             VPos vp;
@@ -229,7 +229,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                             const UnitInfo &ui, int row) {
                 if (warp_uniform(*abort_flag)) return;
                 if (!tree) {
-                    load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, lane, pol);
+                    load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, pol);
                 } else if (lane == 0) {
                     mbar_arrive_expect_tx(full, Lay::TILE_BYTES);
 #pragma unroll
@@ -242,7 +242,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                 const UnitInfo &ui = sg.ui;
                 const int qs = k & 1;
                 const PageUnit pu(p, ui.lbh, ui.b);
-                int z = page_coord<Lay::DCH>(p, pu, sg.j0 * Lay::KT, ui.P, lane);
+                int z = page_coord(p, pu, sg.j0 * Lay::KT, ui.P, lane);
                 mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
                 if (!warp_uniform(*abort_flag) && lane == 0) {
                     mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
@@ -256,7 +256,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                     const bool tree = (j == ui.n_pref);
                     const int row = j * Lay::KT;
                     // the next tile's page numbers are asked for a tile ahead
-                    const int z_next = page_coord<Lay::DCH>(p, pu, row + Lay::KT, ui.P, lane);
+                    const int z_next = page_coord(p, pu, row + Lay::KT, ui.P, lane);
                     mbar_wait(bars + Lay::B_KEMPTY + kp.slot, kp.phase ^ 1u, abort_flag);
                     load(&map_kc, &map_kt, Lay::OFF_K + kp.slot * Lay::TILE_BYTES, bars + Lay::B_KFULL + kp.slot, tree, z, ui, row);
                     kp.advance();

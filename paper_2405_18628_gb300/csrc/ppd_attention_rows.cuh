@@ -314,7 +314,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
     } else if (PAGED && warp == 8) {
         if constexpr (PAGED) {
             // -------------------------------------------------------- TMA producer, page by page
-            // the whole warp: a lane copies one box, 64 columns of a page's rows of the tile
+            // the whole warp walks the tiles, a lane looks up a box's page, one elected lane copies
             const uint64_t pol = p.n_qb > 2 ? l2_policy_evict_normal() : l2_policy_evict_first();
             Pos pos;
             int n_tiles = 0, n_q0 = 0, n_q1 = 0;   // copies issued: ring tiles, Q blocks per slot
@@ -328,7 +328,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                     uint64_t *full = bars + Lay::B_FULL + pos.slot;
                     uint8_t *dst = smem + Lay::OFF_R + pos.slot * Lay::TILE_BYTES;
                     if (!t.tree) {
-                        load_page_tile<Lay::DCH>(p, pages, dst, Lay::GROUP_BYTES, full, t.depth, t.row, t.P, lane, pol);
+                        load_page_tile<Lay::DCH>(p, pages, dst, Lay::GROUP_BYTES, full, t.depth, t.row, t.P, pol);
                     } else if (lane == 0) {
                         mbar_arrive_expect_tx(full, Lay::TILE_BYTES);
 #pragma unroll
@@ -363,13 +363,13 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             for (RowsJob jb; it.next(p, jb); ++k) {
                 const UnitInfo &ui = jb.ui;
                 const PageUnit pu(p, ui.lbh, ui.b);
-                int depth = page_coord<Lay::DCH>(p, pu, jb.j0 * Lay::KT, ui.P, lane);
+                int depth = page_coord(p, pu, jb.j0 * Lay::KT, ui.P, lane);
                 if (!jb.pair) load_q(k & 1, (uint32_t)(k >> 1) & 1u, ui.qb, ui.lbh);
                 for (int j = jb.j0; j < jb.j1; ++j, ++g) {
                     const bool tree = (j >= ui.n_pref);
                     const Tile t{(tree ? j - ui.n_pref : j) * Lay::KT, ui.lbh, ui.P, depth, tree};
                     // the next tile's page numbers are asked for a tile ahead
-                    depth = page_coord<Lay::DCH>(p, pu, (j + 1) * Lay::KT, ui.P, lane);
+                    depth = page_coord(p, pu, (j + 1) * Lay::KT, ui.P, lane);
                     if (jb.pair) {
                         load(&map_kc, &map_kt, t);
                         load(&map_vc, &map_vt, t);
