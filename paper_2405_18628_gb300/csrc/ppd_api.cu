@@ -8,6 +8,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <atomic>
@@ -1302,33 +1303,75 @@ ppd_status ppd_page_append(const void *k_new, const void *v_new, void *k_pages, 
     return cuda_status(ppd::launch_page_append(p, static_cast<cudaStream_t>(stream)));
 }
 
-// How an attention call over pages runs: blocks of query rows, how they are shared out, and where
-// the bf16 copies of fp32 operands and the work split's states lie in the workspace.
+// How an attention call over pages runs: units of query rows of a slice (n_qb of them), how they are
+// shared out, and where the bf16 copies of fp32 operands and the work split's states lie in the
+// workspace.
 struct PagedWs {
-    int rows, n_qb, n_tt;
+    int rows, n_qb, n_tt, pair_units;
     AttnPlan plan;
     size_t rec, part, total;
 };
 
+// Slices of more than 64 rows, by the time that each way takes, in microseconds a job of t_u tiles and at
+// its ends (the tables' capacity standing in for the lengths), as measured with D = 128, pages of
+// 32: a tile of 128 queries 1.09, or 1.47 where every SM streams keys of its own, of a pair of blocks
+// 2.05; whole jobs' ends 6, a cluster's 12, and the work split's 29 (two jobs a CTA, 130 KB of
+// partial state each, and the merge).  Whole / clusters / shared out, heads of 64 tokens:
+//   16 slices, 4 heads, 3001 rows    32.6 /  19.6 /  32.6     96 of 4, ragged to 5001   82.4 /      /  72.6
+//   8 of 4, 20,001                    169 /  41.2 /  42.0     64 of 8                   84.2 /      /  90.5
+//   40 of 2, 4001                    40.2 /  22.6 /  29.7     80 of 8                    119 /      / 105.6
+// (units of the work split: pairs of blocks; single ones 77.4, 100.8 and 125.7 in the last column's cases).
+static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, bool workspace)
+{
+    const long long sms = split_grid(), blocks = (w.rows + 127) / 128, pairs = (blocks + 1) / 2;
+    auto rounds = [&](long long jobs) { return (double)((jobs + sms - 1) / sms); };
+    const double alone = slices * blocks >= sms ? 1.47 : 1.09;
+    double best = rounds(slices * blocks) * alone * t_u + 6;
+    if (blocks > 1) best = std::min(best, rounds(slices * pairs) * 2.05 * t_u + 6);
+    w.plan = {0, 1};
+    w.n_qb = (int)blocks;
+    w.pair_units = 0;
+    for (int c = 2; c <= ppd::kMaxCluster && c <= t_u && slices * blocks * c <= sms; ++c) {
+        const double cost = 1.09 * ((t_u + c - 1) / c) + 12;
+        if (cost < best && slices * blocks <= ppd::max_attention_clusters(c)) {
+            best = cost;
+            w.plan.cluster = c;
+        }
+    }
+    const double shared = rounds(slices * pairs * t_u) * (blocks > 1 ? 2.05 : 1.47) + 29;
+    // (a twentieth less: lengths are seldom alike, and whole jobs take the longest first)
+    if (workspace && B <= ppd::kSplitMaxB && slices * pairs * t_u <= 2147483647ll && shared < 0.95 * best) {
+        w.plan = {1, 1};
+        if (blocks > 1) {
+            w.pair_units = 1;
+            w.n_qb = (int)pairs;
+        }
+    }
+}
+
 static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt, bool workspace)
 {
     PagedWs w{};
-    const long long slices = (long long)L * B * H;
+    const long long slices = (long long)L * B * H, sms = split_grid();
     w.rows = G * T;
-    w.n_qb = w.rows > 64 ? (w.rows + 127) / 128 : 1;
     w.n_tt = w.rows > 64 ? (T + 127) / 128 : 1;
-    const long long units = slices * w.n_qb, t_u = (S_max + 127) / 128 + w.n_tt, sms = split_grid();
-    w.plan = plan_units(units, t_u, B, workspace && units * t_u <= 2147483647ll, true);
-    // (a last, partial round of whole units weighs more here: requests' lengths are seldom alike)
-    if (workspace && units >= sms && B <= ppd::kSplitMaxB && units * t_u <= 2147483647ll &&
-        (units * t_u + sms - 1) / sms + kPagedSplitCostTiles < (units + sms - 1) / sms * t_u)
-        w.plan = {1, 1};
+    const long long t_u = (S_max + 127) / 128 + w.n_tt;
+    if (w.rows > 64) {
+        plan_paged_rows(w, slices, t_u, B, workspace);
+    } else {
+        w.n_qb = 1;
+        w.plan = plan_units(slices, t_u, B, workspace && slices * t_u <= 2147483647ll, true);
+        // (a last, partial round of whole units weighs more here: requests' lengths are seldom alike)
+        if (workspace && slices >= sms && B <= ppd::kSplitMaxB && slices * t_u <= 2147483647ll &&
+            (slices * t_u + sms - 1) / sms + kPagedSplitCostTiles < (slices + sms - 1) / sms * t_u)
+            w.plan = {1, 1};
+    }
     size_t off = dt == PPD_F32 ? align_up((size_t)slices * (w.rows + 2 * (size_t)T) * D * 2) : 0;
     if (w.plan.split) {
         w.rec = off;
         off = align_up(off + (size_t)split_grid() * sizeof(ppd::SplitRecord));
         w.part = off;
-        off = align_up(off + (size_t)2 * split_grid() * ppd::kSplitRows * (D + 2) * sizeof(float));
+        off = align_up(off + (size_t)2 * split_grid() * (w.pair_units ? 2 : 1) * ppd::kSplitRows * (D + 2) * sizeof(float));
     }
     w.total = off;
     return w;
@@ -1405,7 +1448,8 @@ ppd_status ppd_tree_attention_paged(const void *q, const void *k_pages, const vo
     p.max_pages = max_pages, p.n_pages = n_pages, p.n_depth = L * n_pages * H;
     p.page_shift = shift, p.box_shift = shift < 7 ? shift : 7;
     p.rows = w.rows;
-    ppd::plan_rows(p, split_grid());
+    p.pair_units = w.pair_units;
+    if (!w.pair_units) ppd::plan_rows(p, split_grid());
     p.cluster = w.plan.cluster;
     if (w.plan.split) {
         p.split = 1;

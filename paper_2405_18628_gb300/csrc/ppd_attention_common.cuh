@@ -326,8 +326,8 @@ PPD_DEV SplitParts split_parts(long long N, long long off, int n_tiles)
 
 PPD_DEV int split_slot(const SplitParts &sp, int c) { return c == sp.c_a ? sp.slot_a : 2 * c; }
 
-// Floats of one partial-state slot: kSplitRows rows of D, their maxima, their sums.
-PPD_DEV size_t split_slot_floats(int D) { return (size_t)kSplitRows * (D + 2); }
+// Floats of one partial-state slot: `rows` rows of D, their maxima, their sums.
+PPD_DEV size_t split_slot_floats(int D, int rows = kSplitRows) { return (size_t)rows * (D + 2); }
 
 // Merge the partial states of a cut unit whose parts have all arrived: slot
 // row r (output row out_row0 + r), columns [c0, c0 + 8), by one thread.  One
@@ -336,13 +336,13 @@ PPD_DEV size_t split_slot_floats(int D) { return (size_t)kSplitRows * (D + 2); }
 // weighted sum of the parts' O rows over the weighted sum of their row sums.
 // The parts are read eight at a time, every load of a batch issued before any
 // is used, so a batch costs one round trip to L2.
-template <class Out>
+template <class Out, int kRows = kSplitRows>
 static __device__ __forceinline__ void split_merge_chunk(const float *split_part, Out *out, float *lse,
                                                          const SplitParts &sp, long long N, int G,
                                                          size_t out_row0, int r, int c0, int D)
 {
     constexpr int PB = 8;   // parts per batch
-    const size_t sf = split_slot_floats(D);
+    const size_t sf = split_slot_floats(D, kRows);
     const bool dense = N >= G;   // no empty ranges
     float M = -INFINITY, Ls = 0.f;
     float acc[8];
@@ -356,8 +356,8 @@ static __device__ __forceinline__ void split_merge_chunk(const float *split_part
             const int c = cb + y;
             const bool live = c <= sp.c_b && (dense || split_nonempty(c, N, G));
             const float *b_ = split_part + (size_t)split_slot(sp, live ? c : sp.c_a) * sf;
-            mc[y] = live ? __ldcg(b_ + (size_t)kSplitRows * D + r) : -INFINITY;
-            lc[y] = live ? __ldcg(b_ + (size_t)kSplitRows * D + kSplitRows + r) : 0.f;
+            mc[y] = live ? __ldcg(b_ + (size_t)kRows * D + r) : -INFINITY;
+            lc[y] = live ? __ldcg(b_ + (size_t)kRows * D + kRows + r) : 0.f;
             const float4 *o4 = reinterpret_cast<const float4 *>(b_ + (size_t)r * D + c0);
             v[y][0] = live ? __ldcg(o4) : make_float4(0.f, 0.f, 0.f, 0.f);
             v[y][1] = live ? __ldcg(o4 + 1) : make_float4(0.f, 0.f, 0.f, 0.f);

@@ -120,26 +120,28 @@ struct RowsJob {
 };
 
 // Does this CTA take pair jobs (all its jobs are of one kind)?
-template <bool RANGE>
-PPD_DEV bool rows_pair_cta(const AttnParams &p)
+template <bool RANGE, bool PAGED = false>
+PPD_DEV bool rows_pair_cta(const AttnParamsOf<PAGED> &p)
 {
+    if constexpr (PAGED && RANGE) return p.split && p.pair_units;
     return !RANGE && p.pairs && ((p.n_qb & 1) == 0 || (int)blockIdx.x < p.pair_grid);
 }
 
 // Walks a CTA's jobs in order (every role walks the same sequence).  Whole
 // jobs round-robin: single jobs, or n_qb / 2 pair jobs a slice; with an odd n_qb
 // the first p.pair_grid CTAs take the slices' pairs and
-// the others their last blocks.  RANGE (either split): single jobs, the CTA's range
-// of tiles.
+// the others their last blocks.  RANGE (either split): the CTA's range of tiles, single jobs, or
+// in a work split over pages (p.pair_units: units are pairs of blocks, the last one's second
+// may hold no row) pair jobs.
 template <bool RANGE, bool RAGGED = false, bool PAGED = false>
 struct RowsIter {
     SegIter<RANGE, RAGGED> seg;
     int x, step, n, per;
     bool pair;
-    PPD_DEV RowsIter(const AttnParams &p, const WorkRange &w) : seg(w)
+    PPD_DEV RowsIter(const AttnParamsOf<PAGED> &p, const WorkRange &w) : seg(w)
     {
         const int c = (int)blockIdx.x, G = (int)gridDim.x;
-        pair = rows_pair_cta<RANGE>(p);
+        pair = rows_pair_cta<RANGE, PAGED>(p);
         x = c;
         step = G;
         per = p.n_qb;   // jobs a slice
@@ -160,11 +162,19 @@ struct RowsIter {
             j.ui = s.ui;
             j.j0 = s.j0;
             j.j1 = s.j1;
-            j.pair = false;
+            j.pair = PAGED && pair;
+            if (PAGED && pair) j.ui.qb *= 2;
             return true;
         }
         int job = x;
-        if (RAGGED && seg.seq) job = ragged_job(p, seg.seq, x, step, n, per);
+        if (RAGGED && seg.seq) {
+            job = ragged_job(p, seg.seq, x, step, n, per);
+            // over pages every role walks with whole warps, and the compiler is told that a job
+            // read from the order in shared memory is the same in every lane: products of a job that
+            // it does not know to be uniform have every operand moved one by one (30 requests of up
+            // to 5000 rows, 128 query rows each: 130 us, and 91 like this)
+            if (PAGED) job = warp_uniform(job);
+        }
         if (job < 0 || job >= n) return false;
         x += step;
         const int slice = job / per, i = job - slice * per;
@@ -212,7 +222,7 @@ PPD_DEV void rows_prefetch_pages(const PagedParams &p, int lane, const CUtensorM
         prefetch_pages<DCH>(p, lane, kc, vc, w.u_first, w.j_first, min(w.n_tiles, n));
         return;
     }
-    const RowsIter<RANGE> it(p, w);
+    const RowsIter<RANGE, false, true> it(p, w);
     if (it.x < it.n) prefetch_pages<DCH>(p, lane, kc, vc, it.x / it.per * p.n_qb, 0, n);
 }
 
@@ -248,7 +258,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
     const int lane = threadIdx.x & 31;
     const int T = p.T, R = query_rows<PAGED>(p);   // tree tokens, query rows of a slice
 
-    const bool pair_cta = rows_pair_cta<RANGE>(p);
+    const bool pair_cta = rows_pair_cta<RANGE, PAGED>(p);
     if (threadIdx.x == 0) {
         for (int i = 0; i < Lay::NBAR; ++i) {
             uint32_t count = 1;
@@ -812,6 +822,28 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             if (lane == 0) mbar_arrive_n(bars + Lay::B_OFREE + st, n);
         };
 
+        // End of a part of a pair job: this stream's block, unnormalised, beside the other's.
+        auto finish_pair_part = [&](int slot) {
+            const int row = s * Lay::M + q;
+            float *base = p.split_part + (size_t)slot * split_slot_floats(D, 2 * kSplitRows);
+            base[(size_t)2 * kSplitRows * D + row] = m;
+            base[(size_t)2 * kSplitRows * (D + 1) + row] = l;
+            wait_done(s);
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t r[32];
+                tmem_ld32(t_os + c, r);
+                tmem_wait_ld(r);
+                if (c + 32 == D) {
+                    tc_fence_before();
+                    __syncwarp();
+                    o_free(s, 2);
+                }
+                store32(base + (size_t)row * D + c, r, 1.f);
+            }
+        };
+
         // End of a pair job: this stream's block of 128 rows.
         auto finish_pair = [&](const RowsJob &jb) {
             const int qg = (jb.ui.qb + s) * Lay::M + q;
@@ -921,7 +953,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             const UnitInfo &ui = jb.ui;
             const int qb = ui.qb + (jb.pair ? s : 0);
             const int qg = qb * Lay::M + q;   // this thread's row: tree token qg (of a head: qg mod T)
-            if (ui.b * p.n_qb + qb != cur_key) {
+            if (ui.b * (2 * p.n_qb) + qb != cur_key) {
 #pragma unroll
                 for (int w = 0; w < NW; ++w) anc[w] = 0;
                 if (qg < R) {
@@ -933,7 +965,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                         a = pa;
                     }
                 }
-                cur_key = ui.b * p.n_qb + qb;
+                cur_key = ui.b * (2 * p.n_qb) + qb;
             }
 
             const int n = jb.j1 - jb.j0;
@@ -984,20 +1016,22 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             }
             g += n;
 
-            if (jb.pair) {
+            const bool part = RANGE && !(SPLIT && jb.j0 == 0 && jb.j1 == ui.n_tiles);
+            if (jb.pair && !(PAGED && part)) {
                 finish_pair(jb);
             } else {
                 int slot = 0;
-                if (SPLIT && !(jb.j0 == 0 && jb.j1 == ui.n_tiles)) {
+                if (SPLIT && part) {
                     // a part: slot 2c for the range's first segment, 2c + 1 for its last
-                    const int u = ui.lbh * p.n_qb + ui.qb;
+                    const int u = ui.lbh * p.n_qb + (PAGED && jb.pair ? ui.qb / 2 : ui.qb);
                     slot = 2 * (int)blockIdx.x + (u == wr.u_first ? 0 : 1);
                     // the part holding the unit's first tile records it for the merge
                     if (jb.j0 == 0 && threadIdx.x == 0)
                         p.split_rec[blockIdx.x] =
                             SplitRecord{wr.x_first + (wr.n_tiles - it.seg.left) - jb.j1, wr.n_shared, u, ui.n_tiles};
                 }
-                finish_single(jb, st0, n >= 2, slot);
+                if (SPLIT && PAGED && jb.pair) finish_pair_part(slot);
+                else finish_single(jb, st0, n >= 2, slot);
             }
             m = -INFINITY;
             l = 0.f;

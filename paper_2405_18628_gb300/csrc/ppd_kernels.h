@@ -119,6 +119,7 @@ struct PagedParams : AttnParams {
     int n_depth;                // L * n_pages * H
     int page_shift, box_shift;  // log2 of a page's rows, and of min(128, those)
     int rows;                   // query rows of a slice: its G heads' T tokens
+    int pair_units;             // work split, more than 128 rows: units are pairs of blocks of 128 rows
 };
 
 // Work split limits: batch size (the per-CTA range search holds the batch in

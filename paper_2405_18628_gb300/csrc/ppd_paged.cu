@@ -7,7 +7,8 @@
 
 namespace ppd {
 
-// The merge of the units cut by the work split, as split_merge_kernel, bf16 out.
+// The merge of the units cut by the work split, as split_merge_kernel, bf16 out; kRows rows a unit.
+template <int kRows>
 __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedParams p, int D)
 {
     pdl_release();
@@ -16,12 +17,12 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedParams p, i
     if (r.u < 0) return;
     const int per_row = D / 8;
     const int lbh = r.u / p.n_qb, qb = r.u - lbh * p.n_qb;
-    const int n_rows = min(kSplitRows, p.rows - qb * kSplitRows);
+    const int n_rows = min(kRows, p.rows - qb * kRows);
     const int row = (int)(blockIdx.y * (blockDim.x / per_row) + threadIdx.x / per_row);
     if (row >= n_rows) return;
     const SplitParts sp = split_parts(r.n_shared, r.off, r.n_tiles);
-    split_merge_chunk(p.split_part, reinterpret_cast<__nv_bfloat16 *>(p.out), p.lse, sp, r.n_shared, (int)gridDim.x,
-                      (size_t)lbh * p.rows + (size_t)qb * kSplitRows, row, ((int)threadIdx.x % per_row) * 8, D);
+    split_merge_chunk<__nv_bfloat16, kRows>(p.split_part, reinterpret_cast<__nv_bfloat16 *>(p.out), p.lse, sp, r.n_shared, (int)gridDim.x,
+                                            (size_t)lbh * p.rows + (size_t)qb * kRows, row, ((int)threadIdx.x % per_row) * 8, D);
 }
 
 template <int D, int TP>
@@ -44,9 +45,10 @@ cudaError_t launch_paged_attention(const AttnMaps &m, const PagedParams &p, int 
     else if (D == 128) e = p.T_pad == 64 ? launch_paged_t<128, 64>(m, p, num_sms, stream) : launch_paged_t<128, 32>(m, p, num_sms, stream);
     else e = p.T_pad == 64 ? launch_paged_t<64, 64>(m, p, num_sms, stream) : launch_paged_t<64, 32>(m, p, num_sms, stream);
     if (e != cudaSuccess || !p.split) return e;
-    const int rows = p.rows < kSplitRows ? p.rows : kSplitRows, per_block = 256 / (D / 8);
-    return launch_chained(paged_merge_kernel, dim3((unsigned)attention_grid(p, num_sms), (unsigned)((rows + per_block - 1) / per_block)),
-                          dim3(256), dim3(1), stream, p, D);
+    const int most = p.pair_units ? 2 * kSplitRows : kSplitRows, rows = p.rows < most ? p.rows : most, per_block = 256 / (D / 8);
+    const dim3 grid((unsigned)attention_grid(p, num_sms), (unsigned)((rows + per_block - 1) / per_block));
+    return p.pair_units ? launch_chained(paged_merge_kernel<2 * kSplitRows>, grid, dim3(256), dim3(1), stream, p, D)
+                        : launch_chained(paged_merge_kernel<kSplitRows>, grid, dim3(256), dim3(1), stream, p, D);
 }
 
 }  // namespace ppd
