@@ -334,6 +334,19 @@ PPD_DEV void tma_load_2d(void *dst, const CUtensorMap *map, uint64_t *bar, int x
         : "memory");
 }
 
+// Asynchronous copies into shared memory; bytes beyond `n` of the 16 (or 4) read as zero.
+PPD_DEV void cp_async16(uint32_t dst, const void *src, uint32_t n)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+PPD_DEV void cp_async4(uint32_t dst, const void *src, uint32_t n)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+PPD_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+PPD_DEV void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // One lane of a fully active warp (the same one every time): guards the
 // instructions one thread issues for the warp.  The code around it stays
 // warp-uniform, so descriptors and TMEM addresses live in uniform registers; an

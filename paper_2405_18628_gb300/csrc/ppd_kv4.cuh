@@ -98,19 +98,6 @@ PPD_DEV uint32_t movmatrix(uint32_t x)
     return d;
 }
 
-// Asynchronous copies into shared memory; bytes beyond `n` of the 16 (or 4) read as zero.
-PPD_DEV void cp_async16(uint32_t dst, const void *src, uint32_t n)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-PPD_DEV void cp_async4(uint32_t dst, const void *src, uint32_t n)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-PPD_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-PPD_DEV void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 PPD_DEV uint32_t ld_shared_u32(uint32_t a)
 {
     uint32_t v;

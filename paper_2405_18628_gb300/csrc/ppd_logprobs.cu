@@ -20,8 +20,8 @@
 // is the number of better ones).  As many batches as there were before bring about K that beat the
 // K-th best of those, so few are ever pushed.  Where there is no such bound (the first batch), or more
 // than fit were pushed (rows that rise: their batches are gone through again), a batch's K-th
-// best is bounded from below by the K-th best of the maxima of pairs of threads: K pairs hold
-// all that are better.
+// best is bounded from below by the K-th best of the threads' maxima: K threads hold all that are
+// better.
 #include "ppd_device.cuh"
 #include "ppd_kernels.h"
 
@@ -30,10 +30,8 @@
 
 namespace ppd {
 
-constexpr int kLogThreads = 128, kLogWarps = kLogThreads / 32;
 constexpr int kLogLoads = 4;                   // 16-byte loads of a batch and thread
-constexpr int kGroups = kLogThreads / 2;       // of two threads each
-static_assert(kLogMaxK <= kGroups, "the K-th best group exists");
+constexpr int kLogStages = 2;                  // batches on their way or in hand
 
 PPD_DEV uint32_t order_key(float x)
 {
@@ -101,16 +99,20 @@ PPD_DEV float below(float x)
     return __uint_as_float((u & 0x80000000u) ? u + one : u - one);
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kernel(const LogprobParams p)
+template <bool BF16, int THREADS>
+__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobParams p)
 {
     constexpr int E = BF16 ? 8 : 4;            // entries of a load
     constexpr int NV = E * kLogLoads;          // of a batch and thread
-    constexpr int kMaxPush = 2 * kLogMaxK * NV;
+    constexpr int WARPS = THREADS / 32;
+    constexpr int kMaxPush = kLogMaxK * NV;
     constexpr int eb = BF16 ? 2 : 4;
     constexpr uint32_t kAbsent = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
-    __shared__ unsigned long long s_push[kMaxPush], s_list[2][kLogMaxK], s_group[kGroups], s_bound;
-    __shared__ RowStats s_stats[kLogWarps], s_cta;
+    static_assert(kLogMaxK <= THREADS && kLogMaxK * kMaxCluster <= kMaxPush, "lists");
+    __shared__ uint4 s_batch[kLogStages][kLogLoads][THREADS];   // a thread reads what it asked for itself
+    __shared__ unsigned long long s_push[kMaxPush], s_list[2][kLogMaxK], s_bound;
+    __shared__ __align__(16) unsigned long long s_best[THREADS];
+    __shared__ RowStats s_stats[WARPS], s_cta;
     __shared__ int s_n, s_over;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, V = p.V;
@@ -120,26 +122,25 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
     pdl_wait();
     pdl_release();
 
-    // ---- what is asked (the same for the whole cluster); a sequence's status by its first item's CTA
+    // ---- what is asked (the same for the whole cluster)
     auto row_of = [&](int it, int at) { return p.rows ? ld_input(p.rows + it) : at; };
     auto outside = [&](int r, int t) { return r < -1 || r >= p.T || t < -1 || t >= V; };
-    if (i == 0 && rank == 0) {
+    auto sequence_status = [&]() {   // by the last CTA of a sequence's first item
         bool any = false;
-        for (int x = tid; x < p.n; x += kLogThreads) any |= outside(row_of(item + x, x), ld_input(p.tokens + item + x));
+        for (int x = tid; x < p.n; x += THREADS) any |= outside(row_of(item + x, x), ld_input(p.tokens + item + x));
         any = __syncthreads_or(any);
         if (tid == 0) p.dev_status[b] = any ? kErrTree : kOk;
-    }
+    };
     const int row = row_of(item, i), token = ld_input(p.tokens + item);
-    const bool wrong = outside(row, token);
-    const bool none = wrong || row < 0;
-    if (none) {
+    if (row < 0 || outside(row, token)) {
+        if (i == 0 && rank == p.cluster - 1) sequence_status();
         if (rank == 0) {
             if (tid == 0) {
                 p.logprob[item] = 0.f;
                 p.entropy[item] = 0.f;
                 p.rank[item] = -1;
             }
-            for (int x = tid; x < K; x += kLogThreads) {
+            for (int x = tid; x < K; x += THREADS) {
                 p.top_tokens[(size_t)item * K + x] = -1;
                 p.top_logprobs[(size_t)item * K + x] = 0.f;
             }
@@ -151,12 +152,6 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         if (BF16) return __uint_as_float((uint32_t)*reinterpret_cast<const volatile uint16_t *>(x0 + (size_t)c * 2) << 16);
         return ld_input(reinterpret_cast<const float *>(x0) + c);
     };
-    const float xt = token >= 0 ? entry_at(token) : 0.f;
-    const unsigned long long et = order_entry(order_key(xt), token);
-    // entries that are not <= this rank before the token: in columns before it, and after it
-    const float th0 = token < 0 ? INFINITY : below<BF16>(xt), th1 = token < 0 ? INFINITY : xt;
-    const bool odd_token = xt != xt;   // (a NaN is compared as an entry)
-
     // ---- groups of E entries on 16 bytes: group g holds columns [g E - skew, ...), groups
     // [f0, f1) of the CTA's [g0, g1) lie inside the row
     const int skew = (int)(reinterpret_cast<uintptr_t>(x0) & 15) / eb;
@@ -164,6 +159,50 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
     const int g0 = (int)((long long)groups * rank / p.cluster), g1 = (int)((long long)groups * (rank + 1) / p.cluster);
     const int f0 = max(g0, skew ? 1 : 0), f1 = min(g1, (int)(((long long)V + skew) / E));
     const char *xg = x0 - skew * eb;
+    constexpr int kStep = kLogLoads * THREADS;
+    const int batches = (g1 - g0 + kStep - 1) / kStep;
+    // Batch n on its way to its stage (kLogStages - 1 batches ahead of the one in hand: 2 KB a warp each).
+    auto ask = [&](int n) {
+        uint4 *stage = &s_batch[n % kLogStages][0][tid];
+        const int base = g0 + n * kStep;
+        if (base >= f0 && base + kStep <= f1) {
+            const char *src = xg + ((size_t)base + tid) * 16;
+#pragma unroll
+            for (int q = 0; q < kLogLoads; ++q) cp_async16(smem_addr(stage + q * THREADS), src + (size_t)q * THREADS * 16, 16);
+        } else if (base < g1) {
+#pragma unroll 1
+            for (int q = 0; q < kLogLoads; ++q) {
+                const int g = base + q * THREADS + tid;
+                if (g >= f0 && g < f1) {
+                    cp_async16(smem_addr(stage + q * THREADS), xg + (size_t)g * 16, 16);
+                    continue;
+                }
+                // a row's end: the entries that it has
+                uint32_t v[4] = {kAbsent, kAbsent, kAbsent, kAbsent};
+                const long long c = (long long)g * E - skew;
+                if (g < g1) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        if (c + e < 0 || c + e >= V) continue;
+                        const uint32_t y = __float_as_uint(entry_at((int)(c + e)));
+                        if (!BF16) v[e & 3] = y;
+                        else if (e & 1) v[e / 2] = (v[e / 2] & 0xFFFFu) | y;
+                        else v[e / 2] = (v[e / 2] & 0xFFFF0000u) | y >> 16;
+                    }
+                }
+                stage[q * THREADS] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+        }
+        cp_async_commit();
+    };
+#pragma unroll 1
+    for (int n = 0; n < kLogStages - 1; ++n) ask(n);
+
+    const float xt = token >= 0 ? entry_at(token) : 0.f;
+    const unsigned long long et = order_entry(order_key(xt), token);
+    // entries that are not <= this rank before the token: in columns before it, and after it
+    const float th0 = token < 0 ? INFINITY : below<BF16>(xt), th1 = token < 0 ? INFINITY : xt;
+    const bool odd_token = xt != xt;   // (a NaN is compared as an entry)
 
     RowStats st{-INFINITY, 0.f, 0.f, 0, 0};
     float x_low = 0.f;             // no entry below it adds to s: 2^-200 of m
@@ -176,9 +215,10 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
     // The list and the pushed entries together, by the whole block (after a barrier).
     auto rank_pushed = [&]() {
         const int n = s_n;
-        for (int y = tid; y < n + K; y += kLogThreads) {
+        for (int y = tid; y < n + K; y += THREADS) {
             const unsigned long long mine = y < n ? s_push[y] : s_list[cur][y - n];
             int place = 0;
+#pragma unroll 8
             for (int z = 0; z < n; ++z) place += s_push[z] > mine;
             for (int z = 0; z < K; ++z) place += s_list[cur][z] > mine;
             if (mine != 0 && place < K) s_list[cur ^ 1][place] = mine;
@@ -193,67 +233,26 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         __syncthreads();
     };
 
-    // Rare work (a row's ends, the token's own group, numbers near the type's ends, pushes) is
-    // done in rolled loops that pick a load's words by selects: the code of a batch is a
-    // few hundred instructions, which the instruction cache holds.
-    constexpr int kStep = kLogLoads * kLogThreads;
-    uint4 next[kLogLoads];
-    bool fill = true;              // nothing but loads of the batch after
+    // Rare work (the token's own group, numbers near the type's ends, pushes) is done in rolled
+    // loops over what lies in shared memory: the code of a batch is a few hundred instructions,
+    // which the instruction cache holds.
     bool bounded = true;           // batch by batch, with a bound of its own
     bool again = false;            // ... of batches whose sums are taken
-    int from = g0, to = g0 + kStep;   // the batches that are ranked together
-    for (int base = g0 - kStep; base < g1; base += kStep) {
+    int from = 0, to = 1;          // the batches that are ranked together
+#pragma unroll 1
+    for (int n = 0; n < batches; ++n) {
+        ask(n + kLogStages - 1);
+        cp_async_wait<kLogStages - 1>();
+        const uint4 *stage = &s_batch[n % kLogStages][0][tid];
+        const int base = g0 + n * kStep;
         uint4 w[kLogLoads];
 #pragma unroll
-        for (int q = 0; q < kLogLoads; ++q) w[q] = next[q];
-        auto group = [&](int q) { return base + q * kLogThreads + tid; };
-        // the next batch's loads
-        if (base + kStep >= f0 && base + 2 * kStep <= f1) {
-            const uint4 *src = reinterpret_cast<const uint4 *>(xg) + group(0) + kStep;
-#pragma unroll
-            for (int q = 0; q < kLogLoads; ++q) next[q] = ld_input(src + q * kLogThreads);
-        } else if (base + kStep < g1) {
-#pragma unroll
-            for (int q = 0; q < kLogLoads; ++q) {
-                const int g = group(q) + kStep;
-                next[q] = make_uint4(kAbsent, kAbsent, kAbsent, kAbsent);
-                if (g >= f0 && g < f1) next[q] = ld_input(reinterpret_cast<const uint4 *>(xg + (size_t)g * 16));
-            }
-#pragma unroll 1
-            for (int q = 0; q < kLogLoads; ++q) {
-                const int g = group(q) + kStep;
-                if (g >= g1 || (g >= f0 && g < f1)) continue;
-                // a row's end: the entries that it has
-                uint32_t v[4] = {kAbsent, kAbsent, kAbsent, kAbsent};
-                const long long c = (long long)g * E - skew;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (c + e < 0 || c + e >= V) continue;
-                    const uint32_t y = __float_as_uint(entry_at((int)(c + e)));
-                    if (!BF16) v[e & 3] = y;
-                    else if (e & 1) v[e / 2] = (v[e / 2] & 0xFFFFu) | y;
-                    else v[e / 2] = (v[e / 2] & 0xFFFF0000u) | y >> 16;
-                }
-#pragma unroll
-                for (int x = 0; x < kLogLoads; ++x)
-                    if (x == q) next[x] = make_uint4(v[0], v[1], v[2], v[3]);
-            }
-        }
-        if (fill) {
-            fill = false;
-            continue;
-        }
+        for (int q = 0; q < kLogLoads; ++q) w[q] = stage[q * THREADS];
+        auto group = [&](int q) { return base + q * THREADS + tid; };
         auto word = [&](const uint4 &r, int x) { return x == 0 ? r.x : x == 1 ? r.y : x == 2 ? r.z : r.w; };
         auto value = [&](const uint4 &r, int e) {   // entry e of a load's E
             if (!BF16) return __uint_as_float(word(r, e));
             return __uint_as_float((e & 1) ? (word(r, e / 2) & 0xFFFF0000u) : (word(r, e / 2) << 16));
-        };
-        auto pick = [&](int q) {
-            uint4 r = w[0];
-#pragma unroll
-            for (int x = 1; x < kLogLoads; ++x)
-                if (x == q) r = w[x];
-            return r;
         };
         auto column = [&](int q, int e) { return (long long)group(q) * E - skew + e; };
         auto live = [&](int q, int e) { return group(q) < g1 && column(q, e) >= 0 && column(q, e) < V; };
@@ -322,7 +321,7 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         } else {   // numbers whose differences may overflow
 #pragma unroll 1
             for (int q = 0; q < kLogLoads; ++q) {
-                const uint4 r = pick(q);
+                const uint4 r = stage[q * THREADS];
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float d = fmaxf(exponent(value(r, e), st.m, p.k), -200.f);   // (2^-200 is 0; nothing times an infinity)
@@ -351,7 +350,7 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         } else {   // the batch of the token, or a row's end: the loads that hold them entry by entry
 #pragma unroll 1
             for (int q = 0; q < kLogLoads; ++q) {
-                const uint4 r = pick(q);
+                const uint4 r = stage[q * THREADS];
                 const int g = group(q);
                 const long long c = column(q, 0);
                 if (g >= g1) continue;
@@ -370,83 +369,94 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         if (K == 0) continue;
 
         // ---- the K best
-        const bool sees = full ? !(mb <= least) && least == least : group(0) < g1;
-        unsigned long long bound = full ? (unsigned long long)(order_key(least) + 1) << 32 : 1;   // (equal ones come later)
-        if (bounded) {
-            // this thread's best entry: the first of the batch's largest
-            int at = 0;
-#pragma unroll
-            for (int q = kLogLoads - 1; q >= 0; --q)
-#pragma unroll
-                for (int e = E - 1; e >= 0; --e) {
-                    const float v = value(w[q], e);
-                    if (!(v < mb) && (v == mb || v != v) && (mb > -INFINITY || mb != mb)) at = q * E + e;
-                }
-            unsigned long long gm = 0;
-            if (sees) {
-                int q = at / E, e = at % E;
-                if (mb == -INFINITY)   // only -inf: the first entry that there is
-                    while (q < kLogLoads && !live(q, e)) e = e + 1 < E ? e + 1 : 0, q += e == 0;
-                if (q < kLogLoads) gm = order_entry(order_key(mb), (int)column(q, e));
-            }
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, gm, 1);
-            gm = other > gm ? other : gm;
-            if ((lane & 1) == 0) s_group[tid >> 1] = gm;
-            if (tid == 0) s_bound = 0;
-            __syncthreads();
-            if (tid < kGroups) {
-                const unsigned long long g = s_group[tid];
-                int place = 0;
-#pragma unroll 4
-                for (int y = 0; y < kGroups; ++y) place += s_group[y] > g;
-                if (g != 0 && place == K - 1) s_bound = g;   // (fewer pairs than K: no bound)
-            }
-            __syncthreads();
-            bound = s_bound > bound ? s_bound : bound;
-        }
-        if (sees && order_entry(order_key(mb), 0) >= bound) {
-            // the entries that may be among the best, one bit each (few threads have more than
-            // one or two), read again from the row
-            const float t0 = key_value((uint32_t)(bound >> 32)), t = bound > 1 ? below<false>(t0) : NAN;   // those that are not <= t
+        // one bit for each of a thread's entries: of bf16, bit x the low half of word x, bit 16 + x the high one
+        auto bits = [&](auto test2, auto test) {
             uint32_t some = 0;
-            if (BF16) {
-                const __nv_bfloat162 t2 = __bfloat162bfloat162(__float2bfloat16_rd(t));
 #pragma unroll
-                for (int x = 0; x < 4 * kLogLoads; ++x) some |= __hgtu2_mask(as_bf162(word(w[x / 4], x % 4)), t2) & 0x10001u << x;
-            } else {
+            for (int q = 0; q < kLogLoads; ++q)
 #pragma unroll
-                for (int q = 0; q < kLogLoads; ++q)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) some |= (value(w[q], e) <= t ? 0u : 1u) << (q * E + e);
+                for (int x = 0; x < 4; ++x) {
+                    if (BF16) some |= test2(as_bf162(word(w[q], x))) & 0x10001u << (4 * q + x);
+                    else some |= (test(value(w[q], x)) ? 1u : 0u) << (4 * q + x);
+                }
+            return some;
+        };
+        auto in_order = [](int bit) { return BF16 ? 2 * (bit & 15) + (bit >> 4) : bit; };
+        auto stored = [&](int at) {   // entry `at` in order
+            const uint32_t y = reinterpret_cast<const uint32_t *>(stage + at / E * THREADS)[BF16 ? at % E / 2 : at % E];
+            return __uint_as_float(!BF16 ? y : (at & 1) ? (y & 0xFFFF0000u) : y << 16);
+        };
+        const bool sees = full ? !(mb <= least) && least == least : group(0) < g1;
+        const bool plain = full && !bounded;
+        // entries that are not <= t are pushed: all that beat the list (equal ones come later), or
+        // those of at least `bound`
+        float t = least;
+        unsigned long long bound = 0;
+        if (!plain) {
+            bound = full ? (unsigned long long)(order_key(least) + 1) << 32 : 1;
+            if (bounded) {
+                // this thread's best entry: the first of the batch's largest
+                unsigned long long gm = 0;
+                if (sees) {
+                    int at = 0;
+                    if (mb > -INFINITY) {
+                        const __nv_bfloat162 mb2 = __bfloat162bfloat162(__float2bfloat16_rn(mb));
+                        const uint32_t same = bits([&](__nv_bfloat162 v) { return __heq2_mask(v, mb2); }, [&](float v) { return v == mb; });
+                        at = in_order(__ffs(same) - 1);
+                        if (BF16 && (same & 0xFFFFu) && same >> 16) at = min(in_order(__ffs(same & 0xFFFFu) - 1), in_order(__ffs(same >> 16) + 15));
+                    } else if (mb != mb) {
+                        while (stored(at) == stored(at)) ++at;
+                    } else {   // only -inf: the first entry that there is
+                        while (at < NV && !live(at / E, at % E)) ++at;
+                    }
+                    if (at < NV) gm = order_entry(order_key(mb), (int)column(at / E, at % E));
+                }
+                s_best[tid] = gm;
+                if (tid == 0) s_bound = 0;
+                __syncthreads();
+                int place = 0;
+#pragma unroll 8
+                for (int y = 0; y < THREADS; y += 2) {
+                    const ulonglong2 z = *reinterpret_cast<const ulonglong2 *>(s_best + y);
+                    place += (z.x > gm) + (z.y > gm);
+                }
+                if (gm != 0 && place == K - 1) s_bound = gm;   // (fewer than K threads: no bound)
+                __syncthreads();
+                bound = s_bound > bound ? s_bound : bound;
             }
-            while (some) {
-                const int bit = __ffs(some) - 1;
+            t = bound > 1 ? below<false>(key_value((uint32_t)(bound >> 32))) : NAN;
+        }
+        if (sees && !(mb <= t)) {
+            const __nv_bfloat162 t2 = __bfloat162bfloat162(__float2bfloat16_rd(t));
+            uint32_t some = bits([&](__nv_bfloat162 v) { return __hgtu2_mask(v, t2); }, [&](float v) { return !(v <= t); });
+            while (some) {   // (few threads have more than one or two)
+                const int at = in_order(__ffs(some) - 1);
                 some &= some - 1;
-                const int at = BF16 ? 2 * (bit & 15) + (bit >> 4) : bit;
-                const int q = at / E, e = at % E;
-                if (!live(q, e)) continue;
-                const unsigned long long en = order_entry(order_key(entry_at((int)column(q, e))), (int)column(q, e));
-                if (en < bound) continue;
+                const unsigned long long en = order_entry(order_key(stored(at)), (int)column(at / E, at % E));
+                if (!plain && (en < bound || !live(at / E, at % E))) continue;
                 const int place = atomicAdd(&s_n, 1);
                 if (place < kMaxPush) s_push[place] = en;
                 else s_over = 1;   // (not where the batch has a bound)
             }
         }
-        if (bounded || base + kStep >= to || base + kStep >= g1) {
+        if (bounded || n + 1 >= to || n + 1 == batches) {
             __syncthreads();
             if (s_over) {
                 // more than fit: the same batches again, one by one
                 __syncthreads();
                 if (tid == 0) s_n = s_over = 0;   // (barriers before the next push)
-                to = min(to, base + kStep);
-                base = from - 2 * kStep;
-                fill = bounded = again = true;
+                to = min(to, n + 1);
+                bounded = again = true;
+                cp_async_wait<0>();
+#pragma unroll 1
+                for (int x = 0; x < kLogStages - 1; ++x) ask(from + x);
+                n = from - 1;
                 continue;
             }
             rank_pushed();
-            if (base + kStep >= to) {
-                from = base + kStep;
-                to = from + max(from - g0, kStep);
+            if (n + 1 >= to) {
+                from = n + 1;
+                to = 2 * from;
                 bounded = again = false;
             }
         }
@@ -471,12 +481,13 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
     if (cur == 1 && tid < K) s_list[0][tid] = s_list[1][tid];
     __syncthreads();
     if (warp == 0) {
-        st = lane < kLogWarps ? s_stats[lane] : empty;
-        merge_lanes(kLogWarps / 2);
+        st = lane < WARPS ? s_stats[lane] : empty;
+        merge_lanes(WARPS / 2);
         if (lane == 0) s_cta = st;
     }
     if (p.cluster > 1) cluster_sync();
     else __syncthreads();
+    if (i == 0 && rank == p.cluster - 1) sequence_status();
     if (rank == 0) {
         // every warp the whole row's statistics
         st = empty;
@@ -504,12 +515,13 @@ __global__ void __launch_bounds__(kLogThreads, BF16 ? 6 : 7) token_logprobs_kern
         }
         // the CTAs' lists together: an entry's place is the number of better ones
         const int n = p.cluster * K;
-        for (int y = tid; y < n; y += kLogThreads)
+        for (int y = tid; y < n; y += THREADS)
             s_push[y] = y < K ? s_list[0][y] : ld_cluster_u64(cluster_map(smem_addr(&s_list[0][0]) + (uint32_t)(y % K) * 8, y / K));
         __syncthreads();
-        for (int y = tid; y < n; y += kLogThreads) {
+        for (int y = tid; y < n; y += THREADS) {
             const unsigned long long mine = s_push[y];
             int place = 0;
+#pragma unroll 8
             for (int z = 0; z < n; ++z) place += s_push[z] > mine;
             if (mine != 0 && place < K) {
                 p.top_tokens[(size_t)item * K + place] = (int)~(uint32_t)mine;
@@ -524,12 +536,13 @@ cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t str
 {
     // CTAs of a row: as many as find room at once, none for less than a batch
     const long long items = (long long)p.B * p.n;
-    const int batch = kLogThreads * kLogLoads * (p.bf16 ? 8 : 4);
+    constexpr int kThreads = 128;
+    const int batch = kThreads * kLogLoads * (p.bf16 ? 8 : 4);
     p.cluster = 1;
-    while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 4ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
+    while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 6ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
     const dim3 grid((unsigned)(items * p.cluster)), cl((unsigned)p.cluster);
-    return p.bf16 ? launch_chained(token_logprobs_kernel<true>, grid, dim3(kLogThreads), cl, stream, p)
-                  : launch_chained(token_logprobs_kernel<false>, grid, dim3(kLogThreads), cl, stream, p);
+    return p.bf16 ? launch_chained(token_logprobs_kernel<true, kThreads>, grid, dim3(kThreads), cl, stream, p)
+                  : launch_chained(token_logprobs_kernel<false, kThreads>, grid, dim3(kThreads), cl, stream, p);
 }
 
 }  // namespace ppd
