@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
 
     RowStats st{-INFINITY, 0.f, 0.f, 0, 0};
     float x_low = 0.f;             // no entry below it adds to s: 2^-200 of m
-    int cur = 0;                   // the list in use
+    int cur = 0, listed = 0;       // the list in use, its entries
     float least = 0.f;             // the list's last entry, once it has K
     bool full = false;
     if (tid < kLogMaxK) s_list[0][tid] = s_list[1][tid] = 0;
@@ -215,14 +215,16 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
     // The list and the pushed entries together, by the whole block (after a barrier).
     auto rank_pushed = [&]() {
         const int n = s_n;
-        for (int y = tid; y < n + K; y += THREADS) {
+        for (int y = tid; y < n + listed; y += THREADS) {
             const unsigned long long mine = y < n ? s_push[y] : s_list[cur][y - n];
             int place = 0;
 #pragma unroll 8
             for (int z = 0; z < n; ++z) place += s_push[z] > mine;
-            for (int z = 0; z < K; ++z) place += s_list[cur][z] > mine;
-            if (mine != 0 && place < K) s_list[cur ^ 1][place] = mine;
+#pragma unroll 4
+            for (int z = 0; z < listed; ++z) place += s_list[cur][z] > mine;
+            if (place < K) s_list[cur ^ 1][place] = mine;
         }
+        listed = min(K, listed + n);
         __syncthreads();
         if (tid < kLogMaxK) s_list[cur][tid] = 0;   // (for the ranking after the next)
         cur ^= 1;
