@@ -1315,12 +1315,12 @@ struct PagedWs {
 // Slices of more than 64 rows, by the time that each way takes, in microseconds a job of t_u tiles and at
 // its ends (the tables' capacity standing in for the lengths), as measured with D = 128, pages of
 // 32: a tile of 128 queries 1.09, or 1.47 where every SM streams keys of its own, of a pair of blocks
-// 2.05; whole jobs' ends 6, a cluster's 12, and the work split's 29 (two jobs a CTA, 130 KB of
+// 2.05; whole jobs' ends 6, a cluster's 12, and the work split's 24 (two jobs a CTA, 130 KB of
 // partial state each, and the merge).  Whole / clusters / shared out, heads of 64 tokens:
-//   16 slices, 4 heads, 3001 rows    32.6 /  19.6 /  32.6     96 of 4, ragged to 5001   82.4 /      /  72.6
+//   16 slices, 4 heads, 3001 rows    32.6 /  19.6 /  32.6     96 of 4, ragged to 5001   82.4 /      /  67.7
 //   8 of 4, 20,001                    169 /  41.2 /  42.0     64 of 8                   84.2 /      /  90.5
-//   40 of 2, 4001                    40.2 /  22.6 /  29.7     80 of 8                    119 /      / 105.6
-// (units of the work split: pairs of blocks; single ones 77.4, 100.8 and 125.7 in the last column's cases).
+//   40 of 2, 4001                    40.2 /  22.6 /  29.7     80 of 8                    119 /      /  98.7
+// (units of the work split: pairs of blocks; single ones took 5, 10 and 20 us longer in the last column's cases).
 static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, bool workspace)
 {
     const long long sms = split_grid(), blocks = (w.rows + 127) / 128, pairs = (blocks + 1) / 2;
@@ -1338,7 +1338,7 @@ static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, 
             w.plan.cluster = c;
         }
     }
-    const double shared = rounds(slices * pairs * t_u) * (blocks > 1 ? 2.05 : 1.47) + 29;
+    const double shared = rounds(slices * pairs * t_u) * (blocks > 1 ? 2.05 : 1.47) + 24;
     // (a twentieth less: lengths are seldom alike, and whole jobs take the longest first)
     if (workspace && B <= ppd::kSplitMaxB && slices * pairs * t_u <= 2147483647ll && shared < 0.95 * best) {
         w.plan = {1, 1};

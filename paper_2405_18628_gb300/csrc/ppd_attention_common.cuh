@@ -334,14 +334,13 @@ PPD_DEV size_t split_slot_floats(int D, int rows = kSplitRows) { return (size_t)
 // pass over the parts with a running maximum M: part c enters with weight
 // 2^(m_c - M), earlier sums are rescaled when M grows; the output is the
 // weighted sum of the parts' O rows over the weighted sum of their row sums.
-// The parts are read eight at a time, every load of a batch issued before any
+// The parts are read PB at a time, every load of a batch issued before any
 // is used, so a batch costs one round trip to L2.
-template <class Out, int kRows = kSplitRows>
+template <class Out, int kRows = kSplitRows, int PB = 8>
 static __device__ __forceinline__ void split_merge_chunk(const float *split_part, Out *out, float *lse,
                                                          const SplitParts &sp, long long N, int G,
                                                          size_t out_row0, int r, int c0, int D)
 {
-    constexpr int PB = 8;   // parts per batch
     const size_t sf = split_slot_floats(D, kRows);
     const bool dense = N >= G;   // no empty ranges
     float M = -INFINITY, Ls = 0.f;

@@ -30,8 +30,8 @@
 
 namespace ppd {
 
+constexpr int kLogThreads = 128;
 constexpr int kLogLoads = 4;                   // 16-byte loads of a batch and thread
-constexpr int kLogStages = 2;                  // batches on their way or in hand
 
 PPD_DEV uint32_t order_key(float x)
 {
@@ -99,17 +99,18 @@ PPD_DEV float below(float x)
     return __uint_as_float((u & 0x80000000u) ? u + one : u - one);
 }
 
-template <bool BF16, int THREADS>
-__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobParams p)
+// STAGES: batches on their way or in hand.
+template <bool BF16, int STAGES>
+__global__ void __launch_bounds__(kLogThreads) token_logprobs_kernel(const LogprobParams p)
 {
     constexpr int E = BF16 ? 8 : 4;            // entries of a load
     constexpr int NV = E * kLogLoads;          // of a batch and thread
-    constexpr int WARPS = THREADS / 32;
+    constexpr int THREADS = kLogThreads, WARPS = THREADS / 32;
     constexpr int kMaxPush = kLogMaxK * NV;
     constexpr int eb = BF16 ? 2 : 4;
     constexpr uint32_t kAbsent = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
     static_assert(kLogMaxK <= THREADS && kLogMaxK * kMaxCluster <= kMaxPush, "lists");
-    __shared__ uint4 s_batch[kLogStages][kLogLoads][THREADS];   // a thread reads what it asked for itself
+    __shared__ uint4 s_batch[STAGES][kLogLoads][THREADS];   // a thread reads what it asked for itself
     __shared__ unsigned long long s_push[kMaxPush], s_list[2][kLogMaxK], s_bound;
     __shared__ __align__(16) unsigned long long s_best[THREADS];
     __shared__ RowStats s_stats[WARPS], s_cta;
@@ -161,9 +162,9 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
     const char *xg = x0 - skew * eb;
     constexpr int kStep = kLogLoads * THREADS;
     const int batches = (g1 - g0 + kStep - 1) / kStep;
-    // Batch n on its way to its stage (kLogStages - 1 batches ahead of the one in hand: 2 KB a warp each).
+    // Batch n on its way to its stage (STAGES - 1 batches ahead of the one in hand: 2 KB a warp each).
     auto ask = [&](int n) {
-        uint4 *stage = &s_batch[n % kLogStages][0][tid];
+        uint4 *stage = &s_batch[n % STAGES][0][tid];
         const int base = g0 + n * kStep;
         if (base >= f0 && base + kStep <= f1) {
             const char *src = xg + ((size_t)base + tid) * 16;
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
         cp_async_commit();
     };
 #pragma unroll 1
-    for (int n = 0; n < kLogStages - 1; ++n) ask(n);
+    for (int n = 0; n < STAGES - 1; ++n) ask(n);
 
     const float xt = token >= 0 ? entry_at(token) : 0.f;
     const unsigned long long et = order_entry(order_key(xt), token);
@@ -243,9 +244,9 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
     int from = 0, to = 1;          // the batches that are ranked together
 #pragma unroll 1
     for (int n = 0; n < batches; ++n) {
-        ask(n + kLogStages - 1);
-        cp_async_wait<kLogStages - 1>();
-        const uint4 *stage = &s_batch[n % kLogStages][0][tid];
+        ask(n + STAGES - 1);
+        cp_async_wait<STAGES - 1>();
+        const uint4 *stage = &s_batch[n % STAGES][0][tid];
         const int base = g0 + n * kStep;
         uint4 w[kLogLoads];
 #pragma unroll
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
                 bounded = again = true;
                 cp_async_wait<0>();
 #pragma unroll 1
-                for (int x = 0; x < kLogStages - 1; ++x) ask(from + x);
+                for (int x = 0; x < STAGES - 1; ++x) ask(from + x);
                 n = from - 1;
                 continue;
             }
@@ -536,15 +537,21 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
 
 cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t stream)
 {
-    // CTAs of a row: as many as find room at once, none for less than a batch
+    // CTAs of a row: as many as are all resident at once with four stages (five an SM), none for
+    // less than a batch.  1 / 2 / 4 / 8 of them, us, 20 alternatives:
+    //   150 rows of 128,256 fp32   47 / 34 / 33 / 43        320 of 256,000 bf16    67 / 58 / 64 / 80
+    //   16 rows of 128,256 fp32    47 / 31 / 22 / 19        2000 of 32,000 bf16    59 / 78 / 115 / 210
+    // Four stages, 35 to 43 KB, where no more than those run (700 rows of 256,000 bf16: 93 us, with two
+    // stages 122); else two, so that eight CTAs find room (2048 rows of 128,256 bf16: 133 us, with
+    // four 162).
     const long long items = (long long)p.B * p.n;
-    constexpr int kThreads = 128;
-    const int batch = kThreads * kLogLoads * (p.bf16 ? 8 : 4);
+    const int batch = kLogThreads * kLogLoads * (p.bf16 ? 8 : 4);
     p.cluster = 1;
-    while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 6ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
-    const dim3 grid((unsigned)(items * p.cluster)), cl((unsigned)p.cluster);
-    return p.bf16 ? launch_chained(token_logprobs_kernel<true, kThreads>, grid, dim3(kThreads), cl, stream, p)
-                  : launch_chained(token_logprobs_kernel<false, kThreads>, grid, dim3(kThreads), cl, stream, p);
+    while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 5ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
+    const bool deep = items * p.cluster <= 5ll * num_sms;
+    auto *kern = p.bf16 ? (deep ? token_logprobs_kernel<true, 4> : token_logprobs_kernel<true, 2>)
+                        : (deep ? token_logprobs_kernel<false, 4> : token_logprobs_kernel<false, 2>);
+    return launch_chained(kern, dim3((unsigned)(items * p.cluster)), dim3(kLogThreads), dim3((unsigned)p.cluster), stream, p);
 }
 
 }  // namespace ppd

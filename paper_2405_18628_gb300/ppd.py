@@ -433,32 +433,19 @@ def page_pool(L, n_pages, H, page, D, device="cuda"):
     return torch.zeros((L, n_pages, H, page, D), dtype=torch.bfloat16, device=device)
 
 
-def _pointers(tensors, dtypes, shapes, names):
-    """_take for several tensors at once, none of them None: lists compared as wholes take half the time
-    of a loop over the tensors (12 of them: 6.5 us there, more than a small call's kernel)."""
-    if ([t.dtype for t in tensors] == dtypes and [t.shape for t in tensors] == shapes and all([t.is_cuda for t in tensors])
-            and all([t.is_contiguous() for t in tensors])):
-        return [t.data_ptr() for t in tensors]
-    _take(*zip(names, tensors, dtypes, shapes))
-    raise ValueError("libppd takes contiguous CUDA tensors")
-
-
-_ASSIGN = ("old_len", "new_len", "table", "free_pages", "n_free", "new_n_free", "out_len", "slots", "slot_start", "dev_status")
-
-
 def ppd_page_assign(old_len, new_len, page: int, table, free_pages, n_free, new_n_free, out_len, slots, slot_start,
                     dev_status, stream=None):
     """Pages of `page` rows for sequences that grow from old_len to new_len [B], back from those that shrink: table
     [B,max_pages] and the stack free_pages [n_pages] (n_free [1] entries, then new_n_free) in place; the new rows'
     slots [max_slots], b's from slot_start [B+1] on; out_len [B] the lengths that sequences have then."""
-    (B, max_pages), n_pages, max_slots, one = table.shape, free_pages.numel(), slots.numel(), (table.shape[0],)
-    a = _pointers([old_len, new_len, table, free_pages, n_free, new_n_free, out_len, slots, slot_start, dev_status], [torch.int32] * 10,
-                  [one, one, (B, max_pages), (n_pages,), (1,), (1,), one, (max_slots,), (B + 1,), one], _ASSIGN)
+    (B, max_pages), n_pages, max_slots = table.shape, free_pages.numel(), slots.numel()
+    i32, one = torch.int32, (B,)
+    a = _take(("old_len", old_len, i32, one), ("new_len", new_len, i32, one), ("table", table, i32, (B, max_pages)),
+              ("free_pages", free_pages, i32, (n_pages,)), ("n_free", n_free, i32, (1,)), ("new_n_free", new_n_free, i32, (1,)),
+              ("out_len", out_len, i32, one), ("slots", slots, i32, (max_slots,)), ("slot_start", slot_start, i32, (B + 1,)),
+              ("dev_status", dev_status, i32, one))
     st = load().ppd_page_assign(a[0], a[1], B, int(page), n_pages, max_pages, max_slots, *a[2:], _stream(stream))
     _check(st, "ppd_page_assign")
-
-
-_APPEND = ("k_new", "v_new", "k_pages", "v_pages", "slots", "slot_start", "dev_status", "rows")
 
 
 def ppd_page_append(k_new, v_new, k_pages, v_pages, slots, slot_start, dev_status, rows=None, stream=None):
@@ -466,22 +453,16 @@ def ppd_page_append(k_new, v_new, k_pages, v_pages, slots, slot_start, dev_statu
     [L,n_pages,H,page,D]; sequence b's slots are slots[slot_start[b] .. slot_start[b+1] - 1]."""
     L, B, H, T, D = new = k_new.shape
     n_pages, page, max_slots = k_pages.shape[1], k_pages.shape[3], slots.numel()
-    i32, dt, bf, pool = torch.int32, k_new.dtype, torch.bfloat16, (L, n_pages, H, page, D)
-    tensors, dtypes = [k_new, v_new, k_pages, v_pages, slots, slot_start, dev_status], [dt, dt, bf, bf, i32, i32, i32]
-    shapes = [new, new, pool, pool, (max_slots,), (B + 1,), (B,)]
-    if rows is not None:
-        tensors.append(rows), dtypes.append(i32), shapes.append((B, T))
-    a = _pointers(tensors, dtypes, shapes, _APPEND)
-    st = load().ppd_page_append(*a[:4], a[7] if rows is not None else None, a[4], a[5], L, B, H, T, D, page, n_pages, max_slots, _dtype(k_new),
-                                a[6], _stream(stream))
+    pool, i32, dt, bf = (L, n_pages, H, page, D), torch.int32, k_new.dtype, torch.bfloat16
+    a = _take(("k_new", k_new, dt, new), ("v_new", v_new, dt, new), ("k_pages", k_pages, bf, pool), ("v_pages", v_pages, bf, pool),
+              ("rows", rows, i32, (B, T)), ("slots", slots, i32, (max_slots,)), ("slot_start", slot_start, i32, (B + 1,)),
+              ("dev_status", dev_status, i32, (B,)))
+    st = load().ppd_page_append(*a[:7], L, B, H, T, D, page, n_pages, max_slots, _dtype(k_new), a[7], _stream(stream))
     _check(st, "ppd_page_append")
 
 
 def ppd_paged_attention_workspace_bytes(L, B, H, G, T, D, S_max, dtype=PPD_BF16) -> int:
     return int(load().ppd_paged_attention_workspace_bytes(L, B, H, G, T, D, S_max, dtype))
-
-
-_PAGED = ("q", "k_pages", "v_pages", "table", "k_tree", "v_tree", "prefix_len", "parent", "out", "dev_status", "lse")
 
 
 def ppd_tree_attention_paged(q, k_pages, v_pages, table, k_tree, v_tree, prefix_len, parent, out, dev_status, lse=None,
@@ -495,21 +476,15 @@ def ppd_tree_attention_paged(q, k_pages, v_pages, table, k_tree, v_tree, prefix_
     if H < 1 or Hq % H:
         raise ValueError(f"{Hq} query heads over {H} K/V heads")
     i32, dt, bf, pool, tree = torch.int32, q.dtype, torch.bfloat16, (L, n_pages, H, page, D), (L, B, H, T, D)
-    tensors = [q, k_pages, v_pages, table, k_tree, v_tree, prefix_len, parent, out, dev_status]
-    dtypes = [dt, bf, bf, i32, dt, dt, i32, i32, bf, i32]
-    shapes = [rows, pool, pool, (B, max_pages), tree, tree, (B,), (B, T), rows, (B,)]
-    if lse is not None:
-        tensors.append(lse), dtypes.append(torch.float32), shapes.append((L, B, Hq, T))
-    a = _pointers(tensors, dtypes, shapes, _PAGED)
+    a = _take(("q", q, dt, rows), ("k_pages", k_pages, bf, pool), ("v_pages", v_pages, bf, pool), ("table", table, i32, (B, max_pages)),
+              ("k_tree", k_tree, dt, tree), ("v_tree", v_tree, dt, tree), ("prefix_len", prefix_len, i32, (B,)), ("parent", parent, i32, (B, T)),
+              ("out", out, bf, rows), ("lse", lse, torch.float32, (L, B, Hq, T)), ("dev_status", dev_status, i32, (B,)))
     ws, ws_n = None, 0
     if workspace is not None:
         (ws,), ws_n = _ptrs(workspace), workspace.nbytes
-    st = load().ppd_tree_attention_paged(*a[:8], L, B, H, Hq // H, T, D, page, n_pages, max_pages, _dtype(q), float(scale), a[8],
-                                         a[10] if lse is not None else None, a[9], ws, ws_n, _stream(stream))
+    st = load().ppd_tree_attention_paged(*a[:8], L, B, H, Hq // H, T, D, page, n_pages, max_pages, _dtype(q), float(scale), *a[8:], ws, ws_n,
+                                         _stream(stream))
     _check(st, "ppd_tree_attention_paged")
-
-
-_LOGPROBS = ("logits", "tokens", "logprob", "entropy", "rank", "dev_status")
 
 
 def ppd_token_logprobs(logits, tokens, temperature: float, logprob, entropy, rank, dev_status, rows=None, top_tokens=None,
@@ -522,18 +497,10 @@ def ppd_token_logprobs(logits, tokens, temperature: float, logprob, entropy, ran
         raise ValueError("top_tokens and top_logprobs are given together")
     K = top_tokens.shape[2] if top_tokens is not None else 0
     i32, f32, each = torch.int32, torch.float32, (B, n)
-    tensors, dtypes = [logits, tokens, logprob, entropy, rank, dev_status], [logits.dtype, i32, f32, f32, i32, i32]
-    shapes, names, at = [all_rows, each, each, each, each, (B,)], _LOGPROBS, [None] * 3
-    for i, (name, t, dtype, shape) in enumerate((("rows", rows, i32, each), ("top_tokens", top_tokens, i32, (B, n, K)),
-                                                 ("top_logprobs", top_logprobs, f32, (B, n, K)))):
-        if t is not None:
-            at[i] = len(tensors)
-            tensors.append(t), dtypes.append(dtype), shapes.append(shape)
-            names += (name,)
-    a = _pointers(tensors, dtypes, shapes, names)
-    more = [a[i] if i is not None else None for i in at]
-    st = load().ppd_token_logprobs(a[0], a[1], more[0], B, T, V, n, K, _dtype(logits), float(temperature), a[2], a[3], a[4], more[1], more[2], a[5],
-                                   _stream(stream))
+    a = _take(("logits", logits, logits.dtype, all_rows), ("tokens", tokens, i32, each), ("rows", rows, i32, each), ("logprob", logprob, f32, each),
+              ("entropy", entropy, f32, each), ("rank", rank, i32, each), ("top_tokens", top_tokens, i32, (B, n, K)),
+              ("top_logprobs", top_logprobs, f32, (B, n, K)), ("dev_status", dev_status, i32, (B,)))
+    st = load().ppd_token_logprobs(*a[:3], B, T, V, n, K, _dtype(logits), float(temperature), *a[3:], _stream(stream))
     _check(st, "ppd_token_logprobs")
 
 
