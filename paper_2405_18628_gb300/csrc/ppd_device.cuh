@@ -673,6 +673,17 @@ PPD_DEV float rcp(float x)
     return y;
 }
 
+// An entry of a ranking as one integer, larger = earlier: NaN first, then the
+// larger value (-0 = +0), then the lower index (< 2^31).  Never 0.
+PPD_DEV uint32_t rank_key(float x)
+{
+    if (x != x) return 0xFFFFFFFFu;
+    const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+PPD_DEV unsigned long long rank_entry(uint32_t key, int i) { return (unsigned long long)key << 32 | (uint32_t)~i; }
+PPD_DEV int entry_index(unsigned long long e) { return (int)~(uint32_t)e; }
+
 // Maximum of v over the 32 lanes of a warp (every lane gets it).
 PPD_DEV float warp_max(float v)
 {

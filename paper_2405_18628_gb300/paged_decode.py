@@ -58,9 +58,9 @@ class PagedRequests:
         self.n_free, self._n_free = self._n_free, self.n_free
 
     def admit(self, k, v, count):
-        """Prompts for free places: k and v [L,B,H,n,D] of every layer, count int32 [B] rows of each (0: none for
-        this place, and for active ones).  A prompt that finds no pages leaves its place free."""
-        count = torch.where(self.active, 0, count)
+        """Prompts for free places: k and v [L,B,H,n,D] of every layer, count int32 [B] rows of each, n at most (0:
+        none for this place, and for active ones).  A prompt that finds no pages leaves its place free."""
+        count = torch.where(self.active, 0, count.clamp(0, k.shape[3]))
         self._assign(self.length + count)
         ppd.ppd_page_append(k, v, self.k, self.v, self.slots, self.slot_start, self.append_status)
         self.active |= (count > 0) & (self.assign_status == 0)
