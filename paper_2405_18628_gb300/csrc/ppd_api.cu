@@ -289,13 +289,15 @@ bool attn_dims_ok(int L, int B, int H, int T, int D, int S_max, ppd_dtype dt)
 struct AttnPlan {
     int split, cluster;
 };
-constexpr long long kClusterCostTiles = 2, kSplitCostTiles = 6, kPagedSplitCostTiles = 10;
+constexpr long long kClusterCostTiles = 2, kSplitCostTiles = 6;
 
-AttnPlan plan_units(long long units, long long t_u, int B, bool workspace, bool clusters)
+AttnPlan plan_attention(int L, int B, int H, int T, int S_max, bool workspace, bool clusters)
 {
     AttnPlan plan{0, 1};
-    const long long sms = split_grid();
+    const int n_tt = T > 64 ? (T + 127) / 128 : 1;
+    const long long units = (long long)L * B * H * n_tt, sms = split_grid();
     if (units >= sms) return plan;
+    const long long t_u = (S_max + 127) / 128 + n_tt;
     long long best = t_u;
     for (int c = 2; clusters && c <= ppd::kMaxCluster && c <= t_u && units * c <= sms; ++c) {
         const long long cost = (t_u + c - 1) / c + kClusterCostTiles;
@@ -306,12 +308,6 @@ AttnPlan plan_units(long long units, long long t_u, int B, bool workspace, bool 
     }
     if (workspace && B <= ppd::kSplitMaxB && (units * t_u + sms - 1) / sms + kSplitCostTiles < best) plan = {1, 1};
     return plan;
-}
-
-AttnPlan plan_attention(int L, int B, int H, int T, int S_max, bool workspace, bool clusters)
-{
-    const int n_tt = T > 64 ? (T + 127) / 128 : 1;   // also the blocks of queries
-    return plan_units((long long)L * B * H * n_tt, (S_max + 127) / 128 + n_tt, B, workspace, clusters);
 }
 
 // Enqueue the attention of all L*B*H slices (bf16 operands).
@@ -1349,6 +1345,30 @@ static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, 
     }
 }
 
+// Slices of up to 64 rows, fewer than SMs, by the time that each way takes, in microseconds (D = 128,
+// pages of 16, the tables' capacity standing in for the lengths): a tile 1.09, or its share of HBM where
+// many SMs stream; ends 5.6, of the work split 12 and a fifth for each part of a slice past eight.  Lengths
+// of several requests are taken to average 0.8 of the longest.  Clusters / shared out:
+//   2 slices of 6000 rows   12.2 / 18.8    8 of 16,000   24.3 / 23.6     32 of 6000    20.0 / 22.5
+//   2 of 64,000             74.3 / 35.5    8 of 64,000   78.5 / 50.3     32 of 20,000  52.7 / 47.1
+//   8 of 2000                9.2 / 13.8    16 of 6000    15.8 / 19.4     96 of 6000 (whole)  58.5 / 44.4
+static AttnPlan plan_paged_key(long long slices, long long t_u, int B, bool may_split)
+{
+    const double sms = split_grid(), hbm = 1.47;
+    AttnPlan plan{0, 1};
+    double best = 1.09 * t_u + 5.6;
+    for (int c = 2; c <= ppd::kMaxCluster && c <= t_u && slices * c <= split_grid(); ++c) {
+        const double cost = std::max(1.09, hbm * slices * c / sms) * ((t_u + c - 1) / c) + 5.6;
+        if (cost < best && slices <= ppd::max_attention_clusters(c)) {
+            best = cost;
+            plan.cluster = c;
+        }
+    }
+    const double shared = hbm * (B > 1 ? 0.8 : 1.0) * slices * t_u / sms + 12 + 0.2 * std::max(0.0, sms / slices - 8);
+    if (may_split && shared < best) plan = {1, 1};
+    return plan;
+}
+
 static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_max, ppd_dtype dt, bool workspace)
 {
     PagedWs w{};
@@ -1360,11 +1380,11 @@ static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_m
         plan_paged_rows(w, slices, t_u, B, workspace);
     } else {
         w.n_qb = 1;
-        w.plan = plan_units(slices, t_u, B, workspace && slices * t_u <= 2147483647ll, true);
-        // (a last, partial round of whole units weighs more here: requests' lengths are seldom alike)
-        if (workspace && slices >= sms && B <= ppd::kSplitMaxB && slices * t_u <= 2147483647ll &&
-            (slices * t_u + sms - 1) / sms + kPagedSplitCostTiles < (slices + sms - 1) / sms * t_u)
-            w.plan = {1, 1};
+        const bool may_split = workspace && B <= ppd::kSplitMaxB && slices * t_u <= 2147483647ll;
+        w.plan = slices < sms ? plan_paged_key(slices, t_u, B, may_split) : AttnPlan{0, 1};
+        // (a last, partial round of whole units weighs more here than in plan_attention: requests' lengths are
+        // seldom alike.  160 slices of up to 4000 rows: whole 49.5 us, shared out 45.0; of 2000 29.7 and 30.1)
+        if (may_split && slices >= sms && (slices * t_u + sms - 1) / sms + 10 < (slices + sms - 1) / sms * t_u) w.plan = {1, 1};
     }
     size_t off = dt == PPD_F32 ? align_up((size_t)slices * (w.rows + 2 * (size_t)T) * D * 2) : 0;
     if (w.plan.split) {
@@ -1429,11 +1449,12 @@ ppd_status ppd_tree_attention_paged(const void *q, const void *k_pages, const vo
         q = bq, k_tree = bk, v_tree = bv;
     }
     const int T_pad = (w.rows + 31) & ~31, shift = page_shift(page);
+    const uint32_t tree_box = T_pad > 64 ? 128u : (uint32_t)ppd::tree_box_rows(T);
     AttnMaps m;
     if (!encode_3d(&m.q, q, D, w.rows, slices, T_pad > 64 ? 128u : (uint32_t)T_pad) ||
         !encode_3d(&m.kc, k_pages, D, page, (uint64_t)L * n_pages * H, page < 128 ? page : 128) ||
         !encode_3d(&m.vc, v_pages, D, page, (uint64_t)L * n_pages * H, page < 128 ? page : 128) ||
-        !encode_3d(&m.kt, k_tree, D, T, slices, 128) || !encode_3d(&m.vt, v_tree, D, T, slices, 128))
+        !encode_3d(&m.kt, k_tree, D, T, slices, tree_box) || !encode_3d(&m.vt, v_tree, D, T, slices, tree_box))
         return PPD_ERR_CUDA;
     ppd::PagedParams p{};
     p.prefix_len = prefix_len, p.parent = parent;

@@ -20,9 +20,25 @@ struct UnitInfo {
     int lbh, qb, b, P, P_raw, n_pref, n_tiles;
 };
 
+// TAIL (the key-row kernel over pages): the tree's keys lie in the last, partial prefix tile,
+// behind its pages, where they fit there; their first row in it, or 0 where they have a tile of
+// their own.
+PPD_DEV int tail_offset(const AttnParams &p, int P)
+{
+    const int n = P & 127, box = 1 << static_cast<const PagedParams &>(p).box_shift;
+    const int off = (n + box - 1) & ~(box - 1);
+    return n > 0 && off + p.T <= 128 ? off : 0;
+}
+template <bool TAIL>
+PPD_DEV int tree_tiles(const AttnParams &p, int P)
+{
+    if constexpr (TAIL) return tail_offset(p, P) > 0 ? 0 : 1;
+    else return p.n_tt;
+}
+
 // Unit u = (layer, sequence, head) slice lbh and block qb of its query rows
 // (slices of trees over 128 tokens split their queries into blocks of 128).
-template <bool SKIP = false>
+template <bool SKIP = false, bool TAIL = false>
 PPD_DEV UnitInfo unit_info(const AttnParams &p, int u)
 {
     UnitInfo ui;
@@ -34,7 +50,7 @@ PPD_DEV UnitInfo unit_info(const AttnParams &p, int u)
     ui.P_raw = ld_input(p.prefix_len + ui.b);
     ui.P = min(max(ui.P_raw, 0), p.S_max);
     ui.n_pref = (ui.P + 127) >> 7;
-    ui.n_tiles = ui.n_pref + p.n_tt;
+    ui.n_tiles = ui.n_pref + tree_tiles<TAIL>(p, ui.P);
     return ui;
 }
 
@@ -87,14 +103,15 @@ PPD_DEV long long split_start(int c, long long N, int G) { return (long long)c *
 PPD_DEV int split_cta_of(long long x, long long N, int G) { return (int)(((x + 1) * G + N - 1) / N) - 1; }
 
 // This CTA's share of its cluster's unit (the cluster split): no lane needs another's.
-template <bool kHint = false>
+template <bool kHint = false, bool TAIL = false>
 PPD_DEV WorkRange plan_cluster(const AttnParams &p)
 {
     WorkRange w{};
     const int c = (int)blockIdx.x;
     w.u_first = w.u_last = c / p.cluster;
     const int32_t *P = p.prefix_len + w.u_first / (p.H * p.n_qb) % p.B;
-    const int nt = ((min(max(kHint ? ld_relaxed_gpu_s32(P) : ld_input(P), 0), p.S_max) + 127) >> 7) + p.n_tt;
+    const int len = min(max(kHint ? ld_relaxed_gpu_s32(P) : ld_input(P), 0), p.S_max);
+    const int nt = ((len + 127) >> 7) + tree_tiles<TAIL>(p, len);
     const int r = c - w.u_first * p.cluster;
     w.parts = min(p.cluster, nt);
     if (r < w.parts) {
@@ -111,10 +128,10 @@ PPD_DEV WorkRange plan_cluster(const AttnParams &p)
 // jobs; null: always round-robin).  kHint: the prefix
 // lengths are read through L2 because they may still be changing (a plan
 // made before the wait of a chained launch, used for prefetch hints only).
-template <bool kHint = false>
+template <bool kHint = false, bool TAIL = false>
 PPD_DEV WorkRange plan_range(const AttnParams &p, int lane, uint8_t *seq = nullptr)
 {
-    if (p.cluster > 1) return plan_cluster<kHint>(p);
+    if (p.cluster > 1) return plan_cluster<kHint, TAIL>(p);
     WorkRange w{};
     const int G = (int)gridDim.x, c = (int)blockIdx.x;
     // no range of tiles unless one is found below
@@ -128,7 +145,7 @@ PPD_DEV WorkRange plan_range(const AttnParams &p, int lane, uint8_t *seq = nullp
     auto nt_of = [&](int b) {
         const int P = min(max(kHint ? ld_relaxed_gpu_s32(p.prefix_len + b) : ld_input(p.prefix_len + b), 0),
                           p.S_max);
-        return ((P + 127) >> 7) + p.n_tt;
+        return ((P + 127) >> 7) + tree_tiles<TAIL>(p, P);
     };
     if (w.rr_units > 0) {
         if (!seq || p.B < 2 || p.B > kSplitMaxB || p.n_units <= G) return w;
@@ -259,7 +276,7 @@ struct Seg {
 // Walks this CTA's segments in order (every role of the CTA walks the same
 // sequence): whole units round-robin, or (SPLIT) its range of tiles, `left`
 // counting the range's tiles not yet handed out.
-template <bool SPLIT, bool RAGGED = false>
+template <bool SPLIT, bool RAGGED = false, bool TAIL = false>
 struct SegIter {
     int u, j0, left;       // whole units: the next round-robin position; else the range's next unit
     const uint8_t *seq;
@@ -276,7 +293,7 @@ struct SegIter {
             int unit = u;
             if (RAGGED && seq) unit = ragged_job(p, seq, u, (int)gridDim.x, p.n_units, 1);
             if (unit < 0 || unit >= p.n_units) return false;
-            s.ui = unit_info<true>(p, unit);
+            s.ui = unit_info<true, TAIL>(p, unit);
             s.u = unit;
             s.j0 = 0;
             s.j1 = s.ui.n_tiles;
@@ -284,7 +301,7 @@ struct SegIter {
             return true;
         }
         if (left <= 0 || u >= p.n_units) return false;
-        s.ui = unit_info<true>(p, u);
+        s.ui = unit_info<true, TAIL>(p, u);
         s.u = u;
         s.j0 = j0;
         s.j1 = min(s.ui.n_tiles, j0 + left);

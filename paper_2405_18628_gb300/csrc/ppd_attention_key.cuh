@@ -181,7 +181,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     if (p.pdl_wait) {
         if (warp == Lay::SW) {
             if constexpr (PAGED) {
-                const WorkRange w = plan_range<true>(p, lane);
+                const WorkRange w = plan_range<true, true>(p, lane);
                 prefetch_pages<Lay::DCH>(p, lane, &map_kc, &map_vc, RANGE ? w.u_first : (int)blockIdx.x, RANGE ? w.j_first : 0,
                                          RANGE ? min(w.n_tiles, 3) : 3);
             } else {
@@ -192,7 +192,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     }
     WorkRange *wr_s = reinterpret_cast<WorkRange *>(smem + Lay::OFF_RANGE);
     if (warp == Lay::SW) {
-        const WorkRange w = plan_range(p, lane, RAGGED ? smem + Lay::OFF_SEQ : nullptr);   // whole units round-robin without p.split
+        const WorkRange w = plan_range<false, PAGED>(p, lane, RAGGED ? smem + Lay::OFF_SEQ : nullptr);   // whole units round-robin without p.split
         if (lane == 0) {
             *wr_s = w;
             if (SPLIT) p.split_rec[blockIdx.x].u = -1;   // no cut unit recorded yet
@@ -224,17 +224,17 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             KPos kp;
             VPos vp;
             int g = 0, k = 0;
-            SegIter<RANGE, RAGGED> it(wr);
-            auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, uint32_t off, uint64_t *full, bool tree, int z,
+            SegIter<RANGE, RAGGED, PAGED> it(wr);
+            // A tile: pages' boxes and (at row t_row >= 0) the tree's.
+            const uint32_t tree_bytes = (uint32_t)tree_box_rows(T) * 128u * Lay::DCH;
+            auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, uint32_t off, uint64_t *full, int t_row, int z,
                             const UnitInfo &ui, int row) {
                 if (warp_uniform(*abort_flag)) return;
-                if (!tree) {
-                    load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, pol);
-                } else if (lane == 0) {
-                    mbar_arrive_expect_tx(full, Lay::TILE_BYTES);
+                load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, pol, t_row >= 0 ? tree_bytes : 0u);
+                if (t_row >= 0 && elect_one()) {
 #pragma unroll
                     for (int c = 0; c < Lay::DCH; ++c)
-                        tma_load_3d(smem + off + c * Lay::GROUP_BYTES, tree_map, full, c * 64, 0, ui.lbh, pol);
+                        tma_load_3d(smem + off + c * Lay::GROUP_BYTES + t_row * 128, tree_map, full, c * 64, 0, ui.lbh, pol);
                 }
                 __syncwarp();
             };
@@ -252,16 +252,17 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                                     &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
                 }
                 __syncwarp();
+                const int tail = warp_uniform(tail_offset(p, ui.P));
                 for (int j = sg.j0; j < sg.j1; ++j, ++g) {
-                    const bool tree = (j == ui.n_pref);
+                    const int t_row = j == ui.n_pref ? 0 : (tail > 0 && j == ui.n_pref - 1 ? tail : -1);
                     const int row = j * Lay::KT;
                     // the next tile's page numbers are asked for a tile ahead
                     const int z_next = page_coord(p, pu, row + Lay::KT, ui.P, lane);
                     mbar_wait(bars + Lay::B_KEMPTY + kp.slot, kp.phase ^ 1u, abort_flag);
-                    load(&map_kc, &map_kt, Lay::OFF_K + kp.slot * Lay::TILE_BYTES, bars + Lay::B_KFULL + kp.slot, tree, z, ui, row);
+                    load(&map_kc, &map_kt, Lay::OFF_K + kp.slot * Lay::TILE_BYTES, bars + Lay::B_KFULL + kp.slot, t_row, z, ui, row);
                     kp.advance();
                     mbar_wait(bars + Lay::B_VEMPTY + vp.slot, vp.phase ^ 1u, abort_flag);
-                    load(&map_vc, &map_vt, Lay::OFF_V + vp.slot * Lay::TILE_BYTES, bars + Lay::B_VFULL + vp.slot, tree, z, ui, row);
+                    load(&map_vc, &map_vt, Lay::OFF_V + vp.slot * Lay::TILE_BYTES, bars + Lay::B_VFULL + vp.slot, t_row, z, ui, row);
                     vp.advance();
                     z = z_next;
                 }
@@ -283,7 +284,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             KPos kp;
             VPos vp;
             int g = 0, k = 0;
-            SegIter<RANGE, RAGGED> it(wr);
+            SegIter<RANGE, RAGGED, PAGED> it(wr);
             for (Seg sg; it.next(p, sg); ++k) {
                 const UnitInfo &ui = sg.ui;
                 const int u = sg.u;
@@ -383,7 +384,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
         int g = 0, k = 0;
         bool prev_first = false;
         uint32_t prev_to = 0;
-        SegIter<RANGE, RAGGED> it(wr);
+        SegIter<RANGE, RAGGED, PAGED> it(wr);
         for (Seg sg;; ++k) {
             const int n = warp_uniform(it.next(p, sg) ? sg.j1 - sg.j0 : 0);
             if (n == 0) break;
@@ -449,8 +450,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
         uint64_t lacc[NC / 2];   // this key row's share of every owned query's row sum, in pairs
 #pragma unroll
         for (int c = 0; c < NC / 2; ++c) lacc[c] = 0ull;
-        uint32_t dbits = 0;   // bit c: key t (tree node t) is visible to query q0 + c
+        uint32_t dbits = 0;   // bit c: key t (tree node t, or t - tail) is visible to query q0 + c
         int cur_b = -1;
+        int tail = 0;         // over pages: the tree's first row in the last prefix tile (0: a tile of its own)
         int g = 0;
         KPos kp;
         VPos vp;
@@ -611,7 +613,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
         };
 
         int k = 0;
-        SegIter<RANGE, RAGGED> it(wr);
+        SegIter<RANGE, RAGGED, PAGED> it(wr);
         for (Seg sg; it.next(p, sg); ++k) {
             const UnitInfo &ui = sg.ui;
             const int u = sg.u;
@@ -621,6 +623,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             // unit's first tile is on its way)
             const bool new_tree = ui.b != cur_b;
             cur_b = ui.b;
+            if constexpr (PAGED) tail = tail_offset(p, ui.P);
             int par[2] = {-1, -1};
             if (new_tree) {
 #pragma unroll
@@ -655,8 +658,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                     for (int c = 0; c < NC; ++c) {
                         const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)anc, c);
                         const uint32_t hi = TP > 32 ? __shfl_sync(0xffffffffu, (uint32_t)(anc >> 32), c) : 0u;
-                        const uint32_t w = t < 32 ? lo : hi;
-                        if (t < T && ((w >> (t & 31)) & 1u)) dbits |= 1u << c;
+                        const int node = PAGED ? t - tail : t;
+                        const uint32_t w = node < 32 ? lo : hi;
+                        if (node < T && (!PAGED || node >= 0) && ((w >> (node & 31)) & 1u)) dbits |= 1u << c;
                     }
                 }
                 mbar_wait(bars + Lay::B_SFULL + sb, (g >> 1) & 1, abort_flag);
@@ -681,7 +685,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                 }
                 // Done optimistically with the current running maxima; when a score
                 // exceeds its maximum by more than 2^16, again by the exact path.
-                const uint32_t bits = tree ? dbits : (t < n_valid ? 0xffffffffu : 0u);
+                const bool with_tree = PAGED && tail > 0 && j == ui.n_pref - 1;
+                const uint32_t bits = tree ? dbits : (t < n_valid ? 0xffffffffu : (with_tree ? dbits : 0u));
                 if (!masked) {
                     const float maxd = emit(kind_t<0>{}, store_t{}, r, bits, pbuf);
                     if (named_bar_or(1 + wg, 128, maxd > 16.f)) exact_tile(kind_t<0>{}, r, bits, pbuf, first);
@@ -690,10 +695,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                     if (named_bar_or(1 + wg, 128, maxd > 16.f)) exact_tile(kind_t<1>{}, r, bits, pbuf, first);
                 }
 
-                // V rows of invisible keys in a partial prefix tile may be NaN: zero them
-                if (!tree && masked && wg == 0) {
+                // V rows of invisible keys in a partial prefix tile may be NaN (and, over pages, what
+                // a tree's box leaves of its tile): zero them
+                if ((PAGED || !tree) && masked && wg == 0) {
                     mbar_wait(bars + Lay::B_VFULL + vp.slot, vp.phase, abort_flag);
-                    if (t >= n_valid) {
+                    if (t >= n_valid && !(with_tree && t >= tail && t < tail + T)) {
                         const uint32_t vrow = smem_addr(smem + Lay::OFF_V + vp.slot * Lay::TILE_BYTES) + t * 128u;
 #pragma unroll
                         for (int c = 0; c < Lay::DCH; ++c)

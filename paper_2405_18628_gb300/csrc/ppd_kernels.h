@@ -122,6 +122,9 @@ struct PagedParams : AttnParams {
     int pair_units;             // work split, more than 128 rows: units are pairs of blocks of 128 rows
 };
 
+// Rows of a box of the tree's keys or values in the key-row kernel over pages.
+inline __host__ __device__ int tree_box_rows(int T) { return (T + 7) & ~7; }
+
 // Work split limits: batch size (the per-CTA range search holds the batch in
 // two warp-wide registers), CTAs, and query rows of a partial state.
 constexpr int kSplitMaxB = 64;

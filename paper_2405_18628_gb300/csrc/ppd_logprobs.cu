@@ -32,7 +32,6 @@
 
 namespace ppd {
 
-constexpr int kLogThreads = 128;
 constexpr int kLogLoads = 4;                   // 16-byte loads of a batch and thread
 
 // The value behind a rank_key.
@@ -96,12 +95,12 @@ PPD_DEV float below(float x)
 }
 
 // STAGES: batches on their way or in hand.
-template <bool BF16, int STAGES>
-__global__ void __launch_bounds__(kLogThreads) token_logprobs_kernel(const LogprobParams p)
+template <bool BF16, int THREADS, int STAGES>
+__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobParams p)
 {
     constexpr int E = BF16 ? 8 : 4;            // entries of a load
     constexpr int NV = E * kLogLoads;          // of a batch and thread
-    constexpr int THREADS = kLogThreads, WARPS = THREADS / 32;
+    constexpr int WARPS = THREADS / 32;
     constexpr int kMaxPush = kLogMaxK * NV;
     constexpr int eb = BF16 ? 2 : 4;
     constexpr uint32_t kAbsent = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
@@ -541,13 +540,18 @@ cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t str
     // stages 122); else two, so that eight CTAs find room (2048 rows of 128,256 bf16: 133 us, with
     // four 162).
     const long long items = (long long)p.B * p.n;
-    const int batch = kLogThreads * kLogLoads * (p.bf16 ? 8 : 4);
+    const int batch = 128 * kLogLoads * (p.bf16 ? 8 : 4);
     p.cluster = 1;
     while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 5ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
     const bool deep = items * p.cluster <= 5ll * num_sms;
-    auto *kern = p.bf16 ? (deep ? token_logprobs_kernel<true, 4> : token_logprobs_kernel<true, 2>)
-                        : (deep ? token_logprobs_kernel<false, 4> : token_logprobs_kernel<false, 2>);
-    return launch_chained(kern, dim3((unsigned)(items * p.cluster)), dim3(kLogThreads), dim3((unsigned)p.cluster), stream, p);
+    // Many rows of up to 32 KB with few alternatives by single warps: their barriers cost nothing, and more of
+    // them find room.  128 threads / 32, us:
+    //   14,400 rows of 1000 fp32, 5 alternatives   119 / 44       of 8000, 5   190 / 118      of 4000, 32   177 / 182
+    //   4000 rows of 16,000 bf16, 5                 72 / 53       1000 of 32,000 bf16, 5   31 / 34
+    const bool warps = !deep && p.K <= 8 && (long long)p.V * (p.bf16 ? 2 : 4) <= 32768;
+    auto *kern = p.bf16 ? (warps ? token_logprobs_kernel<true, 32, 2> : deep ? token_logprobs_kernel<true, 128, 4> : token_logprobs_kernel<true, 128, 2>)
+                        : (warps ? token_logprobs_kernel<false, 32, 2> : deep ? token_logprobs_kernel<false, 128, 4> : token_logprobs_kernel<false, 128, 2>);
+    return launch_chained(kern, dim3((unsigned)(items * p.cluster)), dim3(warps ? 32 : 128), dim3((unsigned)p.cluster), stream, p);
 }
 
 }  // namespace ppd

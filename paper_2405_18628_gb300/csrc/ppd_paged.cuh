@@ -58,18 +58,19 @@ PPD_DEV int page_coord(const PagedParams &p, const PageUnit &u, int row, int P, 
     return page_depth(p, u, ld_input(u.row + (r >> p.page_shift)));
 }
 
-// The tile itself, by a converged warp: every box that holds a key below P.  One elected lane
+// The tile itself, by a converged warp: every box that holds a key below P (`more`: bytes that the
+// caller copies besides).  One elected lane
 // issues the copies of all of them, from warp-uniform code: lanes that each copied a box took 115 cycles
 // a box, one after the other (48 requests of up to 8192 rows in pages of 16: 224 us, in pages of
 // 64 177 us).
 template <int DCH>
 PPD_DEV void load_page_tile(const PagedParams &p, const CUtensorMap *map, uint8_t *dst, uint32_t group_bytes, uint64_t *full,
-                            int depth, int row, int P, uint64_t policy)
+                            int depth, int row, int P, uint64_t policy, uint32_t more = 0)
 {
-    const int n = warp_uniform((min(128, P - row) + (1 << p.box_shift) - 1) >> p.box_shift);
+    const int n = warp_uniform((max(0, min(128, P - row)) + (1 << p.box_shift) - 1) >> p.box_shift);
     const uint32_t box_bytes = 128u << p.box_shift;
     const int y = warp_uniform(row & ((1 << p.page_shift) - 1));
-    if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)n * DCH * box_bytes);
+    if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)n * DCH * box_bytes + more);
     __syncwarp();
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
