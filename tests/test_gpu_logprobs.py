@@ -181,3 +181,54 @@ def test_the_same_again_and_from_a_graph(cuda_device):
     torch.cuda.synchronize()
     for k, v in first.items():
         assert torch.equal(v, second[k]) and torch.equal(v, out[k]), k
+
+
+def test_logits_past_32_bits(cuda_device):
+    from paper_2405_18628_gb300 import ppd
+    V, T = 128257, 40000
+    logits = torch.empty(1, T, V, dtype=torch.bfloat16, device=cuda_device)
+    g = torch.Generator(device=cuda_device)
+    g.manual_seed(6)
+    rows = [0, 20001, 36000, T - 1]
+    for r in rows:
+        logits[0, r] = (3 * torch.randn(V, device=cuda_device, generator=g)).to(torch.bfloat16)
+    at, tokens = _i32([rows], cuda_device), _i32([[5, V - 1, 70000, 0]], cuda_device)
+    check_items(call(ppd, logits, tokens, 0.7, rows=at, K=4), logits, tokens, 0.7, at, [(0, i) for i in range(4)])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [3, 257, 1000, 4096, 8191])
+def test_many_short_rows(cuda_device, V, dtype):
+    """Rows that single warps take."""
+    from paper_2405_18628_gb300 import ppd
+    g = torch.Generator(device=cuda_device)
+    g.manual_seed(V)
+    B, T = 4, 300
+    logits = (3 * torch.randn(B, T, V, device=cuda_device, generator=g)).to(dtype)
+    logits[0, :5, ::2] = -math.inf
+    logits[1, 3, V // 2] = math.nan
+    tokens = torch.randint(0, V, (B, T), device=cuda_device, generator=g).int()
+    for K in (0, min(V, 8)):
+        r = call(ppd, logits, tokens, 0.8, K=K)
+        check_items(r, logits, tokens, 0.8, None, [(0, 0), (0, 4), (1, 3), (1, 4), (2, 150), (3, 299)])
+        if K:
+            clean = logits.float()[2:]
+            assert torch.equal(r["top"][2:].long(), torch.sort(clean, dim=-1, descending=True, stable=True).indices[..., :K])
+        x = logits.float()[2:]
+        t = tokens[2:].long()[..., None]
+        xt = x.gather(2, t)
+        assert torch.equal(r["rank"][2:].long(), ((x > xt) | ((x == xt) & (torch.arange(V, device=cuda_device) < t))).sum(-1))
+
+
+@pytest.mark.parametrize("V", [40, 3001])
+def test_ties_infinities_and_nan_in_many_rows(cuda_device, V):
+    """The hard rows again where single warps take them."""
+    from paper_2405_18628_gb300 import ppd
+    rows = _hard_rows(V, cuda_device)
+    T = len(rows)
+    logits = torch.stack(list(rows.values())).repeat(70, 1)[None]
+    tokens = _i32([[V - 1] * (70 * T)], cuda_device)
+    r = call(ppd, logits, tokens, 0.9, K=8)
+    check_items(r, logits, tokens, 0.9, None, [(0, i) for i in range(T)])
+    for k in ("logprob", "entropy", "rank", "top", "best"):
+        assert torch.equal(torch.nan_to_num(r[k].float())[0, :T], torch.nan_to_num(r[k].float())[0, -T:]), k

@@ -258,3 +258,55 @@ def test_the_same_as_over_a_contiguous_cache(cuda_device):
         # (sums may be shared out otherwise: a relative 1e-4 covers fp32's, and a rounding of each side)
         assert ((out.float() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4 * want.abs().amax(-1, keepdim=True)).all()
         assert float((lse - wlse).abs().max()) <= 2e-5
+
+
+def test_pools_past_32_bits(cuda_device):
+    """Pages whose elements are more than 2^32 from the pool's start: rows in, and attention over them."""
+    from paper_2405_18628_gb300 import ppd
+    dev, H, D, page, N, T = cuda_device, 4, 128, 128, 70000, 5
+    g = torch.Generator(device=dev)
+    g.manual_seed(8)
+    n = lambda *s: torch.randn(s, dtype=torch.bfloat16, device=dev, generator=g)  # noqa: E731
+    k, v = (torch.empty(1, N, H, page, D, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    assert k.numel() > 2 ** 32
+    table = torch.tensor([[N - 1, 3, N - 2], [66000, N - 3, -1]], dtype=torch.int32, device=dev)
+    lens = [300, 200]
+    kn, vn = n(1, 2, H, 300, D), n(1, 2, H, 300, D)
+    slots = [int(table[b, r // page]) * page + r % page for b in range(2) for r in range(lens[b])]
+    status = _i32([77, 77], dev)
+    ppd.ppd_page_append(kn, vn, k, v, _i32(slots, dev), _i32([0, 300, 500], dev), status)
+    assert (status == 0).all()
+    q, kt, vt = n(1, 2, 2 * H, T, D), n(1, 2, H, T, D), n(1, 2, H, T, D)
+    parent = [[-1, 0, 1, 0, 3]] * 2
+    out, lse = torch.empty(1, 2, 2 * H, T, D, dtype=torch.bfloat16, device=dev), torch.empty(1, 2, 2 * H, T, device=dev)
+    ppd.ppd_tree_attention_paged(q, k, v, table, kt, vt, _i32(lens, dev), _i32(parent, dev), out, status, lse=lse)
+    assert (status == 0).all()
+    for b in range(2):
+        for h in range(H):
+            want, want_lse, mass, size = O.attention(q[0, b, 2 * h:2 * h + 2], kn[0, b, h, :lens[b]], vn[0, b, h, :lens[b]], kt[0, b, h], vt[0, b, h], parent[b])
+            assert ((out[0, b, 2 * h:2 * h + 2].double() - want).abs() <= (2.0 ** -8 + 1e-4 + 2 * D * 2.0 ** -24 * size) * mass + 1e-36).all()
+            assert float((lse[0, b, 2 * h:2 * h + 2].double() - want_lse).abs().max()) <= D * 2.0 ** -24 * size + 1e-5
+
+
+@pytest.mark.parametrize("B,lens", [(300, [0, 5, 40, 129]), (65, [700, 1])])
+def test_many_requests(cuda_device, B, lens):
+    """More requests than the plans for unequal lengths hold."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 1, B, 3, 2, 64, 3, [lens[b % len(lens)] for b in range(B)], 16, seed=B)
+    c.run(ppd)
+    c.check(seqs=range(0, B, 23))
+    assert (c.status == 0).all()
+
+
+@pytest.mark.parametrize("page", [8, 16, 128])
+@pytest.mark.parametrize("T,G", [(1, 2), (8, 1), (9, 3), (57, 1), (64, 1)])
+def test_trees_behind_the_last_rows(cuda_device, page, T, G):
+    """The tree's keys share the last prefix tile where they fit behind its pages: lengths around where
+    they do, one tile and several, whole slices and parts of them."""
+    from paper_2405_18628_gb300 import ppd
+    edge = (128 - T) // page * page
+    lens = sorted({max(0, x + base) for base in (0, 128, 640) for x in (1, edge - 1, edge, edge + 1, edge - page, 127, 128)})
+    for H, spare in ((1, 0), (40, 0), (2, 400)):
+        c = Case(cuda_device, 1, len(lens), H, G, 128, T, lens, page, spare=spare, seed=T + page)
+        c.run(ppd)
+        c.check(seqs=range(0, len(lens), 1 if H < 3 else 7))
