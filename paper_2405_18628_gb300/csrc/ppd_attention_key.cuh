@@ -207,74 +207,74 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     const uint32_t tmem_base = *tmem_ptr;
     const WorkRange &wr = *wr_s;
 
-    if (warp == Lay::SW + 2) {
+    if (!PAGED && warp == Lay::SW + 2) {
         // ------------------------------------------------------------ fused-step side work
-        if constexpr (PAGED) {
-            paged_status_warp(p, lane);
-        } else {
+        if constexpr (!PAGED) {
             if (p.fused) fused_side_warp<true>(p, wr, lane, abort_flag);
             else if (p.set_status) status_warp(p, lane);
             if (p.late_wait) pdl_wait();
         }
-    } else if (PAGED && warp == Lay::SW) {
+    } else if (PAGED && (warp == Lay::SW || warp == Lay::SW + 2)) {
         if constexpr (PAGED) {
-            // -------------------------------------------------------- TMA producer, page by page
-            // the whole warp walks the tiles, a lane looks up a box's page, one elected lane copies
+            // -------------------------------------------------------- TMA producers, page by page
+            // one warp copies Q and K, another V (a copy of a small page takes its issuer some 45 ns: one
+            // warp could not keep up with HBM for pages of 16 rows and fewer); a whole warp walks the tiles,
+            // a lane looks up a box's page, one elected lane copies
+            const bool is_v = warp == Lay::SW + 2;
+            const CUtensorMap *pages = is_v ? &map_vc : &map_kc, *tree_map = is_v ? &map_vt : &map_kt;
+            uint64_t *full0 = bars + (is_v ? Lay::B_VFULL : Lay::B_KFULL), *empty0 = bars + (is_v ? Lay::B_VEMPTY : Lay::B_KEMPTY);
+            uint8_t *ring = smem + (is_v ? Lay::OFF_V : Lay::OFF_K);
+            static_assert(Lay::KS == Lay::VS, "one walk for both rings");
             const uint64_t pol = l2_policy_evict_first();
-            KPos kp;
-            VPos vp;
+            const uint32_t tree_bytes = (uint32_t)tree_box_rows(T) * 128u * Lay::DCH;
+            KPos pos;
             int g = 0, k = 0;
             SegIter<RANGE, RAGGED, PAGED> it(wr);
-            // A tile: pages' boxes and (at row t_row >= 0) the tree's.
-            const uint32_t tree_bytes = (uint32_t)tree_box_rows(T) * 128u * Lay::DCH;
-            auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, uint32_t off, uint64_t *full, int t_row, int z,
-                            const UnitInfo &ui, int row) {
-                if (warp_uniform(*abort_flag)) return;
-                load_page_tile<Lay::DCH>(p, pages, smem + off, Lay::GROUP_BYTES, full, z, row, ui.P, pol, t_row >= 0 ? tree_bytes : 0u);
-                if (t_row >= 0 && elect_one()) {
-#pragma unroll
-                    for (int c = 0; c < Lay::DCH; ++c)
-                        tma_load_3d(smem + off + c * Lay::GROUP_BYTES + t_row * 128, tree_map, full, c * 64, 0, ui.lbh, pol);
-                }
-                __syncwarp();
-            };
             for (Seg sg; it.next(p, sg); ++k) {
                 const UnitInfo &ui = sg.ui;
                 const int qs = k & 1;
                 const PageUnit pu(p, ui.lbh, ui.b);
                 int z = page_coord(p, pu, sg.j0 * Lay::KT, ui.P, lane);
-                mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
-                if (!warp_uniform(*abort_flag) && lane == 0) {
-                    mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
+                if (!is_v) {
+                    mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
+                    if (!warp_uniform(*abort_flag) && lane == 0) {
+                        mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
 #pragma unroll
-                    for (int c = 0; c < Lay::DCH; ++c)
-                        tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::Q_GROUP_BYTES,
-                                    &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
+                        for (int c = 0; c < Lay::DCH; ++c)
+                            tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::Q_GROUP_BYTES,
+                                        &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 const int tail = warp_uniform(tail_offset(p, ui.P));
                 for (int j = sg.j0; j < sg.j1; ++j, ++g) {
+                    // the tree's first row in the tile, if it holds the tree
                     const int t_row = j == ui.n_pref ? 0 : (tail > 0 && j == ui.n_pref - 1 ? tail : -1);
                     const int row = j * Lay::KT;
                     // the next tile's page numbers are asked for a tile ahead
                     const int z_next = page_coord(p, pu, row + Lay::KT, ui.P, lane);
-                    mbar_wait(bars + Lay::B_KEMPTY + kp.slot, kp.phase ^ 1u, abort_flag);
-                    load(&map_kc, &map_kt, Lay::OFF_K + kp.slot * Lay::TILE_BYTES, bars + Lay::B_KFULL + kp.slot, t_row, z, ui, row);
-                    kp.advance();
-                    mbar_wait(bars + Lay::B_VEMPTY + vp.slot, vp.phase ^ 1u, abort_flag);
-                    load(&map_vc, &map_vt, Lay::OFF_V + vp.slot * Lay::TILE_BYTES, bars + Lay::B_VFULL + vp.slot, t_row, z, ui, row);
-                    vp.advance();
+                    mbar_wait(empty0 + pos.slot, pos.phase ^ 1u, abort_flag);
+                    if (!warp_uniform(*abort_flag)) {
+                        uint8_t *dst = ring + pos.slot * Lay::TILE_BYTES;
+                        load_page_tile<Lay::DCH>(p, pages, dst, Lay::GROUP_BYTES, full0 + pos.slot, z, row, ui.P, pol, t_row >= 0 ? tree_bytes : 0u);
+                        if (t_row >= 0 && elect_one()) {
+#pragma unroll
+                            for (int c = 0; c < Lay::DCH; ++c)
+                                tma_load_3d(dst + c * Lay::GROUP_BYTES + t_row * 128, tree_map, full0 + pos.slot, c * 64, 0, ui.lbh, pol);
+                        }
+                        __syncwarp();
+                    }
+                    pos.advance();
                     z = z_next;
                 }
             }
+            if (is_v) paged_status_warp(p, lane);
             if (*abort_flag) {
                 // let every copy already issued land before the CTA can exit
-                for (int i = max(0, g - Lay::KS); i < g; ++i)
-                    mbar_wait_drain(bars + Lay::B_KFULL + i % Lay::KS, (i / Lay::KS) & 1);
-                for (int i = max(0, g - Lay::VS); i < g; ++i)
-                    mbar_wait_drain(bars + Lay::B_VFULL + i % Lay::VS, (i / Lay::VS) & 1);
-                for (int i = max(0, k - Lay::QS); i < k; ++i)
-                    mbar_wait_drain(bars + Lay::B_QFULL + i % Lay::QS, (i / Lay::QS) & 1);
+                for (int i = max(0, g - Lay::KS); i < g; ++i) mbar_wait_drain(full0 + i % Lay::KS, (i / Lay::KS) & 1);
+                if (!is_v)
+                    for (int i = max(0, k - Lay::QS); i < k; ++i)
+                        mbar_wait_drain(bars + Lay::B_QFULL + i % Lay::QS, (i / Lay::QS) & 1);
             }
         }
     } else if (warp == Lay::SW) {
