@@ -19,7 +19,8 @@
 // larger trees fill the tensor core's M side with queries and run the
 // query-row kernel (ppd_attention_rows.cuh).  Warp roles: two softmax warpgroups,
 // each owning half of the query columns, then the TMA producer, the MMA issuer and
-// TMEM owner, and the fused step's argmax / acceptance / compaction.  Four
+// TMEM owner, and the fused step's argmax / acceptance / compaction (with a cache in pages a
+// second TMA producer, then the statuses).  Four
 // warpgroups of a quarter each gain 3 % on long slices of D = 64 with TP = 64 (8 x 16
 // slices of 8000 keys: 302 against 292 us) but leave 96 registers a thread, too few
 // for the side warp: 30 x 16 slices of 1000 keys, 40 tokens, 439 against 510 us.
@@ -217,8 +218,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
     } else if (PAGED && (warp == Lay::SW || warp == Lay::SW + 2)) {
         if constexpr (PAGED) {
             // -------------------------------------------------------- TMA producers, page by page
-            // one warp copies Q and K, another V (a copy of a small page takes its issuer some 45 ns: one
-            // warp could not keep up with HBM for pages of 16 rows and fewer); a whole warp walks the tiles,
+            // one warp copies Q and K, another V, as a copy of a small page takes its issuer some 45 ns
+            // (48 requests of up to 8192 rows, 8 heads: pages of 8 192.9 -> 179.3 us, of 16 180.1 -> 177.5;
+            // 90 of up to 5611, D = 64: 225.8 -> 147.0 and 170.8 -> 133.2); a whole warp walks the tiles,
             // a lane looks up a box's page, one elected lane copies
             const bool is_v = warp == Lay::SW + 2;
             const CUtensorMap *pages = is_v ? &map_vc : &map_kc, *tree_map = is_v ? &map_vt : &map_kt;
@@ -229,6 +231,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             const uint32_t tree_bytes = (uint32_t)tree_box_rows(T) * 128u * Lay::DCH;
             KPos pos;
             int g = 0, k = 0;
+            int n_tiles = 0, n_q = 0;   // copies issued, of g tiles and k blocks of Q
             SegIter<RANGE, RAGGED, PAGED> it(wr);
             for (Seg sg; it.next(p, sg); ++k) {
                 const UnitInfo &ui = sg.ui;
@@ -237,12 +240,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                 int z = page_coord(p, pu, sg.j0 * Lay::KT, ui.P, lane);
                 if (!is_v) {
                     mbar_wait(bars + Lay::B_QEMPTY + qs, ((k >> 1) & 1) ^ 1, abort_flag);
-                    if (!warp_uniform(*abort_flag) && lane == 0) {
-                        mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
+                    if (!warp_uniform(*abort_flag)) {
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(bars + Lay::B_QFULL + qs, Lay::Q_BYTES);
 #pragma unroll
-                        for (int c = 0; c < Lay::DCH; ++c)
-                            tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::Q_GROUP_BYTES,
-                                        &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
+                            for (int c = 0; c < Lay::DCH; ++c)
+                                tma_load_3d(smem + Lay::OFF_Q + qs * Lay::Q_BYTES + c * Lay::Q_GROUP_BYTES,
+                                            &map_q, bars + Lay::B_QFULL + qs, c * 64, 0, sg.u, pol);
+                        }
+                        n_q = k + 1;
                     }
                     __syncwarp();
                 }
@@ -263,6 +269,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                                 tma_load_3d(dst + c * Lay::GROUP_BYTES + t_row * 128, tree_map, full0 + pos.slot, c * 64, 0, ui.lbh, pol);
                         }
                         __syncwarp();
+                        n_tiles = g + 1;
                     }
                     pos.advance();
                     z = z_next;
@@ -271,9 +278,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             if (is_v) paged_status_warp(p, lane);
             if (*abort_flag) {
                 // let every copy already issued land before the CTA can exit
-                for (int i = max(0, g - Lay::KS); i < g; ++i) mbar_wait_drain(full0 + i % Lay::KS, (i / Lay::KS) & 1);
+                for (int i = max(0, n_tiles - Lay::KS); i < n_tiles; ++i)
+                    mbar_wait_drain(full0 + i % Lay::KS, (i / Lay::KS) & 1);
                 if (!is_v)
-                    for (int i = max(0, k - Lay::QS); i < k; ++i)
+                    for (int i = max(0, n_q - Lay::QS); i < n_q; ++i)
                         mbar_wait_drain(bars + Lay::B_QFULL + i % Lay::QS, (i / Lay::QS) & 1);
             }
         }

@@ -58,7 +58,8 @@
 // The sharing of units among CTAs, the fused step's side warp and the merges of
 // partial states are those of the kernel for trees of up to 64 tokens
 // (ppd_attention_key.cuh).  Warp roles (384 threads): warps 0-7 softmax, 8 TMA producer,
-// 9 and 10 the streams' MMA issuers (9 owns TMEM), 11 the fused step's side work.
+// 9 and 10 the streams' MMA issuers (9 owns TMEM), 11 the fused step's side work (with a cache in
+// pages a second TMA producer, then the statuses).
 #pragma once
 
 #include "ppd_attention_common.cuh"
@@ -312,27 +313,35 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
     const uint32_t tmem_base = *tmem_ptr;
     const WorkRange &wr = *wr_s;
 
-    if (warp == 11) {
+    if (!PAGED && warp == 11) {
         // ------------------------------------------------------------ fused-step side work
-        if constexpr (PAGED) {
-            paged_status_warp(p, lane);
-        } else {
+        if constexpr (!PAGED) {
             if (p.fused) fused_side_warp<false>(p, wr, lane, abort_flag);
             else if (p.set_status) status_warp(p, lane);
             if (p.late_wait) pdl_wait();
         }
-    } else if (PAGED && warp == 8) {
+    } else if (PAGED && (warp == 8 || warp == 11)) {
         if constexpr (PAGED) {
-            // -------------------------------------------------------- TMA producer, page by page
-            // the whole warp walks the tiles, a lane looks up a box's page, one elected lane copies
+            // -------------------------------------------------------- TMA producers, page by page
+            // two warps, as a copy of a small page takes its issuer some 45 ns, each with every other
+            // slot of the ring (30 requests of 5000 rows, 64 tokens, 8 heads of 2: pages of 8 110.3 ->
+            // 95.0 us, of 16 95.3 -> 92.8; with D = 64, of 16 72.7 -> 60.7); a whole warp walks the
+            // tiles, a lane looks up a box's page, one elected lane copies
+            const int mine = warp == 11;
             const uint64_t pol = p.n_qb > 2 ? l2_policy_evict_normal() : l2_policy_evict_first();
             Pos pos;
-            int n_tiles = 0, n_q0 = 0, n_q1 = 0;   // copies issued: ring tiles, Q blocks per slot
+            int n_tiles = 0, n_mine = 0;           // ring tiles met, by both warps; those up to this one's last copy
+            int n_q0 = 0, n_q1 = 0;                // copies of Q issued, a slot
             struct Tile {
                 int row, lbh, P, depth;   // first key, slice, keys below this; this lane's page
                 bool tree;
             };
             auto load = [&](const CUtensorMap *pages, const CUtensorMap *tree_map, const Tile &t) {
+                ++n_tiles;
+                if ((pos.slot & 1) != mine) {
+                    pos.advance();
+                    return;
+                }
                 mbar_wait(bars + Lay::B_EMPTY + pos.slot, pos.phase ^ 1u, abort_flag);
                 if (!warp_uniform(*abort_flag)) {
                     uint64_t *full = bars + Lay::B_FULL + pos.slot;
@@ -346,11 +355,12 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                             tma_load_3d(dst + c * Lay::GROUP_BYTES, tree_map, full, c * 64, t.row, t.lbh, pol);
                     }
                     __syncwarp();
-                    ++n_tiles;
+                    n_mine = n_tiles;
                 }
                 pos.advance();
             };
             auto load_q = [&](int qs, uint32_t parity, int qb, int lbh) {
+                if (mine) return;
                 mbar_wait(bars + Lay::B_QEMPTY + qs, parity ^ 1u, abort_flag);
                 if (!warp_uniform(*abort_flag)) {
                     if (lane == 0) {
@@ -399,10 +409,11 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             }
             if (!it.pair)
                 for (int e = max(0, g - 2); e < g; ++e) load(&map_vc, &map_vt, e & 1 ? v1 : v0);
+            if (mine) paged_status_warp(p, lane);
             if (*abort_flag) {
                 // let every copy already issued land before the CTA can exit
-                for (int i = max(0, n_tiles - Lay::RS); i < n_tiles; ++i)
-                    mbar_wait_drain(bars + Lay::B_FULL + i % Lay::RS, (i / Lay::RS) & 1);
+                for (int i = max(0, n_mine - Lay::RS); i < n_mine; ++i)
+                    if ((i % Lay::RS & 1) == mine) mbar_wait_drain(bars + Lay::B_FULL + i % Lay::RS, (i / Lay::RS) & 1);
                 if (n_q0 > 0) mbar_wait_drain(bars + Lay::B_QFULL + 0, (n_q0 - 1) & 1);
                 if (n_q1 > 0) mbar_wait_drain(bars + Lay::B_QFULL + 1, (n_q1 - 1) & 1);
             }

@@ -5,7 +5,7 @@
 // table[b][r / page] in every layer.  The pool's tensor map has a (layer, page, head) as its
 // depth, so a tile is 128 / page boxes of page rows at depths that the table gives (one box where
 // a page holds 128 rows or more).  Boxes start on multiples of eight rows of 128 bytes, so that
-// the swizzled tile is the one that a contiguous cache gives.  A lane of the producer's warp
+// the swizzled tile is the one that a contiguous cache gives.  A lane of a producer's warp
 // looks up a box's page: 8-row pages take 16 of them.
 //
 // A table entry that names no page reads as zeros (a coordinate past the tensor's end), and the
@@ -59,10 +59,9 @@ PPD_DEV int page_coord(const PagedParams &p, const PageUnit &u, int row, int P, 
 }
 
 // The tile itself, by a converged warp: every box that holds a key below P (`more`: bytes that the
-// caller copies besides).  One elected lane
-// issues the copies of all of them, from warp-uniform code: lanes that each copied a box took 115 cycles
-// a box, one after the other (48 requests of up to 8192 rows in pages of 16: 224 us, in pages of
-// 64 177 us).
+// caller copies besides).  One elected lane issues the copies of all of them, from warp-uniform code: lanes
+// that each copied a box took 115 cycles a box, one after the other (with one producer, 48 requests of up to
+// 8192 rows in pages of 16: 224 -> 180 us).
 template <int DCH>
 PPD_DEV void load_page_tile(const PagedParams &p, const CUtensorMap *map, uint8_t *dst, uint32_t group_bytes, uint64_t *full,
                             int depth, int row, int P, uint64_t policy, uint32_t more = 0)
