@@ -1313,10 +1313,11 @@ struct PagedWs {
 // 32: a tile of 128 queries 1.09, or 1.47 where every SM streams keys of its own, of a pair of blocks
 // 2.05; whole jobs' ends 6, a cluster's 12, and the work split's 24 (two jobs a CTA, 130 KB of
 // partial state each, and the merge).  Whole / clusters / shared out, heads of 64 tokens:
-//   16 slices, 4 heads, 3001 rows    32.6 /  19.6 /  32.6     96 of 4, ragged to 5001   82.4 /      /  67.7
-//   8 of 4, 20,001                    169 /  41.2 /  42.0     64 of 8                   84.2 /      /  90.5
-//   40 of 2, 4001                    40.2 /  22.6 /  29.7     80 of 8                    119 /      /  98.7
-// (units of the work split: pairs of blocks; single ones took 5, 10 and 20 us longer in the last column's cases).
+//   16 slices, 4 heads, 3001 rows    30.5 /  18.9 /  30.0     96 of 4, ragged to 5001   82.2 /      /  64.3
+//   8 of 4, 20,001                    149 /  37.3 /  43.2     64 of 4                   46.2 /      /  52.1
+//   40 of 2, 4001                    37.5 /  21.3 /  27.6     80 of 4                   82.5 /      /  58.0
+// (units of the work split: pairs of blocks; single ones took 5, 10 and 20 us longer on 96 slices of 4 heads,
+// 64 and 80 of 8).
 static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, bool workspace)
 {
     const long long sms = split_grid(), blocks = (w.rows + 127) / 128, pairs = (blocks + 1) / 2;
@@ -1349,9 +1350,9 @@ static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, 
 // pages of 16, the tables' capacity standing in for the lengths): a tile 1.09, or its share of HBM where
 // many SMs stream; ends 5.6, of the work split 12 and a fifth for each part of a slice past eight.  Lengths
 // of several requests are taken to average 0.8 of the longest.  Clusters / shared out:
-//   2 slices of 6000 rows   12.2 / 18.8    8 of 16,000   24.3 / 23.6     32 of 6000    20.0 / 22.5
-//   2 of 64,000             74.3 / 35.5    8 of 64,000   78.5 / 50.3     32 of 20,000  52.7 / 47.1
-//   8 of 2000                9.2 / 13.8    16 of 6000    15.8 / 19.4     96 of 6000 (whole)  58.5 / 44.4
+//   2 slices of 6000 rows   10.6 / 26.9    8 of 16,000   19.7 / 22.4     32 of 6000    17.0 / 20.9
+//   2 of 64,000             53.8 / 35.0    8 of 64,000   63.6 / 49.8     32 of 20,000  47.8 / 45.2
+//   8 of 2000                8.8 / 15.4    16 of 6000    14.0 / 19.2     96 of 6000 (whole)  48.7 / 42.5
 static AttnPlan plan_paged_key(long long slices, long long t_u, int B, bool may_split)
 {
     const double sms = split_grid(), hbm = 1.47;
@@ -1382,9 +1383,10 @@ static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_m
         w.n_qb = 1;
         const bool may_split = workspace && B <= ppd::kSplitMaxB && slices * t_u <= 2147483647ll;
         w.plan = slices < sms ? plan_paged_key(slices, t_u, B, may_split) : AttnPlan{0, 1};
-        // (a last, partial round of whole units weighs more here than in plan_attention: requests' lengths are
-        // seldom alike.  160 slices of up to 4000 rows: whole 49.5 us, shared out 45.0; of 2000 29.7 and 30.1)
-        if (may_split && slices >= sms && (slices * t_u + sms - 1) / sms + 10 < (slices + sms - 1) / sms * t_u) w.plan = {1, 1};
+        // (whole units take the longest first; what their last, partial round costs over a share for every SM
+        // has to pay for the work split's merge.  160 slices of up to 4000 rows: whole 44.8 us, shared out 42.9;
+        // of 2000 25.5 and 27.7)
+        if (may_split && slices >= sms && (slices * t_u + sms - 1) / sms + 20 < (slices + sms - 1) / sms * t_u) w.plan = {1, 1};
     }
     size_t off = dt == PPD_F32 ? align_up((size_t)slices * (w.rows + 2 * (size_t)T) * D * 2) : 0;
     if (w.plan.split) {
