@@ -227,6 +227,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
             uint64_t *full0 = bars + (is_v ? Lay::B_VFULL : Lay::B_KFULL), *empty0 = bars + (is_v ? Lay::B_VEMPTY : Lay::B_KEMPTY);
             uint8_t *ring = smem + (is_v ? Lay::OFF_V : Lay::OFF_K);
             static_assert(Lay::KS == Lay::VS, "one walk for both rings");
+            if (is_v) paged_status_none(p, lane);
             const uint64_t pol = l2_policy_evict_first();
             const uint32_t tree_bytes = (uint32_t)tree_box_rows(T) * 128u * Lay::DCH;
             KPos pos;

@@ -328,6 +328,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             // 95.0 us, of 16 95.3 -> 92.8; with D = 64, of 16 72.7 -> 60.7); a whole warp walks the
             // tiles, a lane looks up a box's page, one elected lane copies
             const int mine = warp == 11;
+            if (mine) paged_status_none(p, lane);
             const uint64_t pol = p.n_qb > 2 ? l2_policy_evict_normal() : l2_policy_evict_first();
             Pos pos;
             int n_tiles = 0, n_mine = 0;           // ring tiles met, by both warps; those up to this one's last copy

@@ -104,8 +104,15 @@ PPD_DEV void prefetch_pages(const PagedParams &p, int lane, const CUtensorMap *k
     }
 }
 
-// The statuses, by one spare warp a CTA: sequence b by CTA b mod grid.  A malformed tree, then a
-// prefix outside the table, or an entry of it that names no page.
+// The statuses, by one warp a CTA, sequence b by CTA b mod grid: none yet, before its copies; after them a
+// malformed tree, then a prefix outside the table, or an entry of it that names no page.  (By a maximum: the
+// status of a wait that ran out meanwhile, in any CTA, is the largest, and stays.)
+PPD_DEV void paged_status_none(const PagedParams &p, int lane)
+{
+    for (int b = blockIdx.x + lane * gridDim.x; b < p.B; b += 32 * gridDim.x) p.dev_status[b] = kOk;
+    __syncwarp();
+}
+
 PPD_DEV void paged_status_warp(const PagedParams &p, int lane)
 {
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
@@ -124,7 +131,7 @@ PPD_DEV void paged_status_warp(const PagedParams &p, int lane)
         }
         bad = __any_sync(0xffffffffu, bad);
         gap = __any_sync(0xffffffffu, gap);
-        if (lane == 0) p.dev_status[b] = bad ? kErrTree : (out || gap ? kErrCapacity : kOk);
+        if (lane == 0 && (bad || out || gap)) atomicMax(p.dev_status + b, (int)(bad ? kErrTree : kErrCapacity));
     }
 }
 
