@@ -10,7 +10,7 @@
 // one is worked on.
 //
 // Bound: instructions, then HBM.  With a key made of every entry and sums one entry at a time, 2048 rows
-// of 128,256 bf16 logits took 885 us; 133 now (20 alternatives; 93 without, 77 their bytes alone).
+// of 128,256 bf16 logits took 885 us; 132 now (20 alternatives; 93 without, 77 their bytes alone).
 // A batch's maximum propagates NaN and says whether anything of it may be among the best; bf16 entries
 // are compared, clamped and maximised two at a time, sums take two fp32 operations an instruction;
 // entries are compared with the token as numbers, in columns before it with the next number below it
@@ -29,6 +29,7 @@
 
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 namespace ppd {
 
@@ -101,17 +102,21 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
     constexpr int E = BF16 ? 8 : 4;            // entries of a load
     constexpr int NV = E * kLogLoads;          // of a batch and thread
     constexpr int WARPS = THREADS / 32;
-    constexpr int kMaxPush = kLogMaxK * NV;
     constexpr int eb = BF16 ? 2 : 4;
     constexpr uint32_t kAbsent = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
-    static_assert(kLogMaxK <= THREADS && kLogMaxK * kMaxCluster <= kMaxPush, "lists");
-    __shared__ uint4 s_batch[STAGES][kLogLoads][THREADS];   // a thread reads what it asked for itself
-    __shared__ unsigned long long s_push[kMaxPush], s_list[2][kLogMaxK], s_bound;
-    __shared__ __align__(16) unsigned long long s_best[THREADS];
+    // An entry of a batch among its others: of bf16 the key's upper half (the lower says nothing) and
+    // the column's place from the end, half the instructions of 64 bits.
+    using Best = std::conditional_t<BF16, uint32_t, unsigned long long>;
+    static_assert(kLogMaxK <= THREADS && kMaxCluster <= NV && kLogLoads * THREADS * E <= 65536, "lists");
+    extern __shared__ uint4 s_dyn[];
+    auto s_batch = reinterpret_cast<uint4 (*)[kLogLoads][THREADS]>(s_dyn);   // [STAGES]; a thread reads what it asked for itself
+    auto s_push = reinterpret_cast<unsigned long long *>(s_batch + STAGES);   // [K NV]: K threads' entries, or a cluster's lists
+    __shared__ unsigned long long s_list[2][kLogMaxK], s_bound;
+    __shared__ __align__(16) Best s_best[THREADS];
     __shared__ RowStats s_stats[WARPS], s_cta;
     __shared__ int s_n, s_over;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, V = p.V;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, V = p.V, max_push = K * NV;
     const int rank = (int)blockIdx.x % p.cluster;
     const int item = (int)blockIdx.x / p.cluster;
     const int b = item / p.n, i = item - b * p.n;
@@ -394,9 +399,9 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
             bound = full ? (unsigned long long)(rank_key(least) + 1) << 32 : 1;
             if (bounded) {
                 // this thread's best entry: the first of the batch's largest
-                unsigned long long gm = 0;
+                Best gm = 0;
+                int at = 0;
                 if (sees) {
-                    int at = 0;
                     if (mb > -INFINITY) {
                         const __nv_bfloat162 mb2 = __bfloat162bfloat162(__float2bfloat16_rn(mb));
                         const uint32_t same = bits([&](__nv_bfloat162 v) { return __heq2_mask(v, mb2); }, [&](float v) { return v == mb; });
@@ -407,18 +412,27 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
                     } else {   // only -inf: the first entry that there is
                         while (at < NV && !live(at / E, at % E)) ++at;
                     }
-                    if (at < NV) gm = rank_entry(rank_key(mb), (int)column(at / E, at % E));
+                    if (at < NV) {
+                        if constexpr (BF16) gm = (rank_key(mb) & 0xFFFF0000u) | (0xFFFFu - (at / E * THREADS + tid) * E - at % E);
+                        else gm = rank_entry(rank_key(mb), (int)column(at / E, at % E));
+                    }
                 }
                 s_best[tid] = gm;
                 if (tid == 0) s_bound = 0;
                 __syncthreads();
                 int place = 0;
 #pragma unroll 8
-                for (int y = 0; y < THREADS; y += 2) {
-                    const ulonglong2 z = *reinterpret_cast<const ulonglong2 *>(s_best + y);
-                    place += (z.x > gm) + (z.y > gm);
+                for (int y = 0; y < THREADS; y += 16 / (int)sizeof(Best)) {
+                    if constexpr (BF16) {
+                        const uint4 z = *reinterpret_cast<const uint4 *>(s_best + y);
+                        place += (z.x > gm) + (z.y > gm) + (z.z > gm) + (z.w > gm);
+                    } else {
+                        const ulonglong2 z = *reinterpret_cast<const ulonglong2 *>(s_best + y);
+                        place += (z.x > gm) + (z.y > gm);
+                    }
                 }
-                if (gm != 0 && place == K - 1) s_bound = gm;   // (fewer than K threads: no bound)
+                if (gm != 0 && place == K - 1)   // (fewer than K threads: no bound)
+                    s_bound = rank_entry(rank_key(mb), (int)column(at / E, at % E));
                 __syncthreads();
                 bound = s_bound > bound ? s_bound : bound;
             }
@@ -433,7 +447,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
                 const unsigned long long en = rank_entry(rank_key(stored(at)), (int)column(at / E, at % E));
                 if (!plain && (en < bound || !live(at / E, at % E))) continue;
                 const int place = atomicAdd(&s_n, 1);
-                if (place < kMaxPush) s_push[place] = en;
+                if (place < max_push) s_push[place] = en;
                 else s_over = 1;   // (not where the batch has a bound)
             }
         }
@@ -530,28 +544,49 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
     if (p.cluster > 1) cluster_sync();   // no list that a peer reads goes away
 }
 
+// Threads of a block where rows are many: with fewer, barriers cost less and as many rows as there are find
+// room at once (an SM takes 8, 16 or 32 blocks, by registers), but a warp has more of a long row and of a
+// ranking to itself.  128 / 64 / 32, us:
+//   rows                 of           alternatives: 5               20                   32
+//   14,400 (95 an SM)    1000 fp32    121 /  65 /  42       128 /  71 /  56      134 /  76 / 108
+//   6000 (39)            32,000 bf16  136 / 112 /  99       154 / 133 / 131      166 / 157 / 204
+//   4000 (26)            16,000 bf16   69 /  54 /  47        77 /  64 /  68       83 /  80 / 108
+//   3000 (20)            32,000 bf16   72 /  62 /  69        81 /  74 /  76       88 /  88 / 147
+//   2000 (13)            32,000 bf16   50 /  46 /  44        57 /  54 /  70       62 /  70 /  87
+//   1500 (10)            32,000 bf16   40 /  43 /  38        46 /  50 /  51       50 /  51 /  84
+//   1400 (9)             4000 bf16     17 /  16 /  13        19 /  18 /  17       19 /  18 /  41
+//   4000 (26)            128,256 bf16 212 / 205 / 222       239 / 234 / 265      258 / 270 / 319
+//   2048 (13)            128,256 bf16 117 / 123 / 129       132 / 136 / 187      142 / 166 / 189
+static int log_threads(long long rows_a_sm, int K, long long row_bytes)
+{
+    if (K <= 20 && (row_bytes <= 8192 || (rows_a_sm >= 32 && row_bytes <= 65536))) return 32;
+    if (rows_a_sm >= 16 || (rows_a_sm >= 12 && K <= 20 && row_bytes <= 131072)) return 64;
+    return 128;
+}
+
 cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t stream)
 {
     // CTAs of a row: as many as are all resident at once with four stages (five an SM), none for
     // less than a batch.  1 / 2 / 4 / 8 of them, us, 20 alternatives:
     //   150 rows of 128,256 fp32   47 / 34 / 33 / 43        320 of 256,000 bf16    67 / 58 / 64 / 80
     //   16 rows of 128,256 fp32    47 / 31 / 22 / 19        2000 of 32,000 bf16    59 / 78 / 115 / 210
-    // Four stages, 35 to 43 KB, where no more than those run (700 rows of 256,000 bf16: 93 us, with two
+    // Four stages, 33 to 43 KB, where no more than those run (700 rows of 256,000 bf16: 93 us, with two
     // stages 122); else two, so that eight CTAs find room (2048 rows of 128,256 bf16: 133 us, with
-    // four 162).
+    // four 162), or more of fewer threads.
     const long long items = (long long)p.B * p.n;
     const int batch = 128 * kLogLoads * (p.bf16 ? 8 : 4);
     p.cluster = 1;
     while (p.cluster < kMaxCluster && items * p.cluster * 2 <= 5ll * num_sms && p.V > p.cluster * batch) p.cluster *= 2;
     const bool deep = items * p.cluster <= 5ll * num_sms;
-    // Many rows of up to 32 KB with few alternatives by single warps: their barriers cost nothing, and more of
-    // them find room.  128 threads / 32, us:
-    //   14,400 rows of 1000 fp32, 5 alternatives   119 / 44       of 8000, 5   190 / 118      of 4000, 32   177 / 182
-    //   4000 rows of 16,000 bf16, 5                 72 / 53       1000 of 32,000 bf16, 5   31 / 34
-    const bool warps = !deep && p.K <= 8 && (long long)p.V * (p.bf16 ? 2 : 4) <= 32768;
-    auto *kern = p.bf16 ? (warps ? token_logprobs_kernel<true, 32, 2> : deep ? token_logprobs_kernel<true, 128, 4> : token_logprobs_kernel<true, 128, 2>)
-                        : (warps ? token_logprobs_kernel<false, 32, 2> : deep ? token_logprobs_kernel<false, 128, 4> : token_logprobs_kernel<false, 128, 2>);
-    return launch_chained(kern, dim3((unsigned)(items * p.cluster)), dim3(warps ? 32 : 128), dim3((unsigned)p.cluster), stream, p);
+    const int threads = deep ? 128 : log_threads(items / num_sms, p.K, (long long)p.V * (p.bf16 ? 2 : 4));
+    auto launch = [&](auto kern, int stages) {
+        const uint32_t smem = (uint32_t)(stages * kLogLoads * threads * 16 + p.K * kLogLoads * (p.bf16 ? 8 : 4) * 8);
+        return launch_chained_smem(kern, dim3((unsigned)(items * p.cluster)), dim3((unsigned)threads), dim3((unsigned)p.cluster), smem, stream, p);
+    };
+    if (deep) return p.bf16 ? launch(token_logprobs_kernel<true, 128, 4>, 4) : launch(token_logprobs_kernel<false, 128, 4>, 4);
+    if (threads == 128) return p.bf16 ? launch(token_logprobs_kernel<true, 128, 2>, 2) : launch(token_logprobs_kernel<false, 128, 2>, 2);
+    if (threads == 64) return p.bf16 ? launch(token_logprobs_kernel<true, 64, 2>, 2) : launch(token_logprobs_kernel<false, 64, 2>, 2);
+    return p.bf16 ? launch(token_logprobs_kernel<true, 32, 2>, 2) : launch(token_logprobs_kernel<false, 32, 2>, 2);
 }
 
 }  // namespace ppd

@@ -232,3 +232,28 @@ def test_ties_infinities_and_nan_in_many_rows(cuda_device, V):
     check_items(r, logits, tokens, 0.9, None, [(0, i) for i in range(T)])
     for k in ("logprob", "entropy", "rank", "top", "best"):
         assert torch.equal(torch.nan_to_num(r[k].float())[0, :T], torch.nan_to_num(r[k].float())[0, -T:]), k
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V,K", [(2600, 5001, 0), (2600, 5001, 20), (2600, 5001, 32), (2000, 5001, 5), (2000, 5001, 21), (5200, 5001, 20), (5200, 301, 32), (1000, 2048, 20),
+                                   (1000, 4097, 20)])
+def test_blocks_of_every_size(cuda_device, n, V, K, dtype):
+    """Rows by blocks of every size, batches of every size ending inside them; the hard rows among plain ones."""
+    from paper_2405_18628_gb300 import ppd
+    g = torch.Generator(device=cuda_device)
+    g.manual_seed(V + K)
+    hard = torch.stack(list(_hard_rows(V, cuda_device).values()))
+    logits = (3 * torch.randn(n, V, device=cuda_device, generator=g)).to(dtype)
+    h = len(hard)
+    logits[:h] = logits[n - h:] = hard.to(dtype)
+    logits, tokens = logits[None], torch.randint(0, V, (1, n), device=cuda_device, generator=g).int()
+    tokens[0, n - h:] = tokens[0, :h]
+    r = call(ppd, logits, tokens, 0.8, K=K)
+    check_items(r, logits, tokens, 0.8, None, [(0, i) for i in [*range(h), h, n // 2, n - h - 1]])
+    for k in set(r) - {"status"}:
+        assert torch.equal(torch.nan_to_num(r[k].float())[0, :h], torch.nan_to_num(r[k].float())[0, n - h:]), k
+    x, t = logits.float()[:, h:n - h], tokens[:, h:n - h].long()[..., None]
+    if K:
+        assert torch.equal(r["top"][:, h:n - h].long(), torch.sort(x, dim=-1, descending=True, stable=True).indices[..., :K])
+    xt = x.gather(2, t)
+    assert torch.equal(r["rank"][:, h:n - h].long(), ((x > xt) | ((x == xt) & (torch.arange(V, device=cuda_device) < t))).sum(-1))
