@@ -647,7 +647,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
                 const bool masked = tree || n_valid < Lay::KT;
                 const int sb = g & 1;
                 const int ps = g & 1;
-                if (first && new_tree) {
+                if (PAGED && T == 1) {
+                    // (a token alone: the same for every query)
+                    if (first) dbits = t == tail ? 0xffffffffu : 0u;
+                } else if (first && new_tree) {
                     // ancestor sets by shuffles: lane c walks up from query q0 + c, then every
                     // lane collects its key's bit of each set
                     uint64_t anc = 0;
@@ -713,8 +716,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q,
 #pragma unroll
                         for (int c = 0; c < Lay::DCH; ++c)
 #pragma unroll
-                            for (int x = 0; x < 8; ++x)
-                                st_shared_v4(vrow + c * Lay::GROUP_BYTES + x * 16, 0u, 0u, 0u, 0u);
+                            for (int x = 0; x < 8; ++x)   // (eight rows' chunks in different banks)
+                                st_shared_v4(vrow + c * Lay::GROUP_BYTES + ((x ^ (t & 7)) << 4), 0u, 0u, 0u, 0u);
                     }
                 }
                 kp.advance();

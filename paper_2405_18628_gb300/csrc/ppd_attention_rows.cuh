@@ -1019,7 +1019,7 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
                             for (int c = 0; c < Lay::DCH; ++c)
 #pragma unroll
                                 for (int x = 0; x < 8; ++x)
-                                    st_shared_v4(vrow + c * Lay::GROUP_BYTES + x * 16, 0u, 0u, 0u, 0u);
+                                    st_shared_v4(vrow + c * Lay::GROUP_BYTES + ((x ^ (q & 7)) << 4), 0u, 0u, 0u, 0u);
                         }
                         fence_proxy_async_smem();
                     }
