@@ -804,12 +804,17 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
         auto store32 = [&](auto *dst, const uint32_t (&r)[32], float scale) {
             if constexpr (!std::is_same<decltype(dst), float *>::value) {   // bf16, 16-byte aligned rows
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint32_t w[4];
+                for (int e = 0; e < 32; e += 16) {
+                    uint32_t w[8];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
+                    for (int x = 0; x < 8; ++x)
                         w[x] = pack_bf16(__uint_as_float(r[e + 2 * x]) * scale, __uint_as_float(r[e + 2 * x + 1]) * scale);
-                    *reinterpret_cast<uint4 *>(dst + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (out32) {   // (a thread's stores lie in rows of their own: whole sectors)
+                        st_global_v8(dst + e, w);
+                    } else {
+                        *reinterpret_cast<uint4 *>(dst + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(dst + e + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
                 }
             } else if (PAGED || out32) {   // (partial states are aligned)
 #pragma unroll

@@ -211,6 +211,13 @@ PPD_DEV void st_global_v8(float *dst, const uint32_t *v, float scale)
                  : "memory");
 }
 
+PPD_DEV void st_global_v8(void *dst, const uint32_t (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
 // ---------------------------------------------------------------- clusters
 
 // Barrier over every thread of the cluster: what a thread wrote (to its own

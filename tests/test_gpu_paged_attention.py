@@ -310,3 +310,16 @@ def test_trees_behind_the_last_rows(cuda_device, page, T, G):
         c = Case(cuda_device, 1, len(lens), H, G, 128, T, lens, page, spare=spare, seed=T + page)
         c.run(ppd)
         c.check(seqs=range(0, len(lens), 1 if H < 3 else 7))
+
+
+@pytest.mark.parametrize("D,T,G,lens", [(128, 70, 1, [130, 5]), (64, 40, 4, [300, 0]), (128, 1, 4, [77, 200]), (64, 300, 1, [20, 140])])
+def test_outputs_on_16_bytes(cuda_device, D, T, G, lens):
+    """Outputs that begin between two sectors of 32 bytes."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 1, 2, 2, G, D, T, lens, 16, seed=T)
+    n = c.out.numel()
+    flat = torch.full((n + 16,), 3.0, dtype=torch.bfloat16, device=cuda_device)
+    c.out = flat[8:8 + n].view(c.out.shape)
+    c.run(ppd)
+    c.check()
+    assert (flat[:8] == 3).all() and (flat[8 + n:] == 3).all()
