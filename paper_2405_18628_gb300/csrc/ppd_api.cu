@@ -1347,25 +1347,29 @@ static void plan_paged_rows(PagedWs &w, long long slices, long long t_u, int B, 
 }
 
 // Slices of up to 64 rows, fewer than SMs, by the time that each way takes, in microseconds (D = 128,
-// pages of 16, the tables' capacity standing in for the lengths): a tile 1.09, or its share of HBM where
-// many SMs stream; ends 5.6, of the work split 12 and a fifth for each part of a slice past eight.  Lengths
-// of several requests are taken to average 0.8 of the longest.  Clusters / shared out:
-//   2 slices of 6000 rows   10.6 / 26.9    8 of 16,000   19.7 / 22.4     32 of 6000    17.0 / 20.9
-//   2 of 64,000             53.8 / 35.0    8 of 64,000   63.6 / 49.8     32 of 20,000  47.8 / 45.2
-//   8 of 2000                8.8 / 15.4    16 of 6000    14.0 / 19.2     96 of 6000 (whole)  48.7 / 42.5
-static AttnPlan plan_paged_key(long long slices, long long t_u, int B, bool may_split)
+// pages of 16, the tables' capacity standing in for the lengths): a tile 0.62 and more the more SMs stream; ends
+// 6.2, of the work split 12.5 and 0.8 for each round of the merge's loads past one and a half.  Lengths
+// of several requests are taken to average 0.8 of the longest.  Clusters / shared out (4 query rows):
+//   2 slices of 6000 rows   10.4 / 13.3    8 of 6000     12 / 15.9       32 of 6000    17.0 / 20.4
+//   2 of 10,000             12.9 / 17.0    8 of 16,000   19.5 / 19.5     32 of 20,000  47.6 / 46.0
+//   2 of 16,000             17.0 / 16.6    8 of 64,000   64.2 / 47.2     56 of 6000    28.4 / 27.6
+//   2 of 64,000             55.0 / 23.2    16 of 6000    13.3 / 17.0     96 of 6000 (whole)  48.5 / 42.9
+static AttnPlan plan_paged_key(long long slices, long long t_u, int B, int rows, int D, bool may_split)
 {
-    const double sms = split_grid(), hbm = 1.47;
+    const long long sms = split_grid();
+    auto tile = [](long long ctas) { return 0.62 + 0.0045 * (double)ctas; };
     AttnPlan plan{0, 1};
-    double best = 1.09 * t_u + 5.6;
-    for (int c = 2; c <= ppd::kMaxCluster && c <= t_u && slices * c <= split_grid(); ++c) {
-        const double cost = std::max(1.09, hbm * slices * c / sms) * ((t_u + c - 1) / c) + 5.6;
+    double best = tile(slices) * (double)t_u + 6.2;
+    for (int c = 2; c <= ppd::kMaxCluster && c <= t_u && slices * c <= sms; ++c) {
+        const double cost = tile(slices * c) * (double)((t_u + c - 1) / c) + 6.2;
         if (cost < best && slices <= ppd::max_attention_clusters(c)) {
             best = cost;
             plan.cluster = c;
         }
     }
-    const double shared = hbm * (B > 1 ? 0.8 : 1.0) * slices * t_u / sms + 12 + 0.2 * std::max(0.0, sms / slices - 8);
+    const int ways = ppd::paged_merge_ways(ppd::paged_merge_threads(rows, slices, (int)sms), rows, D);
+    const double trips = (double)sms / (double)slices / 4 / ways;   // of the merge's loads
+    const double shared = 1.35 * (B > 1 ? 0.8 : 1.0) * (double)((slices * t_u + sms - 1) / sms) + 12.5 + 0.8 * std::max(0.0, trips - 1.5);
     if (may_split && shared < best) plan = {1, 1};
     return plan;
 }
@@ -1382,7 +1386,7 @@ static PagedWs paged_workspace(int L, int B, int H, int G, int T, int D, int S_m
     } else {
         w.n_qb = 1;
         const bool may_split = workspace && B <= ppd::kSplitMaxB && slices * t_u <= 2147483647ll;
-        w.plan = slices < sms ? plan_paged_key(slices, t_u, B, may_split) : AttnPlan{0, 1};
+        w.plan = slices < sms ? plan_paged_key(slices, t_u, B, w.rows, D, may_split) : AttnPlan{0, 1};
         // (whole units take the longest first; what their last, partial round costs over a share for every SM
         // has to pay for the work split's merge.  160 slices of up to 4000 rows: whole 44.8 us, shared out 42.9;
         // of 2000 25.5 and 27.7)

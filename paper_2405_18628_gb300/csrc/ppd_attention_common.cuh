@@ -353,24 +353,25 @@ PPD_DEV size_t split_slot_floats(int D, int rows = kSplitRows) { return (size_t)
 // weighted sum of the parts' O rows over the weighted sum of their row sums.
 // The parts are read PB at a time, every load of a batch issued before any
 // is used, so a batch costs one round trip to L2.
-template <class Out, int kRows = kSplitRows, int PB = 8>
-static __device__ __forceinline__ void split_merge_chunk(const float *split_part, Out *out, float *lse,
-                                                         const SplitParts &sp, long long N, int G,
-                                                         size_t out_row0, int r, int c0, int D)
+struct MergeState {
+    float M = -INFINITY, Ls = 0.f, acc[8] = {};
+};
+// The parts from c_a to c_b of sp's.
+template <int kRows, int PB>
+static __device__ __forceinline__ MergeState split_merge_parts(const float *split_part, const SplitParts &sp, int c_a, int c_b,
+                                                               long long N, int G, int r, int c0, int D)
 {
     const size_t sf = split_slot_floats(D, kRows);
     const bool dense = N >= G;   // no empty ranges
-    float M = -INFINITY, Ls = 0.f;
-    float acc[8];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) acc[x] = 0.f;
-    for (int cb = sp.c_a; cb <= sp.c_b; cb += PB) {
+    MergeState st;
+    float &M = st.M, &Ls = st.Ls, (&acc)[8] = st.acc;
+    for (int cb = c_a; cb <= c_b; cb += PB) {
         float mc[PB], lc[PB];
         float4 v[PB][2];
 #pragma unroll
         for (int y = 0; y < PB; ++y) {
             const int c = cb + y;
-            const bool live = c <= sp.c_b && (dense || split_nonempty(c, N, G));
+            const bool live = c <= c_b && (dense || split_nonempty(c, N, G));
             const float *b_ = split_part + (size_t)split_slot(sp, live ? c : sp.c_a) * sf;
             mc[y] = live ? __ldcg(b_ + (size_t)kRows * D + r) : -INFINITY;
             lc[y] = live ? __ldcg(b_ + (size_t)kRows * D + kRows + r) : 0.f;
@@ -395,7 +396,14 @@ static __device__ __forceinline__ void split_merge_chunk(const float *split_part
             M = Mn;
         }
     }
-    const float inv = 1.f / Ls;
+    return st;
+}
+
+template <class Out>
+static __device__ __forceinline__ void split_merge_store(const MergeState &st, Out *out, float *lse, size_t out_row0, int r, int c0, int D)
+{
+    const float (&acc)[8] = st.acc;
+    const float inv = 1.f / st.Ls;
     Out *dst = out + (out_row0 + r) * D + c0;
     if constexpr (!std::is_same<Out, float>::value) {   // bf16, 16-byte aligned rows
         *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv),
@@ -407,7 +415,15 @@ static __device__ __forceinline__ void split_merge_chunk(const float *split_part
 #pragma unroll
         for (int x = 0; x < 8; ++x) dst[x] = acc[x] * inv;
     }
-    if (c0 == 0 && lse) lse[out_row0 + r] = (M + lg2(Ls)) * 0.69314718055994530942f;
+    if (c0 == 0 && lse) lse[out_row0 + r] = (st.M + lg2(st.Ls)) * 0.69314718055994530942f;
+}
+
+template <class Out, int kRows = kSplitRows, int PB = 8>
+static __device__ __forceinline__ void split_merge_chunk(const float *split_part, Out *out, float *lse,
+                                                         const SplitParts &sp, long long N, int G,
+                                                         size_t out_row0, int r, int c0, int D)
+{
+    split_merge_store(split_merge_parts<kRows, PB>(split_part, sp, sp.c_a, sp.c_b, N, G, r, c0, D), out, lse, out_row0, r, c0, D);
 }
 
 // The end of a cluster split: the first `parts` CTAs of the cluster have left their

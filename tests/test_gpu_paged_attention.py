@@ -323,3 +323,17 @@ def test_outputs_on_16_bytes(cuda_device, D, T, G, lens):
     c.run(ppd)
     c.check()
     assert (flat[:8] == 3).all() and (flat[8 + n:] == 3).all()
+
+
+@pytest.mark.parametrize("D,H,G,T,lens,spare", [(128, 2, 4, 1, [30011], 0), (64, 1, 1, 1, [40000], 0), (128, 1, 3, 5, [20001, 7], 0), (128, 2, 1, 1, [0, 9000, 33], 1500),
+                                                (64, 1, 8, 1, [300], 3000), (128, 2, 1, 9, [15000], 0), (64, 2, 1, 33, [25000], 0)])
+def test_few_rows_of_many_parts(cuda_device, D, H, G, T, lens, spare):
+    """Long requests shared by all SMs: the merge's threads take parts each; tables that hold more than there is."""
+    from paper_2405_18628_gb300 import ppd
+    c = Case(cuda_device, 1, len(lens), H, G, D, T, lens, 16, spare=spare, seed=T + G)
+    c.run(ppd)
+    c.check()
+    first = c.out.clone()
+    c.out.fill_(float("nan"))
+    c.run(ppd)
+    assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))
