@@ -1507,8 +1507,9 @@ ppd_status ppd_token_logprobs(const void *logits, const int32_t *tokens, const i
                      {{logits, (size_t)B * T * V * eb}, {tokens, items}, {rows, items}}))
         return PPD_ERR_INVALID_ARG;
     if (K > ppd::kLogMaxK || (double)B * n * ppd::kMaxCluster > 2147483647.0 || V > kMaxRows) return PPD_ERR_UNSUPPORTED;
-    ppd::LogprobParams p{logits, tokens, rows, logprob, entropy, rank, top_tokens, top_logprobs, dev_status, B, T, V, n, K, dt == PPD_BF16,
-                         1.4426950408889634f / temperature, 138.62943611198906f * temperature, 1};
+    const float k = 1.4426950408889634f / temperature, span = 138.62943611198906f * temperature;
+    const ppd::LogScale scale{k, span, span < 1e30f ? 1048576.f / k : 0.f, k < 1.f ? 0.5f : 1.f, k < 1.f ? 2.f * k : k};
+    ppd::LogprobParams p{logits, tokens, rows, logprob, entropy, rank, top_tokens, top_logprobs, dev_status, B, T, V, n, K, dt == PPD_BF16, scale, 1};
     return cuda_status(ppd::launch_token_logprobs(p, num_sms(), static_cast<cudaStream_t>(stream)));
 }
 

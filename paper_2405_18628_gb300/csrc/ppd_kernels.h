@@ -550,6 +550,12 @@ cudaError_t launch_page_append(PageAppendParams p, cudaStream_t stream);
 
 // ---- log probabilities of given tokens
 constexpr int kLogMaxK = 32;
+struct LogScale {
+    float k;                         // log2(e) / temperature
+    float span;                      // 200 / k
+    float fused;                     // of maxima m below this in size |m k| < 2^20, and m - span is a number
+    float h, kh;                     // 1/2 and 2 k where k < 1, else 1 and k
+};
 struct LogprobParams {
     const void *logits;              // [B,T,V] fp32 or bf16
     const int32_t *tokens, *rows;    // [B,n]; rows null: row i
@@ -559,8 +565,7 @@ struct LogprobParams {
     float *top_logprobs;
     int32_t *dev_status;             // [B]
     int B, T, V, n, K, bf16;
-    float k;                         // log2(e) / temperature
-    float span;                      // 200 / k
+    LogScale scale;
     int cluster;                     // CTAs of a row
 };
 cudaError_t launch_token_logprobs(LogprobParams p, int num_sms, cudaStream_t stream);

@@ -48,25 +48,18 @@ struct RowStats {
     int better, bad;
 };
 
-// k (x - m).  m k is rounded once and is then what all sums refer to, so that the products
-// below need one fused operation; numbers of the size of fp32's limits are subtracted first.
-constexpr float kPlain = 1e30f;
-PPD_DEV float exponent(float x, float m, float k)
-{
-    return fabsf(x) < kPlain && fabsf(m) < kPlain ? fmaf(x, k, -__fmul_rn(m, k)) : (x - m) * k;
-}
-// The same between two maxima (each m k rounded).
-PPD_DEV float exponent_of_max(float a, float m, float k)
-{
-    return fmaxf(fabsf(a) < kPlain && fabsf(m) < kPlain ? __fsub_rn(__fmul_rn(a, k), __fmul_rn(m, k)) : (a - m) * k, -200.f);
-}
+// k (x - m).  Half of x and m where k is below 1: their difference may then be past fp32's range
+// and its product with k not.
+PPD_DEV float exponent(float x, float m, const LogScale &r) { return __fmul_rn(fmaf(x, r.h, -r.h * m), r.kh); }
+// The same between two maxima (NaN where both are -inf: -200).
+PPD_DEV float exponent_of_max(float a, float m, const LogScale &r) { return fmaxf(exponent(a, m, r), -200.f); }
 
-PPD_DEV void merge_stats(RowStats &a, const RowStats &o, float k)
+PPD_DEV void merge_stats(RowStats &a, const RowStats &o, const LogScale &r)
 {
     const float nm = fmaxf(a.m, o.m);
     if (nm > -INFINITY) {
         // 2^d (s, u + d s) with d = k (m - nm) <= 0; nothing where there was no entry
-        const float da = exponent_of_max(a.m, nm, k), db = exponent_of_max(o.m, nm, k);
+        const float da = exponent_of_max(a.m, nm, r), db = exponent_of_max(o.m, nm, r);
         const float wa = a.m > -INFINITY ? ex2(da) : 0.f, wb = o.m > -INFINITY ? ex2(db) : 0.f;
         a.u = wa * fmaf(da, a.s, a.u) + wb * fmaf(db, o.s, o.u);
         a.s = wa * a.s + wb * o.s;
@@ -284,17 +277,21 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
         if (!again) {
             st.bad |= !(mb < INFINITY);
             if (mb > st.m) {
-                const float d = exponent_of_max(st.m, mb, p.k), f = ex2(d);   // (s is 0 where m was -inf)
+                const float d = exponent_of_max(st.m, mb, p.scale), f = ex2(d);   // (s is 0 where m was -inf)
                 st.u = f * fmaf(d, st.s, st.u);
                 st.s *= f;
                 st.m = mb;
-                x_low = __fsub_rd(mb, p.span);
+                x_low = __fsub_rd(mb, p.scale.span);
             }
             // ---- sums
+            const bool far = __any_sync(0xffffffffu, mb > -INFINITY && !(fabsf(st.m) < p.scale.fused));   // (a warp together)
             if (mb == -INFINITY) {
                 // nothing to add
-            } else if (fabsf(st.m) < kPlain && p.span < kPlain && p.span > 0.02f) {
-                const uint64_t nm2 = pack2(-__fmul_rn(st.m, p.k), -__fmul_rn(st.m, p.k)), k2 = pack2(p.k, p.k);
+            } else if (!far) {
+                // x k - M in one operation; M, m k rounded, is off by 2^-5 at most, which sums are
+                // freed of after the batch (from |m k| = 2^31 on 2 to that could be past fp32's range)
+                const float nm = -__fmul_rn(st.m, p.scale.k);
+                const uint64_t nm2 = pack2(nm, nm), k2 = pack2(p.scale.k, p.scale.k);
                 uint64_t s2 = 0ull, u2 = 0ull;
                 const __nv_bfloat162 low2 = __bfloat162bfloat162(__float2bfloat16_rd(x_low));
 #pragma unroll
@@ -316,23 +313,35 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
                         u2 = fma2(v2, d2, u2);
                     }
                 }
+                float a, c, e, g;
+                unpack2(s2, a, c);
+                unpack2(u2, e, g);
+                const float off = fmaf(st.m, p.scale.k, nm), f = ex2(-off), s = a + c;
+                st.s = fmaf(f, s, st.s);
+                st.u = fmaf(f, fmaf(-off, s, e + g), st.u);
+            } else {
+                // far from 0: x - m first; exponents clamped, not entries (2048 rows of 128,256 bf16, all but a
+                // ten-thousandth masked with -1e9, 152 us; with -1e4 136)
+                const float nm = -p.scale.h * st.m;
+                uint64_t s2 = 0ull, u2 = 0ull;
+#pragma unroll 1
+                for (int q = 0; q < kLogLoads; ++q) {
+                    const uint4 r = stage[q * THREADS];
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) {
+                        float a, c;
+                        unpack2(mul2(fma2(pack2(value(r, e), value(r, e + 1)), pack2(p.scale.h, p.scale.h), pack2(nm, nm)), pack2(p.scale.kh, p.scale.kh)), a, c);
+                        a = fmaxf(a, -200.f), c = fmaxf(c, -200.f);   // (2^-200 is 0; nothing times an infinity)
+                        const uint64_t v2 = pack2(ex2(a), ex2(c));
+                        s2 = add2(s2, v2);
+                        u2 = fma2(v2, pack2(a, c), u2);
+                    }
+                }
                 float a, c;
                 unpack2(s2, a, c);
                 st.s += a + c;
                 unpack2(u2, a, c);
                 st.u += a + c;
-            } else {   // numbers whose differences may overflow
-#pragma unroll 1
-                for (int q = 0; q < kLogLoads; ++q) {
-                    const uint4 r = stage[q * THREADS];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float d = fmaxf(exponent(value(r, e), st.m, p.k), -200.f);   // (2^-200 is 0; nothing times an infinity)
-                        const float v = ex2(d);
-                        st.s += v;
-                        st.u = fmaf(v, d, st.u);
-                    }
-                }
             }
             // ---- entries that rank before the token
             const long long c0 = (long long)base * E - skew;   // the batch's first column
@@ -484,7 +493,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
             y.u = __shfl_xor_sync(0xffffffffu, st.u, o);
             y.better = __shfl_xor_sync(0xffffffffu, st.better, o);
             y.bad = __shfl_xor_sync(0xffffffffu, st.bad, o);
-            merge_stats(st, y, p.k);
+            merge_stats(st, y, p.scale);
         }
     };
     const RowStats empty{-INFINITY, 0.f, 0.f, 0, 0};
@@ -519,7 +528,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const LogprobPa
         st.bad = __shfl_sync(0xffffffffu, st.bad, 0);
         const bool bad = st.bad || st.m == -INFINITY;
         const float lg = lg2(st.s), ln2 = 0.69314718055994530942f;
-        auto logprob = [&](float x) { return bad ? NAN : (exponent(x, st.m, p.k) - lg) * ln2; };
+        auto logprob = [&](float x) { return bad ? NAN : (exponent(x, st.m, p.scale) - lg) * ln2; };
         if (tid == 0) {
             p.logprob[item] = token < 0 ? 0.f : logprob(xt);
             p.entropy[item] = bad ? NAN : (lg - st.u / st.s) * ln2;
