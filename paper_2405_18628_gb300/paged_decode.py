@@ -63,7 +63,10 @@ class PagedRequests:
         count = torch.where(self.active, 0, count.clamp(0, k.shape[3]))
         self._assign(self.length + count)
         ppd.ppd_page_append(k, v, self.k, self.v, self.slots, self.slot_start, self.append_status)
-        self.active |= (count > 0) & (self.assign_status == 0)
+        came = (count > 0) & (self.assign_status == 0)
+        self.active |= came
+        # what a place is to hold goes with its request: a new one has accepted nothing yet
+        self.wanted.copy_(torch.where(came, self.length, self.wanted))
 
     def attend(self, layer, q, k_tree, v_tree, parent):
         """One layer's attention: q [B,H*G,T,D], k_tree and v_tree [B,H,T,D] -> bf16 [B,H*G,T,D]."""
@@ -87,7 +90,8 @@ class PagedRequests:
         return self.next_token
 
     def commit(self, k_tree, v_tree):
-        """The accepted nodes' rows of every layer, k_tree and v_tree [L,B,H,T,D], enter the pages of active requests."""
+        """The accepted nodes' rows of every layer, k_tree and v_tree [L,B,H,T,D], enter the pages of active requests (of
+        those that have accepted since they came and were not served yet)."""
         self._assign(torch.where(self.active, self.wanted, self.length))
         ppd.ppd_page_append(k_tree, v_tree, self.k, self.v, self.slots, self.slot_start, self.append_status, rows=self.path)
 
@@ -95,6 +99,7 @@ class PagedRequests:
         """Requests that are done, bool [B], give their pages back."""
         self._assign(torch.where(done, 0, self.length))
         self.active &= ~done
+        self.wanted.masked_fill_(done, 0)
 
 
 def main(argv=None):

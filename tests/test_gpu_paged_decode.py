@@ -100,3 +100,123 @@ def test_sizes_that_do_not_fit_are_refused():
     for bad in (dict(prompt=129), dict(prompt=0), dict(n_pages=0)):
         with pytest.raises(ValueError, match="prompts of"):
             S.PagedRequests(**dict(dict(L=1, B=1, H=1, G=1, T=4, D=64, V=10, n_pages=9, page=16, max_pages=8, prompt=100), **bad), device="cpu")
+
+
+class Plain:
+    """Rows that each place holds and is to gain, beside a PagedRequests, with its calls in any order."""
+
+    def __init__(self, dev, B, n_pages, seed, dtype=torch.bfloat16):
+        from paper_2405_18628_gb300 import paged_decode as S
+        self.g = torch.Generator(device=dev)
+        self.g.manual_seed(seed)
+        self.L, self.B, self.H, self.T, self.D, self.V, self.page, self.M, self.prompt = 2, B, 2, 10, 64, 50, 8, 12, 50
+        self.req = S.PagedRequests(self.L, B, self.H, 2, self.T, self.D, self.V, n_pages, self.page, self.M, self.prompt, K=0, device=dev)
+        self.dev, self.dtype = dev, dtype
+        self.rows, self.pending, self.active = [[] for _ in range(B)], [[]] * B, [False] * B
+        self.table, self.stack, self.tree = [[-1] * self.M for _ in range(B)], list(range(n_pages)), None
+
+    def n(self, *s):
+        return torch.randn(s, device=self.dev, generator=self.g).to(self.dtype)
+
+    def assign(self, wanted, new):
+        length, _, status = O.page_assign([len(r) for r in self.rows], wanted, self.page, self.table, self.stack, self.req.slots.numel())
+        for b in range(self.B):
+            self.rows[b] = self.rows[b][:length[b]] + (new[b] if length[b] > len(self.rows[b]) else [])
+        assert self.req.assign_status.tolist() == status
+        return status
+
+    def admit(self, count):
+        k, v = self.n(self.L, self.B, self.H, self.prompt, self.D), self.n(self.L, self.B, self.H, self.prompt, self.D)
+        self.req.admit(k, v, torch.tensor(count, dtype=torch.int32, device=self.dev))
+        count = [0 if a else c for a, c in zip(self.active, count)]
+        status = self.assign([len(r) + c for r, c in zip(self.rows, count)], [[(k[:, b, :, j], v[:, b, :, j]) for j in range(count[b])] for b in range(self.B)])
+        for b in range(self.B):
+            if count[b] and status[b] == 0:
+                self.active[b], self.pending[b] = True, []
+
+    def accept(self, take):
+        """Chains; take[b] rows of each are accepted (1 to T)."""
+        parent = torch.arange(-1, self.T - 1, dtype=torch.int32, device=self.dev).repeat(self.B, 1)
+        logits = torch.randn(self.B, self.T, self.V, device=self.dev, generator=self.g)
+        cand = logits.argmax(-1).int().roll(1, 1)
+        for b, t in enumerate(take):
+            if t < self.T:
+                cand[b, t] = -1
+        self.tree = self.n(self.L, self.B, self.H, self.T, self.D), self.n(self.L, self.B, self.H, self.T, self.D)
+        self.req.accept(logits, cand, parent)
+        assert self.req.accept_len.tolist() == take
+        self.pending = [[(self.tree[0][:, b, :, j], self.tree[1][:, b, :, j]) for j in range(t)] if a else [] for b, (t, a) in enumerate(zip(take, self.active))]
+
+    def commit(self):
+        self.req.commit(*self.tree)
+        status = self.assign([len(r) + len(p) for r, p in zip(self.rows, self.pending)], self.pending)
+        self.pending = [p if s else [] for p, s in zip(self.pending, status)]
+
+    def finish(self, done):
+        self.req.finish(torch.tensor(done, device=self.dev))
+        self.assign([0 if d else len(r) for d, r in zip(done, self.rows)], [[]] * self.B)
+        self.active = [a and not d for a, d in zip(self.active, done)]
+        self.pending = [[] if d else p for d, p in zip(done, self.pending)]
+
+    def check(self):
+        req = self.req
+        assert req.length.tolist() == [len(r) for r in self.rows] and req.active.tolist() == self.active
+        assert req.n_free.tolist() == [len(self.stack)] and (req.append_status == 0).all()
+        for b in range(self.B):
+            held = O.pages_of(len(self.rows[b]), self.page)
+            assert req.table[b, :held].tolist() == self.table[b][:held]
+            for x, pool in enumerate((req.k, req.v)):
+                for l in range(self.L):
+                    got = O.rows_of(pool[l], self.table[b], len(self.rows[b]))
+                    assert not self.rows[b] or torch.equal(got, torch.stack([r[x][l] for r in self.rows[b]], 1).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("prompt", [5, 18, 30])
+def test_a_commit_repeated_after_a_refusal(cuda_device, prompt):
+    """Refused, some requests finished, another in the refused one's place, committed again: the new prompt
+    stays as it is, whether shorter or longer than what the old request was to hold."""
+    p = Plain(cuda_device, 3, 9, prompt)
+    p.admit([24, 20, 8])
+    p.accept([10, 3, 10])
+    p.commit()                       # to 34, 23 and 18 rows: two pages are free, and the first takes them
+    p.check()
+    assert p.req.assign_status.tolist() == [0, 0, 4]
+    p.finish([True, False, True])
+    p.admit([0, 0, prompt])
+    p.check()
+    for _ in range(3):
+        p.commit()
+        p.check()
+    assert p.req.length.tolist() == [0, 23, prompt]
+
+
+def test_a_commit_without_an_acceptance(cuda_device):
+    """Nothing was accepted yet: prompts stay as they are."""
+    p = Plain(cuda_device, 3, 30, 1)
+    p.tree = p.n(2, 3, 2, 10, 64), p.n(2, 3, 2, 10, 64)
+    p.admit([20, 0, 7])
+    p.commit()
+    p.check()
+    p.accept([3, 4, 5])              # of a place that is free: it gains nothing
+    p.admit([0, 9, 0])
+    p.commit()
+    p.check()
+    assert p.req.length.tolist() == [23, 9, 12]
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_calls_in_any_order(cuda_device, seed):
+    rng = np.random.default_rng(seed)
+    p = Plain(cuda_device, 4, 14 if seed % 2 else 40, seed)
+    p.tree = p.n(2, 4, 2, 10, 64), p.n(2, 4, 2, 10, 64)
+    for _ in range(60):
+        what = rng.choice(["admit", "accept", "commit", "commit", "finish"])
+        if what == "admit":
+            p.admit([0 if rng.random() < 0.5 else int(rng.integers(1, p.prompt + 1)) for _ in range(4)])
+        elif what == "accept" and max(len(r) for r in p.rows) <= p.M * p.page - p.T:
+            p.accept([int(rng.integers(1, p.T + 1)) for _ in range(4)])
+        elif what == "commit":
+            p.commit()
+        else:
+            p.finish([bool(rng.random() < (0.9 if len(r) > 70 else 0.2)) for r in p.rows])
+        p.check()
