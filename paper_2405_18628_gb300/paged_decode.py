@@ -24,6 +24,7 @@ class PagedRequests:
     """B places for requests over L layers: pools of n_pages pages of `page` rows, tables of max_pages pages, and
     the buffers of a step.  H K/V heads of G query heads each, trees of T tokens, a vocabulary of V, K alternatives
     for each emitted token; prompts of `prompt` rows at most.  A place is active from its prompt to finish().
+    Projections are bf16 or fp32.
     Nothing here waits for the GPU: lengths, tables and the free pages stay on the device.  Where the pool
     is short, requests keep what they hold and assign_status says so (PPD_ERR_CAPACITY): finish() some and
     commit() or admit() again."""
@@ -48,7 +49,7 @@ class PagedRequests:
         self.top_tokens, self.top_logprobs = (i32(B, T, K), f32(B, T, K)) if K else (None, None)
         self.attend_status, self.accept_status, self.logprob_status = i32(L, B), i32(B), i32(B)
         self.assign_status, self.append_status = i32(B), i32(B)
-        n = ppd.ppd_paged_attention_workspace_bytes(1, B, H, G, T, D, max_pages * page)
+        n = ppd.ppd_paged_attention_workspace_bytes(1, B, H, G, T, D, max_pages * page, ppd.PPD_F32)   # (no less than bf16 needs)
         self.workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
     def _assign(self, wanted):
@@ -69,7 +70,7 @@ class PagedRequests:
         self.wanted.copy_(torch.where(came, self.length, self.wanted))
 
     def attend(self, layer, q, k_tree, v_tree, parent):
-        """One layer's attention: q [B,H*G,T,D], k_tree and v_tree [B,H,T,D] -> bf16 [B,H*G,T,D]."""
+        """One layer's attention: q [B,H*G,T,D], k_tree and v_tree [B,H,T,D], bf16 or fp32 -> bf16 [B,H*G,T,D]."""
         at = slice(layer, layer + 1)
         ppd.ppd_tree_attention_paged(q[None], self.k[at], self.v[at], self.table, k_tree[None], v_tree[None], self.length, parent, self.out[at],
                                      self.attend_status[layer], workspace=self.workspace)

@@ -220,3 +220,23 @@ def test_calls_in_any_order(cuda_device, seed):
         else:
             p.finish([bool(rng.random() < (0.9 if len(r) > 70 else 0.2)) for r in p.rows])
         p.check()
+
+
+def test_fp32_projections(cuda_device):
+    """Prompts, queries and tree rows in fp32, layer by layer."""
+    p = Plain(cuda_device, 3, 30, 2, dtype=torch.float32)
+    p.admit([20, 0, 50])
+    p.accept([3, 1, 10])
+    p.commit()
+    p.check()
+    parent = [[-1, 0, 0, 1, 1, 2, 5, 5, 0, 3]] * 3
+    q, kt, vt = p.n(2, 3, 4, 10, 64), p.n(2, 3, 2, 10, 64), p.n(2, 3, 2, 10, 64)
+    for l in range(2):
+        p.req.attend(l, q[l], kt[l], vt[l], torch.tensor(parent, dtype=torch.int32, device=cuda_device))
+        for b in range(3):
+            k, v = (torch.stack([r[x][l] for r in p.rows[b]], 1).to(torch.bfloat16) if p.rows[b] else kt.new_zeros(2, 0, 64) for x in range(2))
+            for h in range(2):
+                hs = slice(2 * h, 2 * h + 2)
+                out, _, mass, size = O.attention(q[l, b, hs], k[h], v[h], kt[l, b, h], vt[l, b, h], parent[b])
+                assert ((p.req.out[l, b, hs].double() - out).abs() <= (2.0 ** -8 + 1e-4 + 2 * 64 * 2.0 ** -24 * size) * mass + 1e-36).all()
+    assert (p.req.attend_status == 0).all()
