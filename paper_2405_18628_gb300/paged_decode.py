@@ -77,10 +77,12 @@ class PagedRequests:
         return self.out[layer]
 
     def accept(self, logits, cand_tokens, parent):
-        """The longest path that the model's top tokens confirm -> next_token [B]; path and accept_len say what was
-        accepted, tokens [B,T] the emitted tokens (-1 past them), with their log probabilities, entropies, ranks and
-        alternatives."""
+        """The longest path that the model's top tokens confirm, by fp32 logits [B,T,V], the tree's tokens and parents,
+        int32 [B,T] -> next_token [B]; path and accept_len say what was accepted, tokens [B,T] the emitted tokens
+        (-1 past them), with their log probabilities, entropies, ranks and alternatives."""
         V, page, max_pages = self.sizes[6:]
+        each = self.path.shape
+        ppd._take(("logits", logits, torch.float32, (*each, V)), ("cand_tokens", cand_tokens, torch.int32, each), ("parent", parent, torch.int32, each))
         ppd.ppd_node_argmax_noalloc(logits, self.top1)
         ppd.ppd_accept_path(self.top1, cand_tokens, parent, self.length, V, page * max_pages, self.accept_len, self.path, self.next_token, self.wanted,
                             self.accept_status)
