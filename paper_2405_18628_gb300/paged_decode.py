@@ -58,12 +58,19 @@ class PagedRequests:
         self.length, self._length = self._length, self.length
         self.n_free, self._n_free = self._n_free, self.n_free
 
+    def _append(self, k, v, rows=None):
+        try:
+            ppd.ppd_page_append(k, v, self.k, self.v, self.slots, self.slot_start, self.append_status, rows=rows)
+        except Exception:
+            self._assign(self._length.clone())   # lengths exchanged: nothing has changed
+            raise
+
     def admit(self, k, v, count):
         """Prompts for free places: k and v [L,B,H,n,D] of every layer, count int32 [B] rows of each, n at most (0:
         none for this place, and for active ones).  A prompt that finds no pages leaves its place free."""
         count = torch.where(self.active, 0, count.clamp(0, k.shape[3]))
         self._assign(self.length + count)
-        ppd.ppd_page_append(k, v, self.k, self.v, self.slots, self.slot_start, self.append_status)
+        self._append(k, v)
         came = (count > 0) & (self.assign_status == 0)
         self.active |= came
         # what a place is to hold goes with its request: a new one has accepted nothing yet
@@ -96,7 +103,7 @@ class PagedRequests:
         """The accepted nodes' rows of every layer, k_tree and v_tree [L,B,H,T,D], enter the pages of active requests (of
         those that have accepted since they came and were not served yet)."""
         self._assign(torch.where(self.active, self.wanted, self.length))
-        ppd.ppd_page_append(k_tree, v_tree, self.k, self.v, self.slots, self.slot_start, self.append_status, rows=self.path)
+        self._append(k_tree, v_tree, self.path)
 
     def finish(self, done):
         """Requests that are done, bool [B], give their pages back."""

@@ -240,3 +240,26 @@ def test_fp32_projections(cuda_device):
                 out, _, mass, size = O.attention(q[l, b, hs], k[h], v[h], kt[l, b, h], vt[l, b, h], parent[b])
                 assert ((p.req.out[l, b, hs].double() - out).abs() <= (2.0 ** -8 + 1e-4 + 2 * 64 * 2.0 ** -24 * size) * mass + 1e-36).all()
     assert (p.req.attend_status == 0).all()
+
+
+def test_refused_rows_change_nothing(cuda_device):
+    """Rows that cannot be appended: the call raises, and lengths, tables and the pool are as they were."""
+    p = Plain(cuda_device, 3, 30, 3)
+    p.admit([20, 0, 7])
+    n, count = p.n, torch.tensor([0, 30, 0], dtype=torch.int32, device=cuda_device)
+    good = n(2, 3, 2, 50, 64)
+    off = torch.empty(good.numel() + 1, dtype=good.dtype, device=cuda_device)[1:].view(good.shape)
+    for k, v in ((n(1, 3, 2, 50, 64), n(1, 3, 2, 50, 64)), (good, n(2, 3, 2, 49, 64)), (n(2, 3, 1, 50, 64), n(2, 3, 1, 50, 64)), (good.half(), good.half()),
+                 (good, good.float()), (good.transpose(1, 2).contiguous().transpose(1, 2), good), (off, good), (good, good.cpu())):
+        with pytest.raises((ValueError, TypeError, RuntimeError)):
+            p.req.admit(k, v, count)
+        p.check()
+    p.accept([3, 1, 10])
+    for k, v in ((n(2, 3, 2, 9, 64), n(2, 3, 2, 9, 64)), (n(2, 2, 2, 10, 64), n(2, 2, 2, 10, 64)), (p.tree[0], p.tree[1].float())):
+        with pytest.raises((ValueError, TypeError, RuntimeError)):
+            p.req.commit(k, v)
+        p.check()
+    p.commit()
+    p.admit([0, 30, 0])
+    p.check()
+    assert p.req.length.tolist() == [23, 30, 17] and torch.equal(p.req.free[:p.req.n_free[0]].cpu(), torch.tensor(p.stack, dtype=torch.int32))
