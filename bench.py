@@ -83,10 +83,14 @@ MEASURED_TRAFFIC = {
 }
 
 
+ATTENTION_SOURCES = ("ppd_attention.cu", "ppd_attention_key.cuh", "ppd_attention_rows.cu", "ppd_attention_rows.cuh",
+                     "ppd_attention_common.cuh", "ppd_paged.cuh", "ppd_device.cuh", "ppd_accept.cuh", "ppd_kernels.h",
+                     "ppd_api.cu")
+
+
 def attention_source_hash() -> str:
     h = hashlib.sha256()
-    for f in ("ppd_attention.cu", "ppd_attention_key.cuh", "ppd_attention_rows.cu", "ppd_attention_rows.cuh", "ppd_attention_common.cuh",
-              "ppd_device.cuh", "ppd_accept.cuh", "ppd_kernels.h", "ppd_api.cu"):
+    for f in ATTENTION_SOURCES:
         with open(os.path.join(ROOT, "paper_2405_18628_gb300", "csrc", f), "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
