@@ -181,8 +181,9 @@ struct RowsIter {
         const int slice = job / per, i = job - slice * per;
         const int qb = pair ? 2 * i : (p.pairs ? p.n_qb - 1 : i);
         j.ui = unit_info(p, slice * p.n_qb + qb);
-        // a query's ancestors come before it: no tree tile past the job's last block (a block
-        // of several heads' rows may hold any node)
+        // a query's ancestors come before it: no tree tile past the job's last block (over pages a
+        // block of several heads' rows may hold any node; one head's blocks take all tiles too,
+        // which costs large trees over short prefixes: 388 tokens over 9 rows, 20 tiles for 14)
         j.ui.n_tiles = j.ui.n_pref + (PAGED ? p.n_tt : qb + (pair ? 2 : 1));
         j.j0 = 0;
         j.j1 = j.ui.n_tiles;
@@ -617,8 +618,8 @@ tree_attention_rows_kernel(const __grid_constant__ CUtensorMap map_q,
             if (n == 0) break;
             if (pair) {
                 // K0 V0 K1 V1 ...; the job's last tile holds no key that a query of its first
-                // block may see (n >= 2), so stream A stops one tile earlier (with shared K/V
-                // heads either block may hold any node)
+                // block may see (n >= 2), so stream A stops one tile earlier (over pages, where
+                // a block of several heads' rows may hold any node, both take all)
                 for (int i = 0; i < n; ++i) {
                     if (pend) issue_pv(false);
                     else take_turn();

@@ -205,7 +205,8 @@ cudaError_t launch_page_assign(const PageAssignParams &p, int num_sms, cudaStrea
 // ------------------------------------------------------------------ rows into pages
 
 // A block takes kAppendRows rows of a slice, K and V; 16 bytes of a pool's row a thread and
-// step, kInFlight steps' loads in flight.  HBM for prompts, the launch for paths.
+// step, kInFlight steps' loads in flight.  HBM for prompts; for paths the rounds of blocks, most of whose threads
+// have nothing to do (2048 blocks of up to six rows 6.0 us; 576, one round, 3.1; one 2.6).
 constexpr int kAppendRows = 64, kAppendThreads = 256, kInFlight = 4;
 
 template <bool F32>
